@@ -42,7 +42,8 @@ typedef enum {
     QLLM_ERR_MAP = -5,       /* malformed reassembly map or merge list */
     QLLM_ERR_ALIGN = -6,     /* a buffer or stride misses the required alignment */
     QLLM_ERR_WORKSPACE = -7, /* workspace missing or smaller than qllm_workspace_bytes says */
-    QLLM_ERR_HIP = -8        /* the HIP runtime reported an error (launch, attribute, device) */
+    QLLM_ERR_HIP = -8,       /* the HIP runtime reported an error (launch, attribute, device) */
+    QLLM_ERR_PAGES = -9      /* cache pages: too few free ones, a number out of range or a clash (qllm_kv.h) */
 } qllm_status;
 
 typedef enum { QLLM_F32 = 0, QLLM_BF16 = 1 } qllm_dtype;

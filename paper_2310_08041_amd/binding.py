@@ -51,6 +51,20 @@ class _LayerLaunch(C.Structure):
                 ("ahead_bytes", C.c_int64)]
 
 
+class _KVCache(C.Structure):
+    _fields_ = [("heads", C.c_int64), ("dim", C.c_int64), ("page_tokens", C.c_int64), ("n_pages", C.c_int64), ("pages", C.c_void_p)]
+
+
+class _KVBatch(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("n_seqs", C.c_int64), ("row_start", C.c_void_p), ("slot", C.c_void_p), ("n_slots", C.c_int64),
+                ("table_ld", C.c_int64), ("table", C.c_void_p), ("length", C.c_void_p)]
+
+
+class _KVBook(C.Structure):
+    _fields_ = [("page_tokens", C.c_int64), ("n_slots", C.c_int64), ("table_ld", C.c_int64), ("n_pages", C.c_int64), ("table", C.c_void_p),
+                ("length", C.c_void_p), ("refs", C.c_void_p)]
+
+
 _i64, _i32, _vp, _f = C.c_int64, C.c_int32, C.c_void_p, C.c_float
 _sigs = {
     "qllm_norm_reassemble_quant": (_i32, [_vp, _i32, _i64, _i64, _i64, _i32, _vp, _vp, _f, C.POINTER(_Map), _i32,
@@ -94,6 +108,16 @@ _sigs = {
     "qllm_linear_f64": (_i32, [_vp, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _vp]),
     "qllm_sq_error_workspace_bytes": (_i64, [_i64]),
     "qllm_sq_error": (_i32, [_vp, _i32, _i64, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp]),
+    "qllm_kv_page_bytes": (_i64, [_i64, _i64, _i64]),
+    "qllm_kv_append": (_i32, [_vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _vp, C.POINTER(_KVCache), C.POINTER(_KVBatch), _vp]),
+    "qllm_kv_read": (_i32, [C.POINTER(_KVCache), C.POINTER(_KVBatch), _vp, _i64, _vp, _i64, _i32, _vp]),
+    "qllm_kv_attention_workspace_bytes": (_i64, [C.POINTER(_KVCache), C.POINTER(_KVBatch), _i64]),
+    "qllm_kv_attention": (_i32, [_vp, _i32, _i64, _i64, C.POINTER(_KVCache), C.POINTER(_KVBatch), _f, _i64, _vp, _i32, _i64, _vp, _i64, _vp]),
+    "qllm_kv_copy_pages": (_i32, [_vp, _i64, _i64, _i64, _i64, _vp, _vp, _i64, _vp]),
+    "qllm_kv_reserve_host": (_i32, [C.POINTER(_KVBook), _vp, _vp, _i64]),
+    "qllm_kv_fork_host": (_i64, [C.POINTER(_KVBook), _vp, _vp, _i64, _vp, _vp]),
+    "qllm_kv_free_host": (_i32, [C.POINTER(_KVBook), _vp, _i64]),
+    "qllm_kv_compact_host": (_i64, [C.POINTER(_KVBook), _vp, _vp]),
     "qllm_probe_mfma": (_i32, [_i32, _i32, _vp, _vp]),
     "qllm_probe_mfma_fp6": (_i32, [_i32, _i32, _vp, _vp]),
     "qllm_probe_stream": (_i32, [_vp, _vp, _i64, _i32, _vp]),
@@ -671,6 +695,199 @@ def qllm_swiglu(gate, up, x, stream=None):
     ld = lambda t: t.stride(0) if N > 1 else Cc          # the stride of a single row says nothing
     _chk(_lib.qllm_swiglu(_dp(gate), ld(gate), _dp(up), ld(up), int(N), int(Cc), _dp(x), ld(x), _stream(stream)), "qllm_swiglu")
     return x
+
+
+# ---------------------------------------------------------------- the key/value cache in 4-bit codes (include/qllm_kv.h)
+
+ROPE_NONE, ROPE_HALVES, ROPE_PAIRS = 0, 1, 2
+_I32_ONLY, _F64_ONLY = (torch.int32,), (torch.float64,)
+
+
+def _check_on_current(**tensors):
+    """Device tensors, and on the device that the call is going to run on."""
+    _check_on_device(**tensors)
+    here = torch.cuda.current_device()
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != here:
+            _fail(f"{name} is on device {t.get_device()}, the call runs on device {here}")
+
+
+def qllm_kv_page_bytes(heads, dim, page_tokens):
+    v = _lib.qllm_kv_page_bytes(int(heads), int(dim), int(page_tokens))
+    _chk(v if v < 0 else 0, "qllm_kv_page_bytes")
+    return int(v)
+
+
+class DeviceKVCache:
+    """The pages of all layers, [layers, n_pages, page bytes] uint8 (made here unless given), and a C struct for each layer."""
+
+    def __init__(self, layers, n_pages, heads, dim, page_tokens, pages=None, device="cuda"):
+        self.page_bytes = qllm_kv_page_bytes(heads, dim, page_tokens)
+        self.layers, self.n_pages, self.heads, self.dim, self.page_tokens = int(layers), int(n_pages), int(heads), int(dim), int(page_tokens)
+        if pages is None:
+            pages = torch.zeros((self.layers, self.n_pages, self.page_bytes), dtype=torch.uint8, device=device)
+        _check_tensor(pages, "pages", _U8_ONLY, shape=(self.layers, self.n_pages, self.page_bytes))
+        if not pages.is_contiguous():
+            _fail("pages must be contiguous")
+        self.pages = pages
+        step = self.n_pages * self.page_bytes
+        self.c = [_KVCache(self.heads, self.dim, self.page_tokens, self.n_pages, _dp(pages) + i * step) for i in range(self.layers)]
+
+
+class DeviceKVBatch:
+    """The sequences of a step: table [lines, pages] and length [lines] of the cache's lines, row_start [sequences + 1] (None: one row
+    each, in order), slot [sequences] the sequences' lines (None: the lines in order).  int32 device tensors, kept alive here."""
+
+    def __init__(self, rows, table, length, row_start=None, slot=None):
+        _need(hasattr(table, "dim") and table.dim() == 2 and table.is_contiguous(), "table must be a contiguous 2-d tensor [lines, pages]")
+        n_slots, table_ld = table.shape
+        _check_tensor(table, "table", _I32_ONLY)
+        _check_tensor(length, "length", _I32_ONLY, numel=n_slots)
+        self.rows = int(rows)
+        self.n_seqs = int(row_start.numel() - 1 if row_start is not None else slot.numel() if slot is not None else n_slots)
+        _need(self.n_seqs >= 0, "row_start needs one entry more than there are sequences")
+        _check_tensor(row_start, "row_start", _I32_ONLY, numel=self.n_seqs + 1, optional=True)
+        _check_tensor(slot, "slot", _I32_ONLY, numel=self.n_seqs, optional=True)
+        _need(row_start is not None or self.rows >= self.n_seqs, f"{self.n_seqs} sequences of one row each need as many rows, there are {self.rows}")
+        _need(slot is not None or n_slots >= self.n_seqs, f"{self.n_seqs} sequences, but {n_slots} lines in the table")
+        self.table, self.length, self.row_start, self.slot = table, length, row_start, slot
+        self.c = _KVBatch(self.rows, self.n_seqs, _dp(row_start), _dp(slot), n_slots, table_ld, _dp(table), _dp(length))
+
+
+def _check_kv(cache, layer, batch):
+    if not 0 <= int(layer) < cache.layers:
+        _fail(f"layer {layer} of a cache of {cache.layers}")
+    return dict(pages=cache.pages, table=batch.table, length=batch.length, row_start=batch.row_start, slot=batch.slot)
+
+
+def _check_rows(t, name, dtypes, rows, width):
+    if not (hasattr(t, "dim") and t.dim() == 2):
+        _fail(f"{name} must be a 2-d tensor [rows, channels]")
+    _check_tensor(t, name, dtypes, shape=(rows, width))
+    return t.stride(0) if rows > 1 else width          # the stride of a single row says nothing
+
+
+def qllm_kv_append(cache, layer, batch, k, v, q=None, q_out=None, rope=ROPE_NONE, inv_freq=None, stream=None):
+    """Rotary positions on the step's q and k, Eq. (2) at 4 bits on its k and v, codes into the sequences' pages.  k, v [rows, heads *
+    dim], q [rows, query heads * dim] (or None) of one dtype, rows may be strided; q_out receives the rotated queries (q itself
+    will do).  rope: ROPE_*; inv_freq [dim / 2] float64, angle per position."""
+    kv = _check_kv(cache, layer, batch)
+    width, rows, dtype = cache.heads * cache.dim, batch.rows, (k.dtype if isinstance(k, torch.Tensor) else None,)
+    ldk = _check_rows(k, "k", _FLOATS, rows, width)
+    ldv = _check_rows(v, "v", dtype, rows, width)
+    ldq = ldq_out = q_heads = 0
+    if (q is None) != (q_out is None):
+        _fail("q and q_out go together")
+    if q is not None:
+        q_heads = q.shape[-1] // cache.dim
+        ldq = _check_rows(q, "q", dtype, rows, q_heads * cache.dim)
+        ldq_out = _check_rows(q_out, "q_out", dtype, rows, q_heads * cache.dim)
+    if int(rope) != ROPE_NONE:
+        _check_tensor(inv_freq, "inv_freq", _F64_ONLY, numel=cache.dim // 2)
+    _check_on_current(k=k, v=v, q=q, q_out=q_out, inv_freq=inv_freq, **kv)
+    _chk(_lib.qllm_kv_append(_dp(q), ldq, q_heads, _dp(q_out), ldq_out, _dp(k), ldk, _dp(v), ldv, _x_dtype(k), int(rope), _dp(inv_freq),
+                             C.byref(cache.c[layer]), C.byref(batch.c), _stream(stream)), "qllm_kv_append")
+    return q_out
+
+
+def qllm_kv_read(cache, layer, batch, k_out=None, v_out=None, stream=None):
+    """What the cache holds for the step's rows, alpha * (code - beta), in k_out and v_out [rows, heads * dim] of one dtype."""
+    kv = _check_kv(cache, layer, batch)
+    width = cache.heads * cache.dim
+    one = k_out if k_out is not None else v_out
+    if one is None:
+        _fail("k_out or v_out is required")
+    ldk = _check_rows(k_out, "k_out", _FLOATS, batch.rows, width) if k_out is not None else 0
+    ldv = _check_rows(v_out, "v_out", _FLOATS if k_out is None else (k_out.dtype,), batch.rows, width) if v_out is not None else 0
+    _check_on_current(k_out=k_out, v_out=v_out, **kv)
+    _chk(_lib.qllm_kv_read(C.byref(cache.c[layer]), C.byref(batch.c), _dp(k_out), ldk, _dp(v_out), ldv, _x_dtype(one), _stream(stream)),
+         "qllm_kv_read")
+
+
+def qllm_kv_attention_workspace_bytes(cache, batch, q_heads):
+    v = _lib.qllm_kv_attention_workspace_bytes(C.byref(cache.c[0]), C.byref(batch.c), int(q_heads))
+    _chk(v if v < 0 else 0, "qllm_kv_attention_workspace_bytes")
+    return int(v)
+
+
+def qllm_kv_attention(q, cache, layer, batch, scale, out, workspace, window=0, stream=None):
+    """Causal attention of the step's queries [rows, query heads * dim] over the cache into out of the same shape (fp32 / bf16 each);
+    window > 0: only that many newest tokens of each query."""
+    kv = _check_kv(cache, layer, batch)
+    q_heads = q.shape[-1] // cache.dim if hasattr(q, "shape") and q.dim() == 2 else 0
+    ldq = _check_rows(q, "q", _FLOATS, batch.rows, q_heads * cache.dim)
+    ldo = _check_rows(out, "out", _FLOATS, batch.rows, q_heads * cache.dim)
+    _check_tensor(workspace, "workspace", _U8_ONLY)
+    if not workspace.is_contiguous():
+        _fail("workspace must be contiguous")
+    _check_on_current(q=q, out=out, workspace=workspace, **kv)
+    _chk(_lib.qllm_kv_attention(_dp(q), _x_dtype(q), ldq, q_heads, C.byref(cache.c[layer]), C.byref(batch.c), float(scale), int(window),
+                                _dp(out), _x_dtype(out), ldo, _dp(workspace), workspace.numel(), _stream(stream)), "qllm_kv_attention")
+    return out
+
+
+def qllm_kv_copy_pages(cache, src, dst, stream=None):
+    """Page dst[i] becomes a copy of page src[i] in every layer; src, dst: host arrays (what fork and compaction return)."""
+    src, dst = _np(src, np.int32), _np(dst, np.int32)
+    if src.ndim != 1 or src.shape != dst.shape:
+        _fail("src and dst must be 1-d arrays of one length")
+    _check_on_current(pages=cache.pages)
+    _chk(_lib.qllm_kv_copy_pages(_dp(cache.pages), cache.layers, cache.n_pages * cache.page_bytes, cache.n_pages, cache.page_bytes, _hp(src),
+                                 _hp(dst), src.size, _stream(stream)), "qllm_kv_copy_pages")
+
+
+class KVBook:
+    """Which page of a cache belongs to whom: table [lines, pages] (-1: none), length [lines], refs [n_pages], int32 numpy arrays that
+    the qllm_kv_*_host calls work on in place."""
+
+    def __init__(self, page_tokens, table, length, refs):
+        for name, a, dims in (("table", table, 2), ("length", length, 1), ("refs", refs, 1)):
+            _need(isinstance(a, np.ndarray) and a.dtype == np.int32 and a.ndim == dims and a.flags.c_contiguous and a.flags.writeable,
+                  f"{name} must be a writeable contiguous int32 array of {dims} dimensions")
+        _need(length.size == table.shape[0], f"length must hold one entry per line of the table ({table.shape[0]})")
+        self.page_tokens, self.table, self.length, self.refs = int(page_tokens), table, length, refs
+        self.c = _KVBook(self.page_tokens, table.shape[0], table.shape[1], refs.size, _hp(table), _hp(length), _hp(refs))
+
+    @classmethod
+    def empty(cls, lines, pages_per_line, n_pages, page_tokens):
+        return cls(page_tokens, np.full((lines, pages_per_line), -1, np.int32), np.zeros(lines, np.int32), np.zeros(n_pages, np.int32))
+
+
+def _host_list(a, name, size=None):
+    a = np.atleast_1d(_np(a, np.int32))
+    _need(a.ndim == 1 and (size is None or a.size == size), f"{name} must be a list" + ("" if size is None else f" of {size}"))
+    return a
+
+
+def qllm_kv_reserve_host(book, slots, counts):
+    """Room for counts[i] more tokens in line slots[i]."""
+    slots = _host_list(slots, "slots")
+    counts = _host_list(counts, "counts", slots.size)
+    _chk(_lib.qllm_kv_reserve_host(C.byref(book.c), _hp(slots), _hp(counts), slots.size), "qllm_kv_reserve_host")
+
+
+def qllm_kv_fork_host(book, parents, children):
+    """Line children[i] continues line parents[i]; returns (src, dst), the pages to copy."""
+    parents = _host_list(parents, "parents")
+    children = _host_list(children, "children", parents.size)
+    src, dst = np.empty(parents.size, np.int32), np.empty(parents.size, np.int32)
+    n = int(_lib.qllm_kv_fork_host(C.byref(book.c), _hp(parents), _hp(children), parents.size, _hp(src), _hp(dst)))
+    _chk(n if n < 0 else 0, "qllm_kv_fork_host")
+    return src[:n], dst[:n]
+
+
+def qllm_kv_free_host(book, slots):
+    """Empties the lines."""
+    slots = _host_list(slots, "slots")
+    _chk(_lib.qllm_kv_free_host(C.byref(book.c), _hp(slots), slots.size), "qllm_kv_free_host")
+
+
+def qllm_kv_compact_host(book):
+    """Moves the pages in use together; returns (src, dst), the pages to copy."""
+    src, dst = np.empty(book.refs.size, np.int32), np.empty(book.refs.size, np.int32)
+    n = int(_lib.qllm_kv_compact_host(C.byref(book.c), _hp(src), _hp(dst)))
+    _chk(n if n < 0 else 0, "qllm_kv_compact_host")
+    return src[:n], dst[:n]
 
 
 def qllm_probe_mfma(workgroups, iters, sink, stream=None):

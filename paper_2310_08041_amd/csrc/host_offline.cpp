@@ -130,6 +130,7 @@ const char *qllm_status_string(int32_t status)
     case QLLM_ERR_ALIGN: return "buffer or stride not aligned";
     case QLLM_ERR_WORKSPACE: return "workspace missing or too small";
     case QLLM_ERR_HIP: return "HIP runtime error";
+    case QLLM_ERR_PAGES: return "too few free cache pages, a page number out of range or a clash";
     default: return "unknown status";
     }
 }

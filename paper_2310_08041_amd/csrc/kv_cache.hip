@@ -1,0 +1,358 @@
+// Filling the 4-bit key/value cache (rotary positions, Eq. (2) per token and head), reading it back, copying pages.
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+#include <new>
+
+#include "fused_common.h"
+#include "kv_common.h"
+
+namespace {
+
+using namespace qllm_kv_detail;
+using qllm_detail::FAST_LIMIT;
+
+constexpr int THREADS = 256;
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
+// Eight neighbouring values of a row; vec: they are 16-byte aligned.
+template <bool F32>
+__device__ __forceinline__ void load8(const void *base, int64_t at, bool vec, float (&x)[8])
+{
+    if (F32) {
+        const float *p = static_cast<const float *>(base) + at;
+        if (vec) {
+            const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
+            x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = p[e];
+        }
+    } else {
+        const uint16_t *p = static_cast<const uint16_t *>(base) + at;
+        if (vec) {
+            const uint4 a = *reinterpret_cast<const uint4 *>(p);
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[2 * e] = __uint_as_float(w[e] << 16), x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = __uint_as_float((uint32_t)p[e] << 16);
+        }
+    }
+}
+
+template <bool F32>
+__device__ __forceinline__ void store8(void *base, int64_t at, bool vec, const float (&x)[8])
+{
+    if (F32) {
+        float *p = static_cast<float *>(base) + at;
+        if (vec) {
+            *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<float4 *>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = x[e];
+        }
+    } else {
+        uint16_t *p = static_cast<uint16_t *>(base) + at;
+        const uint4 w = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+        if (vec) {
+            *reinterpret_cast<uint4 *>(p) = w;
+        } else {
+            const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = (uint16_t)(v[e / 2] >> (16 * (e & 1)));
+        }
+    }
+}
+
+struct AppendArgs {
+    Step s;
+    const void *q, *k, *v;
+    void *q_out;
+    int64_t ldq, ldq_out, ldk, ldv;
+    int32_t q_heads, rope, vec;
+    const double *inv_freq;
+};
+
+// The token of a row: its sequence is the last one that begins at or before the row.  false: the row is of none, or of a line
+// outside the table, or lies before the first token.
+__device__ __forceinline__ bool token_of(const Step &s, int32_t row, int32_t *line, int32_t *pos)
+{
+    const int32_t i = s.row_start ? last_not_above(s.n_seqs, row, [&](int32_t k) { return (int64_t)row_of(s, k); }) : row;
+    if (i >= s.n_seqs) return false;
+    const Seq q = seq_of(s, i);
+    const int32_t j = row - q.row;
+    *line = q.line;
+    *pos = q.len - q.n + j;
+    return j >= 0 && j < q.n && q.line >= 0 && *pos >= 0;
+}
+
+// One workgroup per row; D / 8 lanes per head, 8 channels per lane.  The angles of the row are worked out once, by D / 2 lanes,
+// and kept in LDS for all heads.
+template <int D, bool F32>
+__global__ __launch_bounds__(THREADS) void append_kernel(const AppendArgs a)
+{
+    constexpr int LANES = D / 8, PER = THREADS / LANES; // lanes of a head, heads at a time
+    __shared__ float2 turn[D / 2];
+    const Step &s = a.s;
+    const int32_t row = blockIdx.x, tid = threadIdx.x;
+    int32_t line, pos;
+    if (!token_of(s, row, &line, &pos)) return; // the same for the whole workgroup
+    if (a.rope != QLLM_ROPE_NONE) {
+        if (tid < D / 2) {
+            const double angle = (double)pos * a.inv_freq[tid];
+            double sn, cs;
+            sincos(angle, &sn, &cs);
+            turn[tid] = make_float2((float)cs, (float)sn);
+        }
+        __syncthreads();
+    }
+    const int32_t page = page_of(s, line, pos);
+    const int32_t P = 1 << s.page_shift, in_page = pos & (P - 1);
+    const int32_t lane = tid % LANES, q_heads = a.q ? a.q_heads : 0, units = q_heads + 2 * s.heads;
+    const bool vec = a.vec;
+    for (int32_t base = 0; base < units; base += PER) { // lanes beyond the last head go through it too: they take part in the exchanges
+        const int32_t u = base + tid / LANES;
+        const int32_t kind = u < q_heads ? 0 : (u < q_heads + s.heads ? 1 : 2); // query, key, value
+        const int32_t head = kind == 0 ? u : (kind == 1 ? u - q_heads : u - q_heads - s.heads);
+        const bool real = u < units;
+        float x[8] = {};
+        if (real) {
+            const void *src = kind == 0 ? a.q : (kind == 1 ? a.k : a.v);
+            const int64_t ld = kind == 0 ? a.ldq : (kind == 1 ? a.ldk : a.ldv);
+            load8<F32>(src, (int64_t)row * ld + head * D + 8 * lane, vec, x);
+        }
+        if (a.rope == QLLM_ROPE_HALVES) { // the partner's channels sit half the head's lanes away
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float y = __shfl_xor(x[e], LANES / 2);
+                const float2 t = turn[8 * (lane % (LANES / 2)) + e];
+                const double turned = (double)x[e] * (double)t.x, other = (double)y * (double)t.y;
+                if (kind != 2) x[e] = (float)(lane < LANES / 2 ? turned - other : turned + other);
+            }
+        } else if (a.rope == QLLM_ROPE_PAIRS && kind != 2) {
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const float2 t = turn[4 * lane + e / 2];
+                const double x1 = x[e], x2 = x[e + 1], c = t.x, sn = t.y;
+                x[e] = (float)(x1 * c - x2 * sn);
+                x[e + 1] = (float)(x2 * c + x1 * sn);
+            }
+        }
+        // Eq. (2) over the head's channels
+        float lo = x[0], hi = x[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) lo = fminf(lo, x[e]), hi = fmaxf(hi, x[e]);
+#pragma unroll
+        for (int o = LANES / 2; o > 0; o >>= 1) lo = fminf(lo, __shfl_xor(lo, o)), hi = fmaxf(hi, __shfl_xor(hi, o));
+        if (!real) continue;
+        if (kind == 0) {
+            store8<F32>(a.q_out, (int64_t)row * a.ldq_out + head * D + 8 * lane, vec, x);
+            continue;
+        }
+        if (page < 0) continue;
+        float alpha = (hi - lo) * (1.0f / 15.0f);
+        if (!(alpha >= 0x1p-126f)) alpha = 1.0f;
+        const float inv = 1.0f / alpha;
+        const int32_t fast = fabsf(lo * inv) < FAST_LIMIT && fabsf(hi * inv) < FAST_LIMIT;
+        int32_t beta;
+        if (fast) {
+            beta = -qllm_detail::rne_product_fast(lo, inv);
+        } else {
+            const double z = -qllm_detail::rne_product_slow(lo, inv);
+            beta = (int32_t)fmin(fmax(z, -2147483647.0), 2147483647.0);
+        }
+        uint32_t codes = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) codes |= (uint32_t)qllm_detail::quant_code<15>(x[e], inv, beta, fast) << (4 * e);
+        uint8_t *part = s.pages + page * s.page_bytes + (int64_t)head * P * (D + 16);
+        const int32_t value = kind - 1;
+        *reinterpret_cast<uint32_t *>(part + ((int64_t)value * P + in_page) * (D / 2) + 4 * lane) = codes;
+        uint8_t *params = part + (int64_t)P * D + 8 * (int64_t)value * P;
+        if (lane == 0) *reinterpret_cast<float *>(params + 4 * in_page) = alpha;
+        if (lane == 1) *reinterpret_cast<int32_t *>(params + 4 * P + 4 * in_page) = beta;
+    }
+}
+
+struct ReadArgs {
+    Step s;
+    void *k_out, *v_out;
+    int64_t ldk, ldv;
+    int32_t vec;
+};
+
+template <int D, bool F32>
+__global__ __launch_bounds__(THREADS) void read_kernel(const ReadArgs a)
+{
+    constexpr int LANES = D / 8, PER = THREADS / LANES;
+    const Step &s = a.s;
+    const int32_t row = blockIdx.x, tid = threadIdx.x;
+    int32_t line, pos;
+    if (!token_of(s, row, &line, &pos)) return;
+    const int32_t page = page_of(s, line, pos);
+    if (page < 0) return;
+    const int32_t P = 1 << s.page_shift, in_page = pos & (P - 1), lane = tid % LANES;
+    for (int32_t u = tid / LANES; u < 2 * s.heads; u += PER) {
+        const int32_t value = u >= s.heads, head = value ? u - s.heads : u;
+        void *out = value ? a.v_out : a.k_out;
+        if (!out) continue;
+        const uint8_t *part = s.pages + page * s.page_bytes + (int64_t)head * P * (D + 16);
+        const uint32_t codes = *reinterpret_cast<const uint32_t *>(part + ((int64_t)value * P + in_page) * (D / 2) + 4 * lane);
+        const uint8_t *params = part + (int64_t)P * D + 8 * (int64_t)value * P;
+        const double alpha = *reinterpret_cast<const float *>(params + 4 * in_page);
+        const double beta = *reinterpret_cast<const int32_t *>(params + 4 * P + 4 * in_page);
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (float)(alpha * ((double)(codes >> (4 * e) & 15u) - beta));
+        store8<F32>(out, (int64_t)row * (value ? a.ldv : a.ldk) + head * D + 8 * lane, a.vec, x);
+    }
+}
+
+// The pairs travel as kernel arguments: no list in device memory, nothing to upload.
+constexpr int PAIRS = 256;
+struct Pairs {
+    int32_t src[PAIRS], dst[PAIRS];
+};
+
+// 16 bytes a lane and step, four steps of a workgroup in flight; grid: pieces of a page, pairs, layers.
+__global__ __launch_bounds__(THREADS) void copy_pages_kernel(uint8_t *pages, int64_t layer_stride, int64_t page_bytes, const Pairs pairs)
+{
+    uint8_t *layer = pages + (int64_t)blockIdx.z * layer_stride;
+    const uint4 *src = reinterpret_cast<const uint4 *>(layer + (int64_t)pairs.src[blockIdx.y] * page_bytes);
+    uint4 *dst = reinterpret_cast<uint4 *>(layer + (int64_t)pairs.dst[blockIdx.y] * page_bytes);
+    const int64_t words = page_bytes / 16, at = (int64_t)blockIdx.x * THREADS * 4 + threadIdx.x;
+    if (at + 3 * THREADS < words) {
+        const uint4 x0 = src[at], x1 = src[at + THREADS], x2 = src[at + 2 * THREADS], x3 = src[at + 3 * THREADS];
+        dst[at] = x0, dst[at + THREADS] = x1, dst[at + 2 * THREADS] = x2, dst[at + 3 * THREADS] = x3;
+    } else {
+        for (int64_t i = at; i < words; i += THREADS) dst[i] = src[i];
+    }
+}
+
+// Rows of 16-byte accesses; else QLLM_ERR_ALIGN where a row misses its own type's alignment.
+int32_t row_access(int32_t dtype, const void *const *ptrs, const int64_t *lds, int n, int32_t *vec)
+{
+    const int64_t size = dtype == QLLM_F32 ? 4 : 2;
+    uintptr_t bits = 0;
+    for (int i = 0; i < n; ++i)
+        if (ptrs[i]) {
+            if (reinterpret_cast<uintptr_t>(ptrs[i]) & (uintptr_t)(size - 1)) return QLLM_ERR_ALIGN;
+            bits |= reinterpret_cast<uintptr_t>(ptrs[i]) | (uintptr_t)(lds[i] * size);
+        }
+    *vec = (bits & 15u) == 0;
+    return QLLM_OK;
+}
+
+} // namespace
+
+extern "C" int32_t qllm_kv_append(const void *q, int64_t ldq, int64_t q_heads, void *q_out, int64_t ldq_out, const void *k, int64_t ldk,
+                                  const void *v, int64_t ldv, int32_t x_dtype, int32_t rope, const double *inv_freq,
+                                  const qllm_kv_cache *cache, const qllm_kv_batch *batch, void *hip_stream)
+{
+    AppendArgs a;
+    const int32_t rc = prepare_step(cache, batch, true, &a.s);
+    if (rc != QLLM_OK) return rc;
+    const bool some = batch->rows > 0; // an empty tensor has no address
+    if (some && (!k || !v)) return QLLM_ERR_NULL;
+    if ((x_dtype != QLLM_F32 && x_dtype != QLLM_BF16) || rope < QLLM_ROPE_NONE || rope > QLLM_ROPE_PAIRS) return QLLM_ERR_DTYPE;
+    if ((some && !q != !q_out) || (rope != QLLM_ROPE_NONE && !inv_freq)) return QLLM_ERR_NULL;
+    const int64_t width = cache->heads * cache->dim;
+    if (ldk < width || ldv < width) return QLLM_ERR_SHAPE;
+    if (q && (q_heads <= 0 || q_heads > (1 << 16) || ldq < q_heads * cache->dim || ldq_out < q_heads * cache->dim)) return QLLM_ERR_SHAPE;
+    if (reinterpret_cast<uintptr_t>(inv_freq) & 7u) return QLLM_ERR_ALIGN;
+    const void *ptrs[4] = {q, q_out, k, v};
+    const int64_t lds[4] = {ldq, ldq_out, ldk, ldv};
+    const int32_t ra = row_access(x_dtype, ptrs, lds, 4, &a.vec);
+    if (ra != QLLM_OK) return ra;
+    if (batch->rows == 0 || batch->n_seqs == 0) return QLLM_OK;
+    a.q = q, a.k = k, a.v = v, a.q_out = q_out;
+    a.ldq = ldq, a.ldq_out = ldq_out, a.ldk = ldk, a.ldv = ldv;
+    a.q_heads = (int32_t)q_heads, a.rope = rope, a.inv_freq = inv_freq;
+    const dim3 grid((unsigned)(batch->row_start ? batch->rows : batch->n_seqs));
+    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();
+    if (cache->dim == 128) {
+        if (x_dtype == QLLM_F32) hipLaunchKernelGGL((append_kernel<128, true>), grid, dim3(THREADS), 0, stream, a);
+        else hipLaunchKernelGGL((append_kernel<128, false>), grid, dim3(THREADS), 0, stream, a);
+    } else {
+        if (x_dtype == QLLM_F32) hipLaunchKernelGGL((append_kernel<64, true>), grid, dim3(THREADS), 0, stream, a);
+        else hipLaunchKernelGGL((append_kernel<64, false>), grid, dim3(THREADS), 0, stream, a);
+    }
+    return launched("cache append: launch");
+}
+
+extern "C" int32_t qllm_kv_read(const qllm_kv_cache *cache, const qllm_kv_batch *batch, void *k_out, int64_t ldk, void *v_out, int64_t ldv,
+                                int32_t dtype, void *hip_stream)
+{
+    ReadArgs a;
+    const int32_t rc = prepare_step(cache, batch, true, &a.s);
+    if (rc != QLLM_OK) return rc;
+    if (dtype != QLLM_F32 && dtype != QLLM_BF16) return QLLM_ERR_DTYPE;
+    const int64_t width = cache->heads * cache->dim;
+    if ((k_out && ldk < width) || (v_out && ldv < width)) return QLLM_ERR_SHAPE;
+    const void *ptrs[2] = {k_out, v_out};
+    const int64_t lds[2] = {ldk, ldv};
+    const int32_t ra = row_access(dtype, ptrs, lds, 2, &a.vec);
+    if (ra != QLLM_OK) return ra;
+    if (batch->rows == 0 || batch->n_seqs == 0 || (!k_out && !v_out)) return QLLM_OK;
+    a.k_out = k_out, a.v_out = v_out, a.ldk = ldk, a.ldv = ldv;
+    const dim3 grid((unsigned)(batch->row_start ? batch->rows : batch->n_seqs));
+    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();
+    if (cache->dim == 128) {
+        if (dtype == QLLM_F32) hipLaunchKernelGGL((read_kernel<128, true>), grid, dim3(THREADS), 0, stream, a);
+        else hipLaunchKernelGGL((read_kernel<128, false>), grid, dim3(THREADS), 0, stream, a);
+    } else {
+        if (dtype == QLLM_F32) hipLaunchKernelGGL((read_kernel<64, true>), grid, dim3(THREADS), 0, stream, a);
+        else hipLaunchKernelGGL((read_kernel<64, false>), grid, dim3(THREADS), 0, stream, a);
+    }
+    return launched("cache read: launch");
+}
+
+extern "C" int32_t qllm_kv_copy_pages(uint8_t *pages, int64_t n_layers, int64_t layer_stride, int64_t n_pages, int64_t page_bytes,
+                                      const int32_t *src_host, const int32_t *dst_host, int64_t n, void *hip_stream)
+{
+    if (!pages || (n > 0 && (!src_host || !dst_host))) return QLLM_ERR_NULL;
+    if (n < 0 || n_layers < 0 || n_layers > 65535 || n_pages <= 0 || n_pages > INT32_MAX || page_bytes <= 0 || page_bytes > (1ll << 40)) return QLLM_ERR_SHAPE;
+    if (n_layers > 1 && layer_stride / page_bytes < n_pages) return QLLM_ERR_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(pages) & 15u) || (page_bytes & 15) || (n_layers > 1 && (layer_stride & 15))) return QLLM_ERR_ALIGN;
+    if (n == 0 || n_layers == 0) return QLLM_OK;
+    if (n > n_pages) return QLLM_ERR_PAGES; // some page is copied to twice
+    for (int64_t i = 0; i < n; ++i)
+        if (src_host[i] < 0 || src_host[i] >= n_pages || dst_host[i] < 0 || dst_host[i] >= n_pages) return QLLM_ERR_PAGES;
+    uint8_t *marks = new (std::nothrow) uint8_t[(size_t)n_pages]();
+    if (!marks) return QLLM_ERR_WORKSPACE;
+    bool clash = false;
+    for (int64_t i = 0; i < n; ++i) {
+        clash |= marks[dst_host[i]] != 0;
+        marks[dst_host[i]] = src_host[i] == dst_host[i] ? 1 : 2; // 2: written to
+    }
+    for (int64_t i = 0; i < n; ++i) clash |= src_host[i] != dst_host[i] && marks[src_host[i]] == 2;
+    delete[] marks;
+    if (clash) return QLLM_ERR_PAGES;
+    const int64_t pieces = (page_bytes / 16 + THREADS * 4 - 1) / (THREADS * 4);
+    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();
+    int64_t at = 0;
+    while (at < n) {
+        Pairs p = {};
+        int m = 0;
+        for (; at < n && m < PAIRS; ++at)
+            if (src_host[at] != dst_host[at]) p.src[m] = src_host[at], p.dst[m] = dst_host[at], ++m;
+        if (!m) break;
+        hipLaunchKernelGGL(copy_pages_kernel, dim3((unsigned)pieces, (unsigned)m, (unsigned)n_layers), dim3(THREADS), 0, stream, pages, layer_stride,
+                           page_bytes, p);
+        const int32_t rc = launched("cache pages: copy");
+        if (rc != QLLM_OK) return rc;
+    }
+    return QLLM_OK;
+}

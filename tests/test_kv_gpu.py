@@ -1,0 +1,453 @@
+"""The 4-bit key/value cache on the device against its numpy statement: pages bit for bit, attention within bounds that come from
+the roundings it makes (see `tolerance`)."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def b():
+    import torch
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    from paper_2310_08041_amd import binding
+    return binding
+
+
+def _t(a, dtype=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(dtype)
+
+
+def _bf16(x):
+    """The float32 values that bfloat16 tensors of x hold."""
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(x, np.float32)).to(torch.bfloat16).float().numpy()
+
+
+def _heads_like(rng, rows, heads, dim):
+    """Roughly normal, with channels that are large for every token, zero vectors, constant and one-sided ones among them."""
+    x = rng.standard_normal((rows, heads, dim)).astype(np.float32)
+    x[..., rng.integers(0, dim, 2)] *= 20.0
+    if rows > 3:
+        x[0] = 0.0
+        x[1, :, :] = 0.75
+        x[2] = np.abs(x[2]) + 30.0
+    return x
+
+
+class Made:
+    pass
+
+
+def make(rng, heads, group, dim, page, lengths, new, slots=None, n_lines=None, rows=None, spare=3, extra_cols=1, garbage=0xFF, filled=True):
+    """A cache of one layer with every token of every line quantized into scattered pages; what no token owns holds `garbage`
+    bytes (NaN as alpha)."""
+    from oracle import kv_cache as okv
+    c = Made()
+    c.heads, c.group, c.dim, c.page = heads, group, dim, page
+    n = len(lengths)
+    n_lines = n if n_lines is None else n_lines
+    c.slot = None if slots is None else np.asarray(slots, np.int32)
+    line_of = list(range(n)) if slots is None else list(slots)
+    c.length = np.zeros(n_lines, np.int32)
+    for i, l in zip(line_of, lengths):
+        if 0 <= i < n_lines:
+            c.length[i] = l
+    need = -(-c.length // page)
+    c.n_pages = int(need.sum()) + spare
+    order = rng.permutation(c.n_pages).astype(np.int32)
+    c.table = np.full((n_lines, max(1, int(need.max()) + extra_cols)), -1, np.int32)
+    at = 0
+    for i in range(n_lines):
+        c.table[i, :need[i]] = order[at:at + need[i]]
+        at += need[i]
+    c.row_start = None if new is None else np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    c.rows = rows if rows is not None else (n if new is None else int(sum(new)))
+    raw = np.full((c.n_pages, heads * page * (dim + 16)), garbage, np.uint8)
+    c.pages = okv.Pages(raw, heads, dim, page)
+    if filled:
+        for i in range(n_lines):
+            l = int(c.length[i])
+            if l:
+                tok = [(r, i, r) for r in range(l)]
+                okv.append(c.pages, c.table, tok, _heads_like(rng, l, heads, dim), _heads_like(rng, l, heads, dim))
+    c.tokens = okv.rows_of(c.rows, c.row_start, c.slot, c.length)
+    return c
+
+
+def on_device(b, c):
+    cache = b.DeviceKVCache(1, c.n_pages, c.heads, c.dim, c.page, pages=_t(c.pages.raw)[None])
+    batch = b.DeviceKVBatch(c.rows, _t(c.table), _t(c.length), None if c.row_start is None else _t(c.row_start),
+                            None if c.slot is None else _t(c.slot))
+    return cache, batch
+
+
+APPEND = [  # dtype, rope, heads, group, dim, page, lengths, new rows, far
+    ("bf16", 1, 2, 4, 128, 64, [1, 64, 65, 200], [1, 64, 3, 130], 0),
+    ("bf16", 2, 3, 1, 64, 32, [33, 32, 31], [33, 1, 0], 0),
+    ("bf16", 0, 1, 7, 128, 256, [300], [300], 0),
+    ("f32", 1, 1, 3, 64, 128, [129, 5], [129, 5], 0),
+    ("f32", 2, 5, 2, 128, 32, [40, 1, 1, 96], None, 0),
+    ("bf16", 1, 40, 1, 128, 64, [17, 100], None, 0),
+    ("f32", 1, 1, 1, 128, 32, [1000000], [40], 1000000),                 # far positions: the angle needs its 64 bits
+]
+
+
+@pytest.mark.parametrize("dtype,rope,heads,group,dim,page,lengths,new,far", APPEND)
+def test_append_writes_the_pages_of_the_definition(oracle, b, dtype, rope, heads, group, dim, page, lengths, new, far):
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(hash((rope, heads, dim, page)) % 1000)
+    if far:
+        c = make(rng, heads, group, dim, page, [64], new, filled=False)
+        # the line holds a million tokens, of which only the last pages are there
+        cols = -(-far // page)
+        c.table = np.full((1, cols), -1, np.int32)
+        c.table[0, cols - 3:] = [2, 0, 1]
+        c.length[0] = far
+        c.tokens = okv.rows_of(c.rows, c.row_start, c.slot, c.length)
+    else:
+        c = make(rng, heads, group, dim, page, lengths, new, filled=False, rows=None if new is None else sum(new) + 2)
+    td = torch.bfloat16 if dtype == "bf16" else torch.float32
+    hq = heads * group
+    qkv = _heads_like(rng, c.rows, hq + 2 * heads, dim)
+    if dtype == "bf16":
+        qkv = _bf16(qkv)
+    inv_freq = 10000.0 ** (-np.arange(0, dim, 2) / dim)
+    cache, batch = on_device(b, c)
+    x = _t(qkv.reshape(c.rows, -1), td)
+    q, k, v = x[:, :hq * dim], x[:, hq * dim:(hq + heads) * dim], x[:, (hq + heads) * dim:]
+    q_out = torch.full((c.rows, hq * dim), 3.0, dtype=td, device="cuda")
+    b.qllm_kv_append(cache, 0, batch, k, v, q=q, q_out=q_out, rope=rope, inv_freq=_t(inv_freq) if rope else None)
+    k_out, v_out = (torch.full((c.rows, heads * dim), 3.0, dtype=td, device="cuda") for _ in range(2))
+    b.qllm_kv_read(cache, 0, batch, k_out, v_out)
+    torch.cuda.synchronize()
+
+    positions = np.zeros(c.rows)
+    owned = np.zeros(c.rows, bool)
+    for r, _, p in c.tokens:
+        positions[r], owned[r] = p, True
+    turned = okv.rotate(qkv[:, :hq + heads], positions, inv_freq, rope)
+    okv.append(c.pages, c.table, c.tokens, turned[:, hq:], qkv[:, hq + heads:])
+    assert np.array_equal(cache.pages[0].cpu().numpy(), c.pages.raw)               # every byte, those of no token too
+    want_q = np.where(owned[:, None, None], _bf16(turned[:, :hq]) if dtype == "bf16" else turned[:, :hq], 3.0)
+    assert np.array_equal(q_out.float().cpu().numpy().reshape(want_q.shape), want_q.astype(np.float32))
+    for value, out in ((0, k_out), (1, v_out)):
+        want = np.full((c.rows, heads, dim), 3.0)
+        for r, line, p in c.tokens:
+            pg = okv.page_at(c.table, c.n_pages, page, line, p)
+            if pg >= 0:
+                for h in range(heads):
+                    want[r, h] = c.pages.get(pg, h, p % page, value)[0]
+        want = want.astype(np.float32)
+        assert np.array_equal(out.float().cpu().numpy().reshape(want.shape), _bf16(want) if dtype == "bf16" else want)
+
+
+def test_append_takes_rows_of_any_stride_and_alignment_and_rotates_in_place(oracle, b):
+    """Rows that miss 16-byte alignment, q rotated in place, no q at all: the same pages."""
+    import torch
+    rng = np.random.default_rng(5)
+    heads, group, dim, page = 2, 2, 64, 32
+    c = make(rng, heads, group, dim, page, [50, 7], [20, 7], filled=False)
+    qkv = _bf16(_heads_like(rng, c.rows, heads * group + 2 * heads, dim)).reshape(c.rows, -1)
+    f = _t(10000.0 ** (-np.arange(0, dim, 2) / dim))
+    wq, wk = heads * group * dim, heads * dim
+    got = []
+    for pad, off in ((0, 0), (8, 8), (3, 1), (1, 5)):
+        cache, batch = on_device(b, c)
+        buf = torch.zeros((c.rows, wq + 2 * wk + pad + off), dtype=torch.bfloat16, device="cuda")
+        x = buf[:, off:off + wq + 2 * wk]
+        x.copy_(_t(qkv))
+        q, k, v = x[:, :wq], x[:, wq:wq + wk], x[:, wq + wk:]
+        b.qllm_kv_append(cache, 0, batch, k, v, q=q, q_out=q, rope=1, inv_freq=f)
+        alone, _ = on_device(b, c)
+        b.qllm_kv_append(alone, 0, batch, k, v, rope=1, inv_freq=f)
+        assert torch.equal(alone.pages, cache.pages)
+        out = torch.zeros((c.rows, wk + pad + off), dtype=torch.bfloat16, device="cuda")
+        b.qllm_kv_read(cache, 0, batch, v_out=out[:, off:off + wk])
+        got.append((cache.pages.clone(), q.clone(), out[:, off:off + wk].clone()))
+    for other in got[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(got[0], other))
+
+
+def test_append_skips_what_is_not_there(oracle, b):
+    """Lines outside the table, pages outside the cache, tokens before the first and behind the line's end: nothing is written for
+    them, the others are as ever."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(6)
+    heads, dim, page = 2, 128, 32
+    c = make(rng, heads, 1, dim, page, [40, 33, 70, 10, 64], [5, 33, 4, 12, 40], slots=[4, -1, 7, 2, 1], n_lines=5, filled=False, rows=100, extra_cols=0)
+    c.length[1] = 90                                        # longer than its line's pages
+    c.table[4, 1] = c.n_pages                               # outside the cache
+    c.table[1, 0] = -7
+    c.tokens = okv.rows_of(c.rows, c.row_start, c.slot, c.length)
+    kv = _heads_like(rng, c.rows, 2 * heads, dim)
+    cache, batch = on_device(b, c)
+    b.qllm_kv_append(cache, 0, batch, _t(kv[:, :heads].reshape(c.rows, -1)), _t(kv[:, heads:].reshape(c.rows, -1)))
+    out = torch.full((c.rows, heads * dim), 9.0, device="cuda")
+    b.qllm_kv_read(cache, 0, batch, out)
+    okv.append(c.pages, c.table, c.tokens, kv[:, :heads], kv[:, heads:])
+    assert np.array_equal(cache.pages[0].cpu().numpy(), c.pages.raw)
+    there = {r for r, line, p in c.tokens if okv.page_at(c.table, c.n_pages, page, line, p) >= 0}
+    assert 0 < len(there) < c.rows
+    kept = (out == 9.0).all(1).cpu().numpy()
+    assert [r for r in range(c.rows) if not kept[r]] == sorted(there)
+
+
+# ---------------------------------------------------------------- attention
+
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}                 # half a step, relative
+
+
+def tolerance(want, absv, err_s, err_o, q_type, out_type):
+    """Roundings, element by element: the output's own; that of every weight p alpha before it meets the values (bf16 for bf16
+    queries, 24 bits for fp32 ones), the same rounded number standing in both sums; the scores' fp32 error, which moves weights
+    and their sum by at most e^E - 1 each; the fp32 sums."""
+    p = HALF[q_type]
+    return HALF[out_type] * (np.abs(want) + p * absv) * (1 + 2.0 ** -7) + p * absv + 2.0 * np.expm1(err_s) * absv + 2.0 * err_o + 1e-30
+
+
+ATTEND = [  # q, out, heads, group, dim, page, lengths, new rows, window, slots, lines, rows behind the last
+    ("bf16", "bf16", 2, 1, 128, 64, [1], None, 0, None, None, 0),
+    ("bf16", "bf16", 1, 8, 128, 64, [1, 31, 32, 33, 64, 500], None, 0, None, None, 0),
+    ("bf16", "f32", 2, 3, 64, 32, [40, 129, 7], None, 0, [2, 0, 3], 4, 0),
+    ("bf16", "bf16", 1, 17, 128, 128, [130, 257], None, 0, None, None, 0),         # more query heads than a tile has rows
+    ("bf16", "bf16", 2, 2, 128, 32, [70, 5, 64], [70, 5, 64], 0, None, None, 3),   # whole prompts, rows of padding
+    ("bf16", "bf16", 1, 4, 128, 64, [300, 90, 0, 12], [33, 1, 0, 12], 0, None, None, 0),
+    ("bf16", "bf16", 1, 5, 64, 32, [200, 77], [100, 3], 50, None, None, 1),        # a window
+    ("bf16", "bf16", 1, 1, 128, 32, [400], None, 1, None, None, 0),                # a window of the token itself
+    ("f32", "f32", 2, 3, 64, 32, [150, 40], [60, 40], 0, None, None, 0),
+    ("f32", "f32", 1, 2, 128, 64, [333, 1, 65], None, 100, None, None, 0),
+    ("f32", "bf16", 1, 1, 128, 256, [270], [270], 0, None, None, 0),
+    ("bf16", "f32", 1, 3, 128, 64, [3, 5], [5, 2], 0, None, None, 0),              # more new rows than tokens: rows that see nothing
+    ("bf16", "bf16", 1, 8, 128, 64, [1500, 2100], None, 0, None, None, 0),         # long enough to be split
+    ("bf16", "bf16", 1, 2, 128, 64, [700], [300], 0, None, None, 0),               # a chunk of a prompt, several tiles
+    ("bf16", "bf16", 2, 1, 64, 32, [330, 140], [140, 140], 90, None, None, 0),
+]
+
+
+@pytest.mark.parametrize("q_type,out_type,heads,group,dim,page,lengths,new,window,slots,lines,tail", ATTEND)
+def test_attention_within_the_bounds_of_its_roundings(oracle, b, q_type, out_type, heads, group, dim, page, lengths, new, window, slots, lines, tail):
+    import torch
+    from oracle import kv_cache as okv
+    types = {"bf16": torch.bfloat16, "f32": torch.float32}
+    rng = np.random.default_rng(sum(lengths) + 7 * dim + window)
+    n_rows = (len(lengths) if new is None else sum(new)) + tail
+    c = make(rng, heads, group, dim, page, lengths, new, slots=slots, n_lines=lines, rows=n_rows)
+    q = rng.standard_normal((c.rows, heads * group, dim)).astype(np.float32)
+    q = _bf16(q) if q_type == "bf16" else q
+    scale = 1.0 / np.sqrt(dim)
+    cache, batch = on_device(b, c)
+    out = torch.full((c.rows, heads * group * dim), 5.0, dtype=types[out_type], device="cuda")
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), types[q_type]), cache, 0, batch, scale, out, ws, window=window)
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(scale), window, out=np.full(q.shape, 5.0))
+    got = out.double().cpu().numpy().reshape(want.shape)
+    assert np.isfinite(got).all()
+    tol = tolerance(want, *bounds, q_type, out_type)
+    for r in set(range(c.rows)) - {t[0] for t in c.tokens}:
+        assert (got[r] == 5.0).all()                          # rows of no sequence
+    worst = np.abs(got - want) / tol
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+def test_attention_does_not_see_tokens_that_are_not_there(oracle, b):
+    """Pages outside the cache, lines outside the table, a length beyond the line: as if those tokens did not exist."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(8)
+    c = make(rng, 1, 4, 128, 32, [200, 64, 50, 100, 96], [3, 2, 4, 5, 1], slots=[3, 5, 0, -1, 2], n_lines=4, extra_cols=0)
+    c.table[3, 2], c.table[3, 4], c.table[0, 0], c.table[0, 1] = -1, c.n_pages + 3, 1 << 30, -(1 << 31)
+    c.length[2] = 200                                         # its line has room for fewer
+    c.tokens = okv.rows_of(c.rows, c.row_start, c.slot, c.length)
+    q = _bf16(rng.standard_normal((c.rows, 4, 128)).astype(np.float32))
+    cache, batch = on_device(b, c)
+    out = torch.full((c.rows, 512), 5.0, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, 4), dtype=torch.uint8, device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), torch.bfloat16), cache, 0, batch, 0.1, out, ws)
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.1))
+    got = out.double().cpu().numpy().reshape(want.shape)
+    assert (np.abs(got - want) <= tolerance(want, *bounds, "bf16", "bf16")).all()
+    assert (want[3:5] == 0).all() and (want[5:9] == 0).all()  # a line outside the table, a line without pages: zeros
+
+
+def test_attention_reaches_pages_beyond_32_bits(oracle, b):
+    """Pages that lie more than 2^32 bytes into the cache: append, read and attention give what they give at its start."""
+    import torch
+    rng = np.random.default_rng(9)
+    heads, dim, page = 8, 128, 256
+    page_bytes = b.qllm_kv_page_bytes(heads, dim, page)
+    n_pages = (1 << 32) // page_bytes + 8
+    pages = torch.empty((1, n_pages, page_bytes), dtype=torch.uint8, device="cuda")
+    cache = b.DeviceKVCache(1, n_pages, heads, dim, page, pages=pages)
+    kv = _t(_heads_like(rng, 300, 2 * heads, dim).reshape(300, -1), torch.bfloat16)
+    q = torch.randn((300, 16 * dim), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(torch.bfloat16)
+    got = []
+    for table in ([[0, 1]], [[n_pages - 1, (1 << 32) // page_bytes + 1]]):
+        batch = b.DeviceKVBatch(300, _t(np.array(table, np.int32)), _t(np.array([300], np.int32)), _t(np.array([0, 300], np.int32)))
+        b.qllm_kv_append(cache, 0, batch, kv[:, :heads * dim], kv[:, heads * dim:])
+        out, back = torch.empty_like(q), torch.empty((300, heads * dim), device="cuda")
+        ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, 16), dtype=torch.uint8, device="cuda")
+        b.qllm_kv_attention(q, cache, 0, batch, 0.1, out, ws)
+        b.qllm_kv_read(cache, 0, batch, back)
+        got.append((out, back))
+        pages[:, :2].fill_(0xFF)                                 # not to be found by the second round
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and torch.isfinite(got[0][0]).all()
+
+
+@pytest.mark.parametrize("layers,n_pages,heads,dim,page,n", [(1, 5, 1, 64, 32, 1), (3, 40, 2, 128, 64, 17), (2, 900, 1, 64, 32, 600)])
+def test_copying_pages_in_every_layer(b, layers, n_pages, heads, dim, page, n):
+    import torch
+    rng = np.random.default_rng(n)
+    raw = rng.integers(0, 256, (layers, n_pages, heads * page * (dim + 16)), dtype=np.uint8)
+    cache = b.DeviceKVCache(layers, n_pages, heads, dim, page, pages=_t(raw))
+    places = rng.permutation(n_pages)
+    dst, src = places[:n], rng.choice(places[n:], n)              # a source may be copied more than once
+    dst, src = np.append(dst, places[n]), np.append(src, places[n])
+    b.qllm_kv_copy_pages(cache, src, dst)
+    raw[:, dst] = raw[:, src]
+    assert np.array_equal(cache.pages.cpu().numpy(), raw)
+    b.qllm_kv_copy_pages(cache, [], [])
+
+
+def _step(b, c, rng, book, cache, slots, n, hq, layers):
+    """One step of a serving loop through every layer: room, append, attention.  Returns the layers' outputs."""
+    import torch
+    if n:
+        b.qllm_kv_reserve_host(book, slots, [n] * len(slots))
+    rows = max(n, 1) * len(slots)
+    start = np.arange(len(slots) + 1, dtype=np.int32) * max(n, 1)
+    batch = b.DeviceKVBatch(rows, _t(book.table), _t(book.length), _t(start), _t(np.asarray(slots, np.int32)))
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, hq), dtype=torch.uint8, device="cuda")
+    outs = []
+    for layer in range(layers):
+        x = _t(rng.standard_normal((rows, (hq + 2 * cache.heads) * cache.dim)).astype(np.float32), torch.bfloat16)
+        q, k, v = x.split([hq * cache.dim, cache.heads * cache.dim, cache.heads * cache.dim], 1)
+        if n:
+            b.qllm_kv_append(cache, layer, batch, k, v, q=q, q_out=q, rope=1, inv_freq=c)
+        out = torch.empty((rows, hq * cache.dim), dtype=torch.bfloat16, device="cuda")
+        outs.append(b.qllm_kv_attention(q, cache, layer, batch, cache.dim ** -0.5, out, ws))
+    return outs
+
+
+def test_a_serving_loop_with_forks_and_compaction(b):
+    """Prompts, tokens, continuations that share pages, requests that end, pages that move together: what attention gives depends on
+    none of it.  A second cache plays the same loop without sharing and without moving."""
+    import torch
+    heads, hq, dim, page, layers = 2, 6, 128, 32, 2
+    f = _t(10000.0 ** (-np.arange(0, dim, 2) / dim))
+    r1, r2 = np.random.default_rng(11), np.random.default_rng(11)
+    book, cache = b.KVBook.empty(6, 12, 40, page), b.DeviceKVCache(layers, 40, heads, dim, page)
+    plain, other = b.KVBook.empty(6, 12, 80, page), b.DeviceKVCache(layers, 80, heads, dim, page)
+    step = lambda bk, ca, rng, slots, n: _step(b, f, rng, bk, ca, slots, n, hq, layers)
+    both = lambda slots, n: [torch.equal(x, y) for x, y in zip(step(book, cache, r1, slots, n), step(plain, other, r2, slots, n))]
+    assert all(both([0, 1, 2], 70))                                     # prompts
+    assert all(both([2, 0, 1], 1))
+    # line 3 and 4 continue line 1, line 5 line 2; the other cache gets whole copies
+    src, dst = b.qllm_kv_fork_host(book, [1, 1, 2], [3, 4, 5])
+    b.qllm_kv_copy_pages(cache, src, dst)
+    assert src.size == 3 and (book.refs > 1).any()
+    for child, parent in ((3, 1), (4, 1), (5, 2)):
+        n = int(plain.length[parent])
+        b.qllm_kv_reserve_host(plain, [child], [n])
+        k = -(-n // page)
+        b.qllm_kv_copy_pages(other, plain.table[parent, :k], plain.table[child, :k])
+    for _ in range(3):
+        assert all(both([5, 1, 3, 4, 0, 2], 1))
+    assert all(both([3, 4], 33))
+    for bk in (book, plain):
+        b.qllm_kv_free_host(bk, [0, 1])
+    src, dst = b.qllm_kv_compact_host(book)
+    assert src.size and (book.table < (book.refs > 0).sum()).all()
+    b.qllm_kv_copy_pages(cache, src, dst)
+    assert all(both([2, 3, 4, 5], 0))                                   # queries only, nothing appended
+    assert all(both([2, 3, 4, 5], 1))
+    b.qllm_kv_free_host(book, [2, 3, 4, 5])
+    assert not book.refs.any() and (book.table == -1).all() and not book.length.any()
+
+
+def test_calls_on_other_streams_and_two_at_once(oracle, b):
+    """Two steps in flight on two streams, each with its own workspace, give what they give one after the other."""
+    import torch
+    rng = np.random.default_rng(12)
+    made = [make(rng, 2, 4, 128, 64, [900, 300, 650], None), make(rng, 2, 4, 128, 64, [800, 70], [60, 70])]
+    work = []
+    for c in made:
+        cache, batch = on_device(b, c)
+        q = _t(rng.standard_normal((c.rows, 8 * 128)).astype(np.float32), torch.bfloat16)
+        ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, 8), dtype=torch.uint8, device="cuda")
+        work.append((cache, batch, q, ws))
+    alone = [b.qllm_kv_attention(q, ca, 0, ba, 0.1, torch.empty_like(q), ws) for ca, ba, q, ws in work]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in work]
+    for _ in range(5):
+        outs = [torch.full_like(q, 9.0) for _, _, q, _ in work]
+        torch.cuda.synchronize()
+        for (ca, ba, q, ws), s, o in zip(work, streams, outs):
+            b.qllm_kv_attention(q, ca, 0, ba, 0.1, o, ws, stream=s)
+            with torch.cuda.stream(s):
+                b.qllm_kv_attention(q, ca, 0, ba, 0.1, o, ws)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(alone, outs))
+
+
+def test_a_decode_step_replayed_as_a_graph(oracle, b):
+    """Append and attention captured once; lengths and rows change between the replays, other work runs in between, a second graph
+    shares the workspace."""
+    import torch
+    rng = np.random.default_rng(13)
+    heads, hq, dim, page = 2, 8, 128, 64
+    c = make(rng, heads, 4, dim, page, [500, 63, 64, 1200], None, extra_cols=2, spare=20)
+    c.table[:, -2:] = np.arange(c.n_pages - 8, c.n_pages, dtype=np.int32).reshape(4, 2)
+    for i in range(4):                                                        # the next pages right behind the present ones
+        k = -(-int(c.length[i]) // page)
+        c.table[i, k:k + 2] = c.table[i, -2:].copy()
+    cache, batch = on_device(b, c)
+    eager, ebatch = on_device(b, c)
+    f = _t(10000.0 ** (-np.arange(0, dim, 2) / dim))
+    x = torch.zeros((4, (hq + 2 * heads) * dim), dtype=torch.bfloat16, device="cuda")
+    q, k, v = x.split([hq * dim, heads * dim, heads * dim], 1)
+    q_out, out = torch.zeros((4, hq * dim), dtype=torch.bfloat16, device="cuda"), torch.zeros((4, hq * dim), dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, hq), dtype=torch.uint8, device="cuda")
+
+    def step(ca, ba, qo, o):
+        b.qllm_kv_append(ca, 0, ba, k, v, q=q, q_out=qo, rope=1, inv_freq=f)
+        b.qllm_kv_attention(qo, ca, 0, ba, 0.09, o, ws)
+
+    fresh = lambda: x.copy_(_t(rng.standard_normal(x.shape).astype(np.float32)))
+    fresh()
+    q2, o2 = torch.empty_like(q_out), torch.empty_like(out)
+    step(cache, batch, q_out, out)                                            # loads the kernels before the capture
+    step(eager, ebatch, q2, o2)
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step(cache, batch, q_out, out)
+        graphs.append(g)
+    for i in range(6):
+        fresh()
+        batch.length.add_(1), ebatch.length.add_(1)
+        graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        step(eager, ebatch, q2, o2)
+        (torch.randn(1000, device="cuda") * 2).sum().item()
+        assert torch.equal(q2, q_out) and torch.equal(o2, out) and torch.equal(cache.pages, eager.pages)
+
+
+def test_empty_steps_are_no_ops(b):
+    import torch
+    cache = b.DeviceKVCache(1, 4, 2, 64, 32)
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    for batch in (b.DeviceKVBatch(0, i32(0, 1)[None], i32(5), i32(0)), b.DeviceKVBatch(0, i32(0, 1)[None], i32(5), i32(0, 0)),
+                  b.DeviceKVBatch(3, i32(0, 1)[None], i32(5), i32(0))):
+        x = torch.full((batch.rows, 128), 2.0, device="cuda")
+        ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, 2), dtype=torch.uint8, device="cuda")
+        b.qllm_kv_append(cache, 0, batch, x, x)
+        b.qllm_kv_read(cache, 0, batch, x)
+        b.qllm_kv_attention(x, cache, 0, batch, 1.0, x, ws)
+        assert (x == 2.0).all() and not cache.pages.any()
