@@ -35,6 +35,9 @@ struct AttendArgs {
     int64_t ldq, ldo;
     int32_t q_heads, group, window; // window 0: none
     float scale2;                   // scale * log2 e
+    int32_t splits;                 // workgroups that may share a tile's tokens
+    float *part_o;                  // their partial results, see partial_at
+    float2 *part_ml;
 };
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
@@ -42,19 +45,27 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
-// 16 + code of nibble i (0..3) of both halves of w, as a pair of bf16
-template <int I>
-__device__ __forceinline__ uint32_t pair16(uint32_t w)
-{
-    const uint32_t t = I == 0 ? w << 3 : w >> (4 * I - 3);
-    return (t & 0x00780078u) | 0x41804180u;
-}
-
-// 8 codes of a dword as a matrix-core operand: elements are codes 0, 4, 1, 5, 2, 6, 3, 7
-__device__ __forceinline__ bf16x8 operand16(uint32_t w)
-{
-    return __builtin_bit_cast(bf16x8, u32x4{pair16<0>(w), pair16<1>(w), pair16<2>(w), pair16<3>(w)});
-}
+// 16 + code of nibble i (0..3) of both halves of w, as a pair of bf16.  The two constants are kept in registers, unknown to the
+// compiler: only then are "and" and "or" one instruction (a literal for each makes them two).
+struct Codes16 {
+    uint32_t mask, sixteen;
+    __device__ __forceinline__ Codes16()
+    {
+        asm("v_mov_b32 %0, 0x780078" : "=v"(mask));
+        asm("v_mov_b32 %0, 0x41804180" : "=v"(sixteen));
+    }
+    template <int I>
+    __device__ __forceinline__ uint32_t pair(uint32_t w) const
+    {
+        const uint32_t t = I == 0 ? w << 3 : w >> (4 * I - 3);
+        return (t & mask) | sixteen;
+    }
+    // 8 codes of a dword as a matrix-core operand: elements are codes 0, 4, 1, 5, 2, 6, 3, 7
+    __device__ __forceinline__ bf16x8 operand(uint32_t w) const
+    {
+        return __builtin_bit_cast(bf16x8, u32x4{pair<0>(w), pair<1>(w), pair<2>(w), pair<3>(w)});
+    }
+};
 
 // A row tile of a workgroup: rows first .. first + 15 of a sequence's n * group rows, and what they may see.
 struct Tile {
@@ -78,6 +89,8 @@ __device__ __forceinline__ Tile tile_of(const AttendArgs &a, int64_t number)
         begin = i * per;
     }
     t.seq = seq_of(a.s, i);
+    t.seq.row = __builtin_amdgcn_readfirstlane(t.seq.row), t.seq.n = __builtin_amdgcn_readfirstlane(t.seq.n); // the same in every lane
+    t.seq.line = __builtin_amdgcn_readfirstlane(t.seq.line), t.seq.len = __builtin_amdgcn_readfirstlane(t.seq.len);
     const int64_t at = (number - begin) * ROWS;
     t.rows = t.seq.n * a.group;
     t.first = at < 0 || at > t.rows ? t.rows : (int32_t)at;
@@ -101,31 +114,119 @@ __device__ __forceinline__ void split(float x, float (&part)[PARTS])
     }
 }
 
+// What a tile's rows see: tokens lo .. hi each, all_lo .. all_hi some of them, each_lo .. each_hi every one.
+struct Sight {
+    int32_t limit, all_lo, all_hi, each_lo, each_hi;
+};
+
+__device__ __forceinline__ int32_t lo_at(const AttendArgs &a, int32_t pos) { return a.window > 0 && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0; }
+__device__ __forceinline__ int32_t hi_at(const Sight &v, int32_t pos) { return pos < v.limit ? pos : v.limit - 1; }
+
+__device__ __forceinline__ Sight sight_of(const AttendArgs &a, const Tile &t, int32_t rows)
+{
+    Sight v;
+    const int32_t cap = a.s.table_ld << a.s.page_shift;
+    v.limit = t.seq.line < 0 ? 0 : (t.seq.len < cap ? t.seq.len : cap);
+    const int32_t last_row = t.first + rows < t.rows ? t.first + rows - 1 : t.rows - 1;
+    const int32_t p_first = t.seq.len - t.seq.n + t.first / a.group, p_last = t.seq.len - t.seq.n + last_row / a.group;
+    v.all_lo = lo_at(a, p_first), v.all_hi = hi_at(v, p_last);
+    v.each_lo = lo_at(a, p_last), v.each_hi = hi_at(v, p_first);
+    return v;
+}
+
+// The steps of a tile are shared out over as many workgroups as have LEAST of them, at most a.splits.
+constexpr int LEAST = 8;
+struct Share {
+    int32_t parts, begin, end; // steps begin .. end - 1 are this part's
+};
+__device__ __forceinline__ Share share_of(const Sight &v, int32_t splits, int32_t part)
+{
+    const int32_t first = v.all_lo / STEP, steps = v.all_hi < v.all_lo ? 0 : v.all_hi / STEP + 1 - first;
+    const int32_t most = (steps + LEAST - 1) / LEAST;
+    Share h;
+    h.parts = most < 1 ? 1 : (most < splits ? most : splits);
+    const int32_t each = (steps + h.parts - 1) / h.parts;
+    h.begin = first + part * each;
+    h.end = h.begin + each < first + steps ? h.begin + each : first + steps;
+    return h;
+}
+
+// What a wave asks of memory for one step: codes of its keys (tokens 16 h + r, channels D / 4 g ..) and values (tokens of
+// element e, channels D / 16 r ..), and one token's alpha and beta, of the keys in lanes 0..31, of the values in the others.
+template <int D>
+struct Loaded {
+    uint32_t k[2][D / 32], v[8], beta;
+    float alpha;
+    int32_t t0; // its first token, -1: nothing
+};
+
+template <int D>
+__device__ __forceinline__ void ask(const Step &s, int32_t head, int32_t lane, int32_t page, int32_t t0, Loaded<D> &x)
+{
+    const int32_t P = 1 << s.page_shift, r = lane & 15, g = lane >> 4, in_page = t0 & (P - 1);
+    const uint8_t *part = s.pages + page * s.page_bytes + (int64_t)head * P * (D + 16);
+    const uint8_t *kc = part + (int64_t)in_page * (D / 2), *vc = kc + (int64_t)P * (D / 2);
+    x.t0 = t0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint8_t *src = kc + (16 * h + r) * (D / 2) + D / 8 * g;
+        if (D == 128) {
+            const uint4 w = *reinterpret_cast<const uint4 *>(src);
+            x.k[h][0] = w.x, x.k[h][1] = w.y, x.k[h][D / 32 - 2] = w.z, x.k[h][D / 32 - 1] = w.w;
+        } else {
+            const uint2 w = *reinterpret_cast<const uint2 *>(src);
+            x.k[h][0] = w.x, x.k[h][1] = w.y;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint8_t *src = vc + (16 * (e >> 2) + 4 * g + (e & 3)) * (D / 2) + D / 32 * r;
+        x.v[e] = D == 128 ? *reinterpret_cast<const uint32_t *>(src) : *reinterpret_cast<const uint16_t *>(src);
+    }
+    const uint32_t *par = reinterpret_cast<const uint32_t *>(part + (int64_t)P * D) + (lane >> 5) * 2 * P + in_page + (lane & 31);
+    x.alpha = __uint_as_float(par[0]);
+    x.beta = par[P];
+}
+
+// Partial results of a part: per row the running maximum and sum, and dim unnormalised sums.
+__device__ __forceinline__ int64_t partial_at(const AttendArgs &a, int64_t tile, int32_t head, int32_t part, int32_t row)
+{
+    return ((tile * a.s.heads + head) * a.splits + part) * ROWS + row;
+}
+
+template <int D, bool F32O>
+__device__ __forceinline__ void put_out(const AttendArgs &a, const Tile &t, int32_t head, int32_t row, int32_t c, float y)
+{
+    const int32_t tok = row / a.group;
+    const int64_t at = (int64_t)(t.seq.row + tok) * a.ldo + (int64_t)(head * a.group + row - tok * a.group) * D + c;
+    if (F32O) static_cast<float *>(a.out)[at] = y;
+    else static_cast<uint16_t *>(a.out)[at] = (uint16_t)pack_bf16(y, 0.0f);
+}
+
+__device__ __forceinline__ float quotient(float o, float sum) { return sum > 0.0f ? o / sum : (sum == 0.0f ? 0.0f : sum); } // a NaN stays
+
 template <int D, bool F32Q, bool F32O>
-__global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a)
+__global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const AttendArgs a)
 {
     constexpr int PARTS = F32Q ? 3 : 1;
     constexpr int KS = D / 32, DT = D / 16; // steps of 32 channels; tiles of 16 channels (one channel of each lane row)
     __shared__ float mrg_m[WAVES][ROWS], mrg_l[WAVES][ROWS], mrg_o[WAVES][ROWS][D + 4];
+    // a token's parameters, worked out by one lane and read by sixteen: a key's factor and 16 + beta, a value's alpha and - (16 + beta)
+    __shared__ __attribute__((aligned(16))) float2 params[WAVES][64];
 
     const Step &s = a.s;
-    const int32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const int32_t head = blockIdx.y, P = 1 << s.page_shift;
+    const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int32_t head = blockIdx.y;
     const Tile t = tile_of(a, blockIdx.x);
     if (t.first >= t.rows) return;
+    const Sight v = sight_of(a, t, ROWS);
+    const Share share = share_of(v, a.splits, blockIdx.z);
+    if ((int32_t)blockIdx.z >= share.parts) return;
 
     // this lane's row (a column of the transposed products) and the tokens it sees: lo .. hi
     const int32_t row = t.first + r, token = row / a.group;
     const bool real = row < t.rows;
-    const int32_t cap = s.table_ld << s.page_shift, limit = t.seq.line < 0 ? 0 : (t.seq.len < cap ? t.seq.len : cap);
-    const auto pos_of = [&](int32_t tok) { return t.seq.len - t.seq.n + tok; };
-    const auto hi_of = [&](int32_t p) { return p < limit ? p : limit - 1; };
-    const auto lo_of = [&](int32_t p) { return a.window > 0 && p - a.window + 1 > 0 ? p - a.window + 1 : 0; };
-    const int32_t pos = pos_of(token), hi = real ? hi_of(pos) : -1, lo = lo_of(pos);
-    const int32_t last_row = t.first + ROWS < t.rows ? t.first + ROWS - 1 : t.rows - 1;
-    const int32_t p_first = pos_of(t.first / a.group), p_last = pos_of(last_row / a.group);
-    const int32_t all_lo = lo_of(p_first), all_hi = hi_of(p_last);       // seen by some row
-    const int32_t each_lo = lo_of(p_last), each_hi = hi_of(p_first);     // seen by every row
+    const int32_t pos = t.seq.len - t.seq.n + token, hi = real ? hi_at(v, pos) : -1, lo = lo_at(a, pos);
 
     // queries: element e of step k of lane group g is channel (D / 4) g + 8 k + {0, 4, 1, 5, 2, 6, 3, 7}[e]
     bf16x8 qo[PARTS][KS];
@@ -153,56 +254,40 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a)
     f32x4 acc[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.0f, off = 0.0f; // running maximum; this lane's parts of the sums of p and of p alpha (16 + beta)
+    float m = -INFINITY, l = 0.0f; // running maximum; this lane's part of the sum of p
+    const Codes16 codes;
+    const float factor = lane < 32 ? a.scale2 : 1.0f, sign = lane < 32 ? 1.0f : -1.0f, exact = lane < 32 ? INFINITY : 256.0f;
 
-    for (int32_t st = all_lo / STEP + wave; st * STEP <= all_hi; st += WAVES) {
-        const int32_t t0 = st * STEP;
-        const int32_t page = page_of(s, t.seq.line, t0);
-        if (page < 0) continue;
-        const uint8_t *part = s.pages + page * s.page_bytes + (int64_t)head * P * (D + 16);
-        const int32_t in_page = t0 & (P - 1);
-        const uint8_t *kc = part + (int64_t)in_page * (D / 2), *vc = kc + (int64_t)P * (D / 2);
-        const float *par = reinterpret_cast<const float *>(part + (int64_t)P * D) + in_page;
-
-        float sc[8], va[8], vb[8]; // scores, alpha and 16 + beta of the values, of tokens 16 h + 4 g + i
+    const auto work = [&](const Loaded<D> &x) {
+        const float zero = sign * ((float)(int32_t)x.beta + 16.0f);
+        params[wave][lane] = make_float2(x.alpha * factor, zero);
+        const bool far = __any(fabsf(zero) > exact); // some - (16 + beta) of a value has more than the 8 bits of a bf16
+        __builtin_amdgcn_wave_barrier();
+        float sc[8], va[8], vz[8]; // scores, the values' alpha and - (16 + beta), of tokens 16 h + 4 g + i
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            uint32_t w[KS];
-            const uint8_t *src = kc + (16 * h + r) * (D / 2) + D / 8 * g;
-            if (D == 128) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(src);
-                w[0] = x.x, w[1] = x.y, w[KS - 2] = x.z, w[KS - 1] = x.w;
-            } else {
-                const uint2 x = *reinterpret_cast<const uint2 *>(src);
-                w[0] = x.x, w[1] = x.y;
-            }
             f32x4 d = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = PARTS - 1; i >= 0; --i)
 #pragma unroll
-                for (int k = 0; k < KS; ++k) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand16(w[k]), qo[i][k], d, 0, 0, 0);
-            const int32_t at = 16 * h + 4 * g;
-            const float4 ka = *reinterpret_cast<const float4 *>(par + at);
-            const int4 kb = *reinterpret_cast<const int4 *>(par + P + at);
-            const float4 wa = *reinterpret_cast<const float4 *>(par + 2 * P + at);
-            const int4 wb = *reinterpret_cast<const int4 *>(par + 3 * P + at);
-            const float kav[4] = {ka.x, ka.y, ka.z, ka.w}, vav[4] = {wa.x, wa.y, wa.z, wa.w};
-            const int32_t kbv[4] = {kb.x, kb.y, kb.z, kb.w}, vbv[4] = {wb.x, wb.y, wb.z, wb.w};
+                for (int k = 0; k < KS; ++k) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes.operand(x.k[h][k]), qo[i][k], d, 0, 0, 0);
+            const float4 *kp = reinterpret_cast<const float4 *>(&params[wave][16 * h + 4 * g]), *vp = kp + STEP / 2;
+            const float4 k0 = kp[0], k1 = kp[1], v0 = vp[0], v1 = vp[1];
+            const float ka[4] = {k0.x, k0.z, k1.x, k1.z}, kb[4] = {k0.y, k0.w, k1.y, k1.w};
+            va[4 * h] = v0.x, va[4 * h + 1] = v0.z, va[4 * h + 2] = v1.x, va[4 * h + 3] = v1.z;
+            vz[4 * h] = v0.y, vz[4 * h + 1] = v0.w, vz[4 * h + 2] = v1.y, vz[4 * h + 3] = v1.w;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                sc[4 * h + i] = kav[i] * a.scale2 * __builtin_fmaf(-((float)kbv[i] + 16.0f), qsum, d[i]);
-                va[4 * h + i] = vav[i];
-                vb[4 * h + i] = (float)vbv[i] + 16.0f;
-            }
+            for (int i = 0; i < 4; ++i) sc[4 * h + i] = ka[i] * __builtin_fmaf(-kb[i], qsum, d[i]);
         }
-        if (t0 < each_lo || t0 + STEP - 1 > each_hi) { // some row does not see some token; what lies there may be anything
+        if (x.t0 < v.each_lo || x.t0 + STEP - 1 > v.each_hi) { // some row does not see some token; what lies there may be anything
+            int32_t t0 = x.t0 + 4 * g;
+            asm volatile("" : "+v"(t0)); // keeps the comparisons in here
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int32_t tok = t0 + 16 * (i >> 2) + 4 * g + (i & 3);
+                const int32_t tok = t0 + 16 * (i >> 2) + (i & 3);
                 const bool seen = tok >= lo && tok <= hi;
                 sc[i] = seen ? sc[i] : -INFINITY;
                 va[i] = seen ? va[i] : 0.0f;
-                vb[i] = seen ? vb[i] : 0.0f;
             }
         }
         float top = sc[0];
@@ -213,79 +298,152 @@ __global__ __launch_bounds__(WAVES * 64) void attend_kernel(const AttendArgs a)
             top = fmaxf(top, __shfl_xor(top, 32));
             const float now = fmaxf(m, top);
             const float f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - now);
-            m = now, l *= f, off *= f;
+            m = now, l *= f;
 #pragma unroll
             for (int i = 0; i < DT; ++i) acc[i] *= f;
         }
         const float base = m == -INFINITY ? 0.0f : m;
-        float pv[8], part_p[8][PARTS];
+        float part_p[8][PARTS];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float p = __builtin_amdgcn_exp2f(sc[i] - base);
             l += p;
-            pv[i] = p * va[i];
-            split<PARTS>(pv[i], part_p[i]);
-#pragma unroll
-            for (int j = 0; j < PARTS; ++j) off = __builtin_fmaf(part_p[i][j], vb[i], off);
+            split<PARTS>(p * va[i], part_p[i]);
         }
-        // values: tokens of element e as the scores have them, 16 (e / 4) + 4 g + e % 4; channels (D / 16) r .. of this lane
-        uint32_t w[8];
+        bf16x8 pw[PARTS];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint8_t *src = vc + (16 * (e >> 2) + 4 * g + (e & 3)) * (D / 2) + D / 32 * r;
-            w[e] = D == 128 ? *reinterpret_cast<const uint32_t *>(src) : *reinterpret_cast<const uint16_t *>(src);
-        }
+        for (int j = 0; j < PARTS; ++j)
+            pw[j] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part_p[0][j], part_p[1][j]), pack_bf16(part_p[2][j], part_p[3][j]),
+                                                     pack_bf16(part_p[4][j], part_p[5][j]), pack_bf16(part_p[6][j], part_p[7][j])});
         uint32_t low[4], high[4]; // codes 0..3 and 4..7 of two neighbouring tokens
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            low[e] = __builtin_amdgcn_perm(w[2 * e + 1], w[2 * e], 0x05040100u);
-            high[e] = __builtin_amdgcn_perm(w[2 * e + 1], w[2 * e], 0x07060302u);
+            low[e] = __builtin_amdgcn_perm(x.v[2 * e + 1], x.v[2 * e], 0x05040100u);
+            high[e] = __builtin_amdgcn_perm(x.v[2 * e + 1], x.v[2 * e], 0x07060302u);
         }
-        const auto tile = [&](int i, bf16x8 v) {
+        // (16 + c) - (16 + beta) in two products: the sums stay as small as the values are, whatever the number of tokens
+        const auto high_halves = [&] { // of - (16 + beta): the number itself where it has 8 bits
+            u32x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = __builtin_amdgcn_perm(__float_as_uint(vz[2 * e + 1]), __float_as_uint(vz[2 * e]), 0x07060302u);
+            return __builtin_bit_cast(bf16x8, y);
+        };
+        const bf16x8 zero0 = high_halves();
+        const auto tile = [&](int i, bf16x8 c) {
 #pragma unroll
             for (int j = PARTS - 1; j >= 0; --j) {
-                const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part_p[0][j], part_p[1][j]), pack_bf16(part_p[2][j], part_p[3][j]),
-                                                                  pack_bf16(part_p[4][j], part_p[5][j]), pack_bf16(part_p[6][j], part_p[7][j])});
-                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, acc[i], 0, 0, 0);
+                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(zero0, pw[j], acc[i], 0, 0, 0);
+                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c, pw[j], acc[i], 0, 0, 0);
             }
         };
-        const auto four = [&](const uint32_t (&x)[4], int at) {
-            tile(at + 0, __builtin_bit_cast(bf16x8, u32x4{pair16<0>(x[0]), pair16<0>(x[1]), pair16<0>(x[2]), pair16<0>(x[3])}));
-            tile(at + 1, __builtin_bit_cast(bf16x8, u32x4{pair16<1>(x[0]), pair16<1>(x[1]), pair16<1>(x[2]), pair16<1>(x[3])}));
-            tile(at + 2, __builtin_bit_cast(bf16x8, u32x4{pair16<2>(x[0]), pair16<2>(x[1]), pair16<2>(x[2]), pair16<2>(x[3])}));
-            tile(at + 3, __builtin_bit_cast(bf16x8, u32x4{pair16<3>(x[0]), pair16<3>(x[1]), pair16<3>(x[2]), pair16<3>(x[3])}));
+        const auto four = [&](const uint32_t (&w)[4], int at) {
+            tile(at + 0, __builtin_bit_cast(bf16x8, u32x4{codes.pair<0>(w[0]), codes.pair<0>(w[1]), codes.pair<0>(w[2]), codes.pair<0>(w[3])}));
+            tile(at + 1, __builtin_bit_cast(bf16x8, u32x4{codes.pair<1>(w[0]), codes.pair<1>(w[1]), codes.pair<1>(w[2]), codes.pair<1>(w[3])}));
+            tile(at + 2, __builtin_bit_cast(bf16x8, u32x4{codes.pair<2>(w[0]), codes.pair<2>(w[1]), codes.pair<2>(w[2]), codes.pair<2>(w[3])}));
+            tile(at + 3, __builtin_bit_cast(bf16x8, u32x4{codes.pair<3>(w[0]), codes.pair<3>(w[1]), codes.pair<3>(w[2]), codes.pair<3>(w[3])}));
         };
         four(low, 0);
         if (D == 128) four(high, DT - 4);
+        if (far) { // values far from zero for their range: what the high halves leave out
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) vz[e] -= __uint_as_float(__float_as_uint(vz[e]) & 0xffff0000u);
+                const bf16x8 rest = high_halves();
+#pragma unroll
+                for (int i = 0; i < DT; ++i)
+#pragma unroll
+                    for (int j = PARTS - 1; j >= 0; --j) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(rest, pw[j], acc[i], 0, 0, 0);
+            }
+        }
+    };
+
+    // The loads of a step are on their way while the step before is worked on.  Nothing in between may wait for memory or hang on
+    // a condition that the compiler cannot see through: the page numbers of up to 64 steps are fetched beforehand, one a lane,
+    // and a step without a page reads page 0 and drops it.
+    const auto ask_for = [&](int32_t page, int32_t st, Loaded<D> &x) { ask<D>(s, head, lane, page < 0 ? 0 : page, st * STEP, x); };
+    for (int32_t first = share.begin + wave; first < share.end; first += 64 * WAVES) {
+        const int32_t mine = first + lane * WAVES;
+        const int32_t pages = mine < share.end ? page_of(s, t.seq.line, mine * STEP) : -1;
+        const int32_t left = (share.end - first + WAVES - 1) / WAVES, count = left < 64 ? left : 64;
+        Loaded<D> x[2];
+        int32_t page = __builtin_amdgcn_readlane(pages, 0);
+        ask_for(page, first, x[0]);
+        for (int32_t n = 0; n < count; n += 2) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int32_t next = n + i + 1 < count ? __builtin_amdgcn_readlane(pages, (n + i + 1) & 63) : -1;
+                ask_for(next, first + (n + i + 1) * WAVES, x[1 - i]);
+                if (page >= 0) work(x[i]);
+                page = next;
+            }
+        }
     }
 
-    l += __shfl_xor(l, 16), off += __shfl_xor(off, 16);
-    l += __shfl_xor(l, 32), off += __shfl_xor(off, 32);
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
     // accumulator i of tile c is channel (D / 16) (4 g + i) + c of this lane's row
     if (g == 0) mrg_m[wave][r] = m, mrg_l[wave][r] = l;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int c = 0; c < DT; ++c) mrg_o[wave][r][DT * (4 * g + i) + c] = acc[c][i] - off;
+        for (int c = 0; c < DT; ++c) mrg_o[wave][r][DT * (4 * g + i) + c] = acc[c][i];
     __syncthreads();
-    for (int32_t x = threadIdx.x; x < ROWS * D; x += WAVES * 64) {
-        const int32_t n = x / D, c = x % D, rw = t.first + n;
+    for (int32_t i = threadIdx.x; i < ROWS * D; i += WAVES * 64) {
+        const int32_t n = i / D, c = i % D, rw = t.first + n;
         if (rw >= t.rows) break;
         float top = -INFINITY, sum = 0.0f, o = 0.0f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) top = fmaxf(top, mrg_m[w][n]);
-        if (top == -INFINITY) top = 0.0f;
+        const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float f = __builtin_amdgcn_exp2f(mrg_m[w][n] - top);
+            const float f = __builtin_amdgcn_exp2f(mrg_m[w][n] - base);
             sum += f * mrg_l[w][n];
             o += f * mrg_o[w][n][c];
         }
-        const float y = sum > 0.0f ? o / sum : (sum == 0.0f ? 0.0f : sum);
-        const int32_t tok = rw / a.group;
-        const int64_t at = (int64_t)(t.seq.row + tok) * a.ldo + (int64_t)(head * a.group + rw - tok * a.group) * D + c;
-        if (F32O) static_cast<float *>(a.out)[at] = y;
-        else static_cast<uint16_t *>(a.out)[at] = (uint16_t)pack_bf16(y, 0.0f);
+        if (share.parts == 1) {
+            put_out<D, F32O>(a, t, head, rw, c, quotient(o, sum));
+        } else {
+            const int64_t at = partial_at(a, blockIdx.x, head, blockIdx.z, n);
+            a.part_o[at * D + c] = o;
+            if (c == 0) a.part_ml[at] = make_float2(top, sum);
+        }
+    }
+}
+
+// The parts of a tile's rows joined, a workgroup per row: each wave takes every fourth part.
+template <int D, bool F32O>
+__global__ __launch_bounds__(WAVES * 64) void join_kernel(const AttendArgs a)
+{
+    __shared__ float sums[WAVES], os[WAVES][D];
+    const int32_t n = blockIdx.z, head = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Tile t = tile_of(a, blockIdx.x);
+    if (t.first + n >= t.rows) return;
+    const Share share = share_of(sight_of(a, t, ROWS), a.splits, 0);
+    if (share.parts == 1) return;
+    float top = -INFINITY;
+    for (int32_t p = lane; p < share.parts; p += 64) top = fmaxf(top, a.part_ml[partial_at(a, blockIdx.x, head, p, n)].x);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float base = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f, o[D / 64] = {};
+#pragma unroll 4
+    for (int32_t p = wave; p < share.parts; p += WAVES) {
+        const int64_t at = partial_at(a, blockIdx.x, head, p, n);
+        const float2 ml = a.part_ml[at];
+        const float f = __builtin_amdgcn_exp2f(ml.x - base);
+        sum += f * ml.y;
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) o[c] += f * a.part_o[at * D + 64 * c + lane];
+    }
+    if (lane == 0) sums[wave] = sum;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) os[wave][64 * c + lane] = o[c];
+    __syncthreads();
+    if (threadIdx.x < D) {
+        const int32_t c = threadIdx.x;
+        put_out<D, F32O>(a, t, head, t.first + n, c, quotient((os[0][c] + os[1][c]) + (os[2][c] + os[3][c]), (sums[0] + sums[1]) + (sums[2] + sums[3])));
     }
 }
 
@@ -296,6 +454,24 @@ int32_t check(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_
     return QLLM_OK;
 }
 
+// Tiles, and parts of a tile's tokens.  Parts are for few tiles: enough for WANTED workgroups, none shorter than the line is long.
+struct Launch {
+    int64_t tiles;
+    int32_t splits;
+};
+constexpr int64_t WANTED = 1024, MOST_SPLITS = 128;
+Launch plan(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads)
+{
+    const int64_t group = q_heads / cache->heads;
+    Launch n;
+    n.tiles = batch->row_start ? batch->rows * group / ROWS + batch->n_seqs : batch->n_seqs * ((group + ROWS - 1) / ROWS);
+    const int64_t workgroups = n.tiles * cache->heads, steps = batch->table_ld * cache->page_tokens / STEP;
+    int64_t splits = workgroups > 0 ? WANTED / workgroups : 1;
+    if (splits > (steps + LEAST - 1) / LEAST) splits = (steps + LEAST - 1) / LEAST;
+    n.splits = (int32_t)(splits < 1 ? 1 : (splits > MOST_SPLITS ? MOST_SPLITS : splits));
+    return n;
+}
+
 } // namespace
 
 extern "C" int64_t qllm_kv_attention_workspace_bytes(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads)
@@ -303,7 +479,9 @@ extern "C" int64_t qllm_kv_attention_workspace_bytes(const qllm_kv_cache *cache,
     Step s;
     int32_t rc = prepare_step(cache, batch, false, &s);
     if (rc == QLLM_OK) rc = check(cache, batch, q_heads);
-    return rc != QLLM_OK ? rc : 256;
+    if (rc != QLLM_OK) return rc;
+    const Launch n = plan(cache, batch, q_heads);
+    return 256 + (n.splits > 1 ? n.tiles * cache->heads * n.splits * ROWS * (cache->dim + 2) * (int64_t)sizeof(float) : 0);
 }
 
 extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq, int64_t q_heads, const qllm_kv_cache *cache,
@@ -327,8 +505,11 @@ extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq
     a.q_heads = (int32_t)q_heads, a.group = (int32_t)(q_heads / cache->heads);
     a.window = window > INT32_MAX ? 0 : (int32_t)window;
     a.scale2 = scale * LOG2E;
-    const int64_t tiles = batch->row_start ? batch->rows * a.group / ROWS + batch->n_seqs : batch->n_seqs * ((a.group + ROWS - 1) / ROWS);
-    const dim3 grid((unsigned)tiles, (unsigned)cache->heads);
+    const Launch n = plan(cache, batch, q_heads);
+    a.splits = n.splits;
+    a.part_ml = static_cast<float2 *>(workspace);
+    a.part_o = static_cast<float *>(workspace) + 2 * n.tiles * cache->heads * n.splits * ROWS;
+    const dim3 grid((unsigned)n.tiles, (unsigned)cache->heads, (unsigned)n.splits), rows((unsigned)n.tiles, (unsigned)cache->heads, ROWS);
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();
 #define QLLM_ATTEND(D, FQ, FO) hipLaunchKernelGGL((attend_kernel<D, FQ, FO>), grid, dim3(WAVES * 64), 0, stream, a)
@@ -344,5 +525,11 @@ extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq
     default: QLLM_ATTEND(128, true, true); break;
     }
 #undef QLLM_ATTEND
-    return launched("cache attention: launch");
+    rc = launched("cache attention: launch");
+    if (rc != QLLM_OK || n.splits == 1) return rc;
+    if (cache->dim == 128 && out_dtype == QLLM_F32) hipLaunchKernelGGL((join_kernel<128, true>), rows, dim3(WAVES * 64), 0, stream, a);
+    else if (cache->dim == 128) hipLaunchKernelGGL((join_kernel<128, false>), rows, dim3(WAVES * 64), 0, stream, a);
+    else if (out_dtype == QLLM_F32) hipLaunchKernelGGL((join_kernel<64, true>), rows, dim3(WAVES * 64), 0, stream, a);
+    else hipLaunchKernelGGL((join_kernel<64, false>), rows, dim3(WAVES * 64), 0, stream, a);
+    return launched("cache attention: parts joined");
 }
