@@ -28,6 +28,7 @@ constexpr int ROWS = 16, STEP = 32, WAVES = 4; // rows of a tile, tokens of a st
 constexpr float LOG2E = 1.44269504088896341f;
 constexpr float SLACK = 8.0f; // the running maximum follows only when the scores pass it by this much: weights stay below 2^8
 
+struct Unfinished;
 struct AttendArgs {
     Step s;
     const void *q;
@@ -35,9 +36,10 @@ struct AttendArgs {
     int64_t ldq, ldo;
     int32_t q_heads, group, window; // window 0: none
     float scale2;                   // scale * log2 e
-    int32_t splits;                 // workgroups that may share a tile's tokens
+    int32_t blocks;                 // workgroups of a kv head
     float *part_o;                  // their partial results, see partial_at
     float2 *part_ml;
+    Unfinished *unfinished;   // [heads][blocks]
 };
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
@@ -67,34 +69,122 @@ struct Codes16 {
     }
 };
 
-// A row tile of a workgroup: rows first .. first + 15 of a sequence's n * group rows, and what they may see.
+// A row tile of a workgroup: rows first .. first + 15 of a sequence's n * group rows.
 struct Tile {
     Seq seq;
     int32_t first, rows;
 };
 
-// Sequence i's tiles begin at number row_start[i] * group / ROWS + i: at least as many numbers as it has tiles, in order.
-__device__ __forceinline__ Tile tile_of(const AttendArgs &a, int64_t number)
+// What rows see: tokens all_lo .. all_hi some of them, each_lo .. each_hi every one.
+struct Sight {
+    int32_t limit, all_lo, all_hi, each_lo, each_hi;
+};
+
+__device__ __forceinline__ int32_t lo_at(const AttendArgs &a, int32_t pos) { return a.window > 0 && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0; }
+__device__ __forceinline__ int32_t hi_at(int32_t limit, int32_t pos) { return pos < limit ? pos : limit - 1; }
+__device__ __forceinline__ int32_t limit_of(const AttendArgs &a, const Seq &q)
 {
-    Tile t;
-    int32_t i;
-    int64_t begin;
-    if (a.s.row_start) {
-        auto first = [&](int32_t k) { return (int64_t)row_of(a.s, k) * a.group / ROWS + k; };
-        i = last_not_above(a.s.n_seqs, number, first);
-        begin = first(i);
-    } else {
-        const int64_t per = (a.group + ROWS - 1) / ROWS;
-        i = (int32_t)(number / per);
-        begin = i * per;
+    const int32_t cap = a.s.table_ld << a.s.page_shift;
+    return q.line < 0 ? 0 : (q.len < cap ? q.len : cap);
+}
+
+__device__ __forceinline__ Sight sight_of(const AttendArgs &a, const Tile &t)
+{
+    Sight v;
+    v.limit = limit_of(a, t.seq);
+    const int32_t last_row = t.first + ROWS < t.rows ? t.first + ROWS - 1 : t.rows - 1;
+    const int32_t p_first = t.seq.len - t.seq.n + t.first / a.group, p_last = t.seq.len - t.seq.n + last_row / a.group;
+    v.all_lo = lo_at(a, p_first), v.all_hi = hi_at(v.limit, p_last);
+    v.each_lo = lo_at(a, p_last), v.each_hi = hi_at(v.limit, p_first);
+    return v;
+}
+
+// The work of a kv head is one long line of steps: sequence after sequence, tile after tile, `steps` of 32 tokens for each tile
+// (what its sequence's rows see together; at least one, for rows that see nothing get their zeros too).  The workgroups of the
+// head share the line out evenly, whatever the lengths: one may end in the middle of a tile and the next go on there.
+struct Work {
+    int32_t tiles, first, steps; // of a sequence; its first step is number `first` of the cache line
+    // (a bound that only a row_start that does not ascend can reach: 2^20 of these still add up)
+    __device__ __forceinline__ int64_t all() const { return min((int64_t)tiles * steps, (int64_t)1 << 42); }
+};
+
+__device__ __forceinline__ Work work_of(const AttendArgs &a, const Seq &q)
+{
+    Work w;
+    w.tiles = (int32_t)(((int64_t)q.n * a.group + ROWS - 1) / ROWS);
+    const int32_t lo = lo_at(a, q.len - q.n), hi = hi_at(limit_of(a, q), q.len - 1);
+    w.first = lo / STEP;
+    w.steps = hi < lo ? 1 : hi / STEP + 1 - w.first;
+    return w;
+}
+
+__device__ __forceinline__ int64_t lane64(int64_t x, int32_t lane) // lane `lane`'s x, the same in every lane and known to be
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int32_t)((uint64_t)x >> 32), lane) << 32 |
+                     (uint32_t)__builtin_amdgcn_readlane((int32_t)x, lane));
+}
+
+// The line as one wave sees it: 64 sequences at a time, one a lane.  Up to 64 are read from memory once.
+struct Line {
+    Seq mine;      // sequence base + lane
+    int64_t upto;  // where it ends
+    int64_t total; // the whole line
+    int32_t base;
+
+    __device__ __forceinline__ void look(const AttendArgs &a, int32_t from, int64_t before)
+    {
+        const int32_t lane = threadIdx.x & 63, i = from + lane;
+        base = from;
+        mine = Seq{0, 0, -1, 0};
+        if (i < a.s.n_seqs) mine = seq_of(a.s, i);
+        upto = work_of(a, mine).all(); // none without rows
+        if (i >= a.s.n_seqs) upto = 0;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int64_t y = __shfl_up(upto, o);
+            if (lane >= o) upto += y;
+        }
+        upto += before;
     }
-    t.seq = seq_of(a.s, i);
-    t.seq.row = __builtin_amdgcn_readfirstlane(t.seq.row), t.seq.n = __builtin_amdgcn_readfirstlane(t.seq.n); // the same in every lane
-    t.seq.line = __builtin_amdgcn_readfirstlane(t.seq.line), t.seq.len = __builtin_amdgcn_readfirstlane(t.seq.len);
-    const int64_t at = (number - begin) * ROWS;
-    t.rows = t.seq.n * a.group;
-    t.first = at < 0 || at > t.rows ? t.rows : (int32_t)at;
-    return t;
+    __device__ __forceinline__ explicit Line(const AttendArgs &a)
+    {
+        total = 0;
+        for (int32_t from = 0; from < a.s.n_seqs; from += 64) {
+            look(a, from, total);
+            total = lane64(upto, 63);
+        }
+        if (total >= (int64_t)1 << 50) total = 0; // see Work::all
+    }
+    // The sequence that step `at` < total belongs to; *begin: where that begins.
+    __device__ __forceinline__ int32_t find(const AttendArgs &a, int64_t at, int64_t *begin)
+    {
+        int64_t before = 0;
+        for (int32_t from = 0; from < a.s.n_seqs; from += 64) {
+            if (a.s.n_seqs > 64) look(a, from, before);
+            const int32_t skipped = __popcll(__ballot(upto <= at)); // sequences that end at or before it
+            if (skipped < 64) {
+                *begin = skipped ? lane64(upto, skipped - 1) : before;
+                return from + skipped;
+            }
+            before = lane64(upto, 63);
+        }
+        return a.s.n_seqs;
+    }
+    __device__ __forceinline__ Seq seq(const AttendArgs &a, int32_t i)
+    {
+        if (i < base || i >= base + 64) look(a, i, 0); // only its sequences are asked for from now on
+        const int32_t k = i - base;
+        return Seq{__builtin_amdgcn_readlane(mine.row, k), __builtin_amdgcn_readlane(mine.n, k), __builtin_amdgcn_readlane(mine.line, k),
+                   __builtin_amdgcn_readlane(mine.len, k)};
+    }
+};
+
+// How many workgroups share the line: none gets less than LEAST steps while another has some.  Share b begins at total * b / of.
+constexpr int LEAST = 16;
+__device__ __forceinline__ int32_t sharers(const AttendArgs &a, int64_t total)
+{
+    const int64_t most = (total + LEAST - 1) / LEAST;
+    return most < a.blocks ? (int32_t)most : a.blocks;
 }
 
 template <bool F32>
@@ -112,43 +202,6 @@ __device__ __forceinline__ void split(float x, float (&part)[PARTS])
         part[i] = __uint_as_float(pack_bf16(x, 0.0f) << 16);
         x -= part[i];
     }
-}
-
-// What a tile's rows see: tokens lo .. hi each, all_lo .. all_hi some of them, each_lo .. each_hi every one.
-struct Sight {
-    int32_t limit, all_lo, all_hi, each_lo, each_hi;
-};
-
-__device__ __forceinline__ int32_t lo_at(const AttendArgs &a, int32_t pos) { return a.window > 0 && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0; }
-__device__ __forceinline__ int32_t hi_at(const Sight &v, int32_t pos) { return pos < v.limit ? pos : v.limit - 1; }
-
-__device__ __forceinline__ Sight sight_of(const AttendArgs &a, const Tile &t, int32_t rows)
-{
-    Sight v;
-    const int32_t cap = a.s.table_ld << a.s.page_shift;
-    v.limit = t.seq.line < 0 ? 0 : (t.seq.len < cap ? t.seq.len : cap);
-    const int32_t last_row = t.first + rows < t.rows ? t.first + rows - 1 : t.rows - 1;
-    const int32_t p_first = t.seq.len - t.seq.n + t.first / a.group, p_last = t.seq.len - t.seq.n + last_row / a.group;
-    v.all_lo = lo_at(a, p_first), v.all_hi = hi_at(v, p_last);
-    v.each_lo = lo_at(a, p_last), v.each_hi = hi_at(v, p_first);
-    return v;
-}
-
-// The steps of a tile are shared out over as many workgroups as have LEAST of them, at most a.splits.
-constexpr int LEAST = 8;
-struct Share {
-    int32_t parts, begin, end; // steps begin .. end - 1 are this part's
-};
-__device__ __forceinline__ Share share_of(const Sight &v, int32_t splits, int32_t part)
-{
-    const int32_t first = v.all_lo / STEP, steps = v.all_hi < v.all_lo ? 0 : v.all_hi / STEP + 1 - first;
-    const int32_t most = (steps + LEAST - 1) / LEAST;
-    Share h;
-    h.parts = most < 1 ? 1 : (most < splits ? most : splits);
-    const int32_t each = (steps + h.parts - 1) / h.parts;
-    h.begin = first + part * each;
-    h.end = h.begin + each < first + steps ? h.begin + each : first + steps;
-    return h;
 }
 
 // What a wave asks of memory for one step: codes of its keys (tokens 16 h + r, channels D / 4 g ..) and values (tokens of
@@ -188,10 +241,14 @@ __device__ __forceinline__ void ask(const Step &s, int32_t head, int32_t lane, i
     x.beta = par[P];
 }
 
-// Partial results of a part: per row the running maximum and sum, and dim unnormalised sums.
-__device__ __forceinline__ int64_t partial_at(const AttendArgs &a, int64_t tile, int32_t head, int32_t part, int32_t row)
+// A workgroup leaves at most two tiles unfinished: the one it begins with (slot 0) and the one it ends with (slot 1).  Per row:
+// running maximum and sum, and dim unnormalised sums.
+struct Unfinished { // a tile whose first steps a workgroup has and whose last it has not; parts 0: there is none
+    int32_t parts, slot, row, first, rows, pad[3];
+};
+__device__ __forceinline__ int64_t partial_at(const AttendArgs &a, int32_t head, int32_t block, int32_t slot, int32_t row)
 {
-    return ((tile * a.s.heads + head) * a.splits + part) * ROWS + row;
+    return (((int64_t)head * a.blocks + block) * 2 + slot) * ROWS + row;
 }
 
 template <int D, bool F32O>
@@ -217,16 +274,48 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
     const Step &s = a.s;
     const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int32_t head = blockIdx.y;
-    const Tile t = tile_of(a, blockIdx.x);
-    if (t.first >= t.rows) return;
-    const Sight v = sight_of(a, t, ROWS);
-    const Share share = share_of(v, a.splits, blockIdx.z);
-    if ((int32_t)blockIdx.z >= share.parts) return;
+    Line line(a);
+    const int32_t of = sharers(a, line.total), block = blockIdx.x;
+    Unfinished left = {};
+    if (block >= of) {
+        if (threadIdx.x == 0) a.unfinished[head * a.blocks + block] = left;
+        return;
+    }
+    const int64_t begin = line.total * block / of, end = line.total * (block + 1) / of;
+    const Codes16 codes;
+    const float factor = lane < 32 ? a.scale2 : 1.0f, sign = lane < 32 ? 1.0f : -1.0f, exact = lane < 32 ? INFINITY : 256.0f;
+
+    int64_t at = begin, seq_begin = 0;
+    int32_t i_seq = line.find(a, begin, &seq_begin);
+    while (at < end && i_seq < s.n_seqs) {
+    Tile t;
+    t.seq = line.seq(a, i_seq);
+    const Work work_here = work_of(a, t.seq);
+    if (at - seq_begin >= work_here.all()) { // on to the next sequence
+        seq_begin += work_here.all(), ++i_seq;
+        continue;
+    }
+    const int64_t number = (at - seq_begin) / work_here.steps;
+    const int32_t skip = (int32_t)(at - seq_begin - number * work_here.steps);
+    const int32_t take = work_here.steps - skip < end - at ? work_here.steps - skip : (int32_t)(end - at);
+    t.first = (int32_t)number * ROWS, t.rows = t.seq.n * a.group;
+    const Sight v = sight_of(a, t);
+    const int32_t step_begin = work_here.first + skip;
+    const int32_t step_end = v.all_hi < 0 || step_begin + take <= v.all_hi / STEP + 1 ? step_begin + take : v.all_hi / STEP + 1;
+    const bool whole = take == work_here.steps;
+    const int32_t slot = at == begin ? 0 : 1;
+    if (skip == 0 && !whole) { // the shares up to the one in which the tile's last step lies
+        const int64_t last = at + work_here.steps - 1;
+        int32_t b = (int32_t)(last * of / line.total);
+        if (b + 1 < of && line.total * (b + 1) / of <= last) ++b;
+        left = Unfinished{b - block + 1, slot, t.seq.row, t.first, t.rows, {}};
+    }
+    at += take;
 
     // this lane's row (a column of the transposed products) and the tokens it sees: lo .. hi
     const int32_t row = t.first + r, token = row / a.group;
     const bool real = row < t.rows;
-    const int32_t pos = t.seq.len - t.seq.n + token, hi = real ? hi_at(v, pos) : -1, lo = lo_at(a, pos);
+    const int32_t pos = t.seq.len - t.seq.n + token, hi = real ? hi_at(v.limit, pos) : -1, lo = lo_at(a, pos);
 
     // queries: element e of step k of lane group g is channel (D / 4) g + 8 k + {0, 4, 1, 5, 2, 6, 3, 7}[e]
     bf16x8 qo[PARTS][KS];
@@ -255,8 +344,6 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
 #pragma unroll
     for (int i = 0; i < DT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.0f; // running maximum; this lane's part of the sum of p
-    const Codes16 codes;
-    const float factor = lane < 32 ? a.scale2 : 1.0f, sign = lane < 32 ? 1.0f : -1.0f, exact = lane < 32 ? INFINITY : 256.0f;
 
     const auto work = [&](const Loaded<D> &x) {
         const float zero = sign * ((float)(int32_t)x.beta + 16.0f);
@@ -362,10 +449,10 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
     // a condition that the compiler cannot see through: the page numbers of up to 64 steps are fetched beforehand, one a lane,
     // and a step without a page reads page 0 and drops it.
     const auto ask_for = [&](int32_t page, int32_t st, Loaded<D> &x) { ask<D>(s, head, lane, page < 0 ? 0 : page, st * STEP, x); };
-    for (int32_t first = share.begin + wave; first < share.end; first += 64 * WAVES) {
+    for (int32_t first = step_begin + wave; first < step_end; first += 64 * WAVES) {
         const int32_t mine = first + lane * WAVES;
-        const int32_t pages = mine < share.end ? page_of(s, t.seq.line, mine * STEP) : -1;
-        const int32_t left = (share.end - first + WAVES - 1) / WAVES, count = left < 64 ? left : 64;
+        const int32_t pages = mine < step_end ? page_of(s, t.seq.line, mine * STEP) : -1;
+        const int32_t left = (step_end - first + WAVES - 1) / WAVES, count = left < 64 ? left : 64;
         Loaded<D> x[2];
         int32_t page = __builtin_amdgcn_readlane(pages, 0);
         ask_for(page, first, x[0]);
@@ -402,48 +489,65 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
             sum += f * mrg_l[w][n];
             o += f * mrg_o[w][n][c];
         }
-        if (share.parts == 1) {
+        if (whole) {
             put_out<D, F32O>(a, t, head, rw, c, quotient(o, sum));
         } else {
-            const int64_t at = partial_at(a, blockIdx.x, head, blockIdx.z, n);
+            const int64_t at = partial_at(a, head, block, slot, n);
             a.part_o[at * D + c] = o;
             if (c == 0) a.part_ml[at] = make_float2(top, sum);
         }
     }
+    __syncthreads(); // before the next tile's results
+    }
+    if (threadIdx.x == 0) a.unfinished[head * a.blocks + block] = left;
 }
 
-// The parts of a tile's rows joined, a workgroup per row: each wave takes every fourth part.
+// The parts of unfinished tiles joined, a workgroup for each that may have begun one: a row's parts are dealt out to as many
+// waves as JOIN_WAVES have for each row.
+constexpr int JOIN_WAVES = 16;
 template <int D, bool F32O>
-__global__ __launch_bounds__(WAVES * 64) void join_kernel(const AttendArgs a)
+__global__ __launch_bounds__(JOIN_WAVES * 64) void join_kernel(const AttendArgs a)
 {
-    __shared__ float sums[WAVES], os[WAVES][D];
-    const int32_t n = blockIdx.z, head = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Tile t = tile_of(a, blockIdx.x);
-    if (t.first + n >= t.rows) return;
-    const Share share = share_of(sight_of(a, t, ROWS), a.splits, 0);
-    if (share.parts == 1) return;
-    float top = -INFINITY;
-    for (int32_t p = lane; p < share.parts; p += 64) top = fmaxf(top, a.part_ml[partial_at(a, blockIdx.x, head, p, n)].x);
+    __shared__ float sums[JOIN_WAVES], os[JOIN_WAVES][D];
+    const int32_t head = blockIdx.y, block = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Unfinished u = a.unfinished[head * a.blocks + block];
+    const int32_t parts = u.parts;
+    if (parts == 0) return;
+    Tile t;
+    t.seq.row = u.row, t.first = u.first, t.rows = u.rows;
+    const int32_t rows = t.rows - t.first < ROWS ? t.rows - t.first : ROWS;
+    const int32_t lanes_of_rows = rows <= 1 ? 1 : 1 << (32 - __clz(rows - 1)), per_row = JOIN_WAVES / lanes_of_rows;
+    const int32_t n = wave % lanes_of_rows, chunk = wave / lanes_of_rows;
+    float top = -INFINITY, sum = 0.0f, o[D / 64] = {};
+    const auto partial = [&](int32_t p) { return partial_at(a, head, block + p, p == 0 ? u.slot : 0, n); };
+    if (n < rows) {
+        for (int32_t p = lane; p < parts; p += 64) top = fmaxf(top, a.part_ml[partial(p)].x);
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float base = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, o[D / 64] = {};
+        for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+        const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll 4
-    for (int32_t p = wave; p < share.parts; p += WAVES) {
-        const int64_t at = partial_at(a, blockIdx.x, head, p, n);
-        const float2 ml = a.part_ml[at];
-        const float f = __builtin_amdgcn_exp2f(ml.x - base);
-        sum += f * ml.y;
+        for (int32_t p = chunk; p < parts; p += per_row) {
+            const int64_t from = partial(p);
+            const float2 ml = a.part_ml[from];
+            const float f = __builtin_amdgcn_exp2f(ml.x - base);
+            sum += f * ml.y;
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) o[c] += f * a.part_o[at * D + 64 * c + lane];
+            for (int c = 0; c < D / 64; ++c) o[c] += f * a.part_o[from * D + 64 * c + lane];
+        }
     }
     if (lane == 0) sums[wave] = sum;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) os[wave][64 * c + lane] = o[c];
     __syncthreads();
-    if (threadIdx.x < D) {
-        const int32_t c = threadIdx.x;
-        put_out<D, F32O>(a, t, head, t.first + n, c, quotient((os[0][c] + os[1][c]) + (os[2][c] + os[3][c]), (sums[0] + sums[1]) + (sums[2] + sums[3])));
+    if (wave < rows) { // row `wave`
+        float all = 0.0f;
+        for (int32_t k = 0; k < per_row; ++k) all += sums[wave + k * lanes_of_rows];
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+            float y = 0.0f;
+            for (int32_t k = 0; k < per_row; ++k) y += os[wave + k * lanes_of_rows][64 * c + lane];
+            put_out<D, F32O>(a, t, head, t.first + wave, 64 * c + lane, quotient(y, all));
+        }
     }
 }
 
@@ -454,22 +558,15 @@ int32_t check(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_
     return QLLM_OK;
 }
 
-// Tiles, and parts of a tile's tokens.  Parts are for few tiles: enough for WANTED workgroups, none shorter than the line is long.
-struct Launch {
-    int64_t tiles;
-    int32_t splits;
-};
-constexpr int64_t WANTED = 1024, MOST_SPLITS = 128;
-Launch plan(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads)
+// Workgroups of a kv head: as many as the card holds at once (three on each of 256 CUs), but none for less than LEAST steps.
+int32_t blocks_of(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads)
 {
+    constexpr int64_t RESIDENT = 768;
     const int64_t group = q_heads / cache->heads;
-    Launch n;
-    n.tiles = batch->row_start ? batch->rows * group / ROWS + batch->n_seqs : batch->n_seqs * ((group + ROWS - 1) / ROWS);
-    const int64_t workgroups = n.tiles * cache->heads, steps = batch->table_ld * cache->page_tokens / STEP;
-    int64_t splits = workgroups > 0 ? WANTED / workgroups : 1;
-    if (splits > (steps + LEAST - 1) / LEAST) splits = (steps + LEAST - 1) / LEAST;
-    n.splits = (int32_t)(splits < 1 ? 1 : (splits > MOST_SPLITS ? MOST_SPLITS : splits));
-    return n;
+    const int64_t tiles = batch->row_start ? batch->rows * group / ROWS + batch->n_seqs : batch->n_seqs * ((group + ROWS - 1) / ROWS);
+    const int64_t most = tiles * (batch->table_ld * cache->page_tokens / STEP) / LEAST + 1; // below 2^62
+    const int64_t blocks = cache->heads < RESIDENT ? RESIDENT / cache->heads : 1;
+    return (int32_t)(blocks < most ? blocks : most);
 }
 
 } // namespace
@@ -480,8 +577,7 @@ extern "C" int64_t qllm_kv_attention_workspace_bytes(const qllm_kv_cache *cache,
     int32_t rc = prepare_step(cache, batch, false, &s);
     if (rc == QLLM_OK) rc = check(cache, batch, q_heads);
     if (rc != QLLM_OK) return rc;
-    const Launch n = plan(cache, batch, q_heads);
-    return 256 + (n.splits > 1 ? n.tiles * cache->heads * n.splits * ROWS * (cache->dim + 2) * (int64_t)sizeof(float) : 0);
+    return cache->heads * blocks_of(cache, batch, q_heads) * (2 * ROWS * (cache->dim + 2) * (int64_t)sizeof(float) + (int64_t)sizeof(Unfinished));
 }
 
 extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq, int64_t q_heads, const qllm_kv_cache *cache,
@@ -505,11 +601,12 @@ extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq
     a.q_heads = (int32_t)q_heads, a.group = (int32_t)(q_heads / cache->heads);
     a.window = window > INT32_MAX ? 0 : (int32_t)window;
     a.scale2 = scale * LOG2E;
-    const Launch n = plan(cache, batch, q_heads);
-    a.splits = n.splits;
-    a.part_ml = static_cast<float2 *>(workspace);
-    a.part_o = static_cast<float *>(workspace) + 2 * n.tiles * cache->heads * n.splits * ROWS;
-    const dim3 grid((unsigned)n.tiles, (unsigned)cache->heads, (unsigned)n.splits), rows((unsigned)n.tiles, (unsigned)cache->heads, ROWS);
+    a.blocks = blocks_of(cache, batch, q_heads);
+    const int64_t parts = cache->heads * a.blocks;
+    a.unfinished = static_cast<Unfinished *>(workspace);
+    a.part_ml = reinterpret_cast<float2 *>(a.unfinished + parts);
+    a.part_o = reinterpret_cast<float *>(a.part_ml + parts * 2 * ROWS);
+    const dim3 grid((unsigned)a.blocks, (unsigned)cache->heads);
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();
 #define QLLM_ATTEND(D, FQ, FO) hipLaunchKernelGGL((attend_kernel<D, FQ, FO>), grid, dim3(WAVES * 64), 0, stream, a)
@@ -526,10 +623,11 @@ extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq
     }
 #undef QLLM_ATTEND
     rc = launched("cache attention: launch");
-    if (rc != QLLM_OK || n.splits == 1) return rc;
-    if (cache->dim == 128 && out_dtype == QLLM_F32) hipLaunchKernelGGL((join_kernel<128, true>), rows, dim3(WAVES * 64), 0, stream, a);
-    else if (cache->dim == 128) hipLaunchKernelGGL((join_kernel<128, false>), rows, dim3(WAVES * 64), 0, stream, a);
-    else if (out_dtype == QLLM_F32) hipLaunchKernelGGL((join_kernel<64, true>), rows, dim3(WAVES * 64), 0, stream, a);
-    else hipLaunchKernelGGL((join_kernel<64, false>), rows, dim3(WAVES * 64), 0, stream, a);
+    if (rc != QLLM_OK || a.blocks == 1) return rc; // one workgroup a head finishes what it begins
+    const dim3 cuts((unsigned)a.blocks, (unsigned)cache->heads);
+    if (cache->dim == 128 && out_dtype == QLLM_F32) hipLaunchKernelGGL((join_kernel<128, true>), cuts, dim3(JOIN_WAVES * 64), 0, stream, a);
+    else if (cache->dim == 128) hipLaunchKernelGGL((join_kernel<128, false>), cuts, dim3(JOIN_WAVES * 64), 0, stream, a);
+    else if (out_dtype == QLLM_F32) hipLaunchKernelGGL((join_kernel<64, true>), cuts, dim3(JOIN_WAVES * 64), 0, stream, a);
+    else hipLaunchKernelGGL((join_kernel<64, false>), cuts, dim3(JOIN_WAVES * 64), 0, stream, a);
     return launched("cache attention: parts joined");
 }
