@@ -12,6 +12,7 @@
 #include <math.h>
 #include <stdint.h>
 
+#include "fused_common.h"
 #include "kv_common.h"
 
 namespace {
@@ -36,10 +37,13 @@ struct AttendArgs {
     int64_t ldq, ldo;
     int32_t q_heads, group, window; // window 0: none
     float scale2;                   // scale * log2 e
+    int32_t q_vec;                  // bf16 queries in 16-byte pieces
+    qllm_detail::QuotientBy by_group; // for numbers below group + ROWS
     int32_t blocks;                 // workgroups of a kv head
     float *part_o;                  // their partial results, see partial_at
     float2 *part_ml;
-    Unfinished *unfinished;   // [heads][blocks]
+    int32_t numbers;                // of tiles, see number_of
+    Unfinished *unfinished;         // [heads][numbers]
 };
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
@@ -88,12 +92,12 @@ __device__ __forceinline__ int32_t limit_of(const AttendArgs &a, const Seq &q)
     return q.line < 0 ? 0 : (q.len < cap ? q.len : cap);
 }
 
-__device__ __forceinline__ Sight sight_of(const AttendArgs &a, const Tile &t)
+__device__ __forceinline__ Sight sight_of(const AttendArgs &a, const Tile &t, int32_t tok0, int32_t head0)
 {
     Sight v;
     v.limit = limit_of(a, t.seq);
-    const int32_t last_row = t.first + ROWS < t.rows ? t.first + ROWS - 1 : t.rows - 1;
-    const int32_t p_first = t.seq.len - t.seq.n + t.first / a.group, p_last = t.seq.len - t.seq.n + last_row / a.group;
+    const int32_t rows = t.rows - t.first < ROWS ? t.rows - t.first : ROWS;
+    const int32_t p_first = t.seq.len - t.seq.n + tok0, p_last = p_first + (int32_t)a.by_group.divide((uint32_t)(head0 + rows - 1));
     v.all_lo = lo_at(a, p_first), v.all_hi = hi_at(v.limit, p_last);
     v.each_lo = lo_at(a, p_last), v.each_hi = hi_at(v.limit, p_first);
     return v;
@@ -104,88 +108,100 @@ __device__ __forceinline__ Sight sight_of(const AttendArgs &a, const Tile &t)
 // head share the line out evenly, whatever the lengths: one may end in the middle of a tile and the next go on there.
 struct Work {
     int32_t tiles, first, steps; // of a sequence; its first step is number `first` of the cache line
-    // (a bound that only a row_start that does not ascend can reach: 2^20 of these still add up)
-    __device__ __forceinline__ int64_t all() const { return min((int64_t)tiles * steps, (int64_t)1 << 42); }
 };
 
 __device__ __forceinline__ Work work_of(const AttendArgs &a, const Seq &q)
 {
     Work w;
-    w.tiles = (int32_t)(((int64_t)q.n * a.group + ROWS - 1) / ROWS);
+    w.tiles = (int32_t)(((uint32_t)(q.n * a.group) + ROWS - 1) / ROWS); // n * group: checked on the host
     const int32_t lo = lo_at(a, q.len - q.n), hi = hi_at(limit_of(a, q), q.len - 1);
     w.first = lo / STEP;
     w.steps = hi < lo ? 1 : hi / STEP + 1 - w.first;
     return w;
 }
 
-__device__ __forceinline__ int64_t lane64(int64_t x, int32_t lane) // lane `lane`'s x, the same in every lane and known to be
-{
-    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int32_t)((uint64_t)x >> 32), lane) << 32 |
-                     (uint32_t)__builtin_amdgcn_readlane((int32_t)x, lane));
-}
-
-// The line as one wave sees it: 64 sequences at a time, one a lane.  Up to 64 are read from memory once.
+// The line as one wave sees it, 64 sequences at a time, one a lane.  Up to 64 are read from memory once and kept in LDS (every
+// wave writes the same there, before it reads).  The host checks that a line stays below 2^31 steps; sums saturate, for a
+// row_start that does not ascend.
+struct Listed {
+    Seq seq;
+    int32_t upto; // where it ends in the line
+};
 struct Line {
-    Seq mine;      // sequence base + lane
-    int64_t upto;  // where it ends
-    int64_t total; // the whole line
-    int32_t base;
+    Listed *list; // [64]
+    int32_t total;
 
-    __device__ __forceinline__ void look(const AttendArgs &a, int32_t from, int64_t before)
+    static __device__ __forceinline__ Listed look(const AttendArgs &a, int32_t from, int32_t before)
     {
         const int32_t lane = threadIdx.x & 63, i = from + lane;
-        base = from;
-        mine = Seq{0, 0, -1, 0};
-        if (i < a.s.n_seqs) mine = seq_of(a.s, i);
-        upto = work_of(a, mine).all(); // none without rows
-        if (i >= a.s.n_seqs) upto = 0;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t y = __shfl_up(upto, o);
-            if (lane >= o) upto += y;
+        Listed x;
+        x.seq = Seq{0, 0, -1, 0};
+        if (i < a.s.n_seqs) x.seq = seq_of(a.s, i);
+        const Work w = work_of(a, x.seq); // without rows: no tiles
+        x.upto = w.tiles * w.steps;
+        for (int32_t o = 1; o < 64 && o < a.s.n_seqs; o <<= 1) {
+            const int32_t y = __shfl_up(x.upto, o);
+            if (lane >= o) x.upto = __builtin_elementwise_add_sat(x.upto, y);
         }
-        upto += before;
+        x.upto = __builtin_elementwise_add_sat(x.upto, before);
+        return x;
     }
-    __device__ __forceinline__ explicit Line(const AttendArgs &a)
+    __device__ __forceinline__ Line(const AttendArgs &a, Listed *room) : list(room), total(0)
     {
-        total = 0;
         for (int32_t from = 0; from < a.s.n_seqs; from += 64) {
-            look(a, from, total);
-            total = lane64(upto, 63);
+            const Listed x = look(a, from, total);
+            if (a.s.n_seqs <= 64) list[threadIdx.x & 63] = x;
+            total = __builtin_amdgcn_readlane(x.upto, a.s.n_seqs - from < 64 ? a.s.n_seqs - from - 1 : 63);
         }
-        if (total >= (int64_t)1 << 50) total = 0; // see Work::all
+        if (total == INT32_MAX) total = 0;
+        __builtin_amdgcn_wave_barrier();
     }
     // The sequence that step `at` < total belongs to; *begin: where that begins.
-    __device__ __forceinline__ int32_t find(const AttendArgs &a, int64_t at, int64_t *begin)
+    __device__ __forceinline__ int32_t find(const AttendArgs &a, int32_t at, int32_t *begin) const
     {
-        int64_t before = 0;
+        const int32_t lane = threadIdx.x & 63;
+        int32_t before = 0;
         for (int32_t from = 0; from < a.s.n_seqs; from += 64) {
-            if (a.s.n_seqs > 64) look(a, from, before);
-            const int32_t skipped = __popcll(__ballot(upto <= at)); // sequences that end at or before it
+            const int32_t upto = a.s.n_seqs <= 64 ? list[lane].upto : look(a, from, before).upto;
+            const int32_t skipped = __popcll(__ballot(from + lane < a.s.n_seqs && upto <= at)); // sequences that end at or before it
+            if (skipped) before = __builtin_amdgcn_readlane(upto, skipped - 1);
             if (skipped < 64) {
-                *begin = skipped ? lane64(upto, skipped - 1) : before;
+                *begin = before;
                 return from + skipped;
             }
-            before = lane64(upto, 63);
         }
         return a.s.n_seqs;
     }
-    __device__ __forceinline__ Seq seq(const AttendArgs &a, int32_t i)
+    __device__ __forceinline__ Seq seq(const AttendArgs &a, int32_t i) const
     {
-        if (i < base || i >= base + 64) look(a, i, 0); // only its sequences are asked for from now on
-        const int32_t k = i - base;
-        return Seq{__builtin_amdgcn_readlane(mine.row, k), __builtin_amdgcn_readlane(mine.n, k), __builtin_amdgcn_readlane(mine.line, k),
-                   __builtin_amdgcn_readlane(mine.len, k)};
+        const Seq q = a.s.n_seqs <= 64 ? list[i].seq : seq_of(a.s, i);
+        return Seq{__builtin_amdgcn_readfirstlane(q.row), __builtin_amdgcn_readfirstlane(q.n), __builtin_amdgcn_readfirstlane(q.line),
+                   __builtin_amdgcn_readfirstlane(q.len)};
     }
 };
 
-// How many workgroups share the line: none gets less than LEAST steps while another has some.  Share b begins at total * b / of.
+// How many workgroups share the line (none gets less than LEAST steps while another has some), and where share b begins: any
+// rising function of b that all workgroups evaluate alike will do, so one product in double does.
 constexpr int LEAST = 16;
-__device__ __forceinline__ int32_t sharers(const AttendArgs &a, int64_t total)
-{
-    const int64_t most = (total + LEAST - 1) / LEAST;
-    return most < a.blocks ? (int32_t)most : a.blocks;
-}
+struct Shares {
+    int32_t total, of;
+    double each;
+    __device__ __forceinline__ Shares(const AttendArgs &a, int32_t steps)
+    {
+        total = steps;
+        of = total / LEAST + (total % LEAST != 0);
+        if (of > a.blocks) of = a.blocks;
+        each = (double)total / (double)(of > 0 ? of : 1);
+    }
+    __device__ __forceinline__ int32_t begin(int32_t b) const { return b >= of ? total : __builtin_amdgcn_readfirstlane((int32_t)(each * (double)b)); }
+    __device__ __forceinline__ int32_t share_of(int32_t step) const // the share that step `step` lies in
+    {
+        int32_t b = __builtin_amdgcn_readfirstlane((int32_t)((double)step / each));
+        while (b > 0 && begin(b) > step) --b; // one off at most
+        while (b + 1 < of && begin(b + 1) <= step) ++b;
+        return b;
+    }
+};
 
 template <bool F32>
 __device__ __forceinline__ float load1(const void *p, int64_t at)
@@ -206,56 +222,71 @@ __device__ __forceinline__ void split(float x, float (&part)[PARTS])
 
 // What a wave asks of memory for one step: codes of its keys (tokens 16 h + r, channels D / 4 g ..) and values (tokens of
 // element e, channels D / 16 r ..), and one token's alpha and beta, of the keys in lanes 0..31, of the values in the others.
+// Addresses are a base for the wave and 32-bit offsets for the lanes.
 template <int D>
-struct Loaded {
-    uint32_t k[2][D / 32], v[8], beta;
+struct Codes {
+    uint32_t k[2][D / 32], v[8];
     float alpha;
-    int32_t t0; // its first token, -1: nothing
+    int32_t beta;
 };
-
 template <int D>
-__device__ __forceinline__ void ask(const Step &s, int32_t head, int32_t lane, int32_t page, int32_t t0, Loaded<D> &x)
-{
-    const int32_t P = 1 << s.page_shift, r = lane & 15, g = lane >> 4, in_page = t0 & (P - 1);
-    const uint8_t *part = s.pages + page * s.page_bytes + (int64_t)head * P * (D + 16);
-    const uint8_t *kc = part + (int64_t)in_page * (D / 2), *vc = kc + (int64_t)P * (D / 2);
-    x.t0 = t0;
+struct Loads {
+    uint32_t key_at, value_at, param_at; // of the lane
+
+    __device__ __forceinline__ Loads(int32_t lane, int32_t P)
+    {
+        const uint32_t r = lane & 15, g = lane >> 4;
+        key_at = r * (D / 2) + D / 8 * g;
+        value_at = 4 * g * (D / 2) + D / 32 * r;
+        param_at = ((lane >> 5) * 2 * P + (lane & 31)) * 4;
+    }
+    __device__ __forceinline__ void ask(const Step &s, int32_t head, int32_t page, int32_t t0, Codes<D> &x) const
+    {
+        const int32_t P = 1 << s.page_shift, in_page = t0 & (P - 1);
+        const uint8_t *part = s.pages + (page < 0 ? 0 : page) * s.page_bytes + (int64_t)head * P * (D + 16);
+        const uint8_t *keys = part + in_page * (D / 2), *values = keys + P * (D / 2), *alphas = part + P * D + in_page * 4;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint8_t *src = kc + (16 * h + r) * (D / 2) + D / 8 * g;
-        if (D == 128) {
-            const uint4 w = *reinterpret_cast<const uint4 *>(src);
-            x.k[h][0] = w.x, x.k[h][1] = w.y, x.k[h][D / 32 - 2] = w.z, x.k[h][D / 32 - 1] = w.w;
-        } else {
-            const uint2 w = *reinterpret_cast<const uint2 *>(src);
-            x.k[h][0] = w.x, x.k[h][1] = w.y;
+        for (int h = 0; h < 2; ++h) {
+            const uint8_t *src = keys + key_at + 16 * h * (D / 2);
+            if (D == 128) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(src);
+                x.k[h][0] = w.x, x.k[h][1] = w.y, x.k[h][D / 32 - 2] = w.z, x.k[h][D / 32 - 1] = w.w;
+            } else {
+                const uint2 w = *reinterpret_cast<const uint2 *>(src);
+                x.k[h][0] = w.x, x.k[h][1] = w.y;
+            }
         }
-    }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint8_t *src = vc + (16 * (e >> 2) + 4 * g + (e & 3)) * (D / 2) + D / 32 * r;
-        x.v[e] = D == 128 ? *reinterpret_cast<const uint32_t *>(src) : *reinterpret_cast<const uint16_t *>(src);
+        for (int e = 0; e < 8; ++e) {
+            const uint8_t *src = values + value_at + (16 * (e >> 2) + (e & 3)) * (D / 2);
+            x.v[e] = D == 128 ? *reinterpret_cast<const uint32_t *>(src) : *reinterpret_cast<const uint16_t *>(src);
+        }
+        x.alpha = *reinterpret_cast<const float *>(alphas + param_at);
+        x.beta = *reinterpret_cast<const int32_t *>(alphas + 4 * P + param_at);
     }
-    const uint32_t *par = reinterpret_cast<const uint32_t *>(part + (int64_t)P * D) + (lane >> 5) * 2 * P + in_page + (lane & 31);
-    x.alpha = __uint_as_float(par[0]);
-    x.beta = par[P];
-}
+};
 
 // A workgroup leaves at most two tiles unfinished: the one it begins with (slot 0) and the one it ends with (slot 1).  Per row:
 // running maximum and sum, and dim unnormalised sums.
-struct Unfinished { // a tile whose first steps a workgroup has and whose last it has not; parts 0: there is none
-    int32_t parts, slot, row, first, rows, pad[3];
+struct Unfinished { // how a tile is to be joined: its parts (1: nothing to join), the workgroup of the first and the slot there,
+    int32_t parts, block, slot, q_row, head0, rows, pad[2]; // its first row, head head0 of row q_row, and how many
 };
+// Sequence i's tiles are numbered from row_start[i] * group / ROWS + i on: at least as many numbers as it has tiles, in order.
+__device__ __forceinline__ int32_t number_of(const AttendArgs &a, int32_t i)
+{
+    return a.s.row_start ? (int32_t)((uint32_t)(row_of(a.s, i) * a.group) / ROWS) + i : i * ((a.group + ROWS - 1) / ROWS);
+}
 __device__ __forceinline__ int64_t partial_at(const AttendArgs &a, int32_t head, int32_t block, int32_t slot, int32_t row)
 {
     return (((int64_t)head * a.blocks + block) * 2 + slot) * ROWS + row;
 }
 
+// Channel c of row n of a tile whose first row is head head0 of row q_row of the step's tensors
 template <int D, bool F32O>
-__device__ __forceinline__ void put_out(const AttendArgs &a, const Tile &t, int32_t head, int32_t row, int32_t c, float y)
+__device__ __forceinline__ void put_out(const AttendArgs &a, int32_t head, int32_t q_row, int32_t head0, int32_t n, int32_t c, float y)
 {
-    const int32_t tok = row / a.group;
-    const int64_t at = (int64_t)(t.seq.row + tok) * a.ldo + (int64_t)(head * a.group + row - tok * a.group) * D + c;
+    const int32_t tok = (int32_t)a.by_group.divide((uint32_t)(head0 + n));
+    const int64_t at = (int64_t)(q_row + tok) * a.ldo + (head * a.group + head0 + n - tok * a.group) * D + c;
     if (F32O) static_cast<float *>(a.out)[at] = y;
     else static_cast<uint16_t *>(a.out)[at] = (uint16_t)pack_bf16(y, 0.0f);
 }
@@ -270,50 +301,52 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
     __shared__ float mrg_m[WAVES][ROWS], mrg_l[WAVES][ROWS], mrg_o[WAVES][ROWS][D + 4];
     // a token's parameters, worked out by one lane and read by sixteen: a key's factor and 16 + beta, a value's alpha and - (16 + beta)
     __shared__ __attribute__((aligned(16))) float2 params[WAVES][64];
+    __shared__ Listed listed[64];
 
     const Step &s = a.s;
     const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int32_t head = blockIdx.y;
-    Line line(a);
-    const int32_t of = sharers(a, line.total), block = blockIdx.x;
-    Unfinished left = {};
-    if (block >= of) {
-        if (threadIdx.x == 0) a.unfinished[head * a.blocks + block] = left;
-        return;
-    }
-    const int64_t begin = line.total * block / of, end = line.total * (block + 1) / of;
+    const Line line(a, listed);
+    const Shares shares(a, line.total);
+    const int32_t block = blockIdx.x;
+    const int32_t begin = shares.begin(block), end = shares.begin(block + 1);
     const Codes16 codes;
     const float factor = lane < 32 ? a.scale2 : 1.0f, sign = lane < 32 ? 1.0f : -1.0f, exact = lane < 32 ? INFINITY : 256.0f;
 
-    int64_t at = begin, seq_begin = 0;
-    int32_t i_seq = line.find(a, begin, &seq_begin);
+    int32_t at = begin, seq_begin = 0, i_seq = 0;
+    if (at < end) i_seq = line.find(a, begin, &seq_begin);
     while (at < end && i_seq < s.n_seqs) {
     Tile t;
     t.seq = line.seq(a, i_seq);
     const Work work_here = work_of(a, t.seq);
-    if (at - seq_begin >= work_here.all()) { // on to the next sequence
-        seq_begin += work_here.all(), ++i_seq;
+    if (at - seq_begin >= work_here.tiles * work_here.steps) { // on to the next sequence
+        seq_begin += work_here.tiles * work_here.steps, ++i_seq;
         continue;
     }
-    const int64_t number = (at - seq_begin) / work_here.steps;
-    const int32_t skip = (int32_t)(at - seq_begin - number * work_here.steps);
-    const int32_t take = work_here.steps - skip < end - at ? work_here.steps - skip : (int32_t)(end - at);
-    t.first = (int32_t)number * ROWS, t.rows = t.seq.n * a.group;
-    const Sight v = sight_of(a, t);
+    const int32_t number = (int32_t)((uint32_t)(at - seq_begin) / (uint32_t)work_here.steps);
+    const int32_t skip = at - seq_begin - number * work_here.steps;
+    const int32_t take = work_here.steps - skip < end - at ? work_here.steps - skip : end - at;
+    t.first = number * ROWS, t.rows = t.seq.n * a.group;
+    const int32_t tok0 = (int32_t)((uint32_t)t.first / (uint32_t)a.group), head0 = t.first - tok0 * a.group; // of the tile's first row
+    const Sight v = sight_of(a, t, tok0, head0);
     const int32_t step_begin = work_here.first + skip;
     const int32_t step_end = v.all_hi < 0 || step_begin + take <= v.all_hi / STEP + 1 ? step_begin + take : v.all_hi / STEP + 1;
     const bool whole = take == work_here.steps;
     const int32_t slot = at == begin ? 0 : 1;
-    if (skip == 0 && !whole) { // the shares up to the one in which the tile's last step lies
-        const int64_t last = at + work_here.steps - 1;
-        int32_t b = (int32_t)(last * of / line.total);
-        if (b + 1 < of && line.total * (b + 1) / of <= last) ++b;
-        left = Unfinished{b - block + 1, slot, t.seq.row, t.first, t.rows, {}};
-    }
+    if (skip == 0 && threadIdx.x == 0 && a.numbers) // numbers 0: every workgroup finishes what it begins
+        a.unfinished[(int64_t)head * a.numbers + number_of(a, i_seq) + number] = Unfinished{
+            whole ? 1 : shares.share_of(at + work_here.steps - 1) - block + 1, block, slot, t.seq.row + tok0, head0, t.rows - t.first < ROWS ? t.rows - t.first : ROWS, {}};
     at += take;
 
+    // page numbers of up to 64 steps of this wave, one a lane
+    const auto pages_from = [&](int32_t first) {
+        const int32_t mine = first + lane * WAVES;
+        return mine < step_end ? page_of(s, t.seq.line, mine * STEP) : -1;
+    };
+    int32_t pages = pages_from(step_begin + wave);
+
     // this lane's row (a column of the transposed products) and the tokens it sees: lo .. hi
-    const int32_t row = t.first + r, token = row / a.group;
+    const int32_t row = t.first + r, token = tok0 + (int32_t)a.by_group.divide((uint32_t)(head0 + r)), head_of_row = head0 + r - (token - tok0) * a.group;
     const bool real = row < t.rows;
     const int32_t pos = t.seq.len - t.seq.n + token, hi = real ? hi_at(v.limit, pos) : -1, lo = lo_at(a, pos);
 
@@ -321,20 +354,38 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
     bf16x8 qo[PARTS][KS];
     float qsum = 0.0f;
     {
-        const int64_t at = (int64_t)(t.seq.row + token) * a.ldq + (int64_t)(head * a.group + row - token * a.group) * D + D / 4 * g;
+        const int64_t from = (int64_t)(t.seq.row + token) * a.ldq + (head * a.group + head_of_row) * D + D / 4 * g;
+        if (!F32Q && a.q_vec) {
+            uint4 w[KS];
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            float x[8], part[8][PARTS];
+            for (int k = 0; k < KS; ++k) w[k] = make_uint4(0, 0, 0, 0);
+            if (real) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[e] = real ? load1<F32Q>(a.q, at + 8 * k + (e >> 1) + 4 * (e & 1)) : 0.0f;
-                qsum += x[e];
-                split<PARTS>(x[e], part[e]);
+                for (int k = 0; k < KS; ++k) w[k] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q) + from + 8 * k);
             }
 #pragma unroll
-            for (int i = 0; i < PARTS; ++i)
-                qo[i][k] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part[0][i], part[1][i]), pack_bf16(part[2][i], part[3][i]),
-                                                            pack_bf16(part[4][i], part[5][i]), pack_bf16(part[6][i], part[7][i])});
+            for (int k = 0; k < KS; ++k) {
+                const uint32_t d[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) qsum += __uint_as_float(d[e] << 16) + __uint_as_float(d[e] & 0xffff0000u);
+                qo[0][k] = __builtin_bit_cast(bf16x8, u32x4{__builtin_amdgcn_perm(d[2], d[0], 0x05040100u), __builtin_amdgcn_perm(d[2], d[0], 0x07060302u),
+                                                            __builtin_amdgcn_perm(d[3], d[1], 0x05040100u), __builtin_amdgcn_perm(d[3], d[1], 0x07060302u)});
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                float x[8], part[8][PARTS];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = real ? load1<F32Q>(a.q, from + 8 * k + (e >> 1) + 4 * (e & 1)) : 0.0f;
+                    qsum += x[e];
+                    split<PARTS>(x[e], part[e]);
+                }
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i)
+                    qo[i][k] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part[0][i], part[1][i]), pack_bf16(part[2][i], part[3][i]),
+                                                                pack_bf16(part[4][i], part[5][i]), pack_bf16(part[6][i], part[7][i])});
+            }
         }
         qsum += __shfl_xor(qsum, 16);
         qsum += __shfl_xor(qsum, 32);
@@ -345,126 +396,139 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
     for (int i = 0; i < DT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.0f; // running maximum; this lane's part of the sum of p
 
-    const auto work = [&](const Loaded<D> &x) {
-        const float zero = sign * ((float)(int32_t)x.beta + 16.0f);
-        params[wave][lane] = make_float2(x.alpha * factor, zero);
-        const bool far = __any(fabsf(zero) > exact); // some - (16 + beta) of a value has more than the 8 bits of a bf16
-        __builtin_amdgcn_wave_barrier();
-        float sc[8], va[8], vz[8]; // scores, the values' alpha and - (16 + beta), of tokens 16 h + 4 g + i
+    const auto work = [&](const Codes<D> &x, int32_t t0, int32_t page) {
+            const float zero = sign * ((float)x.beta + 16.0f);
+            params[wave][lane] = make_float2(x.alpha * factor, zero);
+            const bool far = __any(fabsf(zero) > exact); // some - (16 + beta) of a value has more than the 8 bits of a bf16
+            __builtin_amdgcn_wave_barrier();
+            const float4 *par = reinterpret_cast<const float4 *>(&params[wave][4 * g]); // tokens 16 h + 4 g + i at 8 h + i / 2, values' behind
+            float sc[8];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            f32x4 d = {0.f, 0.f, 0.f, 0.f};
+            for (int h = 0; h < 2; ++h) {
+                f32x4 d = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = PARTS - 1; i >= 0; --i)
+                for (int i = PARTS - 1; i >= 0; --i)
 #pragma unroll
-                for (int k = 0; k < KS; ++k) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes.operand(x.k[h][k]), qo[i][k], d, 0, 0, 0);
-            const float4 *kp = reinterpret_cast<const float4 *>(&params[wave][16 * h + 4 * g]), *vp = kp + STEP / 2;
-            const float4 k0 = kp[0], k1 = kp[1], v0 = vp[0], v1 = vp[1];
-            const float ka[4] = {k0.x, k0.z, k1.x, k1.z}, kb[4] = {k0.y, k0.w, k1.y, k1.w};
-            va[4 * h] = v0.x, va[4 * h + 1] = v0.z, va[4 * h + 2] = v1.x, va[4 * h + 3] = v1.z;
-            vz[4 * h] = v0.y, vz[4 * h + 1] = v0.w, vz[4 * h + 2] = v1.y, vz[4 * h + 3] = v1.w;
+                    for (int k = 0; k < KS; ++k) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes.operand(x.k[h][k]), qo[i][k], d, 0, 0, 0);
+                const float4 k0 = par[8 * h], k1 = par[8 * h + 1];
+                const float ka[4] = {k0.x, k0.z, k1.x, k1.z}, kb[4] = {k0.y, k0.w, k1.y, k1.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sc[4 * h + i] = ka[i] * __builtin_fmaf(-kb[i], qsum, d[i]);
-        }
-        if (x.t0 < v.each_lo || x.t0 + STEP - 1 > v.each_hi) { // some row does not see some token; what lies there may be anything
-            int32_t t0 = x.t0 + 4 * g;
-            asm volatile("" : "+v"(t0)); // keeps the comparisons in here
+                for (int i = 0; i < 4; ++i) sc[4 * h + i] = ka[i] * __builtin_fmaf(-kb[i], qsum, d[i]);
+            }
+            float va[8];
+            bf16x8 zeros; // - (16 + beta) of the values: the high halves, the number itself where it has 8 bits
+            {
+                float vz[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float4 v0 = par[16 + 8 * (i >> 1) + (i & 1)];
+                    va[2 * i] = v0.x, vz[2 * i] = v0.y, va[2 * i + 1] = v0.z, vz[2 * i + 1] = v0.w;
+                }
+                u32x4 y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = __builtin_amdgcn_perm(__float_as_uint(vz[2 * e + 1]), __float_as_uint(vz[2 * e]), 0x07060302u);
+                zeros = __builtin_bit_cast(bf16x8, y);
+            }
+            if (t0 < v.each_lo || t0 + STEP - 1 > v.each_hi || page < 0) { // some row does not see some token; what lies there may be anything
+                int32_t mine = t0 + 4 * g;
+                asm volatile("" : "+v"(mine)); // keeps the comparisons in here
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int32_t tok = mine + 16 * (i >> 2) + (i & 3);
+                    const bool seen = tok >= lo && tok <= hi && page >= 0;
+                    sc[i] = seen ? sc[i] : -INFINITY;
+                    va[i] = seen ? va[i] : 0.0f;
+                }
+            }
+            float top = sc[0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[i]);
+            if (__any(top > m + SLACK)) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float now = fmaxf(m, top);
+                const float f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - now);
+                m = now, l *= f;
+#pragma unroll
+                for (int i = 0; i < DT; ++i) acc[i] *= f;
+            }
+            const float base = m == -INFINITY ? 0.0f : m;
+            float part_p[8][PARTS];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int32_t tok = t0 + 16 * (i >> 2) + (i & 3);
-                const bool seen = tok >= lo && tok <= hi;
-                sc[i] = seen ? sc[i] : -INFINITY;
-                va[i] = seen ? va[i] : 0.0f;
+                const float p = __builtin_amdgcn_exp2f(sc[i] - base);
+                l += p;
+                split<PARTS>(p * va[i], part_p[i]);
             }
-        }
-        float top = sc[0];
+            bf16x8 pw[PARTS];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[i]);
-        if (__any(top > m + SLACK)) {
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float now = fmaxf(m, top);
-            const float f = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - now);
-            m = now, l *= f;
+            for (int j = 0; j < PARTS; ++j)
+                pw[j] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part_p[0][j], part_p[1][j]), pack_bf16(part_p[2][j], part_p[3][j]),
+                                                         pack_bf16(part_p[4][j], part_p[5][j]), pack_bf16(part_p[6][j], part_p[7][j])});
+            uint32_t low[4], high[4]; // codes 0..3 and 4..7 of two neighbouring tokens
 #pragma unroll
-            for (int i = 0; i < DT; ++i) acc[i] *= f;
-        }
-        const float base = m == -INFINITY ? 0.0f : m;
-        float part_p[8][PARTS];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float p = __builtin_amdgcn_exp2f(sc[i] - base);
-            l += p;
-            split<PARTS>(p * va[i], part_p[i]);
-        }
-        bf16x8 pw[PARTS];
-#pragma unroll
-        for (int j = 0; j < PARTS; ++j)
-            pw[j] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part_p[0][j], part_p[1][j]), pack_bf16(part_p[2][j], part_p[3][j]),
-                                                     pack_bf16(part_p[4][j], part_p[5][j]), pack_bf16(part_p[6][j], part_p[7][j])});
-        uint32_t low[4], high[4]; // codes 0..3 and 4..7 of two neighbouring tokens
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            low[e] = __builtin_amdgcn_perm(x.v[2 * e + 1], x.v[2 * e], 0x05040100u);
-            high[e] = __builtin_amdgcn_perm(x.v[2 * e + 1], x.v[2 * e], 0x07060302u);
-        }
-        // (16 + c) - (16 + beta) in two products: the sums stay as small as the values are, whatever the number of tokens
-        const auto high_halves = [&] { // of - (16 + beta): the number itself where it has 8 bits
-            u32x4 y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = __builtin_amdgcn_perm(__float_as_uint(vz[2 * e + 1]), __float_as_uint(vz[2 * e]), 0x07060302u);
-            return __builtin_bit_cast(bf16x8, y);
-        };
-        const bf16x8 zero0 = high_halves();
-        const auto tile = [&](int i, bf16x8 c) {
-#pragma unroll
-            for (int j = PARTS - 1; j >= 0; --j) {
-                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(zero0, pw[j], acc[i], 0, 0, 0);
-                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c, pw[j], acc[i], 0, 0, 0);
+            for (int e = 0; e < 4; ++e) {
+                low[e] = __builtin_amdgcn_perm(x.v[2 * e + 1], x.v[2 * e], 0x05040100u);
+                high[e] = __builtin_amdgcn_perm(x.v[2 * e + 1], x.v[2 * e], 0x07060302u);
             }
-        };
-        const auto four = [&](const uint32_t (&w)[4], int at) {
-            tile(at + 0, __builtin_bit_cast(bf16x8, u32x4{codes.pair<0>(w[0]), codes.pair<0>(w[1]), codes.pair<0>(w[2]), codes.pair<0>(w[3])}));
-            tile(at + 1, __builtin_bit_cast(bf16x8, u32x4{codes.pair<1>(w[0]), codes.pair<1>(w[1]), codes.pair<1>(w[2]), codes.pair<1>(w[3])}));
-            tile(at + 2, __builtin_bit_cast(bf16x8, u32x4{codes.pair<2>(w[0]), codes.pair<2>(w[1]), codes.pair<2>(w[2]), codes.pair<2>(w[3])}));
-            tile(at + 3, __builtin_bit_cast(bf16x8, u32x4{codes.pair<3>(w[0]), codes.pair<3>(w[1]), codes.pair<3>(w[2]), codes.pair<3>(w[3])}));
-        };
-        four(low, 0);
-        if (D == 128) four(high, DT - 4);
-        if (far) { // values far from zero for their range: what the high halves leave out
+            // (16 + c) - (16 + beta) in two products: the sums stay as small as the values are, whatever the number of tokens
+            const auto tile = [&](int i, bf16x8 c) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+                for (int j = PARTS - 1; j >= 0; --j) {
+                    acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(zeros, pw[j], acc[i], 0, 0, 0);
+                    acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c, pw[j], acc[i], 0, 0, 0);
+                }
+            };
+            const auto four = [&](const uint32_t (&w)[4], int at) {
+                tile(at + 0, __builtin_bit_cast(bf16x8, u32x4{codes.pair<0>(w[0]), codes.pair<0>(w[1]), codes.pair<0>(w[2]), codes.pair<0>(w[3])}));
+                tile(at + 1, __builtin_bit_cast(bf16x8, u32x4{codes.pair<1>(w[0]), codes.pair<1>(w[1]), codes.pair<1>(w[2]), codes.pair<1>(w[3])}));
+                tile(at + 2, __builtin_bit_cast(bf16x8, u32x4{codes.pair<2>(w[0]), codes.pair<2>(w[1]), codes.pair<2>(w[2]), codes.pair<2>(w[3])}));
+                tile(at + 3, __builtin_bit_cast(bf16x8, u32x4{codes.pair<3>(w[0]), codes.pair<3>(w[1]), codes.pair<3>(w[2]), codes.pair<3>(w[3])}));
+            };
+            four(low, 0);
+            if (D == 128) four(high, DT - 4);
+            if (far) { // values far from zero for their range: what the high halves leave out, 16 bits in two more parts
+                float vz[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) vz[e] -= __uint_as_float(__float_as_uint(vz[e]) & 0xffff0000u);
-                const bf16x8 rest = high_halves();
+                for (int i = 0; i < 4; ++i) {
+                    const float4 v0 = par[16 + 8 * (i >> 1) + (i & 1)];
+                    vz[2 * i] = v0.y, vz[2 * i + 1] = v0.w;
+                }
 #pragma unroll
-                for (int i = 0; i < DT; ++i)
+                for (int k = 0; k < 2; ++k) {
+                    u32x4 y;
 #pragma unroll
-                    for (int j = PARTS - 1; j >= 0; --j) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(rest, pw[j], acc[i], 0, 0, 0);
+                    for (int e = 0; e < 8; ++e) vz[e] -= __uint_as_float(__float_as_uint(vz[e]) & 0xffff0000u);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = __builtin_amdgcn_perm(__float_as_uint(vz[2 * e + 1]), __float_as_uint(vz[2 * e]), 0x07060302u);
+                    const bf16x8 rest = __builtin_bit_cast(bf16x8, y);
+#pragma unroll
+                    for (int i = 0; i < DT; ++i)
+#pragma unroll
+                        for (int j = PARTS - 1; j >= 0; --j) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(rest, pw[j], acc[i], 0, 0, 0);
+                }
             }
-        }
     };
 
-    // The loads of a step are on their way while the step before is worked on.  Nothing in between may wait for memory or hang on
-    // a condition that the compiler cannot see through: the page numbers of up to 64 steps are fetched beforehand, one a lane,
-    // and a step without a page reads page 0 and drops it.
-    const auto ask_for = [&](int32_t page, int32_t st, Loaded<D> &x) { ask<D>(s, head, lane, page < 0 ? 0 : page, st * STEP, x); };
-    for (int32_t first = step_begin + wave; first < step_end; first += 64 * WAVES) {
-        const int32_t mine = first + lane * WAVES;
-        const int32_t pages = mine < step_end ? page_of(s, t.seq.line, mine * STEP) : -1;
-        const int32_t left = (step_end - first + WAVES - 1) / WAVES, count = left < 64 ? left : 64;
-        Loaded<D> x[2];
+    // The loads of a step are on their way while the step before is worked on.  Nothing in between waits for memory and no condition
+    // stands around them: the page numbers are there beforehand, and a step without a page reads page 0 and sees nothing of it.
+    const Loads<D> from(lane, 1 << s.page_shift);
+    for (int32_t first = step_begin + wave; first < step_end;) {
+        const int32_t left_of = (step_end - first + WAVES - 1) / WAVES, count = left_of < 64 ? left_of : 64;
+        Codes<D> x[2];
         int32_t page = __builtin_amdgcn_readlane(pages, 0);
-        ask_for(page, first, x[0]);
-        for (int32_t n = 0; n < count; n += 2) {
+        from.ask(s, head, page, first * STEP, x[0]);
+        for (int32_t n = 0; n < count;) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int32_t next = n + i + 1 < count ? __builtin_amdgcn_readlane(pages, (n + i + 1) & 63) : -1;
-                ask_for(next, first + (n + i + 1) * WAVES, x[1 - i]);
-                if (page >= 0) work(x[i]);
-                page = next;
+                const int32_t next = n + 1 < count ? __builtin_amdgcn_readlane(pages, n + 1) : -1, t0 = (first + n * WAVES) * STEP;
+                from.ask(s, head, next, t0 + WAVES * STEP, x[1 - i]);
+                if (n < count) work(x[i], t0, page);
+                page = next, ++n;
             }
         }
+        first += 64 * WAVES;
+        if (first < step_end) pages = pages_from(first);
     }
 
     l += __shfl_xor(l, 16);
@@ -477,8 +541,8 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
         for (int c = 0; c < DT; ++c) mrg_o[wave][r][DT * (4 * g + i) + c] = acc[c][i];
     __syncthreads();
     for (int32_t i = threadIdx.x; i < ROWS * D; i += WAVES * 64) {
-        const int32_t n = i / D, c = i % D, rw = t.first + n;
-        if (rw >= t.rows) break;
+        const int32_t n = i / D, c = i % D;
+        if (t.first + n >= t.rows) break;
         float top = -INFINITY, sum = 0.0f, o = 0.0f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) top = fmaxf(top, mrg_m[w][n]);
@@ -490,7 +554,7 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
             o += f * mrg_o[w][n][c];
         }
         if (whole) {
-            put_out<D, F32O>(a, t, head, rw, c, quotient(o, sum));
+            put_out<D, F32O>(a, head, t.seq.row + tok0, head0, n, c, quotient(o, sum));
         } else {
             const int64_t at = partial_at(a, head, block, slot, n);
             a.part_o[at * D + c] = o;
@@ -499,74 +563,112 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
     }
     __syncthreads(); // before the next tile's results
     }
-    if (threadIdx.x == 0) a.unfinished[head * a.blocks + block] = left;
 }
 
-// The parts of unfinished tiles joined, a workgroup for each that may have begun one: a row's parts are dealt out to as many
-// waves as JOIN_WAVES have for each row.
-constexpr int JOIN_WAVES = 16;
+// The parts of unfinished tiles joined: a workgroup for JOIN_ROWS rows of each tile, JOIN_WAVES / JOIN_ROWS waves for a row.  A part
+// of a row takes D / 4 lanes; every read of a batch is on its way before the first is looked at.
+constexpr int JOIN_ROWS = 2, JOIN_WAVES = 8;
 template <int D, bool F32O>
 __global__ __launch_bounds__(JOIN_WAVES * 64) void join_kernel(const AttendArgs a)
 {
-    __shared__ float sums[JOIN_WAVES], os[JOIN_WAVES][D];
-    const int32_t head = blockIdx.y, block = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Unfinished u = a.unfinished[head * a.blocks + block];
-    const int32_t parts = u.parts;
-    if (parts == 0) return;
-    Tile t;
-    t.seq.row = u.row, t.first = u.first, t.rows = u.rows;
-    const int32_t rows = t.rows - t.first < ROWS ? t.rows - t.first : ROWS;
-    const int32_t lanes_of_rows = rows <= 1 ? 1 : 1 << (32 - __clz(rows - 1)), per_row = JOIN_WAVES / lanes_of_rows;
-    const int32_t n = wave % lanes_of_rows, chunk = wave / lanes_of_rows;
-    float top = -INFINITY, sum = 0.0f, o[D / 64] = {};
-    const auto partial = [&](int32_t p) { return partial_at(a, head, block + p, p == 0 ? u.slot : 0, n); };
-    if (n < rows) {
-        for (int32_t p = lane; p < parts; p += 64) top = fmaxf(top, a.part_ml[partial(p)].x);
+    constexpr int PER_ROW = JOIN_WAVES / JOIN_ROWS, AT_ONCE = 64 / (D / 4), BATCH = 6;
+    __shared__ float tops[JOIN_WAVES], sums[JOIN_WAVES], os[JOIN_WAVES][D];
+    const int32_t head = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t number = blockIdx.x;
+    if (a.s.row_start) { // not every number is a tile's
+        const int32_t i = last_not_above(a.s.n_seqs, number, [&](int32_t k) { return (int64_t)number_of(a, k); });
+        const int32_t k = number - number_of(a, i);
+        if (k < 0 || k >= work_of(a, seq_of(a.s, i)).tiles) return;
+    }
+    const Unfinished u = a.unfinished[(int64_t)head * a.numbers + number];
+    const int32_t n = blockIdx.z * JOIN_ROWS + wave / PER_ROW;
+    // (the comparisons with the launch's sizes are for a row_start that does not ascend)
+    if (u.parts <= 1 || u.block < 0 || u.block >= a.blocks || u.parts > a.blocks - u.block || u.q_row < 0 || u.head0 < 0 || u.head0 >= a.group ||
+        u.rows > ROWS || (int64_t)u.q_row * a.group + u.head0 + u.rows > (int64_t)a.s.rows * a.group || (int32_t)blockIdx.z * JOIN_ROWS >= u.rows)
+        return;
+    const int32_t sub = lane / (D / 4), c = lane % (D / 4) * 4;
+    float top = -INFINITY, sum = 0.0f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int32_t p0 = wave % PER_ROW * AT_ONCE + sub; n < u.rows && p0 < u.parts; p0 += PER_ROW * AT_ONCE * BATCH) {
+        float2 ml[BATCH];
+        f32x4 x[BATCH];
 #pragma unroll
-        for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-        const float base = top == -INFINITY ? 0.0f : top;
-#pragma unroll 4
-        for (int32_t p = chunk; p < parts; p += per_row) {
-            const int64_t from = partial(p);
-            const float2 ml = a.part_ml[from];
-            const float f = __builtin_amdgcn_exp2f(ml.x - base);
-            sum += f * ml.y;
+        for (int k = 0; k < BATCH; ++k) {
+            const int32_t p = p0 + k * PER_ROW * AT_ONCE;
+            ml[k] = make_float2(-INFINITY, 0.0f), x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (p < u.parts) {
+                const int64_t from = partial_at(a, head, u.block + p, p == 0 ? u.slot & 1 : 0, n);
+                ml[k] = a.part_ml[from];
+                x[k] = *reinterpret_cast<const f32x4 *>(a.part_o + from * D + c);
+            }
+        }
+        float now = top;
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) o[c] += f * a.part_o[from * D + 64 * c + lane];
+        for (int k = 0; k < BATCH; ++k) now = fmaxf(now, ml[k].x);
+        const float base = now == -INFINITY ? 0.0f : now, f0 = __builtin_amdgcn_exp2f(top - base);
+        sum *= f0, o *= f0, top = now;
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const float f = __builtin_amdgcn_exp2f(ml[k].x - base);
+            sum += f * ml[k].y, o += f * x[k];
         }
     }
-    if (lane == 0) sums[wave] = sum;
+    // the lanes of a wave, then the waves of a row
+    float best = top;
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) os[wave][64 * c + lane] = o[c];
+    for (int k = D / 4; k < 64; k <<= 1) best = fmaxf(best, __shfl_xor(best, k));
+    const float f = __builtin_amdgcn_exp2f(top - (best == -INFINITY ? 0.0f : best));
+    sum *= f, o *= f;
+#pragma unroll
+    for (int k = D / 4; k < 64; k <<= 1) {
+        sum += __shfl_xor(sum, k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k);
+    }
+    if (lane == 0) tops[wave] = best, sums[wave] = sum;
+    if (sub == 0) *reinterpret_cast<f32x4 *>(&os[wave][c]) = o;
     __syncthreads();
-    if (wave < rows) { // row `wave`
-        float all = 0.0f;
-        for (int32_t k = 0; k < per_row; ++k) all += sums[wave + k * lanes_of_rows];
+    for (int32_t i = threadIdx.x; i < JOIN_ROWS * D; i += JOIN_WAVES * 64) {
+        const int32_t k = i / D, ch = i % D, row = blockIdx.z * JOIN_ROWS + k;
+        if (row >= u.rows) break;
+        float all = -INFINITY, total = 0.0f, y = 0.0f;
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-            float y = 0.0f;
-            for (int32_t k = 0; k < per_row; ++k) y += os[wave + k * lanes_of_rows][64 * c + lane];
-            put_out<D, F32O>(a, t, head, t.first + wave, 64 * c + lane, quotient(y, all));
+        for (int w = 0; w < PER_ROW; ++w) all = fmaxf(all, tops[k * PER_ROW + w]);
+        if (all == -INFINITY) all = 0.0f;
+#pragma unroll
+        for (int w = 0; w < PER_ROW; ++w) {
+            const float g = __builtin_amdgcn_exp2f(tops[k * PER_ROW + w] - all);
+            total += g * sums[k * PER_ROW + w], y += g * os[k * PER_ROW + w][ch];
         }
+        put_out<D, F32O>(a, head, u.q_row, u.head0, row, ch, quotient(y, total));
     }
 }
 
 int32_t check(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads)
 {
-    if (q_heads <= 0 || q_heads > (1 << 16) || q_heads % cache->heads || cache->heads > 65535) return QLLM_ERR_SHAPE;
-    if (batch->rows * (q_heads / cache->heads) + batch->n_seqs > INT32_MAX) return QLLM_ERR_SHAPE;
+    if (q_heads <= 0 || q_heads > (1 << 15) || q_heads % cache->heads) return QLLM_ERR_SHAPE;
+    const int64_t rows = batch->rows * (q_heads / cache->heads);
+    if (rows > INT32_MAX || (rows / ROWS + batch->n_seqs) * (batch->table_ld * cache->page_tokens / STEP) >= INT32_MAX) return QLLM_ERR_SHAPE;
     return QLLM_OK;
 }
 
 // Workgroups of a kv head: as many as the card holds at once (three on each of 256 CUs), but none for less than LEAST steps.
-int32_t blocks_of(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads)
+struct Launch {
+    int64_t numbers, blocks; // of tiles (see number_of); of workgroups
+    int64_t marks, parts;    // bytes of the workspace for each kind
+};
+Launch plan(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads)
 {
     constexpr int64_t RESIDENT = 768;
     const int64_t group = q_heads / cache->heads;
-    const int64_t tiles = batch->row_start ? batch->rows * group / ROWS + batch->n_seqs : batch->n_seqs * ((group + ROWS - 1) / ROWS);
-    const int64_t most = tiles * (batch->table_ld * cache->page_tokens / STEP) / LEAST + 1; // below 2^62
+    Launch n;
+    n.numbers = batch->row_start ? batch->rows * group / ROWS + batch->n_seqs : batch->n_seqs * ((group + ROWS - 1) / ROWS);
+    const int64_t most = n.numbers * (batch->table_ld * cache->page_tokens / STEP) / LEAST + 1; // below 2^31
     const int64_t blocks = cache->heads < RESIDENT ? RESIDENT / cache->heads : 1;
-    return (int32_t)(blocks < most ? blocks : most);
+    n.blocks = blocks < most ? blocks : most;
+    n.marks = n.blocks > 1 ? cache->heads * n.numbers * (int64_t)sizeof(Unfinished) : 0;
+    n.parts = n.blocks > 1 ? cache->heads * n.blocks * 2 * ROWS : 0;
+    return n;
 }
 
 } // namespace
@@ -577,7 +679,8 @@ extern "C" int64_t qllm_kv_attention_workspace_bytes(const qllm_kv_cache *cache,
     int32_t rc = prepare_step(cache, batch, false, &s);
     if (rc == QLLM_OK) rc = check(cache, batch, q_heads);
     if (rc != QLLM_OK) return rc;
-    return cache->heads * blocks_of(cache, batch, q_heads) * (2 * ROWS * (cache->dim + 2) * (int64_t)sizeof(float) + (int64_t)sizeof(Unfinished));
+    const Launch n = plan(cache, batch, q_heads);
+    return 256 + n.marks + n.parts * (cache->dim + 2) * (int64_t)sizeof(float);
 }
 
 extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq, int64_t q_heads, const qllm_kv_cache *cache,
@@ -599,13 +702,15 @@ extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq
     if (batch->rows == 0 || batch->n_seqs == 0) return QLLM_OK;
     a.q = q, a.out = out, a.ldq = ldq, a.ldo = ldo;
     a.q_heads = (int32_t)q_heads, a.group = (int32_t)(q_heads / cache->heads);
+    a.by_group = qllm_detail::quotient_by((uint32_t)a.group);
+    a.q_vec = q_dtype == QLLM_BF16 && ((reinterpret_cast<uintptr_t>(q) | (uintptr_t)(2 * ldq)) & 15u) == 0;
     a.window = window > INT32_MAX ? 0 : (int32_t)window;
     a.scale2 = scale * LOG2E;
-    a.blocks = blocks_of(cache, batch, q_heads);
-    const int64_t parts = cache->heads * a.blocks;
+    const Launch n = plan(cache, batch, q_heads);
+    a.blocks = (int32_t)n.blocks, a.numbers = n.blocks > 1 ? (int32_t)n.numbers : 0;
     a.unfinished = static_cast<Unfinished *>(workspace);
-    a.part_ml = reinterpret_cast<float2 *>(a.unfinished + parts);
-    a.part_o = reinterpret_cast<float *>(a.part_ml + parts * 2 * ROWS);
+    a.part_o = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + n.marks);
+    a.part_ml = reinterpret_cast<float2 *>(a.part_o + n.parts * cache->dim);
     const dim3 grid((unsigned)a.blocks, (unsigned)cache->heads);
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();
@@ -624,7 +729,8 @@ extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq
 #undef QLLM_ATTEND
     rc = launched("cache attention: launch");
     if (rc != QLLM_OK || a.blocks == 1) return rc; // one workgroup a head finishes what it begins
-    const dim3 cuts((unsigned)a.blocks, (unsigned)cache->heads);
+    const int64_t rows = batch->row_start || a.group > ROWS ? ROWS : a.group; // of a tile at most
+    const dim3 cuts((unsigned)n.numbers, (unsigned)cache->heads, (unsigned)((rows + JOIN_ROWS - 1) / JOIN_ROWS));
     if (cache->dim == 128 && out_dtype == QLLM_F32) hipLaunchKernelGGL((join_kernel<128, true>), cuts, dim3(JOIN_WAVES * 64), 0, stream, a);
     else if (cache->dim == 128) hipLaunchKernelGGL((join_kernel<128, false>), cuts, dim3(JOIN_WAVES * 64), 0, stream, a);
     else if (out_dtype == QLLM_F32) hipLaunchKernelGGL((join_kernel<64, true>), cuts, dim3(JOIN_WAVES * 64), 0, stream, a);
