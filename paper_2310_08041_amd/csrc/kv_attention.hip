@@ -1,108 +1,17 @@
-// Causal attention over the 4-bit key/value cache.
-//
-// For a kv head the queries of its group of query heads are rows of one matrix: row r of a sequence's n rows x G heads is token
-// r / G, head r % G.  Codes are integers, so with k = alpha (c - beta) the score of a token is
-//     scale alpha (q . (16 + c) - (16 + beta) sum q),
-// the first product on the matrix cores: 16 + c is an exact bf16 whose bits are 0x4180 | c << 3, two vector instructions for a
-// pair of codes.  In the same way sum_t p_t v_t = sum_t (p_t alpha_t)(16 + c_t) - sum_t (p_t alpha_t)(16 + beta_t), with p_t alpha_t
-// rounded to bf16 first and the rounded number used in both sums.  The scores are formed transposed (tokens x rows): their
-// accumulator then is, register for register, the operand that meets the values, and nothing crosses lanes in between.
+// Causal attention over the 4-bit key/value cache: the kernel for single tokens and few rows, which is bound by memory, and the
+// entry points (kv_attend.h has the formulas).
 #include <hip/hip_runtime.h>
 
 #include <math.h>
 #include <stdint.h>
 
-#include "fused_common.h"
-#include "kv_common.h"
+#include "kv_attend.h"
 
 namespace {
 
 using namespace qllm_kv_detail;
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 constexpr int ROWS = 16, STEP = 32, WAVES = 4; // rows of a tile, tokens of a step, waves of a workgroup
-constexpr float LOG2E = 1.44269504088896341f;
-constexpr float SLACK = 8.0f; // the running maximum follows only when the scores pass it by this much: weights stay below 2^8
-
-struct Unfinished;
-struct AttendArgs {
-    Step s;
-    const void *q;
-    void *out;
-    int64_t ldq, ldo;
-    int32_t q_heads, group, window; // window 0: none
-    float scale2;                   // scale * log2 e
-    int32_t q_vec;                  // bf16 queries in 16-byte pieces
-    qllm_detail::QuotientBy by_group; // for numbers below group + ROWS
-    int32_t blocks;                 // workgroups of a kv head
-    float *part_o;                  // their partial results, see partial_at
-    float2 *part_ml;
-    int32_t numbers;                // of tiles, see number_of
-    Unfinished *unfinished;         // [heads][numbers]
-};
-
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
-}
-
-// 16 + code of nibble i (0..3) of both halves of w, as a pair of bf16.  The two constants are kept in registers, unknown to the
-// compiler: only then are "and" and "or" one instruction (a literal for each makes them two).
-struct Codes16 {
-    uint32_t mask, sixteen;
-    __device__ __forceinline__ Codes16()
-    {
-        asm("v_mov_b32 %0, 0x780078" : "=v"(mask));
-        asm("v_mov_b32 %0, 0x41804180" : "=v"(sixteen));
-    }
-    template <int I>
-    __device__ __forceinline__ uint32_t pair(uint32_t w) const
-    {
-        const uint32_t t = I == 0 ? w << 3 : w >> (4 * I - 3);
-        return (t & mask) | sixteen;
-    }
-    // 8 codes of a dword as a matrix-core operand: elements are codes 0, 4, 1, 5, 2, 6, 3, 7
-    __device__ __forceinline__ bf16x8 operand(uint32_t w) const
-    {
-        return __builtin_bit_cast(bf16x8, u32x4{pair<0>(w), pair<1>(w), pair<2>(w), pair<3>(w)});
-    }
-};
-
-// A row tile of a workgroup: rows first .. first + 15 of a sequence's n * group rows.
-struct Tile {
-    Seq seq;
-    int32_t first, rows;
-};
-
-// What rows see: tokens all_lo .. all_hi some of them, each_lo .. each_hi every one.
-struct Sight {
-    int32_t limit, all_lo, all_hi, each_lo, each_hi;
-};
-
-__device__ __forceinline__ int32_t lo_at(const AttendArgs &a, int32_t pos) { return a.window > 0 && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0; }
-__device__ __forceinline__ int32_t hi_at(int32_t limit, int32_t pos) { return pos < limit ? pos : limit - 1; }
-__device__ __forceinline__ int32_t limit_of(const AttendArgs &a, const Seq &q)
-{
-    const int32_t cap = a.s.table_ld << a.s.page_shift;
-    return q.line < 0 ? 0 : (q.len < cap ? q.len : cap);
-}
-
-__device__ __forceinline__ Sight sight_of(const AttendArgs &a, const Tile &t, int32_t tok0, int32_t head0)
-{
-    Sight v;
-    v.limit = limit_of(a, t.seq);
-    const int32_t rows = t.rows - t.first < ROWS ? t.rows - t.first : ROWS;
-    const int32_t p_first = t.seq.len - t.seq.n + tok0, p_last = p_first + (int32_t)a.by_group.divide((uint32_t)(head0 + rows - 1));
-    v.all_lo = lo_at(a, p_first), v.all_hi = hi_at(v.limit, p_last);
-    v.each_lo = lo_at(a, p_last), v.each_hi = hi_at(v.limit, p_first);
-    return v;
-}
-
 // The work of a kv head is one long line of steps: sequence after sequence, tile after tile, `steps` of 32 tokens for each tile
 // (what its sequence's rows see together; at least one, for rows that see nothing get their zeros too).  The workgroups of the
 // head share the line out evenly, whatever the lengths: one may end in the middle of a tile and the next go on there.
@@ -113,7 +22,8 @@ struct Work {
 __device__ __forceinline__ Work work_of(const AttendArgs &a, const Seq &q)
 {
     Work w;
-    w.tiles = (int32_t)(((uint32_t)(q.n * a.group) + ROWS - 1) / ROWS); // n * group: checked on the host
+    const int32_t rows = q.n * a.group; // checked on the host
+    w.tiles = rows > a.few ? 0 : (int32_t)(((uint32_t)rows + ROWS - 1) / ROWS);
     const int32_t lo = lo_at(a, q.len - q.n), hi = hi_at(limit_of(a, q), q.len - 1);
     w.first = lo / STEP;
     w.steps = hi < lo ? 1 : hi / STEP + 1 - w.first;
@@ -203,23 +113,6 @@ struct Shares {
     }
 };
 
-template <bool F32>
-__device__ __forceinline__ float load1(const void *p, int64_t at)
-{
-    return F32 ? static_cast<const float *>(p)[at] : __uint_as_float((uint32_t)static_cast<const uint16_t *>(p)[at] << 16);
-}
-
-// fp32 as a sum of PARTS bf16 (three hold all 24 bits)
-template <int PARTS>
-__device__ __forceinline__ void split(float x, float (&part)[PARTS])
-{
-#pragma unroll
-    for (int i = 0; i < PARTS; ++i) {
-        part[i] = __uint_as_float(pack_bf16(x, 0.0f) << 16);
-        x -= part[i];
-    }
-}
-
 // What a wave asks of memory for one step: codes of its keys (tokens 16 h + r, channels D / 4 g ..) and values (tokens of
 // element e, channels D / 16 r ..), and one token's alpha and beta, of the keys in lanes 0..31, of the values in the others.
 // Addresses are a base for the wave and 32-bit offsets for the lanes.
@@ -267,10 +160,7 @@ struct Loads {
 };
 
 // A workgroup leaves at most two tiles unfinished: the one it begins with (slot 0) and the one it ends with (slot 1).  Per row:
-// running maximum and sum, and dim unnormalised sums.
-struct Unfinished { // how a tile is to be joined: its parts (1: nothing to join), the workgroup of the first and the slot there,
-    int32_t parts, block, slot, q_row, head0, rows, pad[2]; // its first row, head head0 of row q_row, and how many
-};
+// running maximum and sum, and dim unnormalised sums (partial_at).
 // Sequence i's tiles are numbered from row_start[i] * group / ROWS + i on: at least as many numbers as it has tiles, in order.
 __device__ __forceinline__ int32_t number_of(const AttendArgs &a, int32_t i)
 {
@@ -290,8 +180,6 @@ __device__ __forceinline__ void put_out(const AttendArgs &a, int32_t head, int32
     if (F32O) static_cast<float *>(a.out)[at] = y;
     else static_cast<uint16_t *>(a.out)[at] = (uint16_t)pack_bf16(y, 0.0f);
 }
-
-__device__ __forceinline__ float quotient(float o, float sum) { return sum > 0.0f ? o / sum : (sum == 0.0f ? 0.0f : sum); } // a NaN stays
 
 template <int D, bool F32Q, bool F32O>
 __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const AttendArgs a)
@@ -328,7 +216,7 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
     const int32_t take = work_here.steps - skip < end - at ? work_here.steps - skip : end - at;
     t.first = number * ROWS, t.rows = t.seq.n * a.group;
     const int32_t tok0 = (int32_t)((uint32_t)t.first / (uint32_t)a.group), head0 = t.first - tok0 * a.group; // of the tile's first row
-    const Sight v = sight_of(a, t, tok0, head0);
+    const Sight v = sight_of(a, t, tok0, head0, ROWS);
     const int32_t step_begin = work_here.first + skip;
     const int32_t step_end = v.all_hi < 0 || step_begin + take <= v.all_hi / STEP + 1 ? step_begin + take : v.all_hi / STEP + 1;
     const bool whole = take == work_here.steps;
@@ -652,6 +540,14 @@ int32_t check(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_
     return QLLM_OK;
 }
 
+// Whether the prompts kernel takes sequences of more than FEW_ROWS rows: its tiles of 128 rows have to keep most of the card busy.
+constexpr int32_t FEW_ROWS = 64;
+bool prompts_pay(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads, int32_t q_dtype)
+{
+    const int64_t rows = batch->rows * (q_heads / cache->heads);
+    return q_dtype == QLLM_BF16 && batch->row_start && rows / 128 * cache->heads >= 128 && rows > batch->n_seqs * FEW_ROWS / 4;
+}
+
 // Workgroups of a kv head: as many as the card holds at once (three on each of 256 CUs), but none for less than LEAST steps.
 struct Launch {
     int64_t numbers, blocks; // of tiles (see number_of); of workgroups
@@ -704,16 +600,24 @@ extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq
     a.q_heads = (int32_t)q_heads, a.group = (int32_t)(q_heads / cache->heads);
     a.by_group = qllm_detail::quotient_by((uint32_t)a.group);
     a.q_vec = q_dtype == QLLM_BF16 && ((reinterpret_cast<uintptr_t>(q) | (uintptr_t)(2 * ldq)) & 15u) == 0;
+    a.out_vec = ((reinterpret_cast<uintptr_t>(out) | (uintptr_t)(ldo * (out_dtype == QLLM_F32 ? 4 : 2))) & (out_dtype == QLLM_F32 ? 15u : 7u)) == 0;
     a.window = window > INT32_MAX ? 0 : (int32_t)window;
     a.scale2 = scale * LOG2E;
+    // Sequences of many rows are the prompts kernel's, the others this one's.  (One sequence: all of it goes to one of them.)
+    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+    (void)hipGetLastError();
+    a.few = INT32_MAX;
+    if (prompts_pay(cache, batch, q_heads, q_dtype)) {
+        a.few = batch->n_seqs == 1 ? 0 : FEW_ROWS;
+        rc = qllm_kv_launch_prompts(a, cache->dim, out_dtype, stream);
+        if (rc != QLLM_OK || batch->n_seqs == 1) return rc;
+    }
     const Launch n = plan(cache, batch, q_heads);
     a.blocks = (int32_t)n.blocks, a.numbers = n.blocks > 1 ? (int32_t)n.numbers : 0;
     a.unfinished = static_cast<Unfinished *>(workspace);
     a.part_o = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + n.marks);
     a.part_ml = reinterpret_cast<float2 *>(a.part_o + n.parts * cache->dim);
     const dim3 grid((unsigned)a.blocks, (unsigned)cache->heads);
-    hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
-    (void)hipGetLastError();
 #define QLLM_ATTEND(D, FQ, FO) hipLaunchKernelGGL((attend_kernel<D, FQ, FO>), grid, dim3(WAVES * 64), 0, stream, a)
     const int32_t kind = (cache->dim == 128 ? 4 : 0) + (q_dtype == QLLM_F32 ? 2 : 0) + (out_dtype == QLLM_F32 ? 1 : 0);
     switch (kind) {

@@ -1,0 +1,342 @@
+// Causal attention over the 4-bit key/value cache: the kernel for prompts and chunks of prompts, which is bound by the matrix cores
+// and the softmax beside them (kv_attend.h has the formulas).
+//
+// A workgroup of four waves owns 128 rows of a sequence and kv head, a wave 32 of them (columns of the transposed products), and
+// walks the tokens they see in tiles of 64.  A tile's codes become bf16 operands 16 + c in LDS once for the four waves, while the
+// tile before is multiplied: keys token by token with the zero point as 16 more channels (its bf16 parts meet those of the
+// queries' sums), values channel by channel in the order in which the weights come out of the scores.  The values' zero points
+// meet the weights in one product more per 16 tokens, shared by all channels; its sums are added to the others every few tiles,
+// so that the two stay small and lose nothing to each other.
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+#include <stdint.h>
+
+#include "kv_attend.h"
+
+namespace {
+
+using namespace qllm_kv_detail;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int PROWS = 128, TILE = 64, WAVES = 4, THREADS = WAVES * 64; // rows of a workgroup, tokens of a tile
+constexpr int TOGETHER = 4; // tiles between two additions of the zero points' sums
+
+// A tile of tokens as operands.
+template <int D>
+struct Operands {
+    static constexpr int KS = D + 16, VS = TILE + 8; // a token's keys and its zero point; a channel's values (+8: neighbouring rows on other banks)
+    uint16_t k[TILE][KS]; // 8 channels at a time in the order 0, 4, 1, 5, 2, 6, 3, 7
+    uint16_t v[D][VS];    // tokens of 16: the 8 of lane half 0 (0..3, 8..11), then the others
+    float ka[TILE], va[TILE];
+    uint16_t vz[3][TILE]; // - (16 + beta) of the values in three bf16 parts, tokens in the order of v
+};
+
+// What a thread asks of memory for a tile: a quarter of a token's keys, 8 tokens of D / 32 channels of the values, one token's
+// alpha and beta (of its key in quarter 0, of its value in quarter 1).
+template <int D>
+struct Asked {
+    uint32_t k[D / 32], v[8];
+    float alpha;
+    int32_t beta;
+};
+
+template <int D, bool F32O>
+__global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a, int32_t numbers, int32_t folded)
+{
+    constexpr int KSTEPS = D / 16, DT = D / 32;
+    __shared__ __attribute__((aligned(16))) Operands<D> op[2];
+    __shared__ int32_t far_in[2][WAVES]; // some value of the wave's tokens lies far from zero for its range
+
+    const Step &s = a.s;
+    const int32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
+
+    // Workgroups of one kv head go to the same XCD (head fastest) where heads are a multiple of 8: its L2 holds the tokens they share.
+    // The tile with the longest way back first; where two workgroups share each CU for the whole launch (folded) the second
+    // half of them in the opposite order, so that a long tile has a short one beside it.
+    const int32_t head = blockIdx.x % s.heads, k = blockIdx.x / s.heads, half = (numbers + 1) / 2;
+    const int32_t number = !folded || k < half ? numbers - 1 - k : k - half;
+    Tile t;
+    {
+        const auto first = [&](int32_t i) { return (int64_t)row_of(s, i) * a.group / PROWS + i; };
+        const int32_t i = last_not_above(s.n_seqs, number, first);
+        t.seq = seq_of(s, i);
+        t.seq.row = __builtin_amdgcn_readfirstlane(t.seq.row), t.seq.n = __builtin_amdgcn_readfirstlane(t.seq.n); // the same in every lane
+        t.seq.line = __builtin_amdgcn_readfirstlane(t.seq.line), t.seq.len = __builtin_amdgcn_readfirstlane(t.seq.len);
+        t.rows = t.seq.n * a.group;
+        const int64_t at = (number - __builtin_amdgcn_readfirstlane((int32_t)first(i))) * (int64_t)PROWS;
+        if (at < 0 || at >= t.rows || t.rows <= a.few) return;
+        t.first = (int32_t)at;
+    }
+    const int32_t tok0 = (int32_t)((uint32_t)t.first / (uint32_t)a.group), head0 = t.first - tok0 * a.group;
+    const Sight v = sight_of(a, t, tok0, head0, PROWS);
+
+    // this lane's row, and what the wave's rows see
+    const int32_t n = wave * 32 + col, token = tok0 + (int32_t)a.by_group.divide((uint32_t)(head0 + n)), head_of_row = head0 + n - (token - tok0) * a.group;
+    const bool real = t.first + n < t.rows;
+    const int32_t pos = t.seq.len - t.seq.n + token, hi = real ? hi_at(v.limit, pos) : -1, lo = lo_at(a, pos);
+    const int32_t wave_rows = t.rows - t.first - wave * 32 < 32 ? t.rows - t.first - wave * 32 : 32; // may be none
+    const int32_t w_first = t.seq.len - t.seq.n + tok0 + (int32_t)a.by_group.divide((uint32_t)(head0 + wave * 32));
+    const int32_t w_last = t.seq.len - t.seq.n + tok0 + (int32_t)a.by_group.divide((uint32_t)(head0 + wave * 32 + (wave_rows > 0 ? wave_rows - 1 : 0)));
+    const int32_t some_lo = lo_at(a, w_first), some_hi = wave_rows > 0 ? hi_at(v.limit, w_last) : -1;
+    const int32_t each_lo = lo_at(a, w_last), each_hi = hi_at(v.limit, w_first);
+
+    // queries: element e of step k of lane half h is channel 16 k + 8 h + {0, 4, 1, 5, 2, 6, 3, 7}[e]; behind them the parts of their sum
+    bf16x8 q[KSTEPS], qz;
+    {
+        const int64_t from = (int64_t)(t.seq.row + token) * a.ldq + (head * a.group + head_of_row) * D + 8 * h;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KSTEPS; ++i) {
+            uint32_t d[4] = {0, 0, 0, 0};
+            const uint16_t *src = static_cast<const uint16_t *>(a.q) + from + 16 * i;
+            if (real && a.q_vec) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(src);
+                d[0] = w.x, d[1] = w.y, d[2] = w.z, d[3] = w.w;
+            } else if (real) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[e] = src[2 * e] | (uint32_t)src[2 * e + 1] << 16;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += __uint_as_float(d[e] << 16) + __uint_as_float(d[e] & 0xffff0000u);
+            q[i] = __builtin_bit_cast(bf16x8, u32x4{__builtin_amdgcn_perm(d[2], d[0], 0x05040100u), __builtin_amdgcn_perm(d[2], d[0], 0x07060302u),
+                                                    __builtin_amdgcn_perm(d[3], d[1], 0x05040100u), __builtin_amdgcn_perm(d[3], d[1], 0x07060302u)});
+        }
+        sum += __shfl_xor(sum, 32);
+        float part[3];
+        split<3>(sum, part); // zero point parts z, z, z, z', z', z', z'', z'' | z'' meet q, q', q'', q, q', q'', q, q' | q''
+        qz = h == 0 ? __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part[0], part[1]), pack_bf16(part[2], part[0]), pack_bf16(part[1], part[2]), pack_bf16(part[0], part[1])})
+                    : __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part[2], 0.0f), 0, 0, 0});
+    }
+
+    // page numbers of up to 64 blocks of 32 tokens, one a lane
+    const int32_t tile_begin = v.all_lo / TILE, tile_end = v.all_hi < v.all_lo ? tile_begin : v.all_hi / TILE + 1;
+    int32_t listed = tile_begin; // the first tile of the list
+    const auto pages_from = [&](int32_t tile) {
+        const int32_t p = tile * TILE + 32 * lane;
+        return p <= v.all_hi ? page_of(s, t.seq.line, p) : -1;
+    };
+    int32_t pages = pages_from(listed);
+
+    const int32_t P = 1 << s.page_shift;
+    const int32_t k_tok = tid >> 2, k_part = tid & 3;                       // keys: token, quarter
+    const int32_t v_chunk = wave * 2 + h, v_tok = v_chunk / 2 * 16 + 4 * (v_chunk & 1); // values: 8 tokens, v_tok + 0..3 and + 8..11
+    const Codes16 codes;
+    const auto part_of = [&](int32_t page) { return s.pages + (page < 0 ? 0 : page) * s.page_bytes + (int64_t)head * P * (D + 16); };
+    const auto ask = [&](int32_t tile, Asked<D> &x, int32_t (&page)[2]) {
+        if (tile - listed >= 32) listed = tile, pages = pages_from(tile);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) page[b] = tile < tile_end ? __builtin_amdgcn_readlane(pages, 2 * (tile - listed) + b) : -1;
+        const int32_t t0 = tile * TILE;
+        {
+            const int32_t tok = t0 + k_tok; // its block is the same for the whole wave
+            const uint8_t *part = part_of(k_tok < 32 ? page[0] : page[1]);
+            const uint8_t *src = part + (tok & (P - 1)) * (D / 2) + D / 8 * k_part;
+            if (D == 128) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(src);
+                x.k[0] = w.x, x.k[1] = w.y, x.k[D / 32 - 2] = w.z, x.k[D / 32 - 1] = w.w;
+            } else {
+                const uint2 w = *reinterpret_cast<const uint2 *>(src);
+                x.k[0] = w.x, x.k[1] = w.y;
+            }
+            const uint8_t *par = part + P * D + ((k_part & 1) * 2 * P + (tok & (P - 1))) * 4;
+            x.alpha = *reinterpret_cast<const float *>(par);
+            x.beta = *reinterpret_cast<const int32_t *>(par + 4 * P);
+        }
+        {
+            const int32_t tok = t0 + v_tok;
+            const uint8_t *src = part_of(wave < 2 ? page[0] : page[1]) + (P + (tok & (P - 1))) * (D / 2) + D / 64 * col;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint8_t *w = src + (8 * (e >> 2) + (e & 3)) * (D / 2);
+                x.v[e] = D == 128 ? *reinterpret_cast<const uint16_t *>(w) : *w;
+            }
+        }
+    };
+    const auto lay = [&](const Asked<D> &x, int32_t b) { // into buffer b
+        Operands<D> &o = op[b];
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) *reinterpret_cast<bf16x8 *>(&o.k[k_tok][D / 4 * k_part + 8 * i]) = codes.operand(x.k[i]);
+        uint32_t pair[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pair[e] = x.v[2 * e] | x.v[2 * e + 1] << 16;
+        const auto put = [&](int c, u32x4 w) { *reinterpret_cast<u32x4 *>(&o.v[D / 32 * col + c][8 * v_chunk]) = w; };
+        put(0, u32x4{codes.pair<0>(pair[0]), codes.pair<0>(pair[1]), codes.pair<0>(pair[2]), codes.pair<0>(pair[3])});
+        put(1, u32x4{codes.pair<1>(pair[0]), codes.pair<1>(pair[1]), codes.pair<1>(pair[2]), codes.pair<1>(pair[3])});
+        if (D == 128) {
+            put(2, u32x4{codes.pair<2>(pair[0]), codes.pair<2>(pair[1]), codes.pair<2>(pair[2]), codes.pair<2>(pair[3])});
+            put(3, u32x4{codes.pair<3>(pair[0]), codes.pair<3>(pair[1]), codes.pair<3>(pair[2]), codes.pair<3>(pair[3])});
+        }
+        const float zero = -16.0f - (float)x.beta;
+        const bool far = __any(k_part == 1 && fabsf(zero) > 256.0f);
+        if (lane == 0) far_in[b][wave] = far;
+        if (k_part < 2) {
+            float z[3];
+            split<3>(zero, z);
+            if (k_part == 0) {
+                o.ka[k_tok] = x.alpha * a.scale2;
+                *reinterpret_cast<u32x4 *>(&o.k[k_tok][D]) = u32x4{pack_bf16(z[0], z[0]), pack_bf16(z[0], z[1]), pack_bf16(z[1], z[1]), pack_bf16(z[2], z[2])};
+                *reinterpret_cast<u32x4 *>(&o.k[k_tok][D + 8]) = u32x4{pack_bf16(z[2], 0.0f), 0, 0, 0};
+            } else {
+                o.va[k_tok] = x.alpha;
+                const int32_t u = k_tok & 15, place = (k_tok & ~15) + (u >> 2 & 1) * 8 + (u >> 3) * 4 + (u & 3);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) o.vz[i][place] = (uint16_t)(__float_as_uint(z[i]) >> 16);
+            }
+        }
+    };
+
+    f32x16 acc[DT], off;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        off[e] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) acc[i][e] = 0.0f;
+    }
+    float m = -INFINITY, l = 0.0f;
+
+    const auto work = [&](int32_t tile, int32_t b, const int32_t (&page)[2]) {
+        const Operands<D> &o = op[b];
+        const int32_t t0 = tile * TILE;
+        f32x16 sc[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[x][e] = 0.0f;
+            const uint16_t *row = &o.k[32 * x + col][8 * h];
+            sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(row + D), qz, sc[x], 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < KSTEPS; ++i) sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(row + 16 * i), q[i], sc[x], 0, 0, 0);
+        }
+        // x = alpha s - m; the maximum follows where that passes SLACK, or where a row has none yet
+        const float base = m == -INFINITY ? 0.0f : m;
+        float va[2][16];
+        float top = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 ka = *reinterpret_cast<const float4 *>(&o.ka[32 * x + 8 * j + 4 * h]), w = *reinterpret_cast<const float4 *>(&o.va[32 * x + 8 * j + 4 * h]);
+                const float f[4] = {ka.x, ka.y, ka.z, ka.w};
+                va[x][4 * j] = w.x, va[x][4 * j + 1] = w.y, va[x][4 * j + 2] = w.z, va[x][4 * j + 3] = w.w;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sc[x][4 * j + i] = __builtin_fmaf(f[i], sc[x][4 * j + i], -base);
+            }
+        if (t0 < each_lo || t0 + TILE - 1 > each_hi || page[0] < 0 || page[1] < 0) { // some row does not see some token; what lies there may be anything
+            int32_t mine = t0 + 4 * h;
+            asm volatile("" : "+v"(mine)); // keeps the comparisons in here
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int32_t tok = mine + 32 * x + 8 * (e >> 2) + (e & 3);
+                    const bool seen = tok >= lo && tok <= hi && page[x] >= 0;
+                    sc[x][e] = seen ? sc[x][e] : -INFINITY;
+                    va[x][e] = seen ? va[x][e] : 0.0f;
+                }
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[x][e]);
+        const bool fresh = m == -INFINITY;
+        if (__any(top > SLACK || (fresh && top > -INFINITY))) {
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float up = top == -INFINITY ? 0.0f : (fresh ? top : fmaxf(top, 0.0f)), f = fresh ? 1.0f : __builtin_amdgcn_exp2f(-up);
+            m = fresh && top == -INFINITY ? m : base + up;
+            l *= f, off *= f;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) acc[i] *= f;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sc[x][e] -= up;
+        }
+        const bool far = (far_in[b][0] | far_in[b][1] | far_in[b][2] | far_in[b][3]) != 0;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) { // 16 tokens
+            uint32_t pw[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int x = y >> 1, at = 8 * (y & 1) + 2 * e;
+                const float p0 = __builtin_amdgcn_exp2f(sc[x][at]), p1 = __builtin_amdgcn_exp2f(sc[x][at + 1]);
+                l += p0 + p1;
+                pw[e] = pack_bf16(p0 * va[x][at], p1 * va[x][at + 1]);
+            }
+            const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{pw[0], pw[1], pw[2], pw[3]});
+            off = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(&o.vz[0][16 * y + 8 * h]), p, off, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+                acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(&o.v[32 * i + col][16 * y + 8 * h]), p, acc[i], 0, 0, 0);
+            if (far) {
+                off = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(&o.vz[1][16 * y + 8 * h]), p, off, 0, 0, 0);
+                off = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(&o.vz[2][16 * y + 8 * h]), p, off, 0, 0, 0);
+            }
+        }
+        if (far || (tile - tile_begin) % TOGETHER == TOGETHER - 1) {
+#pragma unroll
+            for (int i = 0; i < DT; ++i) acc[i] += off[0];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) off[e] = 0.0f;
+        }
+    };
+
+    Asked<D> asked;
+    int32_t page[2], next[2];
+    ask(tile_begin, asked, page);
+    if (tile_begin < tile_end) lay(asked, 0);
+    __syncthreads();
+    for (int32_t tile = tile_begin; tile < tile_end; ++tile) {
+        const int32_t b = (tile - tile_begin) & 1;
+        ask(tile + 1, asked, next); // past the last: page 0, dropped
+        if (tile * TILE <= some_hi && tile * TILE + TILE - 1 >= some_lo) work(tile, b, page);
+        lay(asked, 1 - b);
+        page[0] = next[0], page[1] = next[1];
+        __syncthreads();
+    }
+
+    if (!real) return;
+    l += __shfl_xor(l, 32); // the other half of the same row: as real as this one
+    const int64_t at = (int64_t)(t.seq.row + token) * a.ldo + (head * a.group + head_of_row) * D + 4 * h;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = quotient(acc[i][4 * j + e] + off[0], l);
+            const int64_t to = at + 32 * i + 8 * j;
+            if (F32O) {
+                float *p = static_cast<float *>(a.out) + to;
+                if (a.out_vec) *reinterpret_cast<float4 *>(p) = make_float4(y[0], y[1], y[2], y[3]);
+                else
+                    for (int e = 0; e < 4; ++e) p[e] = y[e];
+            } else {
+                uint16_t *p = static_cast<uint16_t *>(a.out) + to;
+                const uint2 w = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+                if (a.out_vec) *reinterpret_cast<uint2 *>(p) = w;
+                else p[0] = (uint16_t)w.x, p[1] = (uint16_t)(w.x >> 16), p[2] = (uint16_t)w.y, p[3] = (uint16_t)(w.y >> 16);
+            }
+        }
+}
+
+} // namespace
+
+int32_t qllm_kv_launch_prompts(const AttendArgs &a, int64_t dim, int32_t out_dtype, hipStream_t stream)
+{
+    const int64_t numbers = (int64_t)a.s.rows * a.group / PROWS + a.s.n_seqs, workgroups = numbers * a.s.heads;
+    if (workgroups > INT32_MAX) return QLLM_ERR_SHAPE;
+    const int32_t folded = workgroups <= 2 * 256 + a.s.heads; // (one number of a single sequence has no tile)
+    const dim3 grid((unsigned)workgroups);
+#define QLLM_PROMPTS(D, FO) hipLaunchKernelGGL((prompts_kernel<D, FO>), grid, dim3(THREADS), 0, stream, a, (int32_t)numbers, folded)
+    if (dim == 128) {
+        if (out_dtype == QLLM_F32) QLLM_PROMPTS(128, true);
+        else QLLM_PROMPTS(128, false);
+    } else {
+        if (out_dtype == QLLM_F32) QLLM_PROMPTS(64, true);
+        else QLLM_PROMPTS(64, false);
+    }
+#undef QLLM_PROMPTS
+    return launched("cache attention of prompts: launch");
+}

@@ -254,6 +254,71 @@ def test_attention_within_the_bounds_of_its_roundings(oracle, b, q_type, out_typ
     assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
 
 
+PROMPTS = [  # out, heads, group, dim, page, lengths, new rows, window, rows behind the last: enough rows for the prompts kernel
+    ("bf16", 16, 8, 128, 64, [200], [140], 0, 0),
+    ("bf16", 32, 1, 128, 128, [530], [530], 0, 3),
+    ("f32", 20, 3, 64, 32, [150, 40, 0, 300, 7], [150, 1, 0, 180, 7], 70, 2),    # with single tokens and short ones beside them
+    ("bf16", 24, 5, 128, 32, [333, 128, 65], [60, 128, 1], 0, 0),
+    ("f32", 16, 16, 128, 256, [90], [90], 5, 0),
+    ("bf16", 32, 4, 64, 64, [100, 129], [129, 129], 0, 0),                        # rows before the first token: they see nothing
+]
+
+
+@pytest.mark.parametrize("out_type,heads,group,dim,page,lengths,new,window,tail", PROMPTS)
+def test_attention_of_prompts_within_the_bounds_of_its_roundings(oracle, b, out_type, heads, group, dim, page, lengths, new, window, tail):
+    import torch
+    from oracle import kv_cache as okv
+    td = torch.bfloat16 if out_type == "bf16" else torch.float32
+    rng = np.random.default_rng(sum(lengths) + dim)
+    c = make(rng, heads, group, dim, page, lengths, new, rows=sum(new) + tail)
+    assert c.rows * group // 128 * heads >= 128
+    hq = heads * group
+    q = _bf16(rng.standard_normal((c.rows, hq, dim)).astype(np.float32))
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(dim ** -0.5), window, out=np.full(q.shape, 5.0))
+    tol = tolerance(want, *bounds, "bf16", out_type)
+    cache, batch = on_device(b, c)
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, hq), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    for pad, off in ((0, 0), (5, 3)):                          # 16-byte aligned rows and others
+        qd = torch.zeros((c.rows, hq * dim + pad + off), dtype=torch.bfloat16, device="cuda")[:, off:off + hq * dim]
+        qd.copy_(_t(q.reshape(c.rows, -1)))
+        out = torch.full((c.rows, hq * dim + pad + off), 5.0, dtype=td, device="cuda")
+        b.qllm_kv_attention(qd, cache, 0, batch, dim ** -0.5, out[:, off:off + hq * dim], ws, window=window)
+        got = out[:, off:off + hq * dim].double().cpu().numpy().reshape(want.shape)
+        assert (out[:, :off] == 5.0).all() and (out[:, off + hq * dim:] == 5.0).all()
+        for r in set(range(c.rows)) - {t[0] for t in c.tokens}:
+            assert (got[r] == 5.0).all()
+        worst = np.abs(got - want) / tol
+        assert np.isfinite(got).all() and worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+@pytest.mark.parametrize("q_type,heads,group,lengths,new", [("bf16", 1, 4, [700, 40], None), ("f32", 1, 2, [150], None), ("bf16", 16, 8, [190], [140])])
+def test_attention_over_keys_and_values_far_from_zero(oracle, b, q_type, heads, group, lengths, new):
+    """Vectors whose offset is hundreds to millions of times their range: beta needs more bits than one bf16 has, in places only."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(21)
+    c = make(rng, heads, group, 128, 64, lengths, new)
+    for i, l in enumerate(lengths):
+        far = np.zeros(l)
+        far[rng.integers(0, l, l // 8)] = 1.0
+        far[10:12] = 3e4
+        sign = rng.choice([-1.0, 1.0], (l, heads, 1))
+        k = rng.standard_normal((l, heads, 128)) * 0.02 + far[:, None, None] * sign * 3.0
+        v = rng.standard_normal((l, heads, 128)) * 0.05 + far[:, None, None] * sign * 40.0
+        k[10:12] *= 1e-4
+        okv.append(c.pages, c.table, [(r, i, r) for r in range(l)], k.astype(np.float32), v.astype(np.float32))
+    q = rng.standard_normal((c.rows, heads * group, 128)).astype(np.float32)
+    q = _bf16(q) if q_type == "bf16" else q
+    cache, batch = on_device(b, c)
+    out = torch.empty((c.rows, heads * group * 128), device="cuda")
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), torch.bfloat16 if q_type == "bf16" else torch.float32), cache, 0, batch, 0.05, out, ws)
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.05))
+    got = out.double().cpu().numpy().reshape(want.shape)
+    worst = np.abs(got - want) / tolerance(want, *bounds, q_type, "f32")
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
 def test_attention_does_not_see_tokens_that_are_not_there(oracle, b):
     """Pages outside the cache, lines outside the table, a length beyond the line: as if those tokens did not exist."""
     import torch
