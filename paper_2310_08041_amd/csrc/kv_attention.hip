@@ -607,7 +607,7 @@ extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();
     a.few = INT32_MAX;
-    if (prompts_pay(cache, batch, q_heads, q_dtype)) {
+    if (a.scale2 != 0.0f && prompts_pay(cache, batch, q_heads, q_dtype)) { // (it divides by the scale)
         a.few = batch->n_seqs == 1 ? 0 : FEW_ROWS;
         rc = qllm_kv_launch_prompts(a, cache->dim, out_dtype, stream);
         if (rc != QLLM_OK || batch->n_seqs == 1) return rc;

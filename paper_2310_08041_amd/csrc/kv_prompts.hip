@@ -3,10 +3,14 @@
 //
 // A workgroup of four waves owns 128 rows of a sequence and kv head, a wave 32 of them (columns of the transposed products), and
 // walks the tokens they see in tiles of 64.  A tile's codes become bf16 operands 16 + c in LDS once for the four waves, while the
-// tile before is multiplied: keys token by token with the zero point as 16 more channels (its bf16 parts meet those of the
-// queries' sums), values channel by channel in the order in which the weights come out of the scores.  The values' zero points
-// meet the weights in one product more per 16 tokens, shared by all channels; its sums are added to the others every few tiles,
-// so that the two stay small and lose nothing to each other.
+// tile before is multiplied: keys token by token, values channel by channel in the order in which the weights come out of the
+// scores.  The softmax's vector instructions take as long as the products, so what can be a product is one:
+//   - a key's zero point is 16 more channels (bf16 parts of - (16 + beta) meet those of the query's sum);
+//   - the values' alpha comes in there too, as log2 alpha_v / (scale alpha_k) against a one: the weights leave the exponential as
+//     p alpha_v, ready to be rounded;
+//   - one product more per 16 tokens, shared by all channels, has - (16 + beta) of the values in its rows 0..2 (in parts) and
+//     1 / alpha_v in the next ones: the zero points' share of the values' sums, and the sum of the weights.
+// The zero points' sums are added to the others every few tiles, so that the two stay small and lose nothing to each other.
 #include <hip/hip_runtime.h>
 
 #include <math.h>
@@ -29,16 +33,16 @@ struct Operands {
     static constexpr int KS = D + 16, VS = TILE + 8; // a token's keys and its zero point; a channel's values (+8: neighbouring rows on other banks)
     uint16_t k[TILE][KS]; // 8 channels at a time in the order 0, 4, 1, 5, 2, 6, 3, 7
     uint16_t v[D][VS];    // tokens of 16: the 8 of lane half 0 (0..3, 8..11), then the others
-    float ka[TILE], va[TILE];
-    uint16_t vz[3][TILE]; // - (16 + beta) of the values in three bf16 parts, tokens in the order of v
+    uint16_t rows[8][VS]; // of the shared product, tokens in the order of v: - (16 + beta) of the values and 1 / alpha, three bf16 parts each
+    float ka[TILE];       // scale alpha of the keys
 };
 
 // What a thread asks of memory for a tile: a quarter of a token's keys, 8 tokens of D / 32 channels of the values, one token's
-// alpha and beta (of its key in quarter 0, of its value in quarter 1).
+// alpha and beta (of its key in quarter 0, of its value in quarter 1) and its value's alpha.
 template <int D>
 struct Asked {
     uint32_t k[D / 32], v[8];
-    float alpha;
+    float alpha, value_alpha;
     int32_t beta;
 };
 
@@ -47,7 +51,6 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
 {
     constexpr int KSTEPS = D / 16, DT = D / 32;
     __shared__ __attribute__((aligned(16))) Operands<D> op[2];
-    __shared__ int32_t far_in[2][WAVES]; // some value of the wave's tokens lies far from zero for its range
 
     const Step &s = a.s;
     const int32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
@@ -105,9 +108,9 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
         }
         sum += __shfl_xor(sum, 32);
         float part[3];
-        split<3>(sum, part); // zero point parts z, z, z, z', z', z', z'', z'' | z'' meet q, q', q'', q, q', q'', q, q' | q''
+        split<3>(sum, part); // z, z, z, z', z', z', z'', z'' | z'' meet q, q', q'', q, q', q'', q, q' | q'', three parts more a one
         qz = h == 0 ? __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part[0], part[1]), pack_bf16(part[2], part[0]), pack_bf16(part[1], part[2]), pack_bf16(part[0], part[1])})
-                    : __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part[2], 0.0f), 0, 0, 0});
+                    : __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part[2], 1.0f), pack_bf16(1.0f, 1.0f), 0, 0});
     }
 
     // page numbers of up to 64 blocks of 32 tokens, one a lane
@@ -143,6 +146,7 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
             const uint8_t *par = part + P * D + ((k_part & 1) * 2 * P + (tok & (P - 1))) * 4;
             x.alpha = *reinterpret_cast<const float *>(par);
             x.beta = *reinterpret_cast<const int32_t *>(par + 4 * P);
+            x.value_alpha = *reinterpret_cast<const float *>(part + P * D + (2 * P + (tok & (P - 1))) * 4);
         }
         {
             const int32_t tok = t0 + v_tok;
@@ -168,25 +172,35 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
             put(2, u32x4{codes.pair<2>(pair[0]), codes.pair<2>(pair[1]), codes.pair<2>(pair[2]), codes.pair<2>(pair[3])});
             put(3, u32x4{codes.pair<3>(pair[0]), codes.pair<3>(pair[1]), codes.pair<3>(pair[2]), codes.pair<3>(pair[3])});
         }
-        const float zero = -16.0f - (float)x.beta;
-        const bool far = __any(k_part == 1 && fabsf(zero) > 256.0f);
-        if (lane == 0) far_in[b][wave] = far;
-        if (k_part < 2) {
-            float z[3];
-            split<3>(zero, z);
+        if (k_part < 2) { // (tokens that no row sees may hold anything: nothing here that is not finite meets a weight of zero)
+            float part[3];
+            split<3>(-16.0f - (float)x.beta, part);
             if (k_part == 0) {
-                o.ka[k_tok] = x.alpha * a.scale2;
-                *reinterpret_cast<u32x4 *>(&o.k[k_tok][D]) = u32x4{pack_bf16(z[0], z[0]), pack_bf16(z[0], z[1]), pack_bf16(z[1], z[1]), pack_bf16(z[2], z[2])};
-                *reinterpret_cast<u32x4 *>(&o.k[k_tok][D + 8]) = u32x4{pack_bf16(z[2], 0.0f), 0, 0, 0};
+                // a factor this small is a key that is zero to every query: 2^-90 in its place keeps the quotient finite
+                float ka = x.alpha * a.scale2;
+                ka = fabsf(ka) < 0x1p-90f ? copysignf(0x1p-90f, ka) : ka;
+                float more[3];
+                split<3>(__builtin_amdgcn_logf(x.value_alpha) / ka, more);
+                o.ka[k_tok] = ka;
+                *reinterpret_cast<u32x4 *>(&o.k[k_tok][D]) =
+                    u32x4{pack_bf16(part[0], part[0]), pack_bf16(part[0], part[1]), pack_bf16(part[1], part[1]), pack_bf16(part[2], part[2])};
+                *reinterpret_cast<u32x4 *>(&o.k[k_tok][D + 8]) = u32x4{pack_bf16(part[2], more[0]), pack_bf16(more[1], more[2]), 0, 0};
             } else {
-                o.va[k_tok] = x.alpha;
                 const int32_t u = k_tok & 15, place = (k_tok & ~15) + (u >> 2 & 1) * 8 + (u >> 3) * 4 + (u & 3);
+                float r[3];
+                split<3>(x.alpha > 0.0f && x.alpha < INFINITY ? __builtin_amdgcn_rcpf(x.alpha) : 0.0f, r);
 #pragma unroll
-                for (int i = 0; i < 3; ++i) o.vz[i][place] = (uint16_t)(__float_as_uint(z[i]) >> 16);
+                for (int i = 0; i < 3; ++i) {
+                    o.rows[i][place] = (uint16_t)(__float_as_uint(part[i]) >> 16);
+                    o.rows[3 + i][place] = (uint16_t)(__float_as_uint(r[i]) >> 16);
+                }
             }
         }
     };
 
+    // Row (i & 3) + 8 (i >> 2) + 4 h of the shared product is element i of a lane: both halves find the values' zero points in
+    // elements 0..2 and the sum of the weights in 3..5.
+    const int32_t shared_row = (col & 3) + (col >> 3 == 1 ? 4 : 0);
     f32x16 acc[DT], off;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -194,7 +208,7 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
 #pragma unroll
         for (int i = 0; i < DT; ++i) acc[i][e] = 0.0f;
     }
-    float m = -INFINITY, l = 0.0f;
+    float m = -INFINITY;
 
     const auto work = [&](int32_t tile, int32_t b, const int32_t (&page)[2]) {
         const Operands<D> &o = op[b];
@@ -209,17 +223,15 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
 #pragma unroll
             for (int i = 0; i < KSTEPS; ++i) sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(row + 16 * i), q[i], sc[x], 0, 0, 0);
         }
-        // x = alpha s - m; the maximum follows where that passes SLACK, or where a row has none yet
+        // log2 of p alpha_v, less m; the maximum follows where that passes SLACK, or where a row has none yet
         const float base = m == -INFINITY ? 0.0f : m;
-        float va[2][16];
         float top = -INFINITY;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float4 ka = *reinterpret_cast<const float4 *>(&o.ka[32 * x + 8 * j + 4 * h]), w = *reinterpret_cast<const float4 *>(&o.va[32 * x + 8 * j + 4 * h]);
+                const float4 ka = *reinterpret_cast<const float4 *>(&o.ka[32 * x + 8 * j + 4 * h]);
                 const float f[4] = {ka.x, ka.y, ka.z, ka.w};
-                va[x][4 * j] = w.x, va[x][4 * j + 1] = w.y, va[x][4 * j + 2] = w.z, va[x][4 * j + 3] = w.w;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sc[x][4 * j + i] = __builtin_fmaf(f[i], sc[x][4 * j + i], -base);
             }
@@ -233,7 +245,6 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
                     const int32_t tok = mine + 32 * x + 8 * (e >> 2) + (e & 3);
                     const bool seen = tok >= lo && tok <= hi && page[x] >= 0;
                     sc[x][e] = seen ? sc[x][e] : -INFINITY;
-                    va[x][e] = seen ? va[x][e] : 0.0f;
                 }
         }
 #pragma unroll
@@ -245,7 +256,7 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
             top = fmaxf(top, __shfl_xor(top, 32));
             const float up = top == -INFINITY ? 0.0f : (fresh ? top : fmaxf(top, 0.0f)), f = fresh ? 1.0f : __builtin_amdgcn_exp2f(-up);
             m = fresh && top == -INFINITY ? m : base + up;
-            l *= f, off *= f;
+            off *= f;
 #pragma unroll
             for (int i = 0; i < DT; ++i) acc[i] *= f;
 #pragma unroll
@@ -253,32 +264,23 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sc[x][e] -= up;
         }
-        const bool far = (far_in[b][0] | far_in[b][1] | far_in[b][2] | far_in[b][3]) != 0;
 #pragma unroll
         for (int y = 0; y < 4; ++y) { // 16 tokens
             uint32_t pw[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int x = y >> 1, at = 8 * (y & 1) + 2 * e;
-                const float p0 = __builtin_amdgcn_exp2f(sc[x][at]), p1 = __builtin_amdgcn_exp2f(sc[x][at + 1]);
-                l += p0 + p1;
-                pw[e] = pack_bf16(p0 * va[x][at], p1 * va[x][at + 1]);
-            }
+            for (int e = 0; e < 4; ++e)
+                pw[e] = pack_bf16(__builtin_amdgcn_exp2f(sc[y >> 1][8 * (y & 1) + 2 * e]), __builtin_amdgcn_exp2f(sc[y >> 1][8 * (y & 1) + 2 * e + 1]));
             const bf16x8 p = __builtin_bit_cast(bf16x8, u32x4{pw[0], pw[1], pw[2], pw[3]});
-            off = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(&o.vz[0][16 * y + 8 * h]), p, off, 0, 0, 0);
+            off = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(&o.rows[shared_row][16 * y + 8 * h]), p, off, 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < DT; ++i)
                 acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(&o.v[32 * i + col][16 * y + 8 * h]), p, acc[i], 0, 0, 0);
-            if (far) {
-                off = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(&o.vz[1][16 * y + 8 * h]), p, off, 0, 0, 0);
-                off = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(&o.vz[2][16 * y + 8 * h]), p, off, 0, 0, 0);
-            }
         }
-        if (far || (tile - tile_begin) % TOGETHER == TOGETHER - 1) {
+        if ((tile - tile_begin) % TOGETHER == TOGETHER - 1) {
+            const float zero = off[0] + off[1] + off[2];
 #pragma unroll
-            for (int i = 0; i < DT; ++i) acc[i] += off[0];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) off[e] = 0.0f;
+            for (int i = 0; i < DT; ++i) acc[i] += zero;
+            off[0] = off[1] = off[2] = 0.0f;
         }
     };
 
@@ -297,7 +299,7 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
     }
 
     if (!real) return;
-    l += __shfl_xor(l, 32); // the other half of the same row: as real as this one
+    const float zero = off[0] + off[1] + off[2], l = off[3] + off[4] + off[5];
     const int64_t at = (int64_t)(t.seq.row + token) * a.ldo + (head * a.group + head_of_row) * D + 4 * h;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
@@ -305,7 +307,7 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
         for (int j = 0; j < 4; ++j) {
             float y[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = quotient(acc[i][4 * j + e] + off[0], l);
+            for (int e = 0; e < 4; ++e) y[e] = quotient(acc[i][4 * j + e] + zero, l);
             const int64_t to = at + 32 * i + 8 * j;
             if (F32O) {
                 float *p = static_cast<float *>(a.out) + to;

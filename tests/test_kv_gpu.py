@@ -204,10 +204,11 @@ HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}                 # half a step, rel
 
 def tolerance(want, absv, err_s, err_o, q_type, out_type):
     """Roundings, element by element: the output's own; that of every weight p alpha before it meets the values (bf16 for bf16
-    queries, 24 bits for fp32 ones), the same rounded number standing in both sums; the scores' fp32 error, which moves weights
-    and their sum by at most e^E - 1 each; the fp32 sums."""
+    queries, 24 bits for fp32 ones), the same rounded number standing in all sums: where the weights' own sum is taken of the
+    rounded ones, w (1 + d) gives sum w d (v - out) / (1 + ..), at most half a step of sum w |v| and of |out|; the scores' fp32
+    error, which moves weights and their sum by at most e^E - 1 each; the fp32 sums."""
     p = HALF[q_type]
-    return HALF[out_type] * (np.abs(want) + p * absv) * (1 + 2.0 ** -7) + p * absv + 2.0 * np.expm1(err_s) * absv + 2.0 * err_o + 1e-30
+    return HALF[out_type] * (np.abs(want) + p * absv) * (1 + 2.0 ** -7) + p * (1 + 2.0 ** -7) * (absv + np.abs(want)) + 2.0 * np.expm1(err_s) * absv + 2.0 * err_o + 1e-30
 
 
 ATTEND = [  # q, out, heads, group, dim, page, lengths, new rows, window, slots, lines, rows behind the last
