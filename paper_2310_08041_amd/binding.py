@@ -729,9 +729,10 @@ class DeviceKVCache:
         _check_tensor(pages, "pages", _U8_ONLY, shape=(self.layers, self.n_pages, self.page_bytes))
         if not pages.is_contiguous():
             _fail("pages must be contiguous")
-        self.pages = pages
+        self.pages, self.device = pages, pages.get_device()
         step = self.n_pages * self.page_bytes
         self.c = [_KVCache(self.heads, self.dim, self.page_tokens, self.n_pages, _dp(pages) + i * step) for i in range(self.layers)]
+        self.ref = [C.byref(c) for c in self.c]
 
 
 class DeviceKVBatch:
@@ -751,19 +752,35 @@ class DeviceKVBatch:
         _need(row_start is not None or self.rows >= self.n_seqs, f"{self.n_seqs} sequences of one row each need as many rows, there are {self.rows}")
         _need(slot is not None or n_slots >= self.n_seqs, f"{self.n_seqs} sequences, but {n_slots} lines in the table")
         self.table, self.length, self.row_start, self.slot = table, length, row_start, slot
+        self.device = table.get_device()
+        for name, t in (("length", length), ("row_start", row_start), ("slot", slot)):
+            if t is not None and t.get_device() != self.device:
+                _fail(f"{name} is on another device than the table")
         self.c = _KVBatch(self.rows, self.n_seqs, _dp(row_start), _dp(slot), n_slots, table_ld, _dp(table), _dp(length))
+        self.ref = C.byref(self.c)
 
 
-def _check_kv(cache, layer, batch):
-    if not 0 <= int(layer) < cache.layers:
+def _check_kv(cache, layer, batch, **tensors):
+    """Last of a wrapper's checks: the layer, and everything on the device that the call runs on.  (A decode step is host time: no
+    message is put together, and no list walked twice, unless something is wrong.)"""
+    dev = cache.device
+    if 0 <= layer < cache.layers and dev >= 0 and batch.device == dev and torch.cuda.current_device() == dev:
+        for t in tensors.values():
+            if t is not None and t.get_device() != dev:
+                break
+        else:
+            return
+    if not 0 <= layer < cache.layers:
         _fail(f"layer {layer} of a cache of {cache.layers}")
-    return dict(pages=cache.pages, table=batch.table, length=batch.length, row_start=batch.row_start, slot=batch.slot)
+    _check_on_current(**tensors, pages=cache.pages, table=batch.table)
 
 
 def _check_rows(t, name, dtypes, rows, width):
-    if not (hasattr(t, "dim") and t.dim() == 2):
-        _fail(f"{name} must be a 2-d tensor [rows, channels]")
-    _check_tensor(t, name, dtypes, shape=(rows, width))
+    """[rows, width] of one of the types with dense rows; returns their stride."""
+    if not (isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == (rows, width) and t.stride(1) == 1):
+        if not (hasattr(t, "dim") and t.dim() == 2):
+            _fail(f"{name} must be a 2-d tensor [rows, channels]")
+        _check_tensor(t, name, dtypes, shape=(rows, width))
     return t.stride(0) if rows > 1 else width          # the stride of a single row says nothing
 
 
@@ -771,7 +788,6 @@ def qllm_kv_append(cache, layer, batch, k, v, q=None, q_out=None, rope=ROPE_NONE
     """Rotary positions on the step's q and k, Eq. (2) at 4 bits on its k and v, codes into the sequences' pages.  k, v [rows, heads *
     dim], q [rows, query heads * dim] (or None) of one dtype, rows may be strided; q_out receives the rotated queries (q itself
     will do).  rope: ROPE_*; inv_freq [dim / 2] float64, angle per position."""
-    kv = _check_kv(cache, layer, batch)
     width, rows, dtype = cache.heads * cache.dim, batch.rows, (k.dtype if isinstance(k, torch.Tensor) else None,)
     ldk = _check_rows(k, "k", _FLOATS, rows, width)
     ldv = _check_rows(v, "v", dtype, rows, width)
@@ -784,28 +800,27 @@ def qllm_kv_append(cache, layer, batch, k, v, q=None, q_out=None, rope=ROPE_NONE
         ldq_out = _check_rows(q_out, "q_out", dtype, rows, q_heads * cache.dim)
     if int(rope) != ROPE_NONE:
         _check_tensor(inv_freq, "inv_freq", _F64_ONLY, numel=cache.dim // 2)
-    _check_on_current(k=k, v=v, q=q, q_out=q_out, inv_freq=inv_freq, **kv)
+    _check_kv(cache, layer, batch, k=k, v=v, q=q, q_out=q_out, inv_freq=inv_freq)
     _chk(_lib.qllm_kv_append(_dp(q), ldq, q_heads, _dp(q_out), ldq_out, _dp(k), ldk, _dp(v), ldv, _x_dtype(k), int(rope), _dp(inv_freq),
-                             C.byref(cache.c[layer]), C.byref(batch.c), _stream(stream)), "qllm_kv_append")
+                             cache.ref[layer], batch.ref, _stream(stream)), "qllm_kv_append")
     return q_out
 
 
 def qllm_kv_read(cache, layer, batch, k_out=None, v_out=None, stream=None):
     """What the cache holds for the step's rows, alpha * (code - beta), in k_out and v_out [rows, heads * dim] of one dtype."""
-    kv = _check_kv(cache, layer, batch)
     width = cache.heads * cache.dim
     one = k_out if k_out is not None else v_out
     if one is None:
         _fail("k_out or v_out is required")
     ldk = _check_rows(k_out, "k_out", _FLOATS, batch.rows, width) if k_out is not None else 0
     ldv = _check_rows(v_out, "v_out", _FLOATS if k_out is None else (k_out.dtype,), batch.rows, width) if v_out is not None else 0
-    _check_on_current(k_out=k_out, v_out=v_out, **kv)
-    _chk(_lib.qllm_kv_read(C.byref(cache.c[layer]), C.byref(batch.c), _dp(k_out), ldk, _dp(v_out), ldv, _x_dtype(one), _stream(stream)),
+    _check_kv(cache, layer, batch, k_out=k_out, v_out=v_out)
+    _chk(_lib.qllm_kv_read(cache.ref[layer], batch.ref, _dp(k_out), ldk, _dp(v_out), ldv, _x_dtype(one), _stream(stream)),
          "qllm_kv_read")
 
 
 def qllm_kv_attention_workspace_bytes(cache, batch, q_heads):
-    v = _lib.qllm_kv_attention_workspace_bytes(C.byref(cache.c[0]), C.byref(batch.c), int(q_heads))
+    v = _lib.qllm_kv_attention_workspace_bytes(cache.ref[0], batch.ref, int(q_heads))
     _chk(v if v < 0 else 0, "qllm_kv_attention_workspace_bytes")
     return int(v)
 
@@ -813,15 +828,14 @@ def qllm_kv_attention_workspace_bytes(cache, batch, q_heads):
 def qllm_kv_attention(q, cache, layer, batch, scale, out, workspace, window=0, stream=None):
     """Causal attention of the step's queries [rows, query heads * dim] over the cache into out of the same shape (fp32 / bf16 each);
     window > 0: only that many newest tokens of each query."""
-    kv = _check_kv(cache, layer, batch)
     q_heads = q.shape[-1] // cache.dim if hasattr(q, "shape") and q.dim() == 2 else 0
     ldq = _check_rows(q, "q", _FLOATS, batch.rows, q_heads * cache.dim)
     ldo = _check_rows(out, "out", _FLOATS, batch.rows, q_heads * cache.dim)
-    _check_tensor(workspace, "workspace", _U8_ONLY)
-    if not workspace.is_contiguous():
+    if not (isinstance(workspace, torch.Tensor) and workspace.dtype is torch.uint8 and workspace.is_contiguous()):
+        _check_tensor(workspace, "workspace", _U8_ONLY)
         _fail("workspace must be contiguous")
-    _check_on_current(q=q, out=out, workspace=workspace, **kv)
-    _chk(_lib.qllm_kv_attention(_dp(q), _x_dtype(q), ldq, q_heads, C.byref(cache.c[layer]), C.byref(batch.c), float(scale), int(window),
+    _check_kv(cache, layer, batch, q=q, out=out, workspace=workspace)
+    _chk(_lib.qllm_kv_attention(_dp(q), _x_dtype(q), ldq, q_heads, cache.ref[layer], batch.ref, float(scale), int(window),
                                 _dp(out), _x_dtype(out), ldo, _dp(workspace), workspace.numel(), _stream(stream)), "qllm_kv_attention")
     return out
 
@@ -842,9 +856,10 @@ class KVBook:
 
     def __init__(self, page_tokens, table, length, refs):
         for name, a, dims in (("table", table, 2), ("length", length, 1), ("refs", refs, 1)):
-            _need(isinstance(a, np.ndarray) and a.dtype == np.int32 and a.ndim == dims and a.flags.c_contiguous and a.flags.writeable,
-                  f"{name} must be a writeable contiguous int32 array of {dims} dimensions")
-        _need(length.size == table.shape[0], f"length must hold one entry per line of the table ({table.shape[0]})")
+            if not (isinstance(a, np.ndarray) and a.dtype == np.int32 and a.ndim == dims and a.flags.c_contiguous and a.flags.writeable):
+                _fail(f"{name} must be a writeable contiguous int32 array of {dims} dimensions")
+        if length.size != table.shape[0]:
+            _fail(f"length must hold one entry per line of the table ({table.shape[0]})")
         self.page_tokens, self.table, self.length, self.refs = int(page_tokens), table, length, refs
         self.c = _KVBook(self.page_tokens, table.shape[0], table.shape[1], refs.size, _hp(table), _hp(length), _hp(refs))
 
@@ -855,7 +870,8 @@ class KVBook:
 
 def _host_list(a, name, size=None):
     a = np.atleast_1d(_np(a, np.int32))
-    _need(a.ndim == 1 and (size is None or a.size == size), f"{name} must be a list" + ("" if size is None else f" of {size}"))
+    if a.ndim != 1 or (size is not None and a.size != size):
+        _fail(f"{name} must be a list" + ("" if size is None else f" of {size}"))
     return a
 
 

@@ -22,31 +22,35 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
-// Eight neighbouring values of a row; vec: they are 16-byte aligned.
+// Eight neighbouring values of a row as they lie in memory (bf16: one 16-byte word, fp32: two); vec: they are 16-byte aligned.
 template <bool F32>
-__device__ __forceinline__ void load8(const void *base, int64_t at, bool vec, float (&x)[8])
+struct Raw {
+    uint4 w[F32 ? 2 : 1];
+};
+template <bool F32>
+__device__ __forceinline__ Raw<F32> load8(const void *base, int64_t at, bool vec)
 {
-    if (F32) {
-        const float *p = static_cast<const float *>(base) + at;
-        if (vec) {
-            const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
-            x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-        } else {
+    Raw<F32> r;
+    if (vec) {
+        const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(base) + at * (F32 ? 4 : 2));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = p[e];
-        }
+        for (int i = 0; i < (F32 ? 2 : 1); ++i) r.w[i] = p[i];
+    } else if (F32) {
+        const uint32_t *p = static_cast<const uint32_t *>(base) + at;
+#pragma unroll
+        for (int i = 0; i < (F32 ? 2 : 1); ++i) r.w[i] = make_uint4(p[4 * i], p[4 * i + 1], p[4 * i + 2], p[4 * i + 3]);
     } else {
         const uint16_t *p = static_cast<const uint16_t *>(base) + at;
-        if (vec) {
-            const uint4 a = *reinterpret_cast<const uint4 *>(p);
-            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[2 * e] = __uint_as_float(w[e] << 16), x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = __uint_as_float((uint32_t)p[e] << 16);
-        }
+        r.w[0] = make_uint4(p[0] | (uint32_t)p[1] << 16, p[2] | (uint32_t)p[3] << 16, p[4] | (uint32_t)p[5] << 16, p[6] | (uint32_t)p[7] << 16);
     }
+    return r;
+}
+template <bool F32>
+__device__ __forceinline__ void widen8(const Raw<F32> &r, float (&x)[8])
+{
+    const uint32_t *w = reinterpret_cast<const uint32_t *>(r.w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = F32 ? __uint_as_float(w[F32 ? e : 0]) : __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
 }
 
 template <bool F32>
@@ -96,70 +100,107 @@ __device__ __forceinline__ bool token_of(const Step &s, int32_t row, int32_t *li
     return j >= 0 && j < q.n && q.line >= 0 && *pos >= 0;
 }
 
+// The value of the lane LANES / 2 further in a head's LANES lanes, and a minimum or maximum over them, without a trip through LDS
+// where the hardware can (16 lanes: rotations within a row of 16; 8: mirrored halves, then quads).
+template <int LANES>
+__device__ __forceinline__ float across(float x)
+{
+    const int32_t v = __float_as_int(x);
+    return __int_as_float(LANES == 16 ? __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true) : __builtin_amdgcn_ds_swizzle(v, 0x101f));
+}
+template <int LANES, class F>
+__device__ __forceinline__ float over_lanes(float x, F pick)
+{
+#define QLLM_PICK(CTRL) x = pick(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true)))
+    if (LANES == 16) {
+        QLLM_PICK(0x128);
+        QLLM_PICK(0x124);
+        QLLM_PICK(0x122);
+        QLLM_PICK(0x121);
+    } else {
+        QLLM_PICK(0x141);
+        QLLM_PICK(0xb1);
+        QLLM_PICK(0x4e);
+    }
+#undef QLLM_PICK
+    return x;
+}
+
 // One workgroup per row; D / 8 lanes per head, 8 channels per lane.  The angles of the row are worked out once, by D / 2 lanes,
-// and kept in LDS for all heads.
+// and kept in LDS for all heads; a head's values are asked for while the heads before it are worked on, the first ones before
+// the angles.
 template <int D, bool F32>
 __global__ __launch_bounds__(THREADS) void append_kernel(const AppendArgs a)
 {
     constexpr int LANES = D / 8, PER = THREADS / LANES; // lanes of a head, heads at a time
-    __shared__ float2 turn[D / 2];
+    __shared__ double2 turn[D / 2];
     const Step &s = a.s;
-    const int32_t row = blockIdx.x, tid = threadIdx.x;
+    const int32_t row = blockIdx.x, tid = threadIdx.x, lane = tid % LANES;
+    const int32_t q_heads = a.q ? a.q_heads : 0, units = q_heads + 2 * s.heads;
+    const bool vec = a.vec;
+    // head u of the row: 0 query, 1 key, 2 value
+    const auto kind_of = [&](int32_t u) { return u < q_heads ? 0 : (u < q_heads + s.heads ? 1 : 2); };
+    const auto head_of = [&](int32_t u, int32_t kind) { return u - (kind > 0 ? q_heads : 0) - (kind > 1 ? s.heads : 0); };
+    const auto fetch = [&](int32_t u) {
+        Raw<F32> r = {};
+        if (u < units) {
+            const int32_t kind = kind_of(u);
+            const void *src = kind == 0 ? a.q : (kind == 1 ? a.k : a.v);
+            const int64_t ld = kind == 0 ? a.ldq : (kind == 1 ? a.ldk : a.ldv);
+            r = load8<F32>(src, (int64_t)row * ld + head_of(u, kind) * D + 8 * lane, vec);
+        }
+        return r;
+    };
+    Raw<F32> raw = fetch(tid / LANES);
     int32_t line, pos;
     if (!token_of(s, row, &line, &pos)) return; // the same for the whole workgroup
+    const int32_t page = page_of(s, line, pos);
     if (a.rope != QLLM_ROPE_NONE) {
         if (tid < D / 2) {
-            const double angle = (double)pos * a.inv_freq[tid];
             double sn, cs;
-            sincos(angle, &sn, &cs);
-            turn[tid] = make_float2((float)cs, (float)sn);
+            sincos((double)pos * a.inv_freq[tid], &sn, &cs);
+            turn[tid] = make_double2((float)cs, (float)sn);
         }
         __syncthreads();
     }
-    const int32_t page = page_of(s, line, pos);
     const int32_t P = 1 << s.page_shift, in_page = pos & (P - 1);
-    const int32_t lane = tid % LANES, q_heads = a.q ? a.q_heads : 0, units = q_heads + 2 * s.heads;
-    const bool vec = a.vec;
     for (int32_t base = 0; base < units; base += PER) { // lanes beyond the last head go through it too: they take part in the exchanges
-        const int32_t u = base + tid / LANES;
-        const int32_t kind = u < q_heads ? 0 : (u < q_heads + s.heads ? 1 : 2); // query, key, value
-        const int32_t head = kind == 0 ? u : (kind == 1 ? u - q_heads : u - q_heads - s.heads);
+        const int32_t u = base + tid / LANES, kind = kind_of(u), head = head_of(u, kind);
         const bool real = u < units;
-        float x[8] = {};
-        if (real) {
-            const void *src = kind == 0 ? a.q : (kind == 1 ? a.k : a.v);
-            const int64_t ld = kind == 0 ? a.ldq : (kind == 1 ? a.ldk : a.ldv);
-            load8<F32>(src, (int64_t)row * ld + head * D + 8 * lane, vec, x);
-        }
+        float x[8];
+        widen8<F32>(raw, x);
+        raw = fetch(u + PER);
+        // x1 c - x2 s and x2 c + x1 s: the products are exact in double, the sum is rounded there once (a fused multiply-add
+        // of an exact product is that sum), then to float
         if (a.rope == QLLM_ROPE_HALVES) { // the partner's channels sit half the head's lanes away
+            const double sign = lane < LANES / 2 ? -1.0 : 1.0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float y = __shfl_xor(x[e], LANES / 2);
-                const float2 t = turn[8 * (lane % (LANES / 2)) + e];
-                const double turned = (double)x[e] * (double)t.x, other = (double)y * (double)t.y;
-                if (kind != 2) x[e] = (float)(lane < LANES / 2 ? turned - other : turned + other);
+                const float y = across<LANES>(x[e]);
+                const double2 t = turn[8 * (lane % (LANES / 2)) + e];
+                const float turned = (float)__builtin_fma((double)x[e], t.x, sign * ((double)y * t.y));
+                if (kind != 2) x[e] = turned;
             }
-        } else if (a.rope == QLLM_ROPE_PAIRS && kind != 2) {
+        } else if (a.rope == QLLM_ROPE_PAIRS) {
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {
-                const float2 t = turn[4 * lane + e / 2];
-                const double x1 = x[e], x2 = x[e + 1], c = t.x, sn = t.y;
-                x[e] = (float)(x1 * c - x2 * sn);
-                x[e + 1] = (float)(x2 * c + x1 * sn);
+                const double2 t = turn[4 * lane + e / 2];
+                const double x1 = x[e], x2 = x[e + 1];
+                const float y1 = (float)__builtin_fma(x1, t.x, -(x2 * t.y)), y2 = (float)__builtin_fma(x2, t.x, x1 * t.y);
+                if (kind != 2) x[e] = y1, x[e + 1] = y2;
             }
+        }
+        if (kind == 0) {
+            if (real) store8<F32>(a.q_out, (int64_t)row * a.ldq_out + head * D + 8 * lane, vec, x);
+            if (base + PER <= q_heads) continue; // queries all
         }
         // Eq. (2) over the head's channels
         float lo = x[0], hi = x[0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) lo = fminf(lo, x[e]), hi = fmaxf(hi, x[e]);
-#pragma unroll
-        for (int o = LANES / 2; o > 0; o >>= 1) lo = fminf(lo, __shfl_xor(lo, o)), hi = fmaxf(hi, __shfl_xor(hi, o));
-        if (!real) continue;
-        if (kind == 0) {
-            store8<F32>(a.q_out, (int64_t)row * a.ldq_out + head * D + 8 * lane, vec, x);
-            continue;
-        }
-        if (page < 0) continue;
+        lo = over_lanes<LANES>(lo, [](float p, float q) { return fminf(p, q); });
+        hi = over_lanes<LANES>(hi, [](float p, float q) { return fmaxf(p, q); });
+        if (!real || kind == 0 || page < 0) continue;
         float alpha = (hi - lo) * (1.0f / 15.0f);
         if (!(alpha >= 0x1p-126f)) alpha = 1.0f;
         const float inv = 1.0f / alpha;
