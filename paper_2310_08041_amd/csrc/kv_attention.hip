@@ -453,13 +453,13 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
     }
 }
 
-// The parts of unfinished tiles joined: a workgroup for JOIN_ROWS rows of each tile, JOIN_WAVES / JOIN_ROWS waves for a row.  A part
-// of a row takes D / 4 lanes; every read of a batch is on its way before the first is looked at.
-constexpr int JOIN_ROWS = 2, JOIN_WAVES = 8;
+// The parts of unfinished tiles joined, a workgroup for (some rows of) each tile: a wave for a row of few parts, JOIN_WAVES / 2
+// for a row of many.  A part of a row takes D / 4 lanes; every read of a batch is on its way before the first is looked at.
+constexpr int JOIN_WAVES = 8, JOIN_FEW = 12;
 template <int D, bool F32O>
 __global__ __launch_bounds__(JOIN_WAVES * 64) void join_kernel(const AttendArgs a)
 {
-    constexpr int PER_ROW = JOIN_WAVES / JOIN_ROWS, AT_ONCE = 64 / (D / 4), BATCH = 6;
+    constexpr int AT_ONCE = 64 / (D / 4), BATCH = 6;
     __shared__ float tops[JOIN_WAVES], sums[JOIN_WAVES], os[JOIN_WAVES][D];
     const int32_t head = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int32_t number = blockIdx.x;
@@ -469,66 +469,68 @@ __global__ __launch_bounds__(JOIN_WAVES * 64) void join_kernel(const AttendArgs 
         if (k < 0 || k >= work_of(a, seq_of(a.s, i)).tiles) return;
     }
     const Unfinished u = a.unfinished[(int64_t)head * a.numbers + number];
-    const int32_t n = blockIdx.z * JOIN_ROWS + wave / PER_ROW;
     // (the comparisons with the launch's sizes are for a row_start that does not ascend)
     if (u.parts <= 1 || u.block < 0 || u.block >= a.blocks || u.parts > a.blocks - u.block || u.q_row < 0 || u.head0 < 0 || u.head0 >= a.group ||
-        u.rows > ROWS || (int64_t)u.q_row * a.group + u.head0 + u.rows > (int64_t)a.s.rows * a.group || (int32_t)blockIdx.z * JOIN_ROWS >= u.rows)
+        u.rows > ROWS || (int64_t)u.q_row * a.group + u.head0 + u.rows > (int64_t)a.s.rows * a.group)
         return;
+    const int32_t per_row = u.parts <= JOIN_FEW ? 1 : JOIN_WAVES / 2, at_once = JOIN_WAVES / per_row; // waves of a row, rows of a pass
     const int32_t sub = lane / (D / 4), c = lane % (D / 4) * 4;
-    float top = -INFINITY, sum = 0.0f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int32_t p0 = wave % PER_ROW * AT_ONCE + sub; n < u.rows && p0 < u.parts; p0 += PER_ROW * AT_ONCE * BATCH) {
-        float2 ml[BATCH];
-        f32x4 x[BATCH];
+    for (int32_t row0 = blockIdx.z * at_once; row0 < u.rows; row0 += gridDim.z * at_once) {
+        const int32_t n = row0 + wave / per_row, step = per_row * AT_ONCE;
+        float top = -INFINITY, sum = 0.0f;
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        for (int32_t p0 = wave % per_row * AT_ONCE + sub; n < u.rows && p0 < u.parts; p0 += step * BATCH) {
+            float2 ml[BATCH];
+            f32x4 x[BATCH];
 #pragma unroll
-        for (int k = 0; k < BATCH; ++k) {
-            const int32_t p = p0 + k * PER_ROW * AT_ONCE;
-            ml[k] = make_float2(-INFINITY, 0.0f), x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (p < u.parts) {
-                const int64_t from = partial_at(a, head, u.block + p, p == 0 ? u.slot & 1 : 0, n);
-                ml[k] = a.part_ml[from];
-                x[k] = *reinterpret_cast<const f32x4 *>(a.part_o + from * D + c);
+            for (int k = 0; k < BATCH; ++k) {
+                const int32_t p = p0 + k * step;
+                ml[k] = make_float2(-INFINITY, 0.0f), x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (p < u.parts) {
+                    const int64_t from = partial_at(a, head, u.block + p, p == 0 ? u.slot & 1 : 0, n);
+                    ml[k] = a.part_ml[from];
+                    x[k] = *reinterpret_cast<const f32x4 *>(a.part_o + from * D + c);
+                }
+            }
+            float now = top;
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) now = fmaxf(now, ml[k].x);
+            const float base = now == -INFINITY ? 0.0f : now, f0 = __builtin_amdgcn_exp2f(top - base);
+            sum *= f0, o *= f0, top = now;
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                const float f = __builtin_amdgcn_exp2f(ml[k].x - base);
+                sum += f * ml[k].y, o += f * x[k];
             }
         }
-        float now = top;
+        // the lanes of a wave, then the waves of a row
+        float best = top;
 #pragma unroll
-        for (int k = 0; k < BATCH; ++k) now = fmaxf(now, ml[k].x);
-        const float base = now == -INFINITY ? 0.0f : now, f0 = __builtin_amdgcn_exp2f(top - base);
-        sum *= f0, o *= f0, top = now;
+        for (int k = D / 4; k < 64; k <<= 1) best = fmaxf(best, __shfl_xor(best, k));
+        const float f = __builtin_amdgcn_exp2f(top - (best == -INFINITY ? 0.0f : best));
+        sum *= f, o *= f;
 #pragma unroll
-        for (int k = 0; k < BATCH; ++k) {
-            const float f = __builtin_amdgcn_exp2f(ml[k].x - base);
-            sum += f * ml[k].y, o += f * x[k];
+        for (int k = D / 4; k < 64; k <<= 1) {
+            sum += __shfl_xor(sum, k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k);
         }
-    }
-    // the lanes of a wave, then the waves of a row
-    float best = top;
-#pragma unroll
-    for (int k = D / 4; k < 64; k <<= 1) best = fmaxf(best, __shfl_xor(best, k));
-    const float f = __builtin_amdgcn_exp2f(top - (best == -INFINITY ? 0.0f : best));
-    sum *= f, o *= f;
-#pragma unroll
-    for (int k = D / 4; k < 64; k <<= 1) {
-        sum += __shfl_xor(sum, k);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k);
-    }
-    if (lane == 0) tops[wave] = best, sums[wave] = sum;
-    if (sub == 0) *reinterpret_cast<f32x4 *>(&os[wave][c]) = o;
-    __syncthreads();
-    for (int32_t i = threadIdx.x; i < JOIN_ROWS * D; i += JOIN_WAVES * 64) {
-        const int32_t k = i / D, ch = i % D, row = blockIdx.z * JOIN_ROWS + k;
-        if (row >= u.rows) break;
-        float all = -INFINITY, total = 0.0f, y = 0.0f;
-#pragma unroll
-        for (int w = 0; w < PER_ROW; ++w) all = fmaxf(all, tops[k * PER_ROW + w]);
-        if (all == -INFINITY) all = 0.0f;
-#pragma unroll
-        for (int w = 0; w < PER_ROW; ++w) {
-            const float g = __builtin_amdgcn_exp2f(tops[k * PER_ROW + w] - all);
-            total += g * sums[k * PER_ROW + w], y += g * os[k * PER_ROW + w][ch];
+        if (lane == 0) tops[wave] = best, sums[wave] = sum;
+        if (sub == 0) *reinterpret_cast<f32x4 *>(&os[wave][c]) = o;
+        __syncthreads();
+        for (int32_t i = threadIdx.x; i < at_once * D; i += JOIN_WAVES * 64) {
+            const int32_t k = i / D, ch = i % D, row = row0 + k;
+            if (row >= u.rows) break;
+            float all = -INFINITY, total = 0.0f, y = 0.0f;
+            for (int w = k * per_row; w < (k + 1) * per_row; ++w) all = fmaxf(all, tops[w]);
+            if (all == -INFINITY) all = 0.0f;
+            for (int w = k * per_row; w < (k + 1) * per_row; ++w) {
+                const float g = __builtin_amdgcn_exp2f(tops[w] - all);
+                total += g * sums[w], y += g * os[w][ch];
+            }
+            put_out<D, F32O>(a, head, u.q_row, u.head0, row, ch, quotient(y, total));
         }
-        put_out<D, F32O>(a, head, u.q_row, u.head0, row, ch, quotient(y, total));
+        __syncthreads(); // before the next rows
     }
 }
 
@@ -633,8 +635,9 @@ extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq
 #undef QLLM_ATTEND
     rc = launched("cache attention: launch");
     if (rc != QLLM_OK || a.blocks == 1) return rc; // one workgroup a head finishes what it begins
-    const int64_t rows = batch->row_start || a.group > ROWS ? ROWS : a.group; // of a tile at most
-    const dim3 cuts((unsigned)n.numbers, (unsigned)cache->heads, (unsigned)((rows + JOIN_ROWS - 1) / JOIN_ROWS));
+    // one token each: few tiles, perhaps of many parts, two rows of which a workgroup takes; else many tiles, most of them whole
+    const int64_t rows = a.group < ROWS ? a.group : ROWS;
+    const dim3 cuts((unsigned)n.numbers, (unsigned)cache->heads, batch->row_start ? 1 : (unsigned)((rows + 1) / 2));
     if (cache->dim == 128 && out_dtype == QLLM_F32) hipLaunchKernelGGL((join_kernel<128, true>), cuts, dim3(JOIN_WAVES * 64), 0, stream, a);
     else if (cache->dim == 128) hipLaunchKernelGGL((join_kernel<128, false>), cuts, dim3(JOIN_WAVES * 64), 0, stream, a);
     else if (out_dtype == QLLM_F32) hipLaunchKernelGGL((join_kernel<64, true>), cuts, dim3(JOIN_WAVES * 64), 0, stream, a);

@@ -84,6 +84,7 @@ struct AppendArgs {
     void *q_out;
     int64_t ldq, ldq_out, ldk, ldv;
     int32_t q_heads, rope, vec;
+    int32_t slices, slice; // of a row's heads: how many, heads in each
     const double *inv_freq;
 };
 
@@ -126,101 +127,126 @@ __device__ __forceinline__ float over_lanes(float x, F pick)
     return x;
 }
 
-// One workgroup per row; D / 8 lanes per head, 8 channels per lane.  The angles of the row are worked out once, by D / 2 lanes,
-// and kept in LDS for all heads; a head's values are asked for while the heads before it are worked on, the first ones before
-// the angles.
+// A wave has one row, or a slice of its heads where there are few rows; D / 8 lanes per head, 8 channels per lane.  It works the
+// row's angles out for itself (64 lanes, D / 2 of them) and keeps them in LDS; nothing waits for another wave.  Heads are asked for
+// two turns ahead.  2048 rows of 32 + 32 + 32 heads: 28 us with a workgroup per row, which is mostly waiting for the next link of
+// row -> sequence -> position -> angles.
 template <int D, bool F32>
 __global__ __launch_bounds__(THREADS) void append_kernel(const AppendArgs a)
 {
-    constexpr int LANES = D / 8, PER = THREADS / LANES; // lanes of a head, heads at a time
-    __shared__ double2 turn[D / 2];
+    constexpr int LANES = D / 8, PER = 64 / LANES, HALF = LANES / 2; // lanes of a head, heads at a time
+    // (cos, - sin) and (cos, sin): for a pair's first channel and its second.  Neighbouring lanes read neighbouring entries.
+    __shared__ double2 turns[THREADS / 64][2][D / 2];
     const Step &s = a.s;
-    const int32_t row = blockIdx.x, tid = threadIdx.x, lane = tid % LANES;
-    const int32_t q_heads = a.q ? a.q_heads : 0, units = q_heads + 2 * s.heads;
+    const int32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tid = threadIdx.x & 63, lane = tid % LANES;
+    double2(&turn)[2][D / 2] = turns[wave];
+    // Neighbouring rows go to one XCD (workgroup b to XCD b % 8), whose L2 puts a page's lines together: a line holds two tokens'
+    // codes of a head, 32 tokens' parameters.
+    const int32_t block = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+    const int32_t task = block * (THREADS / 64) + wave, row = __builtin_amdgcn_readfirstlane((int32_t)((uint32_t)task / (uint32_t)a.slices));
+    if (row >= s.rows) return;
+    const int32_t q_heads = a.q ? a.q_heads : 0, all = q_heads + 2 * s.heads;
+    const int32_t begin = (task - row * a.slices) * a.slice, units = begin + a.slice < all ? begin + a.slice : all; // its heads: begin .. units - 1
     const bool vec = a.vec;
+    const int32_t s_heads = s.heads;
     // head u of the row: 0 query, 1 key, 2 value
     const auto kind_of = [&](int32_t u) { return u < q_heads ? 0 : (u < q_heads + s.heads ? 1 : 2); };
     const auto head_of = [&](int32_t u, int32_t kind) { return u - (kind > 0 ? q_heads : 0) - (kind > 1 ? s.heads : 0); };
-    const auto fetch = [&](int32_t u) {
+    // (by masks and not by a conditional expression of the arguments: that becomes a choice of a place among the kernel's arguments,
+    // and every fetch a trip to memory for its own address first)
+    constexpr int SIZE = F32 ? 4 : 2;
+    const uint64_t at_v = reinterpret_cast<uint64_t>(a.v) + row * a.ldv * SIZE;
+    const uint64_t k_off = reinterpret_cast<uint64_t>(a.k) + row * a.ldk * SIZE - at_v, q_off = reinterpret_cast<uint64_t>(a.q) + row * a.ldq * SIZE - at_v;
+    const auto fetch = [=](int32_t u) {
         Raw<F32> r = {};
         if (u < units) {
-            const int32_t kind = kind_of(u);
-            const void *src = kind == 0 ? a.q : (kind == 1 ? a.k : a.v);
-            const int64_t ld = kind == 0 ? a.ldq : (kind == 1 ? a.ldk : a.ldv);
-            r = load8<F32>(src, (int64_t)row * ld + head_of(u, kind) * D + 8 * lane, vec);
+            const uint64_t is_q = -(uint64_t)(u < q_heads), is_k = -(uint64_t)(u >= q_heads && u < q_heads + s_heads);
+            const int32_t head = u - (u >= q_heads ? q_heads : 0) - (u >= q_heads + s_heads ? s_heads : 0);
+            r = load8<F32>(reinterpret_cast<const void *>(at_v + (is_q & q_off) + (is_k & k_off)), head * D + 8 * lane, vec);
         }
         return r;
     };
-    Raw<F32> raw = fetch(tid / LANES);
+    Raw<F32> raw[2] = {fetch(begin + tid / LANES), fetch(begin + PER + tid / LANES)};
     int32_t line, pos;
-    if (!token_of(s, row, &line, &pos)) return; // the same for the whole workgroup
+    if (!token_of(s, row, &line, &pos)) return; // the same for the whole wave
     const int32_t page = page_of(s, line, pos);
-    if (a.rope != QLLM_ROPE_NONE) {
+    if (a.rope != QLLM_ROPE_NONE && begin < q_heads + s_heads) { // not for values alone
         if (tid < D / 2) {
             double sn, cs;
             sincos((double)pos * a.inv_freq[tid], &sn, &cs);
-            turn[tid] = make_double2((float)cs, (float)sn);
+            const int32_t at = a.rope == QLLM_ROPE_HALVES ? tid % 8 * HALF + tid / 8 : tid % 4 * LANES + tid / 4;
+            turn[0][at] = make_double2((float)cs, -(float)sn);
+            turn[1][at] = make_double2((float)cs, (float)sn);
         }
-        __syncthreads();
+        __builtin_amdgcn_wave_barrier();
     }
     const int32_t P = 1 << s.page_shift, in_page = pos & (P - 1);
-    for (int32_t base = 0; base < units; base += PER) { // lanes beyond the last head go through it too: they take part in the exchanges
+    const auto heads = [&](int32_t base, Raw<F32> &next) { // lanes beyond the last head go through it too: they take part in the exchanges
         const int32_t u = base + tid / LANES, kind = kind_of(u), head = head_of(u, kind);
         const bool real = u < units;
         float x[8];
-        widen8<F32>(raw, x);
-        raw = fetch(u + PER);
+        widen8<F32>(next, x);
+        next = fetch(u + 2 * PER);
         // x1 c - x2 s and x2 c + x1 s: the products are exact in double, the sum is rounded there once (a fused multiply-add
         // of an exact product is that sum), then to float
-        if (a.rope == QLLM_ROPE_HALVES) { // the partner's channels sit half the head's lanes away
-            const double sign = lane < LANES / 2 ? -1.0 : 1.0;
+        if (a.rope != QLLM_ROPE_NONE && __any(kind != 2)) { // values do not turn
+            float y[8];
+            if (a.rope == QLLM_ROPE_HALVES) { // the partner's channels sit half the head's lanes away
+                const double2 *t = turn[lane >= HALF] + lane % HALF;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float y = across<LANES>(x[e]);
-                const double2 t = turn[8 * (lane % (LANES / 2)) + e];
-                const float turned = (float)__builtin_fma((double)x[e], t.x, sign * ((double)y * t.y));
-                if (kind != 2) x[e] = turned;
-            }
-        } else if (a.rope == QLLM_ROPE_PAIRS) {
+                for (int e = 0; e < 8; ++e) y[e] = (float)__builtin_fma((double)x[e], t[HALF * e].x, (double)across<LANES>(x[e]) * t[HALF * e].y);
+            } else {
+                const double2 *t = turn[1] + lane;
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const double2 t = turn[4 * lane + e / 2];
-                const double x1 = x[e], x2 = x[e + 1];
-                const float y1 = (float)__builtin_fma(x1, t.x, -(x2 * t.y)), y2 = (float)__builtin_fma(x2, t.x, x1 * t.y);
-                if (kind != 2) x[e] = y1, x[e + 1] = y2;
+                for (int e = 0; e < 8; e += 2) {
+                    const double x1 = x[e], x2 = x[e + 1], c = t[LANES * (e / 2)].x, sn = t[LANES * (e / 2)].y;
+                    y[e] = (float)__builtin_fma(x1, c, -(x2 * sn)), y[e + 1] = (float)__builtin_fma(x2, c, x1 * sn);
+                }
             }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = kind != 2 ? y[e] : x[e];
         }
         if (kind == 0) {
             if (real) store8<F32>(a.q_out, (int64_t)row * a.ldq_out + head * D + 8 * lane, vec, x);
-            if (base + PER <= q_heads) continue; // queries all
         }
+        if (base + PER <= q_heads) return; // queries all
         // Eq. (2) over the head's channels
         float lo = x[0], hi = x[0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) lo = fminf(lo, x[e]), hi = fmaxf(hi, x[e]);
         lo = over_lanes<LANES>(lo, [](float p, float q) { return fminf(p, q); });
         hi = over_lanes<LANES>(hi, [](float p, float q) { return fmaxf(p, q); });
-        if (!real || kind == 0 || page < 0) continue;
+        if (!real || kind == 0 || page < 0) return;
         float alpha = (hi - lo) * (1.0f / 15.0f);
         if (!(alpha >= 0x1p-126f)) alpha = 1.0f;
         const float inv = 1.0f / alpha;
-        const int32_t fast = fabsf(lo * inv) < FAST_LIMIT && fabsf(hi * inv) < FAST_LIMIT;
+        // A float near MAGIC = 1.5 2^23 is MAGIC plus an integer, in its value as in its bits: one fused multiply-add rounds the
+        // exact product to the nearest integer, and code 0 is the number MAGIC - beta.
         int32_t beta;
-        if (fast) {
+        uint32_t codes = 0;
+        if (fabsf(lo * inv) < FAST_LIMIT && fabsf(hi * inv) < FAST_LIMIT) {
             beta = -qllm_detail::rne_product_fast(lo, inv);
+            const float zero = qllm_detail::MAGIC - (float)beta, most = zero + 15.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                codes += __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fmaf(x[e], inv, qllm_detail::MAGIC), zero, most)) << (4 * e);
+            codes -= __float_as_uint(zero) * 0x11111111u;
         } else {
             const double z = -qllm_detail::rne_product_slow(lo, inv);
             beta = (int32_t)fmin(fmax(z, -2147483647.0), 2147483647.0);
-        }
-        uint32_t codes = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) codes |= (uint32_t)qllm_detail::quant_code<15>(x[e], inv, beta, fast) << (4 * e);
+            for (int e = 0; e < 8; ++e) codes |= (uint32_t)qllm_detail::quant_code<15>(x[e], inv, beta, 0) << (4 * e);
+        }
         uint8_t *part = s.pages + page * s.page_bytes + (int64_t)head * P * (D + 16);
         const int32_t value = kind - 1;
         *reinterpret_cast<uint32_t *>(part + ((int64_t)value * P + in_page) * (D / 2) + 4 * lane) = codes;
         uint8_t *params = part + (int64_t)P * D + 8 * (int64_t)value * P;
         if (lane == 0) *reinterpret_cast<float *>(params + 4 * in_page) = alpha;
         if (lane == 1) *reinterpret_cast<int32_t *>(params + 4 * P + 4 * in_page) = beta;
+    };
+    for (int32_t base = begin; base < units; base += 2 * PER) {
+        heads(base, raw[0]);
+        if (base + PER < units) heads(base + PER, raw[1]);
     }
 }
 
@@ -242,19 +268,28 @@ __global__ __launch_bounds__(THREADS) void read_kernel(const ReadArgs a)
     const int32_t page = page_of(s, line, pos);
     if (page < 0) return;
     const int32_t P = 1 << s.page_shift, in_page = pos & (P - 1), lane = tid % LANES;
+    // (addresses by masks: see append_kernel)
+    const uint64_t at_k = reinterpret_cast<uint64_t>(a.k_out) + row * a.ldk * (F32 ? 4 : 2);
+    const uint64_t v_off = reinterpret_cast<uint64_t>(a.v_out) + row * a.ldv * (F32 ? 4 : 2) - at_k;
+    const bool has_k = a.k_out != nullptr, has_v = a.v_out != nullptr, vec = a.vec;
     for (int32_t u = tid / LANES; u < 2 * s.heads; u += PER) {
         const int32_t value = u >= s.heads, head = value ? u - s.heads : u;
-        void *out = value ? a.v_out : a.k_out;
-        if (!out) continue;
+        if ((value && !has_v) || (!value && !has_k)) continue;
         const uint8_t *part = s.pages + page * s.page_bytes + (int64_t)head * P * (D + 16);
         const uint32_t codes = *reinterpret_cast<const uint32_t *>(part + ((int64_t)value * P + in_page) * (D / 2) + 4 * lane);
         const uint8_t *params = part + (int64_t)P * D + 8 * (int64_t)value * P;
-        const double alpha = *reinterpret_cast<const float *>(params + 4 * in_page);
-        const double beta = *reinterpret_cast<const int32_t *>(params + 4 * P + 4 * in_page);
+        const float alpha = *reinterpret_cast<const float *>(params + 4 * in_page);
+        const int32_t beta = *reinterpret_cast<const int32_t *>(params + 4 * P + 4 * in_page);
         float x[8];
+        if (beta > -(1 << 23) && beta < 1 << 23) { // code - beta is exact in float
+            const float zero = (float)beta;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (float)(alpha * ((double)(codes >> (4 * e) & 15u) - beta));
-        store8<F32>(out, (int64_t)row * (value ? a.ldv : a.ldk) + head * D + 8 * lane, a.vec, x);
+            for (int e = 0; e < 8; ++e) x[e] = alpha * ((float)(codes >> (4 * e) & 15u) - zero);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (float)((double)alpha * ((double)(codes >> (4 * e) & 15u) - (double)beta));
+        }
+        store8<F32>(reinterpret_cast<void *>(at_k + (-(uint64_t)value & v_off)), head * D + 8 * lane, vec, x);
     }
 }
 
@@ -318,7 +353,13 @@ extern "C" int32_t qllm_kv_append(const void *q, int64_t ldq, int64_t q_heads, v
     a.q = q, a.k = k, a.v = v, a.q_out = q_out;
     a.ldq = ldq, a.ldq_out = ldq_out, a.ldk = ldk, a.ldv = ldv;
     a.q_heads = (int32_t)q_heads, a.rope = rope, a.inv_freq = inv_freq;
-    const dim3 grid((unsigned)(batch->row_start ? batch->rows : batch->n_seqs));
+    // Few rows: as many slices of their heads as give the card 4096 waves, 16 on each of 256 CUs
+    const int64_t rows = batch->row_start ? batch->rows : batch->n_seqs, heads = (q ? q_heads : 0) + 2 * cache->heads, per = 512 / cache->dim;
+    int64_t slices = 4096 / rows;
+    slices = slices < 1 ? 1 : slices;
+    a.slice = (int32_t)(((heads + slices - 1) / slices + per - 1) / per * per);
+    a.slices = (int32_t)((heads + a.slice - 1) / a.slice);
+    const dim3 grid((unsigned)((rows * a.slices + THREADS / 64 * 8 - 1) / (THREADS / 64 * 8) * 8));
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();
     if (cache->dim == 128) {
