@@ -542,12 +542,18 @@ int32_t check(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_
     return QLLM_OK;
 }
 
-// Whether the prompts kernel takes sequences of more than FEW_ROWS rows: its tiles of 128 rows have to keep most of the card busy.
-constexpr int32_t FEW_ROWS = 64;
+// Whether the prompts kernel takes sequences of more than FEW_ROWS rows.  Its time is that of one workgroup's way through the
+// tokens until two of them are on each CU, this one's grows with every 16 rows, from some 25 us.  D 128, us, this kernel's first:
+//   rows x kv heads x tokens of one sequence: 1024 x 8 x 4000 59 and 118 (64 workgroups), 2048 93 and 119, 4096 167 and 120;
+//     128 x 32 x 128 31 and 16, 256 x 32 x 256 24 and 19, 512 x 32 x 512 35 and 26: few tokens take few workgroups;
+//   sequences x their rows, 8 kv heads, 2000 tokens: 32 x 64 68 and 78, 32 x 128 114 and 69; 32 kv heads, 1000 tokens:
+//     16 x 32 50 and 41, 16 x 64 78 and 48.
+// Where sequences are of few rows on the average this kernel alone saves the other's launch.
+constexpr int32_t FEW_ROWS = 32;
 bool prompts_pay(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads, int32_t q_dtype)
 {
-    const int64_t rows = batch->rows * (q_heads / cache->heads);
-    return q_dtype == QLLM_BF16 && batch->row_start && rows / 128 * cache->heads >= 128 && rows > batch->n_seqs * FEW_ROWS / 4;
+    const int64_t rows = batch->rows * (q_heads / cache->heads), workgroups = rows / 128 * cache->heads, tokens = batch->table_ld * cache->page_tokens;
+    return q_dtype == QLLM_BF16 && batch->row_start && workgroups >= (tokens < 1280 ? tokens / 8 : 160) && rows > batch->n_seqs * FEW_ROWS / 2;
 }
 
 // Workgroups of a kv head: as many as the card holds at once (three on each of 256 CUs), but none for less than LEAST steps.
