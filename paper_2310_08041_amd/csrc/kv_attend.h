@@ -40,7 +40,7 @@ struct AttendArgs {
     int64_t ldq, ldo;
     int32_t q_heads, group, window; // window 0: none
     float scale2;                   // scale * log2 e
-    int32_t q_vec, out_vec;         // bf16 queries in 16-byte pieces; four outputs at a time
+    int32_t q_vec, out_vec;         // queries in 16-byte pieces; four outputs at a time
     qllm_detail::QuotientBy by_group; // for numbers below group + 128
     int32_t blocks;                 // workgroups of a kv head
     float *part_o;                  // their partial results, see partial_at

@@ -12,11 +12,14 @@ namespace {
 using namespace qllm_kv_detail;
 
 constexpr int ROWS = 16, STEP = 32, WAVES = 4; // rows of a tile, tokens of a step, waves of a workgroup
-// The work of a kv head is one long line of steps: sequence after sequence, tile after tile, `steps` of 32 tokens for each tile
-// (what its sequence's rows see together; at least one, for rows that see nothing get their zeros too).  The workgroups of the
-// head share the line out evenly, whatever the lengths: one may end in the middle of a tile and the next go on there.
+// The work of a kv head is one long line of steps: sequence after sequence, tile after tile, `steps` for each tile: first BESIDE
+// empty ones, the time that a tile takes whatever its length (its queries, the first loads, the waves' results put together), then
+// one for every 32 tokens (of what its sequence's rows see together).  The workgroups of the head share the line out evenly,
+// whatever the lengths: one may end in the middle of a tile and the next go on there.  (Chunks of 0 to 260 rows mixed with single
+// tokens, float32, BESIDE 0, 4, 8, 16: 55, 52, 46, 48 us; single tokens behind 3000 to 20000: no difference.)
+constexpr int BESIDE = 8;
 struct Work {
-    int32_t tiles, first, steps; // of a sequence; its first step is number `first` of the cache line
+    int32_t tiles, first, steps; // of a sequence; its first step with tokens is number `first` of the cache line
 };
 
 __device__ __forceinline__ Work work_of(const AttendArgs &a, const Seq &q)
@@ -26,7 +29,7 @@ __device__ __forceinline__ Work work_of(const AttendArgs &a, const Seq &q)
     w.tiles = rows > a.few ? 0 : (int32_t)(((uint32_t)rows + ROWS - 1) / ROWS);
     const int32_t lo = lo_at(a, q.len - q.n), hi = hi_at(limit_of(a, q), q.len - 1);
     w.first = lo / STEP;
-    w.steps = hi < lo ? 1 : hi / STEP + 1 - w.first;
+    w.steps = BESIDE + (hi < lo ? 0 : hi / STEP + 1 - w.first);
     return w;
 }
 
@@ -91,8 +94,9 @@ struct Line {
 };
 
 // How many workgroups share the line (none gets less than LEAST steps while another has some), and where share b begins: any
-// rising function of b that all workgroups evaluate alike will do, so one product in double does.
-constexpr int LEAST = 16;
+// rising function of b that all workgroups evaluate alike will do, so one product in double does.  LEAST 16, 24, 32 for one
+// token behind 480: 17, 12, 12 us (one workgroup a head needs no join); sixteen behind 500: 21, 15, 21; behind 4000: 18, 17, 18.
+constexpr int LEAST = 24;
 struct Shares {
     int32_t total, of;
     double each;
@@ -217,8 +221,8 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
     t.first = number * ROWS, t.rows = t.seq.n * a.group;
     const int32_t tok0 = (int32_t)((uint32_t)t.first / (uint32_t)a.group), head0 = t.first - tok0 * a.group; // of the tile's first row
     const Sight v = sight_of(a, t, tok0, head0, ROWS);
-    const int32_t step_begin = work_here.first + skip;
-    const int32_t step_end = v.all_hi < 0 || step_begin + take <= v.all_hi / STEP + 1 ? step_begin + take : v.all_hi / STEP + 1;
+    const int32_t step_begin = work_here.first + (skip > BESIDE ? skip - BESIDE : 0), last = work_here.first + skip + take - BESIDE;
+    const int32_t step_end = v.all_hi < 0 || last <= v.all_hi / STEP + 1 ? last : v.all_hi / STEP + 1;
     const bool whole = take == work_here.steps;
     const int32_t slot = at == begin ? 0 : 1;
     if (skip == 0 && threadIdx.x == 0 && a.numbers) // numbers 0: every workgroup finishes what it begins
@@ -264,8 +268,17 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
             for (int k = 0; k < KS; ++k) {
                 float x[8], part[8][PARTS];
 #pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+                if (F32Q && real && a.q_vec) {
+                    const float4 *src = reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + from + 8 * k);
+                    const float4 w = src[0], y = src[1];
+                    x[0] = w.x, x[1] = y.x, x[2] = w.y, x[3] = y.y, x[4] = w.z, x[5] = y.z, x[6] = w.w, x[7] = y.w;
+                } else if (real) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = load1<F32Q>(a.q, from + 8 * k + (e >> 1) + 4 * (e & 1));
+                }
+#pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    x[e] = real ? load1<F32Q>(a.q, from + 8 * k + (e >> 1) + 4 * (e & 1)) : 0.0f;
                     qsum += x[e];
                     split<PARTS>(x[e], part[e]);
                 }
@@ -538,7 +551,7 @@ int32_t check(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_
 {
     if (q_heads <= 0 || q_heads > (1 << 15) || q_heads % cache->heads) return QLLM_ERR_SHAPE;
     const int64_t rows = batch->rows * (q_heads / cache->heads);
-    if (rows > INT32_MAX || (rows / ROWS + batch->n_seqs) * (batch->table_ld * cache->page_tokens / STEP) >= INT32_MAX) return QLLM_ERR_SHAPE;
+    if (rows > INT32_MAX || (rows / ROWS + batch->n_seqs) * (batch->table_ld * cache->page_tokens / STEP + BESIDE) >= INT32_MAX) return QLLM_ERR_SHAPE;
     return QLLM_OK;
 }
 
@@ -567,7 +580,7 @@ Launch plan(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_he
     const int64_t group = q_heads / cache->heads;
     Launch n;
     n.numbers = batch->row_start ? batch->rows * group / ROWS + batch->n_seqs : batch->n_seqs * ((group + ROWS - 1) / ROWS);
-    const int64_t most = n.numbers * (batch->table_ld * cache->page_tokens / STEP) / LEAST + 1; // below 2^31
+    const int64_t most = n.numbers * (batch->table_ld * cache->page_tokens / STEP + BESIDE) / LEAST + 1; // below 2^31
     const int64_t blocks = cache->heads < RESIDENT ? RESIDENT / cache->heads : 1;
     n.blocks = blocks < most ? blocks : most;
     n.marks = n.blocks > 1 ? cache->heads * n.numbers * (int64_t)sizeof(Unfinished) : 0;
@@ -607,7 +620,7 @@ extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq
     a.q = q, a.out = out, a.ldq = ldq, a.ldo = ldo;
     a.q_heads = (int32_t)q_heads, a.group = (int32_t)(q_heads / cache->heads);
     a.by_group = qllm_detail::quotient_by((uint32_t)a.group);
-    a.q_vec = q_dtype == QLLM_BF16 && ((reinterpret_cast<uintptr_t>(q) | (uintptr_t)(2 * ldq)) & 15u) == 0;
+    a.q_vec = ((reinterpret_cast<uintptr_t>(q) | (uintptr_t)(ldq * (q_dtype == QLLM_F32 ? 4 : 2))) & 15u) == 0;
     a.out_vec = ((reinterpret_cast<uintptr_t>(out) | (uintptr_t)(ldo * (out_dtype == QLLM_F32 ? 4 : 2))) & (out_dtype == QLLM_F32 ? 15u : 7u)) == 0;
     a.window = window > INT32_MAX ? 0 : (int32_t)window;
     a.scale2 = scale * LOG2E;
