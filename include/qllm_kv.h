@@ -42,6 +42,7 @@ int64_t qllm_kv_page_bytes(int64_t heads, int64_t dim, int64_t page_tokens);
  * or of a line outside the table in qllm_kv_append and qllm_kv_read) are left as they were; sequences may have no rows.
  * Position p of a line lies in page table[line][p / page_tokens]; a page number outside [0, n_pages), or a p beyond the line's
  * end, is "not there": nothing is written, and attention does not see the token.
+ * Limits: rows <= 2^24, n_seqs <= 2^20, table_ld * page_tokens < 2^31, n_pages < 2^31; the cache may be of any size.
  */
 typedef struct {
     int64_t rows;             /* rows of the step's tensors */
@@ -62,7 +63,7 @@ typedef enum {
 /* ------------------------------------------------------------------------------------------
  * Rotary positions on the step's queries and keys, Eq. (2) on its keys and values, codes into the sequences' pages.
  *   q        [rows, ldq], q_heads * dim columns; q_out [rows, ldq_out] receives the rotated queries (may be q itself with the
- *            same stride; must not overlap it otherwise).  Both NULL: keys and values only.
+ *            same stride; must not overlap it, k or v otherwise).  Both NULL: keys and values only.
  *   k, v     [rows, ldk], [rows, ldv], heads * dim columns; x_dtype (fp32 / bf16) for all four.
  *   inv_freq [dim / 2] double, angle per position (ignored, may be NULL, with QLLM_ROPE_NONE: q_out is then a copy).
  * Fixed arithmetic: a = p * inv_freq[d] in double, c = cos a and s = sin a rounded to float; x1' = x1 c - x2 s and
@@ -85,12 +86,16 @@ int32_t qllm_kv_read(const qllm_kv_cache *cache, const qllm_kv_batch *batch, voi
  * h / (q_heads / heads)).  A query at position p sees the tokens t <= p of its line that are there, with window > 0 only
  * t > p - window:
  *     out = sum_t e^(scale q.k_t) v_t / sum_t e^(scale q.k_t),   0 where nothing is seen.
- *   q        [rows, ldq] q_dtype, out [rows, ldo] out_dtype (fp32 / bf16), q_heads * dim columns.
+ *   q        [rows, ldq] q_dtype, out [rows, ldo] out_dtype (fp32 / bf16), q_heads * dim columns.  out may be q itself (one
+ *            type, one stride); must not overlap it otherwise.  q_heads <= 2^15, and with G = q_heads / heads: rows * G < 2^31 and
+ *            (rows * G / 16 + n_seqs) * (table_ld * page_tokens / 32 + 8) < 2^31.
  *   workspace  16-byte aligned, qllm_kv_attention_workspace_bytes(cache, batch, q_heads) bytes (read on the host: of the
  *            two structs only the sizes); contents undefined afterwards, two calls in flight at once need one each.
- * Codes enter the matrix cores as exact bf16 integers; scores, maxima and sums are fp32; with bf16 queries the weights are
- * rounded to bf16 once before they meet the values (half a step: 2^-8 of each at most), with fp32 queries both are
- * taken in three bf16 parts, 24 bits.  Errors: NULL / SHAPE / DTYPE / ALIGN / WORKSPACE / HIP.  rows == 0 or n_seqs == 0: no-op.
+ * Equal calls give equal bits.
+ * Codes enter the matrix cores as exact bf16 integers; scores, maxima and sums are fp32; with bf16 queries the weights (times a
+ * value's alpha) are rounded to bf16 once before they meet the values (half a step: 2^-8 of each at most; in sequences of many
+ * rows the same rounded weights are what is summed below the line), with fp32 queries queries and weights are taken in three
+ * bf16 parts, 24 bits.  A query that is not finite spoils its own row and head alone.  Errors: NULL / SHAPE / DTYPE / ALIGN / WORKSPACE / HIP.  rows == 0 or n_seqs == 0: no-op.
  */
 int64_t qllm_kv_attention_workspace_bytes(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads);
 int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq, int64_t q_heads, const qllm_kv_cache *cache,

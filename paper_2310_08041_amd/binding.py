@@ -724,6 +724,7 @@ class DeviceKVCache:
     def __init__(self, layers, n_pages, heads, dim, page_tokens, pages=None, device="cuda"):
         self.page_bytes = qllm_kv_page_bytes(heads, dim, page_tokens)
         self.layers, self.n_pages, self.heads, self.dim, self.page_tokens = int(layers), int(n_pages), int(heads), int(dim), int(page_tokens)
+        _need(self.layers > 0 and self.n_pages > 0, f"a cache of {self.layers} layers and {self.n_pages} pages")
         if pages is None:
             pages = torch.zeros((self.layers, self.n_pages, self.page_bytes), dtype=torch.uint8, device=device)
         _check_tensor(pages, "pages", _U8_ONLY, shape=(self.layers, self.n_pages, self.page_bytes))

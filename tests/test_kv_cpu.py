@@ -142,6 +142,12 @@ def test_wrappers_refuse_mismatched_tensors():
             call()
 
 
+@pytest.mark.parametrize("layers,n_pages", [(0, 5), (-1, 5), (2, 0)])
+def test_a_cache_without_layers_or_pages_is_refused(layers, n_pages):
+    with pytest.raises(ValueError, match="a cache of"):
+        b.DeviceKVCache(layers, n_pages, 2, 64, 32, device="cpu")
+
+
 def test_wrappers_refuse_tensors_of_another_device(monkeypatch):
     """A tensor of a device that is not the current one is refused (devices are pretended: there is none here)."""
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)

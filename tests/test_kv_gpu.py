@@ -517,3 +517,159 @@ def test_empty_steps_are_no_ops(b):
         b.qllm_kv_read(cache, 0, batch, x)
         b.qllm_kv_attention(x, cache, 0, batch, 1.0, x, ws)
         assert (x == 2.0).all() and not cache.pages.any()
+
+
+@pytest.mark.parametrize("q_type,group,new,slots", [("bf16", 3, True, True), ("f32", 1, True, False), ("bf16", 8, False, True), ("bf16", 1, False, False)])
+def test_attention_of_more_sequences_than_a_wave_has_lanes(oracle, b, q_type, group, new, slots):
+    """Two hundred sequences, some without rows, some without tokens, their lines in any order."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(31 + group)
+    n = 200
+    lengths = rng.integers(0, 60, n)
+    lengths[77] = 700
+    n_new = np.minimum(rng.integers(0, 4, n), lengths).tolist() if new else None
+    c = make(rng, 1, group, 64, 32, lengths.tolist(), n_new, slots=rng.permutation(n).tolist() if slots else None, n_lines=n if slots else None)
+    q = rng.standard_normal((c.rows, group, 64)).astype(np.float32)
+    q = _bf16(q) if q_type == "bf16" else q
+    cache, batch = on_device(b, c)
+    out = torch.full((c.rows, group * 64), 5.0, device="cuda")
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, group), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), torch.bfloat16 if q_type == "bf16" else torch.float32), cache, 0, batch, 0.125, out, ws)
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.125))
+    worst = np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, q_type, "f32")
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+def test_attention_of_many_sequences_over_one_shared_line(oracle, b):
+    """Hundreds of sequences continue one long line: a wave has more steps of a sequence than it has lanes, twice over."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(32)
+    n, tokens, group = 1500, 9000, 2
+    c = make(rng, 1, group, 64, 64, [tokens], None)
+    table = np.repeat(c.table, n, 0)
+    length = np.full(n, tokens, np.int32)
+    length[::3] -= rng.integers(0, 3000, 500).astype(np.int32)
+    cache = b.DeviceKVCache(1, c.n_pages, 1, 64, 64, pages=_t(c.pages.raw)[None])
+    batch = b.DeviceKVBatch(n, _t(table), _t(length))
+    q = _bf16(rng.standard_normal((n, group, 64)).astype(np.float32))
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, group), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    out = torch.empty((n, group * 64), device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(n, -1), torch.bfloat16), cache, 0, batch, 0.125, out, ws)
+    some = [(r, 0, int(length[r]) - 1) for r in range(0, n, 31)]
+    want, *bounds = okv.attention(q, c.pages, c.table, some, c.length, np.float32(0.125))
+    rows = [r for r, _, _ in some]
+    worst = (np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, "bf16", "f32"))[rows]
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+@pytest.mark.parametrize("lengths,new,window", [([2500], [130], 0), ([2300, 40], [140, 3], 0), ([2200], [2200], 2100)])
+def test_attention_of_prompts_behind_many_tokens(oracle, b, lengths, new, window):
+    """More tokens than a wave keeps page numbers of at a time."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(33)
+    heads, group = 2, 256 if window == 0 else 16
+    c = make(rng, heads, group, 64, 32, lengths, new)
+    hq = heads * group
+    if window:                                                # the prompt's last rows are enough to look at
+        c.tokens = c.tokens[-40:]
+    q = _bf16(rng.standard_normal((c.rows, hq, 64)).astype(np.float32))
+    cache, batch = on_device(b, c)
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, hq), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    out = torch.empty((c.rows, hq * 64), dtype=torch.bfloat16, device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), torch.bfloat16), cache, 0, batch, 0.125, out, ws, window=window)
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.125), window)
+    rows = sorted({r for r, _, _ in c.tokens})
+    worst = (np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, "bf16", "bf16"))[rows]
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 1e-30, 3.0])
+@pytest.mark.parametrize("heads,lengths,new", [(1, [300, 20], [3, 20]), (24, [200], [180])])
+def test_attention_with_scales_of_any_sign_and_size(oracle, b, heads, lengths, new, scale):
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(34)
+    c = make(rng, heads, 4, 128, 64, lengths, new)
+    q = _bf16(0.3 * rng.standard_normal((c.rows, heads * 4, 128)).astype(np.float32))
+    cache, batch = on_device(b, c)
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * 4), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    out = torch.empty((c.rows, heads * 512), device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), torch.bfloat16), cache, 0, batch, scale, out, ws)
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(scale))
+    worst = np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, "bf16", "f32")
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+@pytest.mark.parametrize("heads,group,lengths,new", [(2, 4, [900, 40], None), (16, 8, [300], [200]), (16, 2, [300, 70], [260, 1])])
+def test_attention_writes_over_its_queries_and_keeps_rows_apart(oracle, b, heads, group, lengths, new):
+    """out may be q; a query that is not finite spoils its own output alone."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(35)
+    c = make(rng, heads, group, 128, 64, lengths, new)
+    cache, batch = on_device(b, c)
+    x = _bf16(rng.standard_normal((c.rows, heads * group, 128)).astype(np.float32))
+    q = _t(x.reshape(c.rows, -1), torch.bfloat16)
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda")
+    out = b.qllm_kv_attention(q, cache, 0, batch, 0.1, torch.empty_like(q), ws)
+    over = q.clone()
+    b.qllm_kv_attention(over, cache, 0, batch, 0.1, over, ws)
+    assert torch.equal(over, out)
+    at = c.rows // 2
+    q[at, 128] = float("nan")                                # query head 1
+    q[at, 5 * 128] = float("inf")                            # and 5
+    got = b.qllm_kv_attention(q, cache, 0, batch, 0.1, torch.empty_like(q), ws).double().cpu().numpy().reshape(x.shape)
+    want, *bounds = okv.attention(x, c.pages, c.table, c.tokens, c.length, np.float32(0.1))
+    off = np.abs(got - want) / tolerance(want, *bounds, "bf16", "bf16")
+    assert np.isnan(got[at, 1]).all()
+    off[at, [1, 5]] = 0.0
+    assert off.max() <= 1.0, (off.max(), np.unravel_index(off.argmax(), off.shape))
+
+
+def test_chunks_of_a_prompt_replayed_as_a_graph_on_another_stream(oracle, b):
+    """A prompt in chunks of 200 rows beside single tokens, captured on a stream of its own: lengths and rows change between the
+    replays, other work runs in between, a second graph shares the workspace."""
+    import torch
+    rng = np.random.default_rng(36)
+    heads, group, dim, page = 16, 8, 64, 32
+    hq = heads * group
+    c = make(rng, heads, group, dim, page, [200, 50, 33], [200, 1, 1], extra_cols=22, spare=80)
+    free = np.setdiff1d(np.arange(c.n_pages), c.table[c.table >= 0])
+    c.table[c.table < 0] = free[:(c.table < 0).sum()]
+    cache, batch = on_device(b, c)
+    eager, ebatch = on_device(b, c)
+    f = _t(10000.0 ** (-np.arange(0, dim, 2) / dim))
+    x = torch.zeros((c.rows, (hq + 2 * heads) * dim), dtype=torch.bfloat16, device="cuda")
+    q, k, v = x.split([hq * dim, heads * dim, heads * dim], 1)
+    q_out, out, q2, o2 = (torch.zeros((c.rows, hq * dim), dtype=torch.bfloat16, device="cuda") for _ in range(4))
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, hq), dtype=torch.uint8, device="cuda")
+
+    def step(ca, ba, qo, o):
+        b.qllm_kv_append(ca, 0, ba, k, v, q=q, q_out=qo, rope=2, inv_freq=f)
+        b.qllm_kv_attention(qo, ca, 0, ba, 0.125, o, ws)
+
+    fresh = lambda: x.copy_(_t(rng.standard_normal(x.shape).astype(np.float32)))
+    fresh()
+    step(cache, batch, q_out, out)                                            # loads the kernels before the capture
+    step(eager, ebatch, q2, o2)
+    torch.cuda.synchronize()
+    graphs, side = [], torch.cuda.Stream()
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            step(cache, batch, q_out, out)
+        graphs.append(g)
+    more = torch.tensor([200, 1, 1], dtype=torch.int32, device="cuda")
+    for i in range(3):
+        fresh()
+        batch.length.add_(more), ebatch.length.add_(more)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graphs[i % 2].replay()
+        torch.cuda.synchronize()
+        step(eager, ebatch, q2, o2)
+        (torch.randn(1000, device="cuda") * 2).sum().item()
+        assert torch.equal(q2, q_out) and torch.equal(o2, out) and torch.equal(cache.pages, eager.pages)
