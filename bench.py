@@ -118,6 +118,90 @@ def bench_swiglu(args, w, dev):
     return 0 if result.get("parity_checked", {"ok": True})["ok"] else 1
 
 
+def bench_kv(args, dev):
+    """The cache beside the layers: one decoding step of --sequences lines of --context tokens, --heads query heads on --kv-heads
+    key/value heads of 128 channels, bfloat16.  A step = qllm_kv_append (rotary positions, the new tokens' keys and values as
+    4-bit codes) and qllm_kv_attention over all of the codes; 144 bytes per token and head against HBM."""
+    import numpy as np
+    import torch
+
+    from paper_2310_08041_amd import binding as b
+
+    hq, hk, dim, page, n, ctx = args.heads, args.kv_heads, 128, 64, args.sequences, args.context
+    per_line = -(-ctx // page)
+    one = n * per_line * b.qllm_kv_page_bytes(hk, dim, page)
+    layers = max(2, min(32, -(-(768 << 20) // one)))                               # past the last-level cache
+    g = torch.Generator(device=dev).manual_seed(2310)
+    cache = b.DeviceKVCache(layers, n * per_line, hk, dim, page)
+    table = torch.randperm(n * per_line, device=dev, generator=g).to(torch.int32).view(n, per_line).contiguous()
+    inv_freq = 10000.0 ** (-torch.arange(0, dim, 2, dtype=torch.float64, device=dev) / dim)
+    chunk = 1024
+    for at in range(0, ctx, chunk):                                                # the contexts, chunk by chunk, the same in every layer
+        m = min(chunk, ctx - at)
+        rows = torch.arange(0, n * m + 1, m, dtype=torch.int32, device=dev)
+        batch = b.DeviceKVBatch(n * m, table, torch.full((n,), at + m, dtype=torch.int32, device=dev), rows)
+        k, v = (torch.randn((n * m, hk * dim), device=dev, generator=g).to(torch.bfloat16) for _ in range(2))
+        b.qllm_kv_append(cache, 0, batch, k, v, rope=b.ROPE_HALVES, inv_freq=inv_freq)
+    cache.pages[1:] = cache.pages[0]
+    batch = b.DeviceKVBatch(n, table, torch.full((n,), ctx, dtype=torch.int32, device=dev))
+    qkv = torch.randn((n, (hq + 2 * hk) * dim), device=dev, generator=g).to(torch.bfloat16)
+    q, k, v = qkv.split([hq * dim, hk * dim, hk * dim], 1)
+    turned, out = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty((n, hq * dim), dtype=torch.bfloat16, device=dev)
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, hq), dtype=torch.uint8, device=dev)
+    scale = dim ** -0.5
+
+    def step(i):
+        b.qllm_kv_append(cache, i % layers, batch, k, v, q=q, q_out=turned, rope=b.ROPE_HALVES, inv_freq=inv_freq)
+        b.qllm_kv_attention(turned, cache, i % layers, batch, scale, out, ws)
+
+    ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+    warm_ms, warm_steps = 0.0, 0
+    while warm_steps < args.warmup or warm_ms < MIN_WARMUP_MS:
+        ev[0].record()
+        for i in range(64):
+            step(i)
+        ev[1].record()
+        torch.cuda.synchronize()
+        warm_steps += 64
+        warm_ms += ev[0].elapsed_time(ev[1])
+    t0 = time.perf_counter()
+    for i in range(args.steps):
+        step(i)
+    torch.cuda.synchronize()
+    wall = time.perf_counter() - t0
+    ev[0].record()
+    for i in range(args.steps):
+        b.qllm_kv_attention(turned, cache, i % layers, batch, scale, out, ws)
+    ev[1].record()
+    torch.cuda.synchronize()
+    t_attend = ev[0].elapsed_time(ev[1]) * 1e-3 / args.steps
+    nbytes = float(n * ctx * hk * (dim + 16))
+    result = {
+        "metric": "decoding step over the 4-bit key/value cache (append + attention), GB/s of codes read", "value": nbytes / (wall / args.steps) / 1e9,
+        "unit": "GB/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": wall * 1e3 / args.steps,
+        "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
+        "dtype": "bf16 (4-bit codes, fp32 scores and sums)", "data": "synthetic",
+        "config": {"sequences": n, "context": ctx, "heads": hq, "kv_heads": hk, "dim": dim, "page_tokens": page, "layers": layers,
+                   "warmup_done": {"steps": warm_steps, "gpu_ms": warm_ms}},
+        "roofline": {"kernel": "attend_kernel + join_kernel", "bound": "hbm", "achieved": nbytes / t_attend / 1e9, "peak": HBM_PEAK_GBS, "unit": "GB/s",
+                     "frac": nbytes / t_attend / 1e9 / HBM_PEAK_GBS, "avg_launch_us": t_attend * 1e6, "algorithmic_bytes": nbytes, "traffic": None},
+    }
+    if not args.no_cpu_baseline:
+        from oracle import kv_cache as okv
+        last = n - 1                                                               # one sequence of the batch
+        raw = cache.pages[(args.steps - 1) % layers][table[last].long()].cpu().numpy()
+        x = turned[last:].float().cpu().numpy().reshape(1, hq, dim)
+        t1 = time.perf_counter()
+        want, *bounds = okv.attention(x, okv.Pages(raw, hk, dim, page), np.arange(per_line, dtype=np.int32)[None], [(0, 0, ctx - 1)], np.array([ctx]), np.float32(scale))
+        cpu_s = time.perf_counter() - t1
+        off = np.abs(out[last:].double().cpu().numpy().reshape(want.shape) - want) / okv.attention_bound(want, *bounds, 2.0 ** -8, 2.0 ** -8)
+        result["cpu_baseline"] = {"value": ctx * hk * (dim + 16.0) / cpu_s / 1e9, "unit": "GB/s", "cores": 1, "kind": "oracle",
+                                  "sample": f"attention of one sequence of {n}, {cpu_s:.1f} s"}
+        result["parity_checked"] = {"rows": 1, "largest_share_of_the_bound": float(off.max()), "ok": bool(off.max() <= 1.0)}
+    print(json.dumps(result))
+    return 0 if result.get("parity_checked", {"ok": True})["ok"] else 1
+
+
 def bench_matching(args, w, norm, dev):
     """The step before the path: Appendix A steps 1-2 with the distance of Eq. (5) for the workload's
     layer, 256 calibration tokens.  A step = one qllm_match_nearest call (norms + nearest-member search)."""
@@ -251,10 +335,15 @@ def main():
                     help="expansion ratio that fixes theta (Sec. 5.2 varies it up to 0.1); default: the workload's own")
     ap.add_argument("--allow-map-walk", action="store_true",
                     help="do not stop when the fused kernel would fall back to walking the map's CSR rows")
-    ap.add_argument("--stage", default="layer", choices=["layer", "match", "swiglu"],
+    ap.add_argument("--stage", default="layer", choices=["layer", "match", "swiglu", "kv"],
                     help="layer: the hot path (the default, the line the contract asks for); match: the offline "
                          "channel matching of Eq. (5) / Appendix A at the workload's channel count; swiglu: the "
-                         "producer of a down projection's input, silu(gate) * up, at the workload's N x C")
+                         "producer of a down projection's input, silu(gate) * up, at the workload's N x C; kv: a decoding "
+                         "step over the 4-bit key/value cache, sized by the next four")
+    ap.add_argument("--sequences", type=int, default=16)
+    ap.add_argument("--context", type=int, default=16000)
+    ap.add_argument("--heads", type=int, default=64)
+    ap.add_argument("--kv-heads", type=int, default=8)
     args = ap.parse_args()
     if args.gpus != 1 or int(os.environ.get("WORLD_SIZE", "1")) != 1:
         sys.exit("bench.py: this build runs on one GPU only (the path shards over tokens with no "
@@ -282,6 +371,8 @@ def main():
         return bench_matching(args, w, norm, dev)
     if args.stage == "swiglu":
         return bench_swiglu(args, w, dev)
+    if args.stage == "kv":
+        return bench_kv(args, dev)
 
     # ---- synthetic inputs, resident in HBM before anything is timed
     t0 = time.time()

@@ -137,6 +137,12 @@ def attention(q, pages, table, tokens, length, scale, window=0, out=None):
     return out, absv, err_s, err_o
 
 
+def attention_bound(want, absv, err_s, err_o, q_half, out_half):
+    """How far an output may be off: its own rounding (half a step `out_half`), that of each weight to the queries' type (`q_half`)
+    above and below the line, and what `attention` says of the scores' and the sums' fp32 errors."""
+    return (out_half * (np.abs(want) + q_half * absv) + q_half * (absv + np.abs(want))) * (1 + 2.0 ** -7) + 2.0 * np.expm1(err_s) * absv + 2.0 * err_o + 1e-30
+
+
 class Book:
     """Lines as Python lists of pages."""
 
