@@ -87,8 +87,8 @@ int32_t qllm_kv_read(const qllm_kv_cache *cache, const qllm_kv_batch *batch, voi
  * t > p - window:
  *     out = sum_t e^(scale q.k_t) v_t / sum_t e^(scale q.k_t),   0 where nothing is seen.
  *   q        [rows, ldq] q_dtype, out [rows, ldo] out_dtype (fp32 / bf16), q_heads * dim columns.  out may be q itself (one
- *            type, one stride); must not overlap it otherwise.  q_heads <= 2^15, and with G = q_heads / heads: rows * G < 2^31 and
- *            (rows * G / 16 + n_seqs) * (table_ld * page_tokens / 32 + 8) < 2^31.
+ *            type, one stride); must not overlap it otherwise.  q_heads <= 2^15, and with G = q_heads / heads: tiles = rows * G / 16 +
+ *            n_seqs < 2^23 and tiles * (table_ld * page_tokens / 32 + 8) < 2^31.
  *   workspace  16-byte aligned, qllm_kv_attention_workspace_bytes(cache, batch, q_heads) bytes (read on the host: of the
  *            two structs only the sizes); contents undefined afterwards, two calls in flight at once need one each.
  * Equal calls give equal bits.

@@ -551,22 +551,22 @@ int32_t check(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_
 {
     if (q_heads <= 0 || q_heads > (1 << 15) || q_heads % cache->heads) return QLLM_ERR_SHAPE;
     const int64_t rows = batch->rows * (q_heads / cache->heads);
-    if (rows > INT32_MAX || (rows / ROWS + batch->n_seqs) * (batch->table_ld * cache->page_tokens / STEP + BESIDE) >= INT32_MAX) return QLLM_ERR_SHAPE;
-    return QLLM_OK;
+    const int64_t tiles = rows / ROWS + batch->n_seqs, steps = batch->table_ld * cache->page_tokens / STEP + BESIDE;
+    return tiles < (1 << 23) && tiles * steps < INT32_MAX ? QLLM_OK : QLLM_ERR_SHAPE; // (a grid of tiles has less than 2^32 threads)
 }
 
-// Whether the prompts kernel takes sequences of more than FEW_ROWS rows.  Its time is that of one workgroup's way through the
-// tokens until two of them are on each CU, this one's grows with every 16 rows, from some 25 us.  D 128, us, this kernel's first:
-//   rows x kv heads x tokens of one sequence: 1024 x 8 x 4000 59 and 118 (64 workgroups), 2048 93 and 119, 4096 167 and 120;
-//     128 x 32 x 128 31 and 16, 256 x 32 x 256 24 and 19, 512 x 32 x 512 35 and 26: few tokens take few workgroups;
-//   sequences x their rows, 8 kv heads, 2000 tokens: 32 x 64 68 and 78, 32 x 128 114 and 69; 32 kv heads, 1000 tokens:
-//     16 x 32 50 and 41, 16 x 64 78 and 48.
-// Where sequences are of few rows on the average this kernel alone saves the other's launch.
+// Whether the prompts kernel takes sequences of more than FEW_ROWS rows.  Up to 256 workgroups its time is that of one way through
+// the tokens, some 12 us and 17 more for every 1000 (D 128); this kernel's some 22 us and 0.14 for every workgroup of the other and
+// 1000 tokens.  One sequence, rows x kv heads x tokens, this kernel's us first: 512 x 8 x 1000 29 and 30, 1024 x 8 x 1000 36 and 30,
+// 512 x 8 x 4000 37 and 79, 1600 x 8 x 4000 78 and 80, 2048 x 8 x 4000 92 and 80, 2048 x 8 x 16000 287 and 275, 64 x 32 x 64 20 and 14,
+// 1024 x 8 x 300 26 and 20.  Sequences x their rows, 8 heads, 2000 tokens: 32 x 32 46 and 45, 32 x 64 68 and 47, 32 x 128 114 and 51
+// (and some 7 us for this kernel, which finds nothing to do).  (Grids of 2^32 threads and more are refused by the runtime.)
 constexpr int32_t FEW_ROWS = 32;
 bool prompts_pay(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads, int32_t q_dtype)
 {
     const int64_t rows = batch->rows * (q_heads / cache->heads), workgroups = rows / 128 * cache->heads, tokens = batch->table_ld * cache->page_tokens;
-    return q_dtype == QLLM_BF16 && batch->row_start && workgroups >= (tokens < 1280 ? tokens / 8 : 160) && rows > batch->n_seqs * FEW_ROWS / 2;
+    return q_dtype == QLLM_BF16 && batch->row_start && (120 - workgroups) * tokens <= 72000 && rows > batch->n_seqs * FEW_ROWS &&
+           (rows / 128 + batch->n_seqs) * cache->heads < (1 << 24);
 }
 
 // Workgroups of a kv head: as many as the card holds at once (three on each of 256 CUs), but none for less than LEAST steps.

@@ -11,6 +11,12 @@
 //   - one product more per 16 tokens, shared by all channels, has - (16 + beta) of the values in its rows 0..2 (in parts) and
 //     1 / alpha_v in the next ones: the zero points' share of the values' sums, and the sum of the weights.
 // The zero points' sums are added to the others every few tiles, so that the two stay small and lose nothing to each other.
+//
+// Two workgroups share a CU, so that one lays out while the other multiplies.  A launch of no more workgroups than the card holds
+// leaves CUs with one, or with a long and a short one: there a workgroup has two groups of four waves, every other tile of tokens
+// each, each with its own LDS, one of them half a turn behind, and joins their results at the end.  D 128, us, one group first:
+// 2048 tokens x 32 heads 72 and 58, 1024 x 32 40 and 32, 512 rows behind 3500 tokens x 8 heads of 8 117 and 80, 4 x 100 behind
+// 16000 430 and 284; more workgroups, 4096 x 32 171 and 182, 8 x 512 x 32 67 and 80.
 #include <hip/hip_runtime.h>
 
 #include <math.h>
@@ -24,7 +30,7 @@ using namespace qllm_kv_detail;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int PROWS = 128, TILE = 64, WAVES = 4, THREADS = WAVES * 64; // rows of a workgroup, tokens of a tile
+constexpr int PROWS = 128, TILE = 64, WAVES = 4, THREADS = WAVES * 64; // rows of a workgroup, tokens of a tile, waves of a group
 constexpr int TOGETHER = 4; // tiles between two additions of the zero points' sums
 
 // A tile of tokens as operands.
@@ -49,30 +55,52 @@ struct Asked {
     int32_t beta;
 };
 
-template <int D, bool F32O>
-__global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a, int32_t numbers, int32_t folded)
+template <int D, bool F32O, int GROUPS>
+__global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const AttendArgs a)
 {
     constexpr int KSTEPS = D / 16, DT = D / 32;
-    __shared__ __attribute__((aligned(16))) Operands<D> op[2];
+    __shared__ __attribute__((aligned(16))) Operands<D> operands[GROUPS][2];
 
     const Step &s = a.s;
-    const int32_t tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
+    const int32_t tid = threadIdx.x % THREADS, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, h = lane >> 5;
+    const int32_t group = __builtin_amdgcn_readfirstlane(threadIdx.x / THREADS);
+    Operands<D> *const op = operands[group];
 
     // Workgroups of one kv head go to the same XCD (head fastest) where heads are a multiple of 8: its L2 holds the tokens they share.
-    // The tile with the longest way back first; where two workgroups share each CU for the whole launch (folded) the second
-    // half of them in the opposite order, so that a long tile has a short one beside it.
-    const int32_t head = blockIdx.x % s.heads, k = blockIdx.x / s.heads, half = (numbers + 1) / 2;
-    const int32_t number = !folded || k < half ? numbers - 1 - k : k - half;
+    // The tile with the longest way back first, workgroups without a tile last.
+    const int32_t head = blockIdx.x % s.heads;
     Tile t;
     {
-        const auto first = [&](int32_t i) { return (int64_t)row_of(s, i) * a.group / PROWS + i; };
-        const int32_t i = last_not_above(s.n_seqs, number, first);
-        t.seq = seq_of(s, i);
+        const auto tiles_upto = [&](int32_t from, int32_t before) { // a sequence a lane
+            const int32_t i = from + lane, rows = i < s.n_seqs ? (row_of(s, i + 1) - row_of(s, i)) * a.group : 0;
+            int32_t n = rows <= a.few ? 0 : (int32_t)(((uint32_t)rows + PROWS - 1) / PROWS);
+            for (int32_t o = 1; o < 64 && o < s.n_seqs; o <<= 1) {
+                const int32_t y = __shfl_up(n, o);
+                if (lane >= o) n = __builtin_elementwise_add_sat(n, y);
+            }
+            return __builtin_elementwise_add_sat(n, before);
+        };
+        int32_t total = 0, upto = 0;
+        for (int32_t from = 0; from < s.n_seqs; from += 64) {
+            upto = tiles_upto(from, total);
+            total = __builtin_amdgcn_readlane(upto, s.n_seqs - from < 64 ? s.n_seqs - from - 1 : 63);
+        }
+        const int32_t number = total - 1 - (int32_t)(blockIdx.x / s.heads);
+        if (number < 0) return;
+        int32_t i = 0, before = 0;
+        for (int32_t from = 0; from < s.n_seqs; from += 64) {
+            if (s.n_seqs > 64) upto = tiles_upto(from, before);
+            const int32_t skipped = __popcll(__ballot(from + lane < s.n_seqs && upto <= number));
+            if (skipped) before = __builtin_amdgcn_readlane(upto, skipped - 1);
+            i = from + skipped;
+            if (skipped < 64) break;
+        }
+        t.seq = seq_of(s, i < s.n_seqs ? i : s.n_seqs - 1);
         t.seq.row = __builtin_amdgcn_readfirstlane(t.seq.row), t.seq.n = __builtin_amdgcn_readfirstlane(t.seq.n); // the same in every lane
         t.seq.line = __builtin_amdgcn_readfirstlane(t.seq.line), t.seq.len = __builtin_amdgcn_readfirstlane(t.seq.len);
         t.rows = t.seq.n * a.group;
-        const int64_t at = (number - __builtin_amdgcn_readfirstlane((int32_t)first(i))) * (int64_t)PROWS;
-        if (at < 0 || at >= t.rows || t.rows <= a.few) return;
+        const int64_t at = (number - before) * (int64_t)PROWS;
+        if (at < 0 || at >= t.rows) return; // (for a row_start that does not ascend)
         t.first = (int32_t)at;
     }
     const int32_t tok0 = (int32_t)((uint32_t)t.first / (uint32_t)a.group), head0 = t.first - tok0 * a.group;
@@ -216,7 +244,7 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
     }
     float m = -INFINITY;
 
-    const auto work = [&](int32_t tile, int32_t b, const int32_t (&page)[2]) {
+    const auto work = [&](int32_t tile, int32_t b, bool add, const int32_t (&page)[2]) {
         const Operands<D> &o = op[b];
         const int32_t t0 = tile * TILE;
         f32x16 sc[2];
@@ -311,7 +339,7 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, DT + 1, 0);
-        if ((tile - tile_begin) % TOGETHER == TOGETHER - 1) {
+        if (add) {
             const float zero = off[0] + off[1] + off[2];
 #pragma unroll
             for (int i = 0; i < DT; ++i) acc[i] += zero;
@@ -320,32 +348,60 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
     };
 
     Asked<D> asked;
-    int32_t page[2], next[2];
-    ask(tile_begin, asked, page);
+    int32_t page[2], next[2], later[2];
+    ask(tile_begin + group, asked, page);
     lay_params(asked, 0);
     lay_codes(asked, 0);
-    ask(tile_begin + 1, asked, next); // past the last: page 0, dropped
+    ask(tile_begin + group + GROUPS, asked, next); // past the last: page 0, dropped
     __syncthreads();
-    for (int32_t tile = tile_begin; tile < tile_end; ++tile) {
-        const int32_t b = (tile - tile_begin) & 1;
-        __builtin_amdgcn_s_setprio(1); // laying a tile out gives way to the work of the CU's other workgroup (1184 -> 1139 us for 2000 tokens behind 14000)
-        if (tile * TILE <= some_hi && tile * TILE + TILE - 1 >= some_lo) work(tile, b, page);
+    for (int32_t i = 0; tile_begin + GROUPS * i < tile_end; ++i) {
+        const int32_t b = i & 1, tile = tile_begin + GROUPS * i + group;
+        const auto lay = [&] {
+            lay_params(asked, 1 - b);
+            lay_codes(asked, 1 - b);
+            ask(tile + 2 * GROUPS, asked, later);
+        };
+        if (GROUPS > 1 && group == 1) lay();
+        __builtin_amdgcn_s_setprio(1); // laying a tile out gives way to the work of the CU's other waves (1184 -> 1139 us for 2000 tokens behind 14000)
+        if (tile * TILE <= some_hi && tile * TILE + TILE - 1 >= some_lo) work(tile, b, i % TOGETHER == TOGETHER - 1, page);
         __builtin_amdgcn_s_setprio(0);
-        lay_params(asked, 1 - b);
-        lay_codes(asked, 1 - b);
-        page[0] = next[0], page[1] = next[1];
-        ask(tile + 2, asked, next);
+        if (GROUPS == 1 || group == 0) lay();
+        page[0] = next[0], page[1] = next[1], next[0] = later[0], next[1] = later[1];
         __syncthreads();
     }
 
+    const float zero = off[0] + off[1] + off[2];
+    float l = off[3] + off[4] + off[5];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) acc[i] += zero;
+    if (GROUPS > 1) { // the second group's results to the first
+        constexpr int Q = DT * 4;
+        f32x4 *room = reinterpret_cast<f32x4 *>(&operands[0][0]) + wave * (Q + 1) * 64 + lane;
+        static_assert(sizeof(operands) >= WAVES * (Q + 1) * 64 * sizeof(f32x4), "a group's results fit where the operands were");
+        if (group == 1) {
+#pragma unroll
+            for (int i = 0; i < Q; ++i) room[i * 64] = f32x4{acc[i / 4][i % 4 * 4], acc[i / 4][i % 4 * 4 + 1], acc[i / 4][i % 4 * 4 + 2], acc[i / 4][i % 4 * 4 + 3]};
+            room[Q * 64] = f32x4{m, l, 0.0f, 0.0f};
+        }
+        __syncthreads();
+        if (group == 1) return;
+        const f32x4 ml = room[Q * 64];
+        const float top = fmaxf(m, ml[0]), base = top == -INFINITY ? 0.0f : top, f = __builtin_amdgcn_exp2f(m - base), g = __builtin_amdgcn_exp2f(ml[0] - base);
+        l = f * l + g * ml[1];
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            const f32x4 o = room[i * 64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i / 4][i % 4 * 4 + e] = f * acc[i / 4][i % 4 * 4 + e] + g * o[e];
+        }
+    }
     if (!real) return;
-    const float zero = off[0] + off[1] + off[2], l = off[3] + off[4] + off[5];
     const int64_t at = (int64_t)(t.seq.row + token) * a.ldo + (head * a.group + head_of_row) * D;
 #pragma unroll
     for (int j = 0; j < 16; j += 4 / DT) { // channels DT (8 (j / 4) + 4 h + j % 4) .. of the row: four at a time
         float y[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = quotient(acc[e % DT][j + e / DT] + zero, l);
+        for (int e = 0; e < 4; ++e) y[e] = quotient(acc[e % DT][j + e / DT], l);
         const int64_t to = at + DT * (8 * (j >> 2) + 4 * h + (j & 3));
         if (F32O) {
             float *dst = static_cast<float *>(a.out) + to;
@@ -365,11 +421,14 @@ __global__ __launch_bounds__(THREADS, 2) void prompts_kernel(const AttendArgs a,
 
 int32_t qllm_kv_launch_prompts(const AttendArgs &a, int64_t dim, int32_t out_dtype, hipStream_t stream)
 {
-    const int64_t numbers = (int64_t)a.s.rows * a.group / PROWS + a.s.n_seqs, workgroups = numbers * a.s.heads;
-    if (workgroups > INT32_MAX) return QLLM_ERR_SHAPE;
-    const int32_t folded = workgroups <= 2 * 256 + a.s.heads; // (one number of a single sequence has no tile)
+    const int64_t workgroups = ((int64_t)a.s.rows * a.group / PROWS + a.s.n_seqs) * a.s.heads; // at least as many as there are tiles
+    const bool two = workgroups <= 2 * 256 + a.s.heads; // two for each CU; the last tile of a single sequence may not be there
     const dim3 grid((unsigned)workgroups);
-#define QLLM_PROMPTS(D, FO) hipLaunchKernelGGL((prompts_kernel<D, FO>), grid, dim3(THREADS), 0, stream, a, (int32_t)numbers, folded)
+#define QLLM_PROMPTS(D, FO)                                                                                \
+    do {                                                                                                   \
+        if (two) hipLaunchKernelGGL((prompts_kernel<D, FO, 2>), grid, dim3(2 * THREADS), 0, stream, a);    \
+        else hipLaunchKernelGGL((prompts_kernel<D, FO, 1>), grid, dim3(THREADS), 0, stream, a);            \
+    } while (0)
     if (dim == 128) {
         if (out_dtype == QLLM_F32) QLLM_PROMPTS(128, true);
         else QLLM_PROMPTS(128, false);

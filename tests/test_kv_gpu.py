@@ -673,3 +673,26 @@ def test_chunks_of_a_prompt_replayed_as_a_graph_on_another_stream(oracle, b):
         step(eager, ebatch, q2, o2)
         (torch.randn(1000, device="cuda") * 2).sum().item()
         assert torch.equal(q2, q_out) and torch.equal(o2, out) and torch.equal(cache.pages, eager.pages)
+
+
+@pytest.mark.parametrize("out_type,heads,group,dim,lengths,new,window", [
+    ("bf16", 40, 16, 64, [150], [140], 0),                                     # more tiles than the card holds workgroups
+    ("f32", 32, 16, 128, [200, 90, 40], [130, 1, 3], 60),
+    ("bf16", 16, 8, 64, [20 + i for i in range(90)], [5 + i % 9 for i in range(90)], 0),   # more sequences than a wave has lanes
+    ("bf16", 2, 20, 128, [4 + i % 7 for i in range(130)], [i % 6 for i in range(130)], 0),
+])
+def test_attention_of_many_prompt_tiles_and_of_many_prompts(oracle, b, out_type, heads, group, dim, lengths, new, window):
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(37)
+    new = [min(n, l) for n, l in zip(new, lengths)]
+    c = make(rng, heads, group, dim, 32, lengths, new)
+    hq = heads * group
+    q = _bf16(rng.standard_normal((c.rows, hq, dim)).astype(np.float32))
+    cache, batch = on_device(b, c)
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, hq), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    out = torch.full((c.rows, hq * dim), 5.0, dtype=torch.bfloat16 if out_type == "bf16" else torch.float32, device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), torch.bfloat16), cache, 0, batch, 0.125, out, ws, window=window)
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.125), window)
+    worst = np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, "bf16", out_type)
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
