@@ -846,7 +846,8 @@ def qllm_kv_copy_pages(cache, src, dst, stream=None):
     src, dst = _np(src, np.int32), _np(dst, np.int32)
     if src.ndim != 1 or src.shape != dst.shape:
         _fail("src and dst must be 1-d arrays of one length")
-    _check_on_current(pages=cache.pages)
+    if not (cache.device >= 0 and torch.cuda.current_device() == cache.device):
+        _check_on_current(pages=cache.pages)
     _chk(_lib.qllm_kv_copy_pages(_dp(cache.pages), cache.layers, cache.n_pages * cache.page_bytes, cache.n_pages, cache.page_bytes, _hp(src),
                                  _hp(dst), src.size, _stream(stream)), "qllm_kv_copy_pages")
 
@@ -887,10 +888,11 @@ def qllm_kv_fork_host(book, parents, children):
     """Line children[i] continues line parents[i]; returns (src, dst), the pages to copy."""
     parents = _host_list(parents, "parents")
     children = _host_list(children, "children", parents.size)
-    src, dst = np.empty(parents.size, np.int32), np.empty(parents.size, np.int32)
-    n = int(_lib.qllm_kv_fork_host(C.byref(book.c), _hp(parents), _hp(children), parents.size, _hp(src), _hp(dst)))
+    copies = np.empty((2, parents.size), np.int32)
+    at = _hp(copies)
+    n = int(_lib.qllm_kv_fork_host(C.byref(book.c), _hp(parents), _hp(children), parents.size, at, at + 4 * parents.size))
     _chk(n if n < 0 else 0, "qllm_kv_fork_host")
-    return src[:n], dst[:n]
+    return copies[0, :n], copies[1, :n]
 
 
 def qllm_kv_free_host(book, slots):
@@ -901,10 +903,11 @@ def qllm_kv_free_host(book, slots):
 
 def qllm_kv_compact_host(book):
     """Moves the pages in use together; returns (src, dst), the pages to copy."""
-    src, dst = np.empty(book.refs.size, np.int32), np.empty(book.refs.size, np.int32)
-    n = int(_lib.qllm_kv_compact_host(C.byref(book.c), _hp(src), _hp(dst)))
+    moves = np.empty((2, book.refs.size), np.int32)
+    at = _hp(moves)
+    n = int(_lib.qllm_kv_compact_host(C.byref(book.c), at, at + 4 * book.refs.size))
     _chk(n if n < 0 else 0, "qllm_kv_compact_host")
-    return src[:n], dst[:n]
+    return moves[0, :n], moves[1, :n]
 
 
 def qllm_probe_mfma(workgroups, iters, sink, stream=None):

@@ -98,17 +98,19 @@ extern "C" int64_t qllm_kv_fork_host(const qllm_kv_book *b, const int32_t *paren
     if (rc != QLLM_OK) return rc;
     if (n < 0) return QLLM_ERR_SHAPE;
     if (n > 0 && (!parents || !children || !src || !dst)) return QLLM_ERR_NULL;
-    std::unique_ptr<uint8_t[]> is_child(new (std::nothrow) uint8_t[(size_t)b->n_slots]());
-    if (!is_child) return QLLM_ERR_WORKSPACE;
+    constexpr uint8_t CHILD = 1, SOUND = 2; // of a line: a child of this call; a parent that has been checked
+    std::unique_ptr<uint8_t[]> known(new (std::nothrow) uint8_t[(size_t)b->n_slots]());
+    if (!known) return QLLM_ERR_WORKSPACE;
     int64_t fresh = 0;
     for (int64_t i = 0; i < n; ++i) {
         if (!line_ok(b, parents[i]) || !line_ok(b, children[i])) return QLLM_ERR_SHAPE;
-        if (b->length[children[i]] != 0 || is_child[children[i]]) return QLLM_ERR_SHAPE;
-        is_child[children[i]] = 1;
+        if (b->length[children[i]] != 0 || known[children[i]]) return QLLM_ERR_SHAPE;
+        known[children[i]] = CHILD;
     }
     for (int64_t i = 0; i < n; ++i) {
-        if (is_child[parents[i]]) return QLLM_ERR_SHAPE;
-        if (!line_is_sound(b, parents[i])) return QLLM_ERR_PAGES;
+        if (known[parents[i]] == CHILD) return QLLM_ERR_SHAPE;
+        if (known[parents[i]] != SOUND && !line_is_sound(b, parents[i])) return QLLM_ERR_PAGES;
+        known[parents[i]] = SOUND;
         // n_slots lines share a page at most, far below int32
         fresh += b->length[parents[i]] % b->page_tokens != 0;
     }
