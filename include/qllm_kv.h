@@ -42,7 +42,7 @@ int64_t qllm_kv_page_bytes(int64_t heads, int64_t dim, int64_t page_tokens);
  * or of a line outside the table in qllm_kv_append and qllm_kv_read) are left as they were; sequences may have no rows.
  * Position p of a line lies in page table[line][p / page_tokens]; a page number outside [0, n_pages), or a p beyond the line's
  * end, is "not there": nothing is written, and attention does not see the token.
- * Limits: rows <= 2^24, n_seqs <= 2^20, table_ld * page_tokens < 2^31, n_pages < 2^31; the cache may be of any size.
+ * Limits: rows < 2^24, n_seqs <= 2^20, table_ld * page_tokens < 2^31, n_pages < 2^31; the cache may be of any size.
  */
 typedef struct {
     int64_t rows;             /* rows of the step's tensors */
@@ -95,7 +95,11 @@ int32_t qllm_kv_read(const qllm_kv_cache *cache, const qllm_kv_batch *batch, voi
  * Codes enter the matrix cores as exact bf16 integers; scores, maxima and sums are fp32; with bf16 queries the weights (times a
  * value's alpha) are rounded to bf16 once before they meet the values (half a step: 2^-8 of each at most; in sequences of many
  * rows the same rounded weights are what is summed below the line), with fp32 queries queries and weights are taken in three
- * bf16 parts, 24 bits.  A query that is not finite spoils its own row and head alone.  Errors: NULL / SHAPE / DTYPE / ALIGN / WORKSPACE / HIP.  rows == 0 or n_seqs == 0: no-op.
+ * bf16 parts, 24 bits.  A query that is not finite spoils the output of its own row and head alone.
+ * In sequences of many rows with bf16 queries a key whose |scale| alpha is below 2^-90 counts as one of 2^-90 (which is nothing
+ * for queries below 2^60), and a token whose value's alpha is less than 2^-100 of another's that the query sees may count for
+ * less than its share below the line.
+ * Errors: NULL / SHAPE / DTYPE / ALIGN / WORKSPACE / HIP.  rows == 0 or n_seqs == 0: no-op.
  */
 int64_t qllm_kv_attention_workspace_bytes(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads);
 int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq, int64_t q_heads, const qllm_kv_cache *cache,

@@ -79,7 +79,7 @@ inline int32_t prepare_step(const qllm_kv_cache *cache, const qllm_kv_batch *bat
     const int64_t pb = qllm_kv_page_bytes(cache->heads, cache->dim, cache->page_tokens);
     if (pb < 0) return QLLM_ERR_SHAPE;
     if (cache->n_pages <= 0 || cache->n_pages > INT32_MAX) return QLLM_ERR_SHAPE;
-    if (batch->rows < 0 || batch->rows > (1 << 24) || batch->n_seqs < 0 || batch->n_seqs > (1 << 20)) return QLLM_ERR_SHAPE;
+    if (batch->rows < 0 || batch->rows >= (1 << 24) || batch->n_seqs < 0 || batch->n_seqs > (1 << 20)) return QLLM_ERR_SHAPE;
     if (batch->n_slots <= 0 || batch->n_slots > INT32_MAX || batch->table_ld <= 0) return QLLM_ERR_SHAPE;
     if (batch->table_ld > INT32_MAX / cache->page_tokens) return QLLM_ERR_SHAPE; // positions are int32
     if (!batch->row_start && batch->rows < batch->n_seqs) return QLLM_ERR_SHAPE;

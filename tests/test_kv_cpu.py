@@ -332,3 +332,13 @@ def test_statement_of_the_pages_and_of_attention():
     assert (absv >= np.abs(out) - 1e-12).all() and (err_s >= 0).all() and err_s.max() < 1e-2 and err_o.max() < 1e-3
     late = okv.attention(q[:3], pages, table, [(0, 0, -1), (1, 5, 3), (2, 0, 0)], length, 0.2)[0]
     assert not late[:2].any() and late[2].any()
+
+
+def test_limits_of_a_step():
+    f = b.raw().qllm_kv_attention_workspace_bytes
+    bytes_for = lambda hq, ck={}, **tk: f(C.byref(cache(pages=None, **ck)), C.byref(batch(table=None, length=None, **tk)), hq)
+    assert bytes_for(4, rows=(1 << 24) - 1, row_start=A) > 0 and bytes_for(4, rows=1 << 24, row_start=A) == SHAPE
+    assert bytes_for(4, n_seqs=(1 << 20) + 1, rows=1 << 21, row_start=A) == SHAPE
+    assert bytes_for(1 << 15) > 0 and bytes_for(1 << 16) == SHAPE
+    assert bytes_for(64, rows=(1 << 22) - 64, row_start=A) > 0 and bytes_for(64, rows=1 << 22, row_start=A) == SHAPE     # 2^23 tiles of 16 rows
+    assert bytes_for(4, rows=1 << 21, row_start=A, n_slots=8, ld=1 << 14) == SHAPE                                 # 2^31 steps of 32 tokens

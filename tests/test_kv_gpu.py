@@ -696,3 +696,25 @@ def test_attention_of_many_prompt_tiles_and_of_many_prompts(oracle, b, out_type,
     want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.125), window)
     worst = np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, "bf16", out_type)
     assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+@pytest.mark.parametrize("heads,group,lengths,new", [(1, 4, [300, 40], None), (16, 8, [190], [140])])
+def test_attention_over_values_of_very_different_ranges(oracle, b, heads, group, lengths, new):
+    """Values from 2^-45 to 2^45 in one line, keys of all ranges below one, some of them nothing but rounding noise."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(38)
+    c = make(rng, heads, group, 128, 64, lengths, new)
+    for i, l in enumerate(lengths):
+        k = rng.standard_normal((l, heads, 128)) * np.exp2(rng.integers(-40, 1, (l, heads, 1)))
+        v = rng.standard_normal((l, heads, 128)) * np.exp2(rng.integers(-45, 46, (l, heads, 1)))
+        k[5], v[6], v[7] = 1e-38, 0.0, -3.0
+        okv.append(c.pages, c.table, [(r, i, r) for r in range(l)], k.astype(np.float32), v.astype(np.float32))
+    q = _bf16(rng.standard_normal((c.rows, heads * group, 128)).astype(np.float32))
+    cache, batch = on_device(b, c)
+    out = torch.empty((c.rows, heads * group * 128), device="cuda")
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), torch.bfloat16), cache, 0, batch, 0.09, out, ws)
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.09))
+    worst = np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, "bf16", "f32")
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
