@@ -48,6 +48,7 @@ struct AttendArgs {
     int32_t few;                    // sequences of more rows than this are left to the kernel for prompts
     int32_t numbers;                // of tiles, see number_of
     Unfinished *unfinished;         // [heads][numbers]
+    int32_t parts;                  // of a prompts tile's tokens, at most
 };
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
@@ -129,6 +130,11 @@ __device__ __forceinline__ float quotient(float o, float sum) { return sum > 0.0
 } // namespace qllm_kv_detail
 
 // The kernel for prompts (kv_prompts.hip): sequences of more than a.few rows, bf16 queries.
-int32_t qllm_kv_launch_prompts(const qllm_kv_detail::AttendArgs &a, int64_t dim, int32_t out_dtype, hipStream_t stream);
+struct QllmKvPrompts {
+    int64_t workgroups, parts, groups; // as many as there may be tiles; each tile's tokens shared by `parts` of them, of `groups` of waves
+    int64_t sums, bytes;               // of the workspace for the parts' sums, and altogether
+};
+QllmKvPrompts qllm_kv_plan_prompts(const qllm_kv_batch &batch, int64_t heads, int64_t group, int64_t dim, int64_t tokens);
+int32_t qllm_kv_launch_prompts(const qllm_kv_detail::AttendArgs &a, const QllmKvPrompts &n, int64_t dim, int32_t out_dtype, void *workspace, hipStream_t stream);
 
 #endif

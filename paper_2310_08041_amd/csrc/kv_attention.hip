@@ -555,18 +555,23 @@ int32_t check(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_
     return tiles < (1 << 23) && tiles * steps < INT32_MAX ? QLLM_OK : QLLM_ERR_SHAPE; // (a grid of tiles has less than 2^32 threads)
 }
 
-// Whether the prompts kernel takes sequences of more than FEW_ROWS rows.  Up to 256 workgroups its time is that of one way through
-// the tokens, some 12 us and 17 more for every 1000 (D 128); this kernel's some 22 us and 0.14 for every workgroup of the other and
-// 1000 tokens.  One sequence, rows x kv heads x tokens, this kernel's us first: 512 x 8 x 1000 29 and 30, 1024 x 8 x 1000 36 and 30,
-// 512 x 8 x 4000 37 and 79, 1600 x 8 x 4000 78 and 80, 2048 x 8 x 4000 92 and 80, 2048 x 8 x 16000 287 and 275, 64 x 32 x 64 20 and 14,
-// 1024 x 8 x 300 26 and 20.  Sequences x their rows, 8 heads, 2000 tokens: 32 x 32 46 and 45, 32 x 64 68 and 47, 32 x 128 114 and 51
-// (and some 7 us for this kernel, which finds nothing to do).  (Grids of 2^32 threads and more are refused by the runtime.)
+// Whether the prompts kernel takes sequences of more than FEW_ROWS rows: few tiles of 128 rows leave most of the card to wait for
+// one way through the tokens, beyond what its sharing of them makes good.  One sequence, tiles x tokens, this kernel's us first
+// (D 128): 8 x 4000 29 and 29, 16 x 4000 32 and 30, 32 x 4000 37 and 32, 64 x 4000 58 and 37, 128 x 4000 92 and 55, 128 x 16000 288
+// and 157, 32 x 1000 29 and 30, 64 x 1000 36 and 30, 32 x 300 26 and 20, 32 x 64 20 and 14.  With several sequences this kernel runs
+// beside it, some 7 us if it finds nothing: 8 x 64 rows behind 2000, 32 tiles, 36 and 35 + 7; 8 x 128, 64 tiles, 47 and 37 + 7.
+// FEW_ROWS: sequences x rows, 8 heads, 2000 tokens: 32 x 32 46 and 45, 32 x 64 68 and 47, 32 x 128 114 and 51.
+// (A grid of 2^32 threads would be refused by the runtime.)
 constexpr int32_t FEW_ROWS = 32;
 bool prompts_pay(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads, int32_t q_dtype)
 {
-    const int64_t rows = batch->rows * (q_heads / cache->heads), workgroups = rows / 128 * cache->heads, tokens = batch->table_ld * cache->page_tokens;
-    return q_dtype == QLLM_BF16 && batch->row_start && (120 - workgroups) * tokens <= 72000 && rows > batch->n_seqs * FEW_ROWS &&
-           (rows / 128 + batch->n_seqs) * cache->heads < (1 << 24);
+    const int64_t rows = batch->rows * (q_heads / cache->heads), tiles = rows / 128 * cache->heads, tokens = batch->table_ld * cache->page_tokens;
+    return q_dtype == QLLM_BF16 && batch->row_start && ((batch->n_seqs == 1 ? 24 : 48) - tiles) * tokens <= 16000 &&
+           rows > batch->n_seqs * FEW_ROWS && (rows / 128 + batch->n_seqs) * cache->heads < (1 << 24);
+}
+QllmKvPrompts plan_prompts(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads)
+{
+    return qllm_kv_plan_prompts(*batch, cache->heads, q_heads / cache->heads, cache->dim, batch->table_ld * cache->page_tokens);
 }
 
 // Workgroups of a kv head: as many as the card holds at once (three on each of 256 CUs), but none for less than LEAST steps.
@@ -597,7 +602,10 @@ extern "C" int64_t qllm_kv_attention_workspace_bytes(const qllm_kv_cache *cache,
     if (rc == QLLM_OK) rc = check(cache, batch, q_heads);
     if (rc != QLLM_OK) return rc;
     const Launch n = plan(cache, batch, q_heads);
-    return 256 + n.marks + n.parts * (cache->dim + 2) * (int64_t)sizeof(float);
+    const int64_t bytes = n.marks + n.parts * (cache->dim + 2) * (int64_t)sizeof(float);
+    if (!prompts_pay(cache, batch, q_heads, QLLM_BF16)) return 256 + bytes;
+    const int64_t prompts = plan_prompts(cache, batch, q_heads).bytes; // before the others: the same place
+    return 256 + (bytes > prompts ? bytes : prompts);
 }
 
 extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq, int64_t q_heads, const qllm_kv_cache *cache,
@@ -630,7 +638,7 @@ extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq
     a.few = INT32_MAX;
     if (a.scale2 != 0.0f && prompts_pay(cache, batch, q_heads, q_dtype)) { // (it divides by the scale)
         a.few = batch->n_seqs == 1 ? 0 : FEW_ROWS;
-        rc = qllm_kv_launch_prompts(a, cache->dim, out_dtype, stream);
+        rc = qllm_kv_launch_prompts(a, plan_prompts(cache, batch, q_heads), cache->dim, out_dtype, workspace, stream);
         if (rc != QLLM_OK || batch->n_seqs == 1) return rc;
     }
     const Launch n = plan(cache, batch, q_heads);

@@ -17,6 +17,9 @@
 // each, each with its own LDS, one of them half a turn behind, and joins their results at the end.  D 128, us, one group first:
 // 2048 tokens x 32 heads 72 and 58, 1024 x 32 40 and 32, 512 rows behind 3500 tokens x 8 heads of 8 117 and 80, 4 x 100 behind
 // 16000 430 and 284; more workgroups, 4096 x 32 171 and 182, 8 x 512 x 32 67 and 80.
+// Where even so half of the CUs had nothing to do, a tile's tokens are shared by several workgroups, whose results a second kernel
+// joins.  One part first, 8 heads of 8: 128 tokens behind 16000 273 and 90, behind 4000 79 and 37, 8 x 16 behind 2000 47 and 38;
+// 128 behind 900 30 and 36.
 #include <hip/hip_runtime.h>
 
 #include <math.h>
@@ -32,6 +35,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int PROWS = 128, TILE = 64, WAVES = 4, THREADS = WAVES * 64; // rows of a workgroup, tokens of a tile, waves of a group
 constexpr int TOGETHER = 4; // tiles between two additions of the zero points' sums
+constexpr int LEAST = 8;    // tiles of tokens of a part
 
 // A tile of tokens as operands.
 template <int D>
@@ -55,6 +59,91 @@ struct Asked {
     int32_t beta;
 };
 
+// Tile `k` of a kv head, from the one with the longest way back on (sequence after sequence, the tiles of a sequence in order, all
+// of it backwards); false: there are no more.  By one wave.
+__device__ __forceinline__ bool tile_at(const AttendArgs &a, int32_t k, Tile *t)
+{
+    const Step &s = a.s;
+    const int32_t lane = threadIdx.x & 63;
+    const auto tiles_upto = [&](int32_t from, int32_t before) { // a sequence a lane
+        const int32_t i = from + lane, rows = i < s.n_seqs ? (row_of(s, i + 1) - row_of(s, i)) * a.group : 0;
+        int32_t n = rows <= a.few ? 0 : (int32_t)(((uint32_t)rows + PROWS - 1) / PROWS);
+        for (int32_t o = 1; o < 64 && o < s.n_seqs; o <<= 1) {
+            const int32_t y = __shfl_up(n, o);
+            if (lane >= o) n = __builtin_elementwise_add_sat(n, y);
+        }
+        return __builtin_elementwise_add_sat(n, before);
+    };
+    int32_t total = 0, upto = 0;
+    for (int32_t from = 0; from < s.n_seqs; from += 64) {
+        upto = tiles_upto(from, total);
+        total = __builtin_amdgcn_readlane(upto, s.n_seqs - from < 64 ? s.n_seqs - from - 1 : 63);
+    }
+    const int32_t number = total - 1 - k;
+    if (number < 0) return false;
+    int32_t i = 0, before = 0;
+    for (int32_t from = 0; from < s.n_seqs; from += 64) {
+        if (s.n_seqs > 64) upto = tiles_upto(from, before);
+        const int32_t skipped = __popcll(__ballot(from + lane < s.n_seqs && upto <= number));
+        if (skipped) before = __builtin_amdgcn_readlane(upto, skipped - 1);
+        i = from + skipped;
+        if (skipped < 64) break;
+    }
+    t->seq = seq_of(s, i < s.n_seqs ? i : s.n_seqs - 1);
+    t->seq.row = __builtin_amdgcn_readfirstlane(t->seq.row), t->seq.n = __builtin_amdgcn_readfirstlane(t->seq.n); // the same in every lane
+    t->seq.line = __builtin_amdgcn_readfirstlane(t->seq.line), t->seq.len = __builtin_amdgcn_readfirstlane(t->seq.len);
+    t->rows = t->seq.n * a.group;
+    const int64_t at = (number - before) * (int64_t)PROWS;
+    t->first = (int32_t)at;
+    return at >= 0 && at < t->rows; // (not so for a row_start that does not ascend)
+}
+
+// The tiles of tokens that some row of a tile sees, and how many workgroups share them.
+struct Span {
+    int32_t begin, end, parts;
+};
+__device__ __forceinline__ Span span_of(const AttendArgs &a, const Sight &v)
+{
+    Span x;
+    x.begin = v.all_lo / TILE, x.end = v.all_hi < v.all_lo ? x.begin : v.all_hi / TILE + 1;
+    x.parts = (x.end - x.begin) / LEAST;
+    x.parts = x.parts < 1 ? 1 : (x.parts > a.parts ? a.parts : x.parts);
+    return x;
+}
+
+// Quarter k of a row: element e of it of tile c is channel D / 32 (8 k + 4 h + e) + c.
+template <int D, bool F32O>
+__device__ __forceinline__ void put_quarter(const AttendArgs &a, int32_t head, int32_t q_row, int32_t head_of_row, int32_t k, const f32x4 (&x)[D / 32], float l)
+{
+    constexpr int DT = D / 32;
+    const int32_t h = (threadIdx.x & 63) >> 5;
+    const int64_t at = (int64_t)q_row * a.ldo + (head * a.group + head_of_row) * D + DT * (8 * k + 4 * h);
+#pragma unroll
+    for (int j = 0; j < 4; j += 4 / DT) { // four channels at a time
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = quotient(x[e % DT][j + e / DT], l);
+        if (F32O) {
+            float *dst = static_cast<float *>(a.out) + at + DT * j;
+            if (a.out_vec) *reinterpret_cast<float4 *>(dst) = make_float4(y[0], y[1], y[2], y[3]);
+            else
+                for (int e = 0; e < 4; ++e) dst[e] = y[e];
+        } else {
+            uint16_t *dst = static_cast<uint16_t *>(a.out) + at + DT * j;
+            const uint2 w = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+            if (a.out_vec) *reinterpret_cast<uint2 *>(dst) = w;
+            else dst[0] = (uint16_t)w.x, dst[1] = (uint16_t)(w.x >> 16), dst[2] = (uint16_t)w.y, dst[3] = (uint16_t)(w.y >> 16);
+        }
+    }
+}
+__device__ __forceinline__ f32x4 quarter_of(const f32x16 &x, int k) { return f32x4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]}; }
+
+// Where a wave of a part keeps its results: the quarters of a lane's sums one after the other, 16 bytes a lane; a maximum and a sum.
+__device__ __forceinline__ int64_t part_at(const AttendArgs &a, int32_t head, int32_t k, int32_t part, int32_t wave)
+{
+    return (((int64_t)k * a.s.heads + head) * a.parts + part) * WAVES + wave;
+}
+
 template <int D, bool F32O, int GROUPS>
 __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const AttendArgs a)
 {
@@ -68,43 +157,13 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
 
     // Workgroups of one kv head go to the same XCD (head fastest) where heads are a multiple of 8: its L2 holds the tokens they share.
     // The tile with the longest way back first, workgroups without a tile last.
-    const int32_t head = blockIdx.x % s.heads;
+    const int32_t head = blockIdx.x % s.heads, part = (int32_t)(blockIdx.x / s.heads) % a.parts, k_tile = (int32_t)(blockIdx.x / s.heads) / a.parts;
     Tile t;
-    {
-        const auto tiles_upto = [&](int32_t from, int32_t before) { // a sequence a lane
-            const int32_t i = from + lane, rows = i < s.n_seqs ? (row_of(s, i + 1) - row_of(s, i)) * a.group : 0;
-            int32_t n = rows <= a.few ? 0 : (int32_t)(((uint32_t)rows + PROWS - 1) / PROWS);
-            for (int32_t o = 1; o < 64 && o < s.n_seqs; o <<= 1) {
-                const int32_t y = __shfl_up(n, o);
-                if (lane >= o) n = __builtin_elementwise_add_sat(n, y);
-            }
-            return __builtin_elementwise_add_sat(n, before);
-        };
-        int32_t total = 0, upto = 0;
-        for (int32_t from = 0; from < s.n_seqs; from += 64) {
-            upto = tiles_upto(from, total);
-            total = __builtin_amdgcn_readlane(upto, s.n_seqs - from < 64 ? s.n_seqs - from - 1 : 63);
-        }
-        const int32_t number = total - 1 - (int32_t)(blockIdx.x / s.heads);
-        if (number < 0) return;
-        int32_t i = 0, before = 0;
-        for (int32_t from = 0; from < s.n_seqs; from += 64) {
-            if (s.n_seqs > 64) upto = tiles_upto(from, before);
-            const int32_t skipped = __popcll(__ballot(from + lane < s.n_seqs && upto <= number));
-            if (skipped) before = __builtin_amdgcn_readlane(upto, skipped - 1);
-            i = from + skipped;
-            if (skipped < 64) break;
-        }
-        t.seq = seq_of(s, i < s.n_seqs ? i : s.n_seqs - 1);
-        t.seq.row = __builtin_amdgcn_readfirstlane(t.seq.row), t.seq.n = __builtin_amdgcn_readfirstlane(t.seq.n); // the same in every lane
-        t.seq.line = __builtin_amdgcn_readfirstlane(t.seq.line), t.seq.len = __builtin_amdgcn_readfirstlane(t.seq.len);
-        t.rows = t.seq.n * a.group;
-        const int64_t at = (number - before) * (int64_t)PROWS;
-        if (at < 0 || at >= t.rows) return; // (for a row_start that does not ascend)
-        t.first = (int32_t)at;
-    }
+    if (!tile_at(a, k_tile, &t)) return;
     const int32_t tok0 = (int32_t)((uint32_t)t.first / (uint32_t)a.group), head0 = t.first - tok0 * a.group;
     const Sight v = sight_of(a, t, tok0, head0, PROWS);
+    const Span span = span_of(a, v);
+    if (part >= span.parts) return;
 
     // this lane's row, and what the wave's rows see
     const int32_t n = wave * 32 + col, token = tok0 + (int32_t)a.by_group.divide((uint32_t)(head0 + n)), head_of_row = head0 + n - (token - tok0) * a.group;
@@ -145,7 +204,8 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
     }
 
     // page numbers of up to 64 blocks of 32 tokens, one a lane
-    const int32_t tile_begin = v.all_lo / TILE, tile_end = v.all_hi < v.all_lo ? tile_begin : v.all_hi / TILE + 1;
+    const int32_t tile_begin = span.begin + (int32_t)((int64_t)(span.end - span.begin) * part / span.parts);
+    const int32_t tile_end = span.begin + (int32_t)((int64_t)(span.end - span.begin) * (part + 1) / span.parts);
     int32_t listed = tile_begin; // the first tile of the list
     const auto pages_from = [&](int32_t tile) {
         const int32_t p = tile * TILE + 32 * lane;
@@ -380,14 +440,14 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
         static_assert(sizeof(operands) >= WAVES * (Q + 1) * 64 * sizeof(f32x4), "a group's results fit where the operands were");
         if (group == 1) {
 #pragma unroll
-            for (int i = 0; i < Q; ++i) room[i * 64] = f32x4{acc[i / 4][i % 4 * 4], acc[i / 4][i % 4 * 4 + 1], acc[i / 4][i % 4 * 4 + 2], acc[i / 4][i % 4 * 4 + 3]};
+            for (int i = 0; i < Q; ++i) room[i * 64] = quarter_of(acc[i / 4], i % 4);
             room[Q * 64] = f32x4{m, l, 0.0f, 0.0f};
         }
         __syncthreads();
         if (group == 1) return;
         const f32x4 ml = room[Q * 64];
         const float top = fmaxf(m, ml[0]), base = top == -INFINITY ? 0.0f : top, f = __builtin_amdgcn_exp2f(m - base), g = __builtin_amdgcn_exp2f(ml[0] - base);
-        l = f * l + g * ml[1];
+        l = f * l + g * ml[1], m = top;
 #pragma unroll
         for (int i = 0; i < Q; ++i) {
             const f32x4 o = room[i * 64];
@@ -395,39 +455,83 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
             for (int e = 0; e < 4; ++e) acc[i / 4][i % 4 * 4 + e] = f * acc[i / 4][i % 4 * 4 + e] + g * o[e];
         }
     }
-    if (!real) return;
-    const int64_t at = (int64_t)(t.seq.row + token) * a.ldo + (head * a.group + head_of_row) * D;
+    if (span.parts > 1) {
+        const int64_t to = part_at(a, head, k_tile, part, wave);
+        f32x4 *o = reinterpret_cast<f32x4 *>(a.part_o) + to * (DT * 4) * 64 + lane;
 #pragma unroll
-    for (int j = 0; j < 16; j += 4 / DT) { // channels DT (8 (j / 4) + 4 h + j % 4) .. of the row: four at a time
-        float y[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = quotient(acc[e % DT][j + e / DT], l);
-        const int64_t to = at + DT * (8 * (j >> 2) + 4 * h + (j & 3));
-        if (F32O) {
-            float *dst = static_cast<float *>(a.out) + to;
-            if (a.out_vec) *reinterpret_cast<float4 *>(dst) = make_float4(y[0], y[1], y[2], y[3]);
-            else
-                for (int e = 0; e < 4; ++e) dst[e] = y[e];
-        } else {
-            uint16_t *dst = static_cast<uint16_t *>(a.out) + to;
-            const uint2 w = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-            if (a.out_vec) *reinterpret_cast<uint2 *>(dst) = w;
-            else dst[0] = (uint16_t)w.x, dst[1] = (uint16_t)(w.x >> 16), dst[2] = (uint16_t)w.y, dst[3] = (uint16_t)(w.y >> 16);
-        }
+        for (int i = 0; i < DT * 4; ++i) o[i * 64] = quarter_of(acc[i % DT], i / DT);
+        a.part_ml[to * 64 + lane] = make_float2(m, l);
+        return;
     }
+    if (!real) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        f32x4 x[DT];
+#pragma unroll
+        for (int c = 0; c < DT; ++c) x[c] = quarter_of(acc[c], k);
+        put_quarter<D, F32O>(a, head, t.seq.row + token, head_of_row, k, x, l);
+    }
+}
+
+// The parts of a tile joined, a workgroup for a quarter of its channels: every wave its 32 rows, lanes as in the products.
+template <int D, bool F32O>
+__global__ __launch_bounds__(THREADS) void join_prompts_kernel(const AttendArgs a)
+{
+    constexpr int DT = D / 32;
+    const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t head = blockIdx.x % a.s.heads, k_tile = blockIdx.x / a.s.heads, quarter = blockIdx.y;
+    Tile t;
+    if (!tile_at(a, k_tile, &t)) return;
+    const int32_t tok0 = (int32_t)((uint32_t)t.first / (uint32_t)a.group), head0 = t.first - tok0 * a.group;
+    const Span span = span_of(a, sight_of(a, t, tok0, head0, PROWS));
+    if (span.parts <= 1) return;
+    const int64_t from = part_at(a, head, k_tile, 0, wave);
+    const float2 *ml = a.part_ml + from * 64 + lane;
+    const f32x4 *o = reinterpret_cast<const f32x4 *>(a.part_o) + (from * 4 + quarter) * DT * 64 + lane;
+    float top = -INFINITY, l = 0.0f;
+    for (int32_t p = 0; p < span.parts; ++p) top = fmaxf(top, ml[p * WAVES * 64].x);
+    if (top == -INFINITY) top = 0.0f;
+    f32x4 x[DT];
+#pragma unroll
+    for (int c = 0; c < DT; ++c) x[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int32_t p = 0; p < span.parts; ++p) {
+        const float f = __builtin_amdgcn_exp2f(ml[p * WAVES * 64].x - top);
+        l += f * ml[p * WAVES * 64].y;
+#pragma unroll
+        for (int c = 0; c < DT; ++c) x[c] += f * o[(p * WAVES * 4 * DT + c) * 64];
+    }
+    const int32_t n = wave * 32 + (lane & 31), token = tok0 + (int32_t)a.by_group.divide((uint32_t)(head0 + n));
+    if (t.first + n < t.rows) put_quarter<D, F32O>(a, head, t.seq.row + token, head0 + n - (token - tok0) * a.group, quarter, x, l);
 }
 
 } // namespace
 
-int32_t qllm_kv_launch_prompts(const AttendArgs &a, int64_t dim, int32_t out_dtype, hipStream_t stream)
+QllmKvPrompts qllm_kv_plan_prompts(const qllm_kv_batch &batch, int64_t heads, int64_t group, int64_t dim, int64_t tokens)
 {
-    const int64_t workgroups = ((int64_t)a.s.rows * a.group / PROWS + a.s.n_seqs) * a.s.heads; // at least as many as there are tiles
-    const bool two = workgroups <= 2 * 256 + a.s.heads; // two for each CU; the last tile of a single sequence may not be there
-    const dim3 grid((unsigned)workgroups);
-#define QLLM_PROMPTS(D, FO)                                                                                \
-    do {                                                                                                   \
-        if (two) hipLaunchKernelGGL((prompts_kernel<D, FO, 2>), grid, dim3(2 * THREADS), 0, stream, a);    \
-        else hipLaunchKernelGGL((prompts_kernel<D, FO, 1>), grid, dim3(THREADS), 0, stream, a);            \
+    QllmKvPrompts n;
+    const int64_t rows = batch.rows * group, tiles = batch.n_seqs == 1 ? (rows + PROWS - 1) / PROWS : rows / PROWS + batch.n_seqs; // at most
+    n.workgroups = tiles * heads;
+    n.groups = n.workgroups <= 2 * 256 ? 2 : 1;
+    n.parts = n.workgroups > 0 && n.workgroups <= 128 && tokens >= 1280 ? 256 / n.workgroups : 1;
+    if (n.parts > 32) n.parts = 32;
+    n.sums = n.parts > 1 ? n.workgroups * n.parts * PROWS * dim * (int64_t)sizeof(float) : 0;
+    n.bytes = n.parts > 1 ? n.sums + n.workgroups * n.parts * WAVES * 64 * (int64_t)sizeof(float2) : 0;
+    return n;
+}
+
+int32_t qllm_kv_launch_prompts(const AttendArgs &args, const QllmKvPrompts &n, int64_t dim, int32_t out_dtype, void *workspace, hipStream_t stream)
+{
+    AttendArgs a = args;
+    a.parts = (int32_t)n.parts;
+    a.part_o = static_cast<float *>(workspace);
+    a.part_ml = reinterpret_cast<float2 *>(static_cast<uint8_t *>(workspace) + n.sums);
+    const dim3 grid((unsigned)(n.workgroups * n.parts)), tiles((unsigned)n.workgroups, 4);
+#define QLLM_PROMPTS(D, FO)                                                                                     \
+    do {                                                                                                        \
+        if (n.groups == 2) hipLaunchKernelGGL((prompts_kernel<D, FO, 2>), grid, dim3(2 * THREADS), 0, stream, a); \
+        else hipLaunchKernelGGL((prompts_kernel<D, FO, 1>), grid, dim3(THREADS), 0, stream, a);                 \
+        if (n.parts > 1) hipLaunchKernelGGL((join_prompts_kernel<D, FO>), tiles, dim3(THREADS), 0, stream, a);  \
     } while (0)
     if (dim == 128) {
         if (out_dtype == QLLM_F32) QLLM_PROMPTS(128, true);

@@ -718,3 +718,32 @@ def test_attention_over_values_of_very_different_ranges(oracle, b, heads, group,
     want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.09))
     worst = np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, "bf16", "f32")
     assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+@pytest.mark.parametrize("out_type,heads,group,dim,page,lengths,new,window", [
+    ("bf16", 2, 16, 128, 64, [3000], [130], 0),
+    ("f32", 2, 32, 64, 32, [2100], [70], 0),
+    ("bf16", 4, 16, 128, 128, [2600, 400, 1500], [70, 1, 40], 0),             # a line of one part, a single token beside them
+    ("f32", 4, 16, 64, 32, [2600, 300, 1500], [70, 20, 40], 1100),            # parts that some rows see nothing of
+    ("bf16", 1, 64, 128, 64, [5000], [60], 0),                                # as many parts as a tile can have
+])
+def test_attention_of_prompts_shared_by_workgroups(oracle, b, out_type, heads, group, dim, page, lengths, new, window):
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(39)
+    c = make(rng, heads, group, dim, page, lengths, new)
+    hq = heads * group
+    tiles, tokens = c.rows * group // 128 * heads, c.table.shape[1] * page
+    assert ((24 if len(new) == 1 else 48) - tiles) * tokens <= 16000 and (c.rows * group // 128 + len(new)) * heads <= 128 and tokens >= 1280
+    q = _bf16(rng.standard_normal((c.rows, hq, dim)).astype(np.float32))
+    cache, batch = on_device(b, c)
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, hq), dtype=torch.uint8, device="cuda")
+    qd, outs = _t(q.reshape(c.rows, -1), torch.bfloat16), []
+    for garbage in (0xFF, 0x00):
+        ws.fill_(garbage)
+        out = torch.full((c.rows, hq * dim), 5.0, dtype=torch.bfloat16 if out_type == "bf16" else torch.float32, device="cuda")
+        outs.append(b.qllm_kv_attention(qd, cache, 0, batch, 0.1, out, ws, window=window))
+    assert torch.equal(*outs)
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.1), window)
+    worst = np.abs(outs[0].double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, "bf16", out_type)
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
