@@ -245,6 +245,9 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
     // queries: element e of step k of lane group g is channel (D / 4) g + 8 k + {0, 4, 1, 5, 2, 6, 3, 7}[e]
     bf16x8 qo[PARTS][KS];
     float qsum = 0.0f;
+    // float32: - 24 times the sums of the queries' first parts over a step of channels, and of the other parts over all.  A matrix
+    // operation on bf16 rounds once, the accumulator's share included: what cancels inside of one costs no bits.
+    float centre[F32Q ? KS : 1], rest = 0.0f;
     {
         const int64_t from = (int64_t)(t.seq.row + token) * a.ldq + (head * a.group + head_of_row) * D + D / 4 * g;
         if (!F32Q && a.q_vec) {
@@ -267,6 +270,7 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
                 float x[8], part[8][PARTS];
+                float sum0 = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = 0.0f;
                 if (F32Q && real && a.q_vec) {
@@ -279,8 +283,14 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    qsum += x[e];
+                    if (!F32Q) qsum += x[e];
                     split<PARTS>(x[e], part[e]);
+                    if (F32Q) sum0 += part[e][0], rest += x[e] - part[e][0];
+                }
+                if (F32Q) {
+                    sum0 += __shfl_xor(sum0, 16);
+                    sum0 += __shfl_xor(sum0, 32);
+                    centre[k] = -24.0f * sum0, qsum += sum0;
                 }
 #pragma unroll
                 for (int i = 0; i < PARTS; ++i)
@@ -288,8 +298,10 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
                                                                 pack_bf16(part[4][i], part[5][i]), pack_bf16(part[6][i], part[7][i])});
             }
         }
-        qsum += __shfl_xor(qsum, 16);
-        qsum += __shfl_xor(qsum, 32);
+        float &part_sum = F32Q ? rest : qsum;
+        part_sum += __shfl_xor(part_sum, 16);
+        part_sum += __shfl_xor(part_sum, 32);
+        if (F32Q) qsum += rest, rest *= -24.0f;
     }
 
     f32x4 acc[DT];
@@ -299,18 +311,23 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
 
     const auto work = [&](const Codes<D> &x, int32_t t0, int32_t page) {
             const float zero = sign * ((float)x.beta + 16.0f);
-            params[wave][lane] = make_float2(x.alpha * factor, zero);
+            params[wave][lane] = make_float2(x.alpha * factor, F32Q && lane < 32 ? (float)x.beta - 8.0f : zero);
             const bool far = __any(fabsf(zero) > exact); // some - (16 + beta) of a value has more than the 8 bits of a bf16
             __builtin_amdgcn_wave_barrier();
             const float4 *par = reinterpret_cast<const float4 *>(&params[wave][4 * g]); // tokens 16 h + 4 g + i at 8 h + i / 2, values' behind
             float sc[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                f32x4 d = {0.f, 0.f, 0.f, 0.f};
+                f32x4 d = f32x4{1.f, 1.f, 1.f, 1.f} * rest;
 #pragma unroll
-                for (int i = PARTS - 1; i >= 0; --i)
+                for (int i = PARTS - 1; i >= (F32Q ? 1 : 0); --i)
 #pragma unroll
                     for (int k = 0; k < KS; ++k) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes.operand(x.k[h][k]), qo[i][k], d, 0, 0, 0);
+                if (F32Q) { // one rounding for 32 channels, of a sum of (c - 8) q: 16 + c and what is taken off meet in one operation
+#pragma unroll
+                    for (int k = 0; k < KS; ++k)
+                        d += __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes.operand(x.k[h][k]), qo[0][k], f32x4{1.f, 1.f, 1.f, 1.f} * centre[k], 0, 0, 0);
+                }
                 const float4 k0 = par[8 * h], k1 = par[8 * h + 1];
                 const float ka[4] = {k0.x, k0.z, k1.x, k1.z}, kb[4] = {k0.y, k0.w, k1.y, k1.w};
 #pragma unroll
@@ -372,12 +389,21 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
                 low[e] = __builtin_amdgcn_perm(x.v[2 * e + 1], x.v[2 * e], 0x05040100u);
                 high[e] = __builtin_amdgcn_perm(x.v[2 * e + 1], x.v[2 * e], 0x07060302u);
             }
-            // (16 + c) - (16 + beta) in two products: the sums stay as small as the values are, whatever the number of tokens
+            // (16 + c) - (16 + beta) in two products: the sums stay as small as the values are, whatever the number of tokens.
+            // float32, the weights' first parts: 16 tokens' codes and zero points in one operation, which rounds once, what it adds to the
+            // accumulator; the other parts are 2^-8 of it.
             const auto tile = [&](int i, bf16x8 c) {
 #pragma unroll
-                for (int j = PARTS - 1; j >= 0; --j) {
+                for (int j = PARTS - 1; j >= (F32Q ? 1 : 0); --j) {
                     acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(zeros, pw[j], acc[i], 0, 0, 0);
                     acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c, pw[j], acc[i], 0, 0, 0);
+                }
+                if (F32Q) {
+                    const u32x4 w = __builtin_bit_cast(u32x4, c), z = __builtin_bit_cast(u32x4, zeros), p = __builtin_bit_cast(u32x4, pw[0]);
+#pragma unroll
+                    for (int h = 0; h < 4; h += 2)
+                        acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{w[h], w[h + 1], z[h], z[h + 1]}),
+                                                                         __builtin_bit_cast(bf16x8, u32x4{p[h], p[h + 1], p[h], p[h + 1]}), acc[i], 0, 0, 0);
                 }
             };
             const auto four = [&](const uint32_t (&w)[4], int at) {
@@ -574,19 +600,20 @@ QllmKvPrompts plan_prompts(const qllm_kv_cache *cache, const qllm_kv_batch *batc
     return qllm_kv_plan_prompts(*batch, cache->heads, q_heads / cache->heads, cache->dim, batch->table_ld * cache->page_tokens);
 }
 
-// Workgroups of a kv head: as many as the card holds at once (three on each of 256 CUs), but none for less than LEAST steps.
+// Workgroups of a kv head: as many as the card holds at once (on each of 256 CUs three, two for float32 queries, whose parts take
+// registers: 768 there 42.9 against 39.1 us for sixteen single tokens behind 5000), but none for less than LEAST steps.
 struct Launch {
     int64_t numbers, blocks; // of tiles (see number_of); of workgroups
     int64_t marks, parts;    // bytes of the workspace for each kind
 };
-Launch plan(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads)
+Launch plan(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads, int32_t q_dtype)
 {
-    constexpr int64_t RESIDENT = 768;
+    const int64_t resident = q_dtype == QLLM_F32 ? 2 * 256 : 3 * 256;
     const int64_t group = q_heads / cache->heads;
     Launch n;
     n.numbers = batch->row_start ? batch->rows * group / ROWS + batch->n_seqs : batch->n_seqs * ((group + ROWS - 1) / ROWS);
     const int64_t most = n.numbers * (batch->table_ld * cache->page_tokens / STEP + BESIDE) / LEAST + 1; // below 2^31
-    const int64_t blocks = cache->heads < RESIDENT ? RESIDENT / cache->heads : 1;
+    const int64_t blocks = cache->heads < resident ? resident / cache->heads : 1;
     n.blocks = blocks < most ? blocks : most;
     n.marks = n.blocks > 1 ? cache->heads * n.numbers * (int64_t)sizeof(Unfinished) : 0;
     n.parts = n.blocks > 1 ? cache->heads * n.blocks * 2 * ROWS : 0;
@@ -601,7 +628,7 @@ extern "C" int64_t qllm_kv_attention_workspace_bytes(const qllm_kv_cache *cache,
     int32_t rc = prepare_step(cache, batch, false, &s);
     if (rc == QLLM_OK) rc = check(cache, batch, q_heads);
     if (rc != QLLM_OK) return rc;
-    const Launch n = plan(cache, batch, q_heads);
+    const Launch n = plan(cache, batch, q_heads, QLLM_BF16); // no less than for float32
     const int64_t bytes = n.marks + n.parts * (cache->dim + 2) * (int64_t)sizeof(float);
     if (!prompts_pay(cache, batch, q_heads, QLLM_BF16)) return 256 + bytes;
     const int64_t prompts = plan_prompts(cache, batch, q_heads).bytes; // before the others: the same place
@@ -641,7 +668,7 @@ extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq
         rc = qllm_kv_launch_prompts(a, plan_prompts(cache, batch, q_heads), cache->dim, out_dtype, workspace, stream);
         if (rc != QLLM_OK || batch->n_seqs == 1) return rc;
     }
-    const Launch n = plan(cache, batch, q_heads);
+    const Launch n = plan(cache, batch, q_heads, q_dtype);
     a.blocks = (int32_t)n.blocks, a.numbers = n.blocks > 1 ? (int32_t)n.numbers : 0;
     a.unfinished = static_cast<Unfinished *>(workspace);
     a.part_o = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + n.marks);
