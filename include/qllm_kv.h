@@ -92,10 +92,10 @@ int32_t qllm_kv_read(const qllm_kv_cache *cache, const qllm_kv_batch *batch, voi
  *   workspace  16-byte aligned, qllm_kv_attention_workspace_bytes(cache, batch, q_heads) bytes (read on the host: of the
  *            two structs only the sizes); contents undefined afterwards, two calls in flight at once need one each.
  * Equal calls give equal bits.
- * Codes enter the matrix cores as exact bf16 integers; scores, maxima and sums are fp32; with bf16 queries the weights (times a
- * value's alpha) are rounded to bf16 once before they meet the values (half a step: 2^-8 of each at most; in sequences of many
- * rows the same rounded weights are what is summed below the line), with fp32 queries queries and weights are taken in three
- * bf16 parts, 24 bits.  A query that is not finite spoils the output of its own row and head alone.
+ * Codes enter the matrix cores as exact bf16 integers; scores, maxima and sums are fp32.  The weights (times a value's alpha)
+ * meet the values in bf16 parts: with fp32 queries, which come in three parts too, 24 bits; with bf16 queries 2^-16 of each is
+ * left out at most, in sequences of many rows 2^-8 (one part, rounded, which is also what is summed below the line).
+ * A query that is not finite spoils the output of its own row and head alone.
  * In sequences of many rows with bf16 queries a key whose |scale| alpha is below 2^-90 counts as one of 2^-90 (which is nothing
  * for queries below 2^60), and a token whose value's alpha is less than 2^-100 of another's that the query sees may count for
  * less than its share below the line.

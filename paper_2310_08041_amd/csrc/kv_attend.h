@@ -5,7 +5,7 @@
 //     scale alpha (q . (16 + c) - (16 + beta) sum q),
 // the first product on the matrix cores: 16 + c is an exact bf16 whose bits are 0x4180 | c << 3, two vector instructions for a
 // pair of codes.  In the same way sum_t p_t v_t = sum_t (p_t alpha_t)(16 + c_t) - sum_t (p_t alpha_t)(16 + beta_t), with p_t alpha_t
-// rounded to bf16 first and the rounded number used in both sums, which are taken together on the matrix cores.  The scores are
+// in bf16 parts, the same in both sums, which are taken together on the matrix cores.  The scores are
 // formed transposed (tokens x rows): their accumulator then is, register for register, the operand that meets the values, and
 // nothing crosses lanes in between.
 #ifndef QLLM_KV_ATTEND_H

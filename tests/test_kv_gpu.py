@@ -747,3 +747,34 @@ def test_attention_of_prompts_shared_by_workgroups(oracle, b, out_type, heads, g
     want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.1), window)
     worst = np.abs(outs[0].double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, "bf16", out_type)
     assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+@pytest.mark.parametrize("heads,group,dim,lengths,new", [(5, 3, 64, [373, 900, 1400], None), (40, 1, 128, [38, 56, 20], [38, 38, 20]), (8, 8, 128, [62, 15], [59, 2]), (2, 8, 128, [4000], None)])
+def test_float32_attention_is_as_exact_as_float32_arithmetic(oracle, b, heads, group, dim, lengths, new):
+    """The error against 64 bits (norms) is at most twice that of float32 softmax attention on the cache's values themselves, for
+    keys and values without a large common part; the codes' offsets of 16 and the zero points cost no bits."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(40)
+    c = make(rng, heads, group, dim, 64, lengths, new)
+    for i, l in enumerate(lengths):
+        okv.append(c.pages, c.table, [(r, i, r) for r in range(l)], *(rng.standard_normal((l, heads, dim)).astype(np.float32) for _ in range(2)))
+    q = rng.standard_normal((c.rows, heads * group, dim)).astype(np.float32)
+    cache, batch = on_device(b, c)
+    out = torch.empty((c.rows, heads * group * dim), device="cuda")
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1)), cache, 0, batch, dim ** -0.5, out, ws)
+    want = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(dim ** -0.5))[0]
+    plain = np.zeros(want.shape)
+    for i, l in enumerate(lengths):
+        every = b.DeviceKVBatch(l, _t(c.table[i:i + 1]), _t(np.array([l], np.int32)), _t(np.array([0, l], np.int32)))
+        k, v = (torch.empty((l, heads * dim), device="cuda") for _ in range(2))
+        b.qllm_kv_read(cache, 0, every, k, v)
+        k, v = (x.cpu().reshape(l, heads, dim) for x in (k, v))
+        for r, line, p in (t for t in c.tokens if t[1] == i):
+            for o in range(heads * group):
+                s = (k[:p + 1, o // group] @ torch.from_numpy(q[r, o])) * np.float32(dim ** -0.5)
+                plain[r, o] = (torch.softmax(s, 0) @ v[:p + 1, o // group]).numpy()
+    got = out.double().cpu().numpy().reshape(want.shape)
+    off, plain_off = np.linalg.norm(got - want), np.linalg.norm(plain - want)
+    assert off <= 2.0 * plain_off + 2.0 ** -25 * np.linalg.norm(want), (off / plain_off, off / np.linalg.norm(want))
