@@ -56,20 +56,22 @@ __device__ __forceinline__ int32_t page_of(const Step &s, int32_t line, int32_t 
     return page >= 0 && page < s.n_pages ? page : -1;
 }
 
-// The largest i < n_seqs with first(i) <= x for an ascending first, by one wave: 64 candidates per trip to memory.
-// Any answer in [0, n_seqs) where first does not ascend.
+// The largest i < n_seqs with first(i) <= x for an ascending first, by one wave: 64 candidates per trip to memory, then 64 between
+// two of them.  Any answer in [0, n_seqs) where first does not ascend.
 template <class F>
 __device__ __forceinline__ int32_t last_not_above(int32_t n_seqs, int64_t x, F first)
 {
     const int32_t lane = threadIdx.x & 63;
-    int32_t found = 0;
-    for (int32_t base = 0; base < n_seqs; base += 64) {
-        const bool in = base + lane < n_seqs && first(base + lane) <= x;
+    int32_t found = 0, width = n_seqs;
+    for (;;) {
+        const int32_t step = (int32_t)((uint32_t)(width + 63) / 64u);
+        const bool in = lane * step < width && first(found + lane * step) <= x;
         const int32_t count = __popcll(__ballot(in));
-        if (count) found = base + count - 1;
-        if (count < 64) break;
+        const int32_t skipped = count > 1 ? (count - 1) * step : 0;
+        found += skipped;
+        if (step <= 1) return found;
+        width = step < width - skipped ? step : width - skipped;
     }
-    return found;
 }
 
 // Checks shared by the entry points; fills a Step.

@@ -60,42 +60,39 @@ struct Asked {
 };
 
 // Tile `k` of a kv head, from the one with the longest way back on (sequence after sequence, the tiles of a sequence in order, all
-// of it backwards); false: there are no more.  By one wave.
+// of it backwards); false: there is none.  By one wave.  More sequences than it has lanes: their tiles are numbered from
+// row_start * group / PROWS + i on, with gaps, which takes no sum over all of them.
 __device__ __forceinline__ bool tile_at(const AttendArgs &a, int32_t k, Tile *t)
 {
     const Step &s = a.s;
     const int32_t lane = threadIdx.x & 63;
-    const auto tiles_upto = [&](int32_t from, int32_t before) { // a sequence a lane
-        const int32_t i = from + lane, rows = i < s.n_seqs ? (row_of(s, i + 1) - row_of(s, i)) * a.group : 0;
-        int32_t n = rows <= a.few ? 0 : (int32_t)(((uint32_t)rows + PROWS - 1) / PROWS);
-        for (int32_t o = 1; o < 64 && o < s.n_seqs; o <<= 1) {
-            const int32_t y = __shfl_up(n, o);
-            if (lane >= o) n = __builtin_elementwise_add_sat(n, y);
+    int32_t i, number;
+    if (s.n_seqs <= 64) { // a sequence a lane
+        const int32_t rows = lane < s.n_seqs ? (row_of(s, lane + 1) - row_of(s, lane)) * a.group : 0;
+        const int32_t tiles = rows <= a.few ? 0 : (int32_t)(((uint32_t)rows + PROWS - 1) / PROWS);
+        int32_t upto = tiles;
+        for (int32_t o = 1; o < s.n_seqs; o <<= 1) {
+            const int32_t y = __shfl_up(upto, o);
+            if (lane >= o) upto = __builtin_elementwise_add_sat(upto, y);
         }
-        return __builtin_elementwise_add_sat(n, before);
-    };
-    int32_t total = 0, upto = 0;
-    for (int32_t from = 0; from < s.n_seqs; from += 64) {
-        upto = tiles_upto(from, total);
-        total = __builtin_amdgcn_readlane(upto, s.n_seqs - from < 64 ? s.n_seqs - from - 1 : 63);
+        number = __builtin_amdgcn_readlane(upto, s.n_seqs - 1) - 1 - k;
+        if (number < 0) return false;
+        i = __popcll(__ballot(lane < s.n_seqs && upto <= number));
+        i = i < s.n_seqs ? i : s.n_seqs - 1;
+        number -= __builtin_amdgcn_readlane(upto - tiles, i);
+    } else {
+        const auto first = [&](int32_t j) { return (int64_t)row_of(s, j) * a.group / PROWS + j; };
+        number = (int32_t)((int64_t)s.rows * a.group / PROWS) + s.n_seqs - 1 - k;
+        i = last_not_above(s.n_seqs, number, first);
+        number -= (int32_t)first(i);
     }
-    const int32_t number = total - 1 - k;
-    if (number < 0) return false;
-    int32_t i = 0, before = 0;
-    for (int32_t from = 0; from < s.n_seqs; from += 64) {
-        if (s.n_seqs > 64) upto = tiles_upto(from, before);
-        const int32_t skipped = __popcll(__ballot(from + lane < s.n_seqs && upto <= number));
-        if (skipped) before = __builtin_amdgcn_readlane(upto, skipped - 1);
-        i = from + skipped;
-        if (skipped < 64) break;
-    }
-    t->seq = seq_of(s, i < s.n_seqs ? i : s.n_seqs - 1);
+    t->seq = seq_of(s, i);
     t->seq.row = __builtin_amdgcn_readfirstlane(t->seq.row), t->seq.n = __builtin_amdgcn_readfirstlane(t->seq.n); // the same in every lane
     t->seq.line = __builtin_amdgcn_readfirstlane(t->seq.line), t->seq.len = __builtin_amdgcn_readfirstlane(t->seq.len);
     t->rows = t->seq.n * a.group;
-    const int64_t at = (number - before) * (int64_t)PROWS;
+    const int64_t at = __builtin_amdgcn_readfirstlane(number) * (int64_t)PROWS;
     t->first = (int32_t)at;
-    return at >= 0 && at < t->rows; // (not so for a row_start that does not ascend)
+    return at >= 0 && at < t->rows && t->rows > a.few;
 }
 
 // The tiles of tokens that some row of a tile sees, and how many workgroups share them.
