@@ -36,18 +36,21 @@ __device__ __forceinline__ Work work_of(const AttendArgs &a, const Seq &q)
     return w;
 }
 
-// The line as one wave sees it, 64 sequences at a time, one a lane.  Up to 64 are read from memory once and kept in LDS (every
-// wave writes the same there, before it reads).  The host checks that a line stays below 2^31 steps; sums saturate, for a
-// row_start that does not ascend.
+// The line, 64 sequences at a time, one a lane.  Up to LISTED are read from memory once and kept in LDS: by every wave for itself
+// where they are 64 (all write the same there, before they read), else by the workgroup's waves in turn.  The host checks that a
+// line stays below 2^31 steps; sums saturate, for a row_start that does not ascend.  (256 single tokens behind 1000, 8 heads of 8: 84 us,
+// 91 us with every wave reading all sequences again and again.)
+constexpr int LISTED = 512;
 struct Listed {
     Seq seq;
-    int32_t upto; // where it ends in the line
+    int32_t upto; // where it ends in its 64 sequences' part of the line
 };
 struct Line {
-    Listed *list; // [64]
+    Listed *list;      // [LISTED]
+    int32_t *part;     // [LISTED / 64] steps of 64 sequences
     int32_t total;
 
-    static __device__ __forceinline__ Listed look(const AttendArgs &a, int32_t from, int32_t before)
+    static __device__ __forceinline__ Listed look(const AttendArgs &a, int32_t from)
     {
         const int32_t lane = threadIdx.x & 63, i = from + lane;
         Listed x;
@@ -59,38 +62,60 @@ struct Line {
             const int32_t y = __shfl_up(x.upto, o);
             if (lane >= o) x.upto = __builtin_elementwise_add_sat(x.upto, y);
         }
-        x.upto = __builtin_elementwise_add_sat(x.upto, before);
         return x;
     }
-    __device__ __forceinline__ Line(const AttendArgs &a, Listed *room) : list(room), total(0)
+    static __device__ __forceinline__ int32_t last_of(const AttendArgs &a, int32_t from) { return a.s.n_seqs - from < 64 ? a.s.n_seqs - from - 1 : 63; }
+
+    __device__ __forceinline__ Line(const AttendArgs &a, Listed *room, int32_t *parts) : list(room), part(parts), total(0)
     {
-        for (int32_t from = 0; from < a.s.n_seqs; from += 64) {
-            const Listed x = look(a, from, total);
-            if (a.s.n_seqs <= 64) list[threadIdx.x & 63] = x;
-            total = __builtin_amdgcn_readlane(x.upto, a.s.n_seqs - from < 64 ? a.s.n_seqs - from - 1 : 63);
+        const int32_t lane = threadIdx.x & 63, n = a.s.n_seqs;
+        if (n <= 64) {
+            const Listed x = look(a, 0);
+            list[lane] = x;
+            total = __builtin_amdgcn_readlane(x.upto, last_of(a, 0));
+            part[0] = total;
+            __builtin_amdgcn_wave_barrier();
+        } else if (n <= LISTED) {
+            for (int32_t from = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 64; from < n; from += WAVES * 64) {
+                const Listed x = look(a, from);
+                list[from + lane] = x;
+                part[from / 64] = __builtin_amdgcn_readlane(x.upto, last_of(a, from));
+            }
+            __syncthreads();
+            for (int32_t from = 0; from < n; from += 64) total = __builtin_elementwise_add_sat(total, part[from / 64]);
+        } else {
+            for (int32_t from = 0; from < n; from += 64) total = __builtin_elementwise_add_sat(total, __builtin_amdgcn_readlane(look(a, from).upto, last_of(a, from)));
         }
+        total = __builtin_amdgcn_readfirstlane(total);
         if (total == INT32_MAX) total = 0;
-        __builtin_amdgcn_wave_barrier();
     }
     // The sequence that step `at` < total belongs to; *begin: where that begins.
     __device__ __forceinline__ int32_t find(const AttendArgs &a, int32_t at, int32_t *begin) const
     {
-        const int32_t lane = threadIdx.x & 63;
+        const int32_t lane = threadIdx.x & 63, n = a.s.n_seqs;
         int32_t before = 0;
-        for (int32_t from = 0; from < a.s.n_seqs; from += 64) {
-            const int32_t upto = a.s.n_seqs <= 64 ? list[lane].upto : look(a, from, before).upto;
-            const int32_t skipped = __popcll(__ballot(from + lane < a.s.n_seqs && upto <= at)); // sequences that end at or before it
-            if (skipped) before = __builtin_amdgcn_readlane(upto, skipped - 1);
-            if (skipped < 64) {
-                *begin = before;
-                return from + skipped;
+        for (int32_t from = 0; from < n; from += 64) {
+            int32_t upto = 0, steps;
+            if (n <= LISTED) {
+                steps = __builtin_amdgcn_readfirstlane(part[from / 64]);
+            } else {
+                upto = look(a, from).upto;
+                steps = __builtin_amdgcn_readlane(upto, last_of(a, from));
             }
+            if (at - before >= steps) {
+                before += steps;
+                continue;
+            }
+            if (n <= LISTED) upto = list[from + lane].upto;
+            const int32_t skipped = __popcll(__ballot(from + lane < n && upto <= at - before)); // sequences that end at or before it
+            *begin = before + (skipped ? __builtin_amdgcn_readlane(upto, skipped - 1) : 0);
+            return from + skipped;
         }
-        return a.s.n_seqs;
+        return n;
     }
     __device__ __forceinline__ Seq seq(const AttendArgs &a, int32_t i) const
     {
-        const Seq q = a.s.n_seqs <= 64 ? list[i].seq : seq_of(a.s, i);
+        const Seq q = a.s.n_seqs <= LISTED ? list[i].seq : seq_of(a.s, i);
         return Seq{__builtin_amdgcn_readfirstlane(q.row), __builtin_amdgcn_readfirstlane(q.n), __builtin_amdgcn_readfirstlane(q.line),
                    __builtin_amdgcn_readfirstlane(q.len)};
     }
@@ -196,12 +221,13 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
     __shared__ float mrg_m[WAVES][ROWS], mrg_l[WAVES][ROWS], mrg_o[WAVES][ROWS][D + 4];
     // a token's parameters, worked out by one lane and read by sixteen: a key's factor and 16 + beta, a value's alpha and - (16 + beta)
     __shared__ __attribute__((aligned(16))) float2 params[WAVES][64];
-    __shared__ Listed listed[64];
+    __shared__ Listed listed[LISTED];
+    __shared__ int32_t parts[LISTED / 64];
 
     const Step &s = a.s;
     const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int32_t head = blockIdx.y;
-    const Line line(a, listed);
+    const Line line(a, listed, parts);
     const Shares shares(a, line.total);
     const int32_t block = blockIdx.x;
     const int32_t begin = shares.begin(block), end = shares.begin(block + 1);
