@@ -120,30 +120,41 @@ def bench_swiglu(args, w, dev):
 
 def bench_kv(args, dev):
     """The cache beside the layers: one decoding step of --sequences lines of --context tokens, --heads query heads on --kv-heads
-    key/value heads of 128 channels, bfloat16.  A step = qllm_kv_append (rotary positions, the new tokens' keys and values as
-    4-bit codes) and qllm_kv_attention over all of the codes; 144 bytes per token and head against HBM."""
+    key/value heads of 128 channels, bfloat16; the first --shared tokens are one prompt, whose pages all lines share.  A step =
+    qllm_kv_append (rotary positions, the new tokens' keys and values as 4-bit codes) and qllm_kv_attention over all of the codes;
+    144 bytes per token and head against HBM."""
     import numpy as np
     import torch
 
     from paper_2310_08041_amd import binding as b
 
     hq, hk, dim, page, n, ctx = args.heads, args.kv_heads, 128, 64, args.sequences, args.context
+    shared = max(0, min(args.shared, ctx - 1))
     per_line = -(-ctx // page)
-    one = n * per_line * b.qllm_kv_page_bytes(hk, dim, page)
-    layers = max(2, min(32, -(-(768 << 20) // one)))                               # past the last-level cache
+    book = b.KVBook.empty(n, per_line, n * per_line, page)
+    cached = (n * (ctx - shared) + shared) * b.qllm_kv_page_bytes(hk, dim, page) // page
+    layers = max(2, min(32, -(-(768 << 20) // cached)))                            # past the last-level cache
     g = torch.Generator(device=dev).manual_seed(2310)
     cache = b.DeviceKVCache(layers, n * per_line, hk, dim, page)
-    table = torch.randperm(n * per_line, device=dev, generator=g).to(torch.int32).view(n, per_line).contiguous()
     inv_freq = 10000.0 ** (-torch.arange(0, dim, 2, dtype=torch.float64, device=dev) / dim)
-    chunk = 1024
-    for at in range(0, ctx, chunk):                                                # the contexts, chunk by chunk, the same in every layer
-        m = min(chunk, ctx - at)
-        rows = torch.arange(0, n * m + 1, m, dtype=torch.int32, device=dev)
-        batch = b.DeviceKVBatch(n * m, table, torch.full((n,), at + m, dtype=torch.int32, device=dev), rows)
-        k, v = (torch.randn((n * m, hk * dim), device=dev, generator=g).to(torch.bfloat16) for _ in range(2))
-        b.qllm_kv_append(cache, 0, batch, k, v, rope=b.ROPE_HALVES, inv_freq=inv_freq)
-    cache.pages[1:] = cache.pages[0]
-    batch = b.DeviceKVBatch(n, table, torch.full((n,), ctx, dtype=torch.int32, device=dev))
+    upload = lambda a: torch.from_numpy(a.copy()).to(dev)
+
+    def extend(lines, upto):                                                       # contexts, chunk by chunk
+        while book.length[lines[0]] < upto:
+            m = min(1024, upto - int(book.length[lines[0]]))
+            b.qllm_kv_reserve_host(book, lines, [m] * len(lines))
+            rows = torch.arange(0, len(lines) * m + 1, m, dtype=torch.int32, device=dev)
+            batch = b.DeviceKVBatch(len(lines) * m, upload(book.table), upload(book.length), rows, upload(np.asarray(lines, np.int32)))
+            k, v = (torch.randn((len(lines) * m, hk * dim), device=dev, generator=g).to(torch.bfloat16) for _ in range(2))
+            b.qllm_kv_append(cache, 0, batch, k, v, rope=b.ROPE_HALVES, inv_freq=inv_freq)
+
+    if shared:
+        extend([0], shared)
+        b.qllm_kv_copy_pages(cache, *b.qllm_kv_fork_host(book, [0] * (n - 1), list(range(1, n))))
+    extend(list(range(n)), ctx)
+    cache.pages[1:] = cache.pages[0]                                               # the same in every layer
+    table = upload(book.table)
+    batch = b.DeviceKVBatch(n, table, upload(book.length))
     qkv = torch.randn((n, (hq + 2 * hk) * dim), device=dev, generator=g).to(torch.bfloat16)
     q, k, v = qkv.split([hq * dim, hk * dim, hk * dim], 1)
     turned, out = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty((n, hq * dim), dtype=torch.bfloat16, device=dev)
@@ -181,7 +192,8 @@ def bench_kv(args, dev):
         "unit": "GB/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": wall * 1e3 / args.steps,
         "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
         "dtype": "bf16 (4-bit codes, fp32 scores and sums)", "data": "synthetic",
-        "config": {"sequences": n, "context": ctx, "heads": hq, "kv_heads": hk, "dim": dim, "page_tokens": page, "layers": layers,
+        "config": {"sequences": n, "context": ctx, "heads": hq, "kv_heads": hk, "dim": dim, "page_tokens": page, "layers": layers, "shared": shared,
+                   "pages_in_use": int((book.refs > 0).sum()),
                    "warmup_done": {"steps": warm_steps, "gpu_ms": warm_ms}},
         "roofline": {"kernel": "attend_kernel + join_kernel", "bound": "hbm", "achieved": nbytes / t_attend / 1e9, "peak": HBM_PEAK_GBS, "unit": "GB/s",
                      "frac": nbytes / t_attend / 1e9 / HBM_PEAK_GBS, "avg_launch_us": t_attend * 1e6, "algorithmic_bytes": nbytes, "traffic": None},
@@ -339,9 +351,10 @@ def main():
                     help="layer: the hot path (the default, the line the contract asks for); match: the offline "
                          "channel matching of Eq. (5) / Appendix A at the workload's channel count; swiglu: the "
                          "producer of a down projection's input, silu(gate) * up, at the workload's N x C; kv: a decoding "
-                         "step over the 4-bit key/value cache, sized by the next four")
+                         "step over the 4-bit key/value cache, sized by the next five")
     ap.add_argument("--sequences", type=int, default=16)
     ap.add_argument("--context", type=int, default=16000)
+    ap.add_argument("--shared", type=int, default=0, help="tokens of a prompt that all of the sequences continue, in shared pages")
     ap.add_argument("--heads", type=int, default=64)
     ap.add_argument("--kv-heads", type=int, default=8)
     args = ap.parse_args()
