@@ -620,17 +620,19 @@ int32_t check(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_
 }
 
 // Whether the prompts kernel takes sequences of more than FEW_ROWS rows: few tiles of 128 rows leave most of the card to wait for
-// one way through the tokens, beyond what its sharing of them makes good.  One sequence, tiles x tokens, this kernel's us first
-// (D 128): 8 x 4000 29 and 29, 16 x 4000 32 and 30, 32 x 4000 37 and 32, 64 x 4000 58 and 37, 128 x 4000 92 and 55, 128 x 16000 288
-// and 157, 32 x 1000 29 and 30, 64 x 1000 36 and 30, 32 x 300 26 and 20, 32 x 64 20 and 14.  With several sequences this kernel runs
-// beside it, some 7 us if it finds nothing: 8 x 64 rows behind 2000, 32 tiles, 36 and 35 + 7; 8 x 128, 64 tiles, 47 and 37 + 7.
-// FEW_ROWS: sequences x rows, 8 heads, 2000 tokens: 32 x 32 46 and 45, 32 x 64 68 and 47, 32 x 128 114 and 51.
+// one way through the tokens, beyond what its sharing of them makes good; this kernel's time grows with tiles and tokens alike.
+// One sequence, tiles x tokens, this kernel's us first (D 128): 8 x 4000 30 and 30, 8 x 16000 40 and 49, 16 x 1000 26 and 31,
+// 16 x 4000 34 and 30, 16 x 16000 58 and 47, 32 x 1000 30 and 31, 32 x 4000 40 and 32, 64 x 4000 63 and 38, 128 x 4000 101 and 55,
+// 128 x 16000 323 and 160; 32 x 300 27 and 20, 16 x 64 20 and 14.  With several sequences this kernel runs beside it, some 5 us if
+// it finds nothing: 8 x 64 rows behind 2000, 32 tiles, 37 and 35 + 5; 8 x 128, 64 tiles, 48 and 38 + 4.
+// FEW_ROWS: sequences x rows, 8 heads, 2000 tokens: 32 x 32 47 and 47, 32 x 64 71 and 48, 32 x 128 119 and 53.
 // (A grid of 2^32 threads would be refused by the runtime.)
 constexpr int32_t FEW_ROWS = 32;
 bool prompts_pay(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads, int32_t q_dtype)
 {
     const int64_t rows = batch->rows * (q_heads / cache->heads), tiles = rows / 128 * cache->heads, tokens = batch->table_ld * cache->page_tokens;
-    return q_dtype == QLLM_BF16 && batch->row_start && ((batch->n_seqs == 1 ? 24 : 48) - tiles) * tokens <= 16000 &&
+    const int64_t least = batch->n_seqs == 1 ? 16 : 48;
+    return q_dtype == QLLM_BF16 && batch->row_start && (tokens <= 640 || (tiles >= least && tiles * tokens >= 2000 * least)) &&
            rows > batch->n_seqs * FEW_ROWS && (rows / 128 + batch->n_seqs) * cache->heads < (1 << 24);
 }
 QllmKvPrompts plan_prompts(const qllm_kv_cache *cache, const qllm_kv_batch *batch, int64_t q_heads)
