@@ -848,8 +848,13 @@ def qllm_kv_copy_pages(cache, src, dst, stream=None):
         _fail("src and dst must be 1-d arrays of one length")
     if not (cache.device >= 0 and torch.cuda.current_device() == cache.device):
         _check_on_current(pages=cache.pages)
-    _chk(_lib.qllm_kv_copy_pages(_dp(cache.pages), cache.layers, cache.n_pages * cache.page_bytes, cache.n_pages, cache.page_bytes, _hp(src),
-                                 _hp(dst), src.size, _stream(stream)), "qllm_kv_copy_pages")
+    _chk(_lib.qllm_kv_copy_pages(_dp(cache.pages), cache.layers, cache.n_pages * cache.page_bytes, cache.n_pages, cache.page_bytes, _host_at(src),
+                                 _host_at(dst), src.size, _stream(stream)), "qllm_kv_copy_pages")
+
+
+def _host_at(a):
+    """The address of a contiguous host array (numpy's own way takes three times as long, and a fork is host time)."""
+    return C.addressof(C.c_char.from_buffer(a)) if a.size and a.flags.writeable else a.ctypes.data
 
 
 class KVBook:
@@ -863,7 +868,7 @@ class KVBook:
         if length.size != table.shape[0]:
             _fail(f"length must hold one entry per line of the table ({table.shape[0]})")
         self.page_tokens, self.table, self.length, self.refs = int(page_tokens), table, length, refs
-        self.c = _KVBook(self.page_tokens, table.shape[0], table.shape[1], refs.size, _hp(table), _hp(length), _hp(refs))
+        self.c = _KVBook(self.page_tokens, table.shape[0], table.shape[1], refs.size, _host_at(table), _host_at(length), _host_at(refs))
 
     @classmethod
     def empty(cls, lines, pages_per_line, n_pages, page_tokens):
@@ -881,7 +886,7 @@ def qllm_kv_reserve_host(book, slots, counts):
     """Room for counts[i] more tokens in line slots[i]."""
     slots = _host_list(slots, "slots")
     counts = _host_list(counts, "counts", slots.size)
-    _chk(_lib.qllm_kv_reserve_host(C.byref(book.c), _hp(slots), _hp(counts), slots.size), "qllm_kv_reserve_host")
+    _chk(_lib.qllm_kv_reserve_host(C.byref(book.c), _host_at(slots), _host_at(counts), slots.size), "qllm_kv_reserve_host")
 
 
 def qllm_kv_fork_host(book, parents, children):
@@ -889,8 +894,8 @@ def qllm_kv_fork_host(book, parents, children):
     parents = _host_list(parents, "parents")
     children = _host_list(children, "children", parents.size)
     copies = np.empty((2, parents.size), np.int32)
-    at = _hp(copies)
-    n = int(_lib.qllm_kv_fork_host(C.byref(book.c), _hp(parents), _hp(children), parents.size, at, at + 4 * parents.size))
+    at = _host_at(copies)
+    n = int(_lib.qllm_kv_fork_host(C.byref(book.c), _host_at(parents), _host_at(children), parents.size, at, at + 4 * parents.size))
     _chk(n if n < 0 else 0, "qllm_kv_fork_host")
     return copies[0, :n], copies[1, :n]
 
@@ -898,13 +903,13 @@ def qllm_kv_fork_host(book, parents, children):
 def qllm_kv_free_host(book, slots):
     """Empties the lines."""
     slots = _host_list(slots, "slots")
-    _chk(_lib.qllm_kv_free_host(C.byref(book.c), _hp(slots), slots.size), "qllm_kv_free_host")
+    _chk(_lib.qllm_kv_free_host(C.byref(book.c), _host_at(slots), slots.size), "qllm_kv_free_host")
 
 
 def qllm_kv_compact_host(book):
     """Moves the pages in use together; returns (src, dst), the pages to copy."""
     moves = np.empty((2, book.refs.size), np.int32)
-    at = _hp(moves)
+    at = _host_at(moves)
     n = int(_lib.qllm_kv_compact_host(C.byref(book.c), at, at + 4 * book.refs.size))
     _chk(n if n < 0 else 0, "qllm_kv_compact_host")
     return moves[0, :n], moves[1, :n]
