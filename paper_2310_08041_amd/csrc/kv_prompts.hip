@@ -68,7 +68,9 @@ __device__ __forceinline__ bool tile_at(const AttendArgs &a, int32_t k, Tile *t)
     const int32_t lane = threadIdx.x & 63;
     int32_t i, number;
     if (s.n_seqs <= 64) { // a sequence a lane
-        const int32_t rows = lane < s.n_seqs ? (row_of(s, lane + 1) - row_of(s, lane)) * a.group : 0;
+        Seq mine = {0, 0, -1, 0};
+        if (lane < s.n_seqs) mine = seq_of(s, lane);
+        const int32_t rows = mine.n * a.group;
         const int32_t tiles = rows <= a.few ? 0 : (int32_t)(((uint32_t)rows + PROWS - 1) / PROWS);
         int32_t upto = tiles;
         for (int32_t o = 1; o < s.n_seqs; o <<= 1) {
@@ -80,15 +82,17 @@ __device__ __forceinline__ bool tile_at(const AttendArgs &a, int32_t k, Tile *t)
         i = __popcll(__ballot(lane < s.n_seqs && upto <= number));
         i = i < s.n_seqs ? i : s.n_seqs - 1;
         number -= __builtin_amdgcn_readlane(upto - tiles, i);
+        t->seq = Seq{__builtin_amdgcn_readlane(mine.row, i), __builtin_amdgcn_readlane(mine.n, i), __builtin_amdgcn_readlane(mine.line, i),
+                     __builtin_amdgcn_readlane(mine.len, i)};
     } else {
         const auto first = [&](int32_t j) { return (int64_t)row_of(s, j) * a.group / PROWS + j; };
         number = (int32_t)((int64_t)s.rows * a.group / PROWS) + s.n_seqs - 1 - k;
         i = last_not_above(s.n_seqs, number, first);
         number -= (int32_t)first(i);
+        const Seq q = seq_of(s, i); // the same in every lane
+        t->seq = Seq{__builtin_amdgcn_readfirstlane(q.row), __builtin_amdgcn_readfirstlane(q.n), __builtin_amdgcn_readfirstlane(q.line),
+                     __builtin_amdgcn_readfirstlane(q.len)};
     }
-    t->seq = seq_of(s, i);
-    t->seq.row = __builtin_amdgcn_readfirstlane(t->seq.row), t->seq.n = __builtin_amdgcn_readfirstlane(t->seq.n); // the same in every lane
-    t->seq.line = __builtin_amdgcn_readfirstlane(t->seq.line), t->seq.len = __builtin_amdgcn_readfirstlane(t->seq.len);
     t->rows = t->seq.n * a.group;
     const int64_t at = __builtin_amdgcn_readfirstlane(number) * (int64_t)PROWS;
     t->first = (int32_t)at;
@@ -171,34 +175,6 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
     const int32_t w_last = t.seq.len - t.seq.n + tok0 + (int32_t)a.by_group.divide((uint32_t)(head0 + wave * 32 + (wave_rows > 0 ? wave_rows - 1 : 0)));
     const int32_t some_lo = lo_at(a, w_first), some_hi = wave_rows > 0 ? hi_at(v.limit, w_last) : -1;
     const int32_t each_lo = lo_at(a, w_last), each_hi = hi_at(v.limit, w_first);
-
-    // queries: element e of step k of lane half h is channel 16 k + 8 h + {0, 4, 1, 5, 2, 6, 3, 7}[e]; behind them the parts of their sum
-    bf16x8 q[KSTEPS], qz;
-    {
-        const int64_t from = (int64_t)(t.seq.row + token) * a.ldq + (head * a.group + head_of_row) * D + 8 * h;
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < KSTEPS; ++i) {
-            uint32_t d[4] = {0, 0, 0, 0};
-            const uint16_t *src = static_cast<const uint16_t *>(a.q) + from + 16 * i;
-            if (real && a.q_vec) {
-                const uint4 w = *reinterpret_cast<const uint4 *>(src);
-                d[0] = w.x, d[1] = w.y, d[2] = w.z, d[3] = w.w;
-            } else if (real) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) d[e] = src[2 * e] | (uint32_t)src[2 * e + 1] << 16;
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum += __uint_as_float(d[e] << 16) + __uint_as_float(d[e] & 0xffff0000u);
-            q[i] = __builtin_bit_cast(bf16x8, u32x4{__builtin_amdgcn_perm(d[2], d[0], 0x05040100u), __builtin_amdgcn_perm(d[2], d[0], 0x07060302u),
-                                                    __builtin_amdgcn_perm(d[3], d[1], 0x05040100u), __builtin_amdgcn_perm(d[3], d[1], 0x07060302u)});
-        }
-        sum += __shfl_xor(sum, 32);
-        float part[3];
-        split<3>(sum, part); // z, z, z, z', z', z', z'', z'' | z'' meet q, q', q'', q, q', q'', q, q' | q'', three parts more a one
-        qz = h == 0 ? __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part[0], part[1]), pack_bf16(part[2], part[0]), pack_bf16(part[1], part[2]), pack_bf16(part[0], part[1])})
-                    : __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part[2], 1.0f), pack_bf16(1.0f, 1.0f), 0, 0});
-    }
 
     // page numbers of up to 64 blocks of 32 tokens, one a lane
     const int32_t tile_begin = span.begin + (int32_t)((int64_t)(span.end - span.begin) * part / span.parts);
@@ -288,6 +264,38 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
             put(3, u32x4{codes.pair<3>(pair[0]), codes.pair<3>(pair[1]), codes.pair<3>(pair[2]), codes.pair<3>(pair[3])});
         }
     };
+
+    Asked<D> asked;
+    int32_t page[2], next[2], later[2];
+    ask(tile_begin + group, asked, page); // on its way while the queries come
+
+    // queries: element e of step k of lane half h is channel 16 k + 8 h + {0, 4, 1, 5, 2, 6, 3, 7}[e]; behind them the parts of their sum
+    bf16x8 q[KSTEPS], qz;
+    {
+        const int64_t from = (int64_t)(t.seq.row + token) * a.ldq + (head * a.group + head_of_row) * D + 8 * h;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KSTEPS; ++i) {
+            uint32_t d[4] = {0, 0, 0, 0};
+            const uint16_t *src = static_cast<const uint16_t *>(a.q) + from + 16 * i;
+            if (real && a.q_vec) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(src);
+                d[0] = w.x, d[1] = w.y, d[2] = w.z, d[3] = w.w;
+            } else if (real) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[e] = src[2 * e] | (uint32_t)src[2 * e + 1] << 16;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += __uint_as_float(d[e] << 16) + __uint_as_float(d[e] & 0xffff0000u);
+            q[i] = __builtin_bit_cast(bf16x8, u32x4{__builtin_amdgcn_perm(d[2], d[0], 0x05040100u), __builtin_amdgcn_perm(d[2], d[0], 0x07060302u),
+                                                    __builtin_amdgcn_perm(d[3], d[1], 0x05040100u), __builtin_amdgcn_perm(d[3], d[1], 0x07060302u)});
+        }
+        sum += __shfl_xor(sum, 32);
+        float part[3];
+        split<3>(sum, part); // z, z, z, z', z', z', z'', z'' | z'' meet q, q', q'', q, q', q'', q, q' | q'', three parts more a one
+        qz = h == 0 ? __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part[0], part[1]), pack_bf16(part[2], part[0]), pack_bf16(part[1], part[2]), pack_bf16(part[0], part[1])})
+                    : __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part[2], 1.0f), pack_bf16(1.0f, 1.0f), 0, 0});
+    }
 
     // Row (i & 3) + 8 (i >> 2) + 4 h of the shared product is element i of a lane: both halves find the values' zero points in
     // elements 0..2 and the sum of the weights in 3..5.
@@ -404,9 +412,6 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
         }
     };
 
-    Asked<D> asked;
-    int32_t page[2], next[2], later[2];
-    ask(tile_begin + group, asked, page);
     lay_params(asked, 0);
     lay_codes(asked, 0);
     ask(tile_begin + group + GROUPS, asked, next); // past the last: page 0, dropped
