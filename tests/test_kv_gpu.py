@@ -778,3 +778,57 @@ def test_float32_attention_is_as_exact_as_float32_arithmetic(oracle, b, heads, g
     got = out.double().cpu().numpy().reshape(want.shape)
     off, plain_off = np.linalg.norm(got - want), np.linalg.norm(plain - want)
     assert off <= 2.0 * plain_off + 2.0 ** -25 * np.linalg.norm(want), (off / plain_off, off / np.linalg.norm(want))
+
+
+def test_append_read_and_copies_on_a_stream_and_in_a_graph(oracle, b):
+    """A stream given by hand and the current one, then one graph of append, copy and read whose inputs change between the replays:
+    the graph keeps the list of pages that it was captured with."""
+    import torch
+    rng = np.random.default_rng(41)
+    heads, dim, page = 3, 64, 32
+    c = make(rng, heads, 2, dim, page, [40, 70], [40, 70], filled=False, spare=8)
+    used = c.table[c.table >= 0]
+    free = np.setdiff1d(np.arange(c.n_pages), used)
+    src, dst = used[:4].copy(), free[:4].astype(np.int32)
+    f = _t(10000.0 ** (-np.arange(0, dim, 2) / dim))
+    k, v, k_out = (torch.zeros((c.rows, heads * dim), dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    fresh = lambda: [t.copy_(_t(rng.standard_normal(t.shape).astype(np.float32))) for t in (k, v)]
+
+    def step(ca, ba, out, s=None):
+        b.qllm_kv_append(ca, 0, ba, k, v, rope=1, inv_freq=f, stream=s)
+        b.qllm_kv_copy_pages(ca, src, dst, stream=s)
+        b.qllm_kv_read(ca, 0, ba, out, stream=s)
+
+    def same(x, y):
+        torch.cuda.synchronize()
+        (torch.randn(1000, device="cuda") * 2).sum().item()
+        assert torch.equal(x[0].pages, y[0].pages) and torch.equal(x[1], y[1])
+        pages = x[0].pages[0].cpu().numpy()
+        assert np.array_equal(pages[dst], pages[src])
+
+    fresh()
+    eager, ebatch = on_device(b, c)
+    want = torch.zeros_like(k_out)
+    step(eager, ebatch, want)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    other, obatch = on_device(b, c)
+    torch.cuda.synchronize()
+    step(other, obatch, k_out, side)
+    same((other, k_out), (eager, want))
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        step(other, obatch, k_out)
+    kept = src.copy()
+    for _ in range(3):
+        fresh()
+        k_out.zero_()
+        torch.cuda.synchronize()
+        src[:] = -1                                            # the caller's list may change once the call is back
+        with torch.cuda.stream(side):
+            g.replay()
+        torch.cuda.synchronize()
+        src[:] = kept
+        step(eager, ebatch, want)
+        same((other, k_out), (eager, want))
