@@ -125,6 +125,23 @@ __device__ __forceinline__ void split(float x, float (&part)[PARTS])
     }
 }
 
+// Eight of them: the high halves as they are, what they leave out in the next part, rounded in the last.
+template <int PARTS>
+__device__ __forceinline__ void split8(float (&x)[8], bf16x8 (&part)[PARTS])
+{
+#pragma unroll
+    for (int j = 0; j < PARTS; ++j) {
+        u32x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x0 = __float_as_uint(x[2 * e]), x1 = __float_as_uint(x[2 * e + 1]);
+            y[e] = j == PARTS - 1 ? pack_bf16(x[2 * e], x[2 * e + 1]) : __builtin_amdgcn_perm(x1, x0, 0x07060302u);
+            x[2 * e] -= __uint_as_float(x0 & 0xffff0000u), x[2 * e + 1] -= __uint_as_float(x1 & 0xffff0000u);
+        }
+        part[j] = __builtin_bit_cast(bf16x8, y);
+    }
+}
+
 __device__ __forceinline__ float quotient(float o, float sum) { return sum > 0.0f ? o / sum : (sum == 0.0f ? 0.0f : sum); } // a NaN stays
 
 } // namespace qllm_kv_detail

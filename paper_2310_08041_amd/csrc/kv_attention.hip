@@ -298,8 +298,7 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
         } else {
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                float x[8], part[8][PARTS];
-                float sum0 = 0.0f;
+                float x[8], sum0 = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = 0.0f;
                 if (F32Q && real && a.q_vec) {
@@ -310,21 +309,23 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] = load1<F32Q>(a.q, from + 8 * k + (e >> 1) + 4 * (e & 1));
                 }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (!F32Q) qsum += x[e];
-                    split<PARTS>(x[e], part[e]);
-                    if (F32Q) sum0 += part[e][0], rest += x[e] - part[e][0];
-                }
                 if (F32Q) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float high = __uint_as_float(__float_as_uint(x[e]) & 0xffff0000u);
+                        sum0 += high, rest += x[e] - high;
+                    }
                     sum0 += __shfl_xor(sum0, 16);
                     sum0 += __shfl_xor(sum0, 32);
                     centre[k] = -24.0f * sum0, qsum += sum0;
-                }
+                } else {
 #pragma unroll
-                for (int i = 0; i < PARTS; ++i)
-                    qo[i][k] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(part[0][i], part[1][i]), pack_bf16(part[2][i], part[3][i]),
-                                                                pack_bf16(part[4][i], part[5][i]), pack_bf16(part[6][i], part[7][i])});
+                    for (int e = 0; e < 8; ++e) qsum += x[e];
+                }
+                bf16x8 part[PARTS];
+                split8<PARTS>(x, part);
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i) qo[i][k] = part[i];
             }
         }
         float &part_sum = F32Q ? rest : qsum;
@@ -407,20 +408,10 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
                 l += p;
                 w[i] = p * va[i];
             }
-            // in bf16 parts: the high halves as they are, what they leave out in the next, rounded in the last: 2^-16 of a weight at most
-            // for bf16 queries (one part, 2^-8, makes a bf16 output's error 1.4 times as large and saves 3 % of the time), 24 bits for float32
+            // in bf16 parts, which leave out 2^-16 of a weight at most for bf16 queries (one part, 2^-8, makes a bf16 output's error
+            // 1.4 times as large and saves 3 % of the time) and hold 24 bits for float32
             bf16x8 pw[WPARTS];
-#pragma unroll
-            for (int j = 0; j < WPARTS; ++j) {
-                u32x4 y;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t w0 = __float_as_uint(w[2 * e]), w1 = __float_as_uint(w[2 * e + 1]);
-                    y[e] = j == WPARTS - 1 ? pack_bf16(w[2 * e], w[2 * e + 1]) : __builtin_amdgcn_perm(w1, w0, 0x07060302u);
-                    w[2 * e] -= __uint_as_float(w0 & 0xffff0000u), w[2 * e + 1] -= __uint_as_float(w1 & 0xffff0000u);
-                }
-                pw[j] = __builtin_bit_cast(bf16x8, y);
-            }
+            split8<WPARTS>(w, pw);
             uint32_t low[4], high[4]; // codes 0..3 and 4..7 of two neighbouring tokens
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
