@@ -477,8 +477,8 @@ __global__ __launch_bounds__(WAVES * 64, F32Q ? 2 : 3) void attend_kernel(const 
         for (int32_t n = 0; n < count;) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int32_t next = n + 1 < count ? __builtin_amdgcn_readlane(pages, n + 1) : -1, t0 = (first + n * WAVES) * STEP;
-                from.ask(s, head, next, t0 + WAVES * STEP, x[1 - i]);
+                const int32_t next = n + 1 < count ? __builtin_amdgcn_readlane(pages, n + 1) : -1, t0 = (int32_t)((uint32_t)(first + n * WAVES) * STEP);
+                from.ask(s, head, next, (int32_t)((uint32_t)t0 + WAVES * STEP), x[1 - i]);
                 if (n < count) work(x[i], t0, page);
                 page = next, ++n;
             }

@@ -6,6 +6,7 @@
 
 #include <stdint.h>
 
+#include "kv_index.h"
 #include "qllm_kv.h"
 
 extern "C" void qllm_note_hip_error(const char *step, const char *name);
@@ -47,11 +48,11 @@ __device__ __forceinline__ Seq seq_of(const Step &s, int32_t i)
     return q;
 }
 
-// The page of position p >= 0 of a line, -1 where it is not there.
+// The page of position p of a line, -1 where it is not there (any p).
 __device__ __forceinline__ int32_t page_of(const Step &s, int32_t line, int32_t p)
 {
-    const int32_t k = p >> s.page_shift;
-    if (line < 0 || k >= s.table_ld) return -1;
+    const int32_t k = entry_of(p, s.page_shift, s.table_ld);
+    if (line < 0 || k < 0) return -1;
     const int32_t page = s.table[(int64_t)line * s.table_ld + k];
     return page >= 0 && page < s.n_pages ? page : -1;
 }

@@ -34,6 +34,7 @@ using namespace qllm_kv_detail;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int PROWS = 128, TILE = 64, WAVES = 4, THREADS = WAVES * 64; // rows of a workgroup, tokens of a tile, waves of a group
+static_assert(TILE == 1 << 6, "tiles are compared by shifts");
 constexpr int TOGETHER = 4; // tiles between two additions of the zero points' sums
 constexpr int LEAST = 8;    // tiles of tokens of a part
 
@@ -180,10 +181,7 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
     const int32_t tile_begin = span.begin + (int32_t)((int64_t)(span.end - span.begin) * part / span.parts);
     const int32_t tile_end = span.begin + (int32_t)((int64_t)(span.end - span.begin) * (part + 1) / span.parts);
     int32_t listed = tile_begin; // the first tile of the list
-    const auto pages_from = [&](int32_t tile) {
-        const int32_t p = tile * TILE + 32 * lane;
-        return p <= v.all_hi ? page_of(s, t.seq.line, p) : -1;
-    };
+    const auto pages_from = [&](int32_t tile) { return page_of(s, t.seq.line, block_begin(tile * (TILE / 32) + lane, v.all_hi)); };
     int32_t pages = pages_from(listed);
 
     const int32_t P = 1 << s.page_shift;
@@ -195,7 +193,7 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
         if (tile - listed >= 32) listed = tile, pages = pages_from(tile);
 #pragma unroll
         for (int b = 0; b < 2; ++b) page[b] = tile < tile_end ? __builtin_amdgcn_readlane(pages, 2 * (tile - listed) + b) : -1;
-        const int32_t t0 = tile * TILE;
+        const int32_t t0 = (int32_t)((uint32_t)tile * TILE); // (a tile behind the longest line's end begins at 2^31: only its place in a page counts)
         {
             const int32_t tok = t0 + k_tok; // its block is the same for the whole wave
             const uint8_t *part = part_of(k_tok < 32 ? page[0] : page[1]);
@@ -425,7 +423,7 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
         };
         if (GROUPS > 1 && group == 1) lay();
         __builtin_amdgcn_s_setprio(1); // laying a tile out gives way to the work of the CU's other waves (1184 -> 1139 us for 2000 tokens behind 14000)
-        if (tile * TILE <= some_hi && tile * TILE + TILE - 1 >= some_lo) work(tile, b, i % TOGETHER == TOGETHER - 1, page);
+        if (tile <= some_hi >> 6 && tile >= some_lo >> 6) work(tile, b, i % TOGETHER == TOGETHER - 1, page);
         __builtin_amdgcn_s_setprio(0);
         if (GROUPS == 1 || group == 0) lay();
         page[0] = next[0], page[1] = next[1], next[0] = later[0], next[1] = later[1];

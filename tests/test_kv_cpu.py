@@ -1,6 +1,8 @@
 """The 4-bit key/value cache without a GPU: refusals of every entry point before anything is launched, the book of pages against a
 plain Python one, and pins of the numpy statement that the device tests compare with."""
 import ctypes as C
+import os
+import subprocess
 import types
 
 import numpy as np
@@ -342,3 +344,40 @@ def test_limits_of_a_step():
     assert bytes_for(1 << 15) > 0 and bytes_for(1 << 16) == SHAPE
     assert bytes_for(64, rows=(1 << 22) - 64, row_start=A) > 0 and bytes_for(64, rows=1 << 22, row_start=A) == SHAPE     # 2^23 tiles of 16 rows
     assert bytes_for(4, rows=1 << 21, row_start=A, n_slots=8, ld=1 << 14) == SHAPE                                 # 2^31 steps of 32 tokens
+
+
+# ---------------------------------------------------------------- index arithmetic of the kernels, compiled for the host
+
+@pytest.fixture(scope="module")
+def index(tmp_path_factory):
+    """csrc/kv_index.h as a host library."""
+    here = tmp_path_factory.mktemp("kv_index")
+    (here / "index.cpp").write_text('''#include "kv_index.h"
+using namespace qllm_kv_detail;
+extern "C" int32_t entry(int32_t p, int32_t shift, int32_t ld) { return entry_of(p, shift, ld); }
+extern "C" int32_t block(int32_t b, int32_t last) { return block_begin(b, last); }
+''')
+    csrc = os.path.join(os.path.dirname(b.__file__), "csrc")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-I", csrc, str(here / "index.cpp"), "-o", str(here / "index.so")], check=True)
+    return C.CDLL(str(here / "index.so"))
+
+
+@pytest.mark.parametrize("page", [32, 64, 128, 256])
+def test_table_entries_stay_in_their_line_up_to_the_last_position(index, page):
+    """The lists of page numbers that the prompts kernel makes (64 blocks of 32 tokens from a tile of 64 on, two tiles and more ahead of
+    the last): every entry lies in the line, is that of the block, and blocks behind the last position have none."""
+    shift, ld = page.bit_length() - 1, (2 ** 31 - 1) // page
+    top = ld * page
+    for last in (-1, 0, 31, 32, top - 1, top - 33, top - 2016, top - 2017, top - 4096):
+        for tile in {0, 1, max(last, 0) // 64 - 32, max(last, 0) // 64 - 1, max(last, 0) // 64, max(last, 0) // 64 + 4, (2 ** 31 - 1) // 64}:
+            if tile < 0:
+                continue
+            for lane in range(64):
+                want = (tile * 2 + lane) * 32                                # exact: no 32 bits here
+                p = index.block(tile * 2 + lane, last)
+                assert p == (want if want <= last else -1), (last, tile, lane)
+                k = index.entry(p, shift, ld)
+                assert k == (want // page if want <= last else -1), (last, tile, lane)
+    for p in (-1, -32, -page, -2 ** 31, -2 ** 31 + 1, -2016):
+        assert index.entry(p, shift, ld) == -1 and index.entry(p, shift, 1) == -1
+    assert index.entry(top - 1, shift, ld) == ld - 1 and index.entry(2 ** 31 - 1, shift, ld - 1) == -1 and index.entry(page, shift, 1) == -1

@@ -832,3 +832,30 @@ def test_append_read_and_copies_on_a_stream_and_in_a_graph(oracle, b):
         src[:] = kept
         step(eager, ebatch, want)
         same((other, k_out), (eager, want))
+
+
+@pytest.mark.parametrize("heads,group,new,window", [(8, 16, 30, 700), (8, 160, 3, 2200), (1, 3, 5, 700)])
+def test_attention_at_the_last_positions_that_a_line_can_have(oracle, b, heads, group, new, window):
+    """A line of 2^31 tokens less a few, of which the last pages are there: what its newest queries see is what they see in a short line
+    that ends in the same way."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(43)
+    dim, page, tokens = 64, 256, 2500
+    hq = heads * group
+    c = make(rng, heads, group, dim, page, [tokens], [new], extra_cols=0)
+    columns = (2 ** 31 - 1) // page
+    far = torch.full((2, columns), -1, dtype=torch.int32, device="cuda")       # two lines: nothing of the first may be found
+    far[0] = 0
+    far[1, columns - c.table.shape[1]:] = _t(c.table[0])
+    length = columns * page - (c.table.shape[1] * page - tokens)
+    q = _bf16(rng.standard_normal((new, hq, dim)).astype(np.float32))
+    cache, _ = on_device(b, c)
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    batch = b.DeviceKVBatch(new, far, i32(7, length), i32(0, new), i32(1))
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, hq), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    out = torch.full((new, hq * dim), 5.0, device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(new, -1), torch.bfloat16), cache, 0, batch, 0.125, out, ws, window=window)
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.125), window)
+    worst = np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, "bf16", "f32")
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
