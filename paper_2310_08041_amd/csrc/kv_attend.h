@@ -89,7 +89,7 @@ struct Sight {
     int32_t limit, all_lo, all_hi, each_lo, each_hi;
 };
 
-__device__ __forceinline__ int32_t lo_at(const AttendArgs &a, int32_t pos) { return a.window > 0 && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0; }
+__device__ __forceinline__ int32_t lo_at(const AttendArgs &a, int32_t pos) { return first_seen(pos, a.window); }
 __device__ __forceinline__ int32_t hi_at(int32_t limit, int32_t pos) { return pos < limit ? pos : limit - 1; }
 __device__ __forceinline__ int32_t limit_of(const AttendArgs &a, const Seq &q)
 {

@@ -24,6 +24,10 @@ QLLM_KV_INDEX int32_t entry_of(int32_t p, int32_t page_shift, int32_t table_ld)
 // that reach beyond the longest line ask for blocks that begin at 2^31 and later.)
 QLLM_KV_INDEX int32_t block_begin(int32_t block, int32_t last) { return block >= 0 && block <= last >> 5 ? block * 32 : -1; }
 
+// The first position that a query at position pos sees: 0, or with window > 0 the first of the newest `window`.  (Compared before
+// subtracted: pos may be as low as -2^24, the window as large as 2^31 - 1.)
+QLLM_KV_INDEX int32_t first_seen(int32_t pos, int32_t window) { return window > 0 && pos >= window ? pos - window + 1 : 0; }
+
 } // namespace qllm_kv_detail
 
 #endif

@@ -355,6 +355,7 @@ def index(tmp_path_factory):
     (here / "index.cpp").write_text('''#include "kv_index.h"
 using namespace qllm_kv_detail;
 extern "C" int32_t entry(int32_t p, int32_t shift, int32_t ld) { return entry_of(p, shift, ld); }
+extern "C" int32_t first(int32_t pos, int32_t window) { return first_seen(pos, window); }
 extern "C" int32_t block(int32_t b, int32_t last) { return block_begin(b, last); }
 ''')
     csrc = os.path.join(os.path.dirname(b.__file__), "csrc")
@@ -381,3 +382,12 @@ def test_table_entries_stay_in_their_line_up_to_the_last_position(index, page):
     for p in (-1, -32, -page, -2 ** 31, -2 ** 31 + 1, -2016):
         assert index.entry(p, shift, ld) == -1 and index.entry(p, shift, 1) == -1
     assert index.entry(top - 1, shift, ld) == ld - 1 and index.entry(2 ** 31 - 1, shift, ld - 1) == -1 and index.entry(page, shift, 1) == -1
+
+
+def test_first_token_of_a_window_at_the_ends_of_its_range(index):
+    """Rows before the first token, and windows up to the largest (a common way to say "none"), do not wrap around."""
+    edges = [0, 1, 2, 3, 31, 32, 1000, 2 ** 24 - 1, 2 ** 24, 2 ** 30, 2 ** 31 - 2 ** 24, 2 ** 31 - 3, 2 ** 31 - 2, 2 ** 31 - 1]
+    for pos in edges + [-e for e in edges if e <= 2 ** 24]:
+        for window in edges:
+            want = max(0, pos - window + 1) if window else 0
+            assert index.first(pos, window) == want, (pos, window)

@@ -859,3 +859,25 @@ def test_attention_at_the_last_positions_that_a_line_can_have(oracle, b, heads, 
     want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.125), window)
     worst = np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, "bf16", "f32")
     assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 2 ** 24, 1 << 40])
+@pytest.mark.parametrize("q_type,heads,group,lengths,new", [("bf16", 1, 2, [5, 40], [12, 3]), ("f32", 1, 3, [70], [90]), ("bf16", 16, 8, [100], [140]),
+                                                            ("bf16", 32, 4, [100, 129], [129, 129])])
+def test_a_window_larger_than_any_line_with_rows_before_the_first_token(oracle, b, q_type, heads, group, lengths, new, window):
+    """The largest windows are no window, also where a sequence has more new rows than tokens."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(44)
+    c = make(rng, heads, group, 64, 32, lengths, new)
+    hq = heads * group
+    q = rng.standard_normal((c.rows, hq, 64)).astype(np.float32)
+    q = _bf16(q) if q_type == "bf16" else q
+    cache, batch = on_device(b, c)
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, hq), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    qd = _t(q.reshape(c.rows, -1), torch.bfloat16 if q_type == "bf16" else torch.float32)
+    outs = [b.qllm_kv_attention(qd, cache, 0, batch, 0.125, torch.full((c.rows, hq * 64), 5.0, device="cuda"), ws, window=w) for w in (window, 0)]
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.125), window)
+    worst = np.abs(outs[0].double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, q_type, "f32")
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+    assert torch.equal(*outs) and (outs[0] != 0).any()
