@@ -69,7 +69,7 @@ def rows_of(rows, row_start, slot, length):
         r0, r1 = (row_start[i], row_start[i + 1]) if row_start is not None else (i, i + 1)
         line = slot[i] if slot is not None else i
         for r in range(r0, r1):
-            out.append((r, int(line), int(length[line]) - r1 + r if 0 <= line < len(length) else -1))
+            out.append((int(r), int(line), int(length[line]) - int(r1) + int(r) if 0 <= line < len(length) else -1))
     return out
 
 

@@ -391,3 +391,18 @@ def test_first_token_of_a_window_at_the_ends_of_its_range(index):
         for window in edges:
             want = max(0, pos - window + 1) if window else 0
             assert index.first(pos, window) == want, (pos, window)
+
+
+def test_statement_of_attention_with_the_largest_windows():
+    """Positions are exact whatever the arrays' type: a window that no line reaches is no window, for rows before the first token too."""
+    rng = np.random.default_rng(6)
+    pages = okv.Pages(np.zeros((1, 32 * 80), np.uint8), 1, 64, 32)
+    table, length, start = np.zeros((1, 1), np.int32), np.array([4], np.int32), np.array([0, 9], np.int32)
+    tok = okv.rows_of(9, start, None, length)
+    assert [p for _, _, p in tok] == list(range(-5, 4)) and all(type(p) is int for _, _, p in tok)
+    k, v = (rng.standard_normal((9, 1, 64)).astype(np.float32) for _ in range(2))
+    okv.append(pages, table, tok, k, v)
+    q = rng.standard_normal((9, 2, 64)).astype(np.float32)
+    want = okv.attention(q, pages, table, tok, length, 0.1)[0]
+    for window in (2 ** 31 - 1, 2 ** 31 - 2, 1 << 40):
+        assert np.array_equal(okv.attention(q, pages, table, tok, length, 0.1, window)[0], want) and want[5:].any() and not want[:5].any()
