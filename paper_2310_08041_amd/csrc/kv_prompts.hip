@@ -238,7 +238,7 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
             } else {
                 const int32_t u = k_tok & 15, place = (k_tok & ~15) + (u >> 2 & 1) * 8 + (u >> 3) * 4 + (u & 3);
                 float r[3];
-                split<3>(x.alpha > 0.0f && x.alpha < INFINITY ? __builtin_amdgcn_rcpf(x.alpha) : 0.0f, r);
+                split<3>(x.alpha >= 0x1p-126f && x.alpha < INFINITY ? __builtin_amdgcn_rcpf(x.alpha) : 0.0f, r); // (a subnormal's is infinite)
 #pragma unroll
                 for (int i = 0; i < 3; ++i) {
                     o.rows[i][place] = (uint16_t)(__float_as_uint(part[i]) >> 16);

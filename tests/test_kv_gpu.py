@@ -881,3 +881,24 @@ def test_a_window_larger_than_any_line_with_rows_before_the_first_token(oracle, 
     worst = np.abs(outs[0].double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, *bounds, q_type, "f32")
     assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
     assert torch.equal(*outs) and (outs[0] != 0).any()
+
+
+KINDS = [(2, 3, 64, [70, 200], None), (16, 8, 128, [190], [140]), (24, 5, 64, [333, 128, 65], [60, 128, 1])]   # single tokens; prompts; both
+
+
+@pytest.mark.parametrize("bits", [0x00000001, 0x00200000, 0x007fffff, 0x80000001, 0x00000000, 0x7f800000, 0xff800000, 0xbf800000])
+@pytest.mark.parametrize("heads,group,dim,lengths,new", KINDS)
+def test_what_lies_in_unseen_places_does_not_matter(oracle, b, heads, group, dim, lengths, new, bits):
+    """Places of no token hold any numbers, as alpha too: subnormal ones (whose reciprocal is infinite), zero, infinities, negative ones."""
+    import torch
+    rng = np.random.default_rng(45)
+    word = np.frombuffer(np.uint32(bits).tobytes(), np.uint8)
+    outs = []
+    for garbage in (0x3c, np.tile(word, heads * 32 * (dim + 16) // 4)):
+        rng = np.random.default_rng(45)
+        c = make(rng, heads, group, dim, 32, lengths, new, garbage=garbage)
+        q = _t(rng.standard_normal((c.rows, heads * group * dim)).astype(np.float32), torch.bfloat16)
+        cache, batch = on_device(b, c)
+        ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda").fill_(0xFF)
+        outs.append(b.qllm_kv_attention(q, cache, 0, batch, 0.1, torch.empty((c.rows, heads * group * dim), device="cuda"), ws))
+    assert torch.isfinite(outs[0]).all() and torch.equal(*outs)
