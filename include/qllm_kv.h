@@ -27,6 +27,9 @@ extern "C" {
  *   codes of the values  [page_tokens][dim / 2]
  *   alpha of the keys    [page_tokens] float        beta of the keys    [page_tokens] int32
  *   alpha of the values  [page_tokens] float        beta of the values  [page_tokens] int32
+ * qllm_kv_append writes alphas from 2^-126 on.  Attention takes what others wrote too: an alpha of 0 (a page of zero bytes, tokens that
+ * a length counts before they are appended) is a key or value of 0, a value's alpha below 2^-126 may count as 0, and one that is
+ * negative or not finite spoils the rows that see the token.  What lies in places of no token may be anything.
  */
 typedef struct {
     int64_t heads, dim, page_tokens, n_pages;

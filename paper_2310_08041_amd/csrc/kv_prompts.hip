@@ -220,17 +220,20 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
             }
         }
     };
+    // An alpha that append does not write, in a page of zeros say: the value is 0 whatever its codes, its token weighs as any other.  It
+    // goes through the products as alpha 1, zero point 0 and operands 0.  (No logarithm of 0, no infinite reciprocal of a subnormal.)
+    const auto is_nothing = [](float value_alpha) { return fabsf(value_alpha) < 0x1p-126f; };
     const auto lay_params = [&](const Asked<D> &x, int32_t b) { // into buffer b
         Operands<D> &o = op[b];
         if (k_part < 2) { // (tokens that no row sees may hold anything: nothing here that is not finite meets a weight of zero)
             float part[3];
-            split<3>(-16.0f - (float)x.beta, part);
+            split<3>(k_part == 1 && is_nothing(x.alpha) ? 0.0f : -16.0f - (float)x.beta, part);
             if (k_part == 0) {
                 // a factor this small is a key that is zero to every query: 2^-90 in its place keeps the quotient finite
                 float ka = x.alpha * a.scale2;
                 ka = fabsf(ka) < 0x1p-90f ? copysignf(0x1p-90f, ka) : ka;
                 float more[3];
-                split<3>(__builtin_amdgcn_logf(x.value_alpha) / ka, more);
+                split<3>(__builtin_amdgcn_logf(is_nothing(x.value_alpha) ? 1.0f : x.value_alpha) / ka, more);
                 o.ka[k_tok] = ka;
                 *reinterpret_cast<u32x4 *>(&o.k[k_tok][D]) =
                     u32x4{pack_bf16(part[0], part[0]), pack_bf16(part[0], part[1]), pack_bf16(part[1], part[1]), pack_bf16(part[2], part[2])};
@@ -238,7 +241,7 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
             } else {
                 const int32_t u = k_tok & 15, place = (k_tok & ~15) + (u >> 2 & 1) * 8 + (u >> 3) * 4 + (u & 3);
                 float r[3];
-                split<3>(x.alpha >= 0x1p-126f && x.alpha < INFINITY ? __builtin_amdgcn_rcpf(x.alpha) : 0.0f, r); // (a subnormal's is infinite)
+                split<3>(is_nothing(x.alpha) ? 1.0f : (x.alpha > 0.0f && x.alpha < INFINITY ? __builtin_amdgcn_rcpf(x.alpha) : 0.0f), r);
 #pragma unroll
                 for (int i = 0; i < 3; ++i) {
                     o.rows[i][place] = (uint16_t)(__float_as_uint(part[i]) >> 16);
@@ -254,12 +257,24 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
         uint32_t pair[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) pair[e] = x.v[2 * e] | x.v[2 * e + 1] << 16;
-        const auto put = [&](int c, u32x4 w) { *reinterpret_cast<u32x4 *>(&o.v[32 * c + col][8 * v_chunk]) = w; };
-        put(0, u32x4{codes.pair<0>(pair[0]), codes.pair<0>(pair[1]), codes.pair<0>(pair[2]), codes.pair<0>(pair[3])});
-        put(1, u32x4{codes.pair<1>(pair[0]), codes.pair<1>(pair[1]), codes.pair<1>(pair[2]), codes.pair<1>(pair[3])});
+        const auto place = [&](int c) { return reinterpret_cast<u32x4 *>(&o.v[32 * c + col][8 * v_chunk]); };
+        *place(0) = u32x4{codes.pair<0>(pair[0]), codes.pair<0>(pair[1]), codes.pair<0>(pair[2]), codes.pair<0>(pair[3])};
+        *place(1) = u32x4{codes.pair<1>(pair[0]), codes.pair<1>(pair[1]), codes.pair<1>(pair[2]), codes.pair<1>(pair[3])};
         if (D == 128) {
-            put(2, u32x4{codes.pair<2>(pair[0]), codes.pair<2>(pair[1]), codes.pair<2>(pair[2]), codes.pair<2>(pair[3])});
-            put(3, u32x4{codes.pair<3>(pair[0]), codes.pair<3>(pair[1]), codes.pair<3>(pair[2]), codes.pair<3>(pair[3])});
+            *place(2) = u32x4{codes.pair<2>(pair[0]), codes.pair<2>(pair[1]), codes.pair<2>(pair[2]), codes.pair<2>(pair[3])};
+            *place(D / 32 - 1) = u32x4{codes.pair<3>(pair[0]), codes.pair<3>(pair[1]), codes.pair<3>(pair[2]), codes.pair<3>(pair[3])};
+        }
+        // the wave lays values of the 16 tokens whose parameters it has, token u of them in lanes 4 u ..
+        const uint64_t nothing = __ballot(is_nothing(x.value_alpha));
+        if (nothing) {
+            u32x4 keep;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int32_t u = 4 * h + 8 * (e >> 1) + 2 * (e & 1);
+                keep[e] = (nothing >> (4 * u) & 1 ? 0u : 0xffffu) | (nothing >> (4 * u + 4) & 1 ? 0u : 0xffff0000u);
+            }
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) *place(c) &= keep;
         }
     };
 

@@ -902,3 +902,35 @@ def test_what_lies_in_unseen_places_does_not_matter(oracle, b, heads, group, dim
         ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda").fill_(0xFF)
         outs.append(b.qllm_kv_attention(q, cache, 0, batch, 0.1, torch.empty((c.rows, heads * group * dim), device="cuda"), ws))
     assert torch.isfinite(outs[0]).all() and torch.equal(*outs)
+
+
+@pytest.mark.parametrize("every", [1, 3, 17])
+@pytest.mark.parametrize("heads,group,dim,lengths,new", KINDS)
+def test_tokens_that_nobody_wrote_are_zero_keys_and_values(oracle, b, heads, group, dim, lengths, new, every):
+    """A length may count tokens that were never appended, in pages of zeros; and an alpha of zero, or one below the normal floats,
+    makes a zero value whatever the codes: it takes its share of the weights, in both kernels."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(46)
+    c = make(rng, heads, group, dim, 32, lengths, new)
+    for line in range(len(lengths)):
+        for t in range(0, lengths[line], every):
+            p = okv.page_at(c.table, c.n_pages, 32, line, t)
+            for h in range(heads):
+                kind = (t // every + h) % 3 if every > 1 else 0
+                if kind == 0:                                            # as a new cache has it
+                    for value in (0, 1):
+                        c.pages.put(p, h, t % 32, value, np.zeros(dim, np.uint8), 0.0, 0)
+                else:                                                    # codes and zero point of any value
+                    c.pages.put(p, h, t % 32, 1, rng.integers(0, 16, dim).astype(np.uint8), 0.0 if kind == 1 else 1e-40, int(rng.integers(-300, 300)))
+    q = _bf16(rng.standard_normal((c.rows, heads * group, dim)).astype(np.float32))
+    cache, batch = on_device(b, c)
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    out = torch.empty((c.rows, heads * group * dim), device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), torch.bfloat16), cache, 0, batch, 0.1, out, ws)
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.1))
+    got = out.double().cpu().numpy().reshape(want.shape)
+    worst = np.abs(got - want) / tolerance(want, *bounds, "bf16", "f32")
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+    if every == 1:
+        assert not got.any()
