@@ -89,6 +89,7 @@ int32_t qllm_kv_read(const qllm_kv_cache *cache, const qllm_kv_batch *batch, voi
  * h / (q_heads / heads)).  A query at position p sees the tokens t <= p of its line that are there, with window > 0 only
  * t > p - window:
  *     out = sum_t e^(scale q.k_t) v_t / sum_t e^(scale q.k_t),   0 where nothing is seen.
+ *   scale    any sign; |scale| below 2.35e38 (scores are held in base 2, times log2 e; larger ones: SHAPE).
  *   q        [rows, ldq] q_dtype, out [rows, ldo] out_dtype (fp32 / bf16), q_heads * dim columns.  out may be q itself (one
  *            type, one stride); must not overlap it otherwise.  q_heads <= 2^15, and with G = q_heads / heads: tiles = rows * G / 16 +
  *            n_seqs < 2^23 and tiles * (table_ld * page_tokens / 32 + 8) < 2^31.

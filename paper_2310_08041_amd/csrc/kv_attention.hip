@@ -677,7 +677,7 @@ extern "C" int32_t qllm_kv_attention(const void *q, int32_t q_dtype, int64_t ldq
     rc = check(cache, batch, q_heads);
     if (rc != QLLM_OK) return rc;
     if ((q_dtype != QLLM_F32 && q_dtype != QLLM_BF16) || (out_dtype != QLLM_F32 && out_dtype != QLLM_BF16)) return QLLM_ERR_DTYPE;
-    if (ldq < q_heads * cache->dim || ldo < q_heads * cache->dim || window < 0 || !(fabsf(scale) <= 3e38f)) return QLLM_ERR_SHAPE;
+    if (ldq < q_heads * cache->dim || ldo < q_heads * cache->dim || window < 0 || !isfinite(scale * LOG2E)) return QLLM_ERR_SHAPE;
     if ((reinterpret_cast<uintptr_t>(q) & (q_dtype == QLLM_F32 ? 3u : 1u)) || (reinterpret_cast<uintptr_t>(out) & (out_dtype == QLLM_F32 ? 3u : 1u)))
         return QLLM_ERR_ALIGN;
     if (!workspace || workspace_bytes < qllm_kv_attention_workspace_bytes(cache, batch, q_heads)) return QLLM_ERR_WORKSPACE;

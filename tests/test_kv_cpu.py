@@ -393,6 +393,15 @@ def test_first_token_of_a_window_at_the_ends_of_its_range(index):
             assert index.first(pos, window) == want, (pos, window)
 
 
+def test_a_scale_that_overflows_in_base_2_is_refused():
+    """scale log2 e is what the kernels multiply by: infinite from 2.3587e38 on, although the scale itself is finite."""
+    limit = float(np.finfo(np.float32).max) / 1.44269504088896341
+    for scale in (1.001 * limit, 2.9e38, 3.3e38, -2.9e38):
+        assert attend(scale=scale) == SHAPE and attend(scale=scale, t=batch(rows=0, n_seqs=0)) == SHAPE
+    for scale in (0.999 * limit, -0.999 * limit, 0.0, 1e-45):
+        assert attend(scale=scale, t=batch(rows=0, n_seqs=0)) == 0
+
+
 def test_statement_of_attention_with_the_largest_windows():
     """Positions are exact whatever the arrays' type: a window that no line reaches is no window, for rows before the first token too."""
     rng = np.random.default_rng(6)
