@@ -91,9 +91,10 @@ def append(pages, table, tokens, k, v):
                     pages.put(p, h, pos % pages.page, value, codes[r, h], alpha[r, h], beta[r, h])
 
 
-def attention(q, pages, table, tokens, length, scale, window=0, out=None):
+def attention(q, pages, table, tokens, length, scale, window=0, out=None, close=False):
     """q [rows, q_heads, dim] float32 -> (out, bound on sum w |v|, bound on the scores' fp32 error, bound on the sums' fp32 error),
-    float64 of q's shape; rows of no token keep what `out` has.  2^-24 is half a step of fp32."""
+    float64 of q's shape; rows of no token keep what `out` has.  2^-24 is half a step of fp32.  The bounds allow a rounding per addend in any
+    order; close: as many as sums on the matrix cores make, 32 addends to a rounding, split over four waves."""
     heads, dim = pages.heads, pages.dim
     group = q.shape[1] // heads
     out = np.zeros(q.shape) if out is None else out.astype(np.float64)
@@ -131,9 +132,14 @@ def attention(q, pages, table, tokens, length, scale, window=0, out=None):
                 out[r, o] = w @ v
                 absv[r, o] = w @ np.abs(v)
                 # sums of dim products (16 + code) q, (16 + beta) sum q, and a few roundings of the score itself
-                sums = abs(scale) * a[:, 0] * (47.0 + b[:, 0]) * np.abs(x).sum() * (dim + 8)
+                if close:  # an operation per 32 channels; the queries' sum: dim / 8 additions and three across lanes
+                    sums = abs(scale) * a[:, 0] * (31.0 * (dim // 32 + 1) + (16.0 + b[:, 0]) * (dim // 8 + 5)) * np.abs(x).sum()
+                    adds = 4 * (seen.sum() // 128 + 1) + 16  # two operations a step of 32 tokens for each part of the weights, waves and parts joined
+                else:
+                    sums = abs(scale) * a[:, 0] * (47.0 + b[:, 0]) * np.abs(x).sum() * (dim + 8)
+                    adds = seen.sum() + 32
                 err_s[r, o] = 2.0 ** -24 * (sums.max() + 8 * np.abs(s).max() + 16)
-                err_o[r, o] = 2.0 ** -24 * (seen.sum() + 32) * (w * a[:, 1] * (32.0 + b[:, 1])).sum()
+                err_o[r, o] = 2.0 ** -24 * adds * (w * a[:, 1] * ((47.0 if close else 32.0) + b[:, 1])).sum()
     return out, absv, err_s, err_o
 
 

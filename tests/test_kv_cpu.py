@@ -9,6 +9,7 @@ import numpy as np
 import pytest
 import torch
 
+import test_kv_gpu as tg
 from oracle import kv_cache as okv
 from paper_2310_08041_amd import binding as b
 
@@ -415,3 +416,67 @@ def test_statement_of_attention_with_the_largest_windows():
     want = okv.attention(q, pages, table, tok, length, 0.1)[0]
     for window in (2 ** 31 - 1, 2 ** 31 - 2, 1 << 40):
         assert np.array_equal(okv.attention(q, pages, table, tok, length, 0.1, window)[0], want) and want[5:].any() and not want[:5].any()
+
+
+# ---------------------------------------------------------------- do the attention tests' bounds have teeth?
+
+def _bits(x, n):
+    """float64 rounded to n significant bits."""
+    m, e = np.frexp(x)
+    return np.ldexp(np.rint(np.ldexp(m, n)), e - n)
+
+
+def mistaken(c, q, scale, window, weight_bits=None, wider=0, newest=0):
+    """The statement of attention with a mistake planted: weights times alpha of so many bits, a window of `wider` tokens more, the
+    `newest` tokens left out."""
+    out = np.zeros(q.shape)
+    for r, line, pos in c.tokens:
+        hi = min(pos, int(c.length[line]) - 1) - newest
+        lo = max(0, pos - (window + wider) + 1) if window else 0
+        for h in range(c.heads):
+            got = [[c.pages.get(int(c.table[line, t // c.page]), h, t % c.page, value) for t in range(lo, hi + 1)] for value in (0, 1)]
+            if not got[0]:
+                continue
+            k, v = (np.array([x[0] for x in side]) for side in got)
+            alpha = np.array([x[1] for x in got[1]])
+            for j in range(c.group):
+                o = h * c.group + j
+                s = float(scale) * (k @ q[r, o].astype(np.float64))
+                w = np.exp(s - s.max())
+                above = w if weight_bits is None else _bits(w * alpha, weight_bits) / alpha
+                out[r, o] = (above @ v) / w.sum()
+    return out
+
+
+@pytest.mark.parametrize("case", tg.CLOSE, ids=str)
+def test_close_bounds_reject_planted_mistakes(oracle, case):
+    window = case[7]
+    c, q, want, bound = tg.close_case(*case)
+    scale = np.float32(c.dim ** -0.5)
+    share = lambda **k: (np.abs(mistaken(c, q, scale, window, **k) - want) / bound).max()
+    assert share() < 1e-3 and share(weight_bits=24) < 0.1                       # nothing planted; float32's own rounding
+    if case[0] == "bf16":
+        assert share(weight_bits=17) <= 1.0                                     # what the header allows
+    assert share(weight_bits=8) > 1.0 and share(newest=1) > 1.0
+    if window:
+        assert share(wider=1) > 1.0 and share(wider=-1) > 1.0
+
+
+@pytest.mark.parametrize("case", tg.CLOSE_PROMPTS, ids=str)
+def test_close_bounds_of_prompts_reject_planted_mistakes(oracle, case):
+    window = case[7]
+    c, q, want, bound = tg.close_prompts_case(*case)
+    share = lambda **k: (np.abs(mistaken(c, q, np.float32(c.dim ** -0.5), window, **k) - want) / bound).max()
+    assert share() < 1e-3 and share(weight_bits=8) <= 1.0                       # what the header allows
+    assert share(weight_bits=5) > 1.0 and share(newest=1) > 1.0
+    if window:
+        assert share(wider=1) > 1.0 and share(wider=-1) > 1.0
+
+
+@pytest.mark.parametrize("case", tg.WINDOWED, ids=str)
+def test_exactness_of_float32_rejects_weights_of_16_bits(oracle, case):
+    c, q, want, plain = tg.windowed_case(*case)
+    scale = np.float32(c.dim ** -0.5)
+    off = lambda **k: tg.exactness(mistaken(c, q, scale, case[6], **k), want, plain)
+    assert off(weight_bits=24) <= 1.0 and off(weight_bits=16) > 1.0 and off(weight_bits=8) > 1.0
+    assert off(wider=1) > 1.0 and off(wider=-1) > 1.0 and off(newest=1) > 1.0

@@ -934,3 +934,113 @@ def test_tokens_that_nobody_wrote_are_zero_keys_and_values(oracle, b, heads, gro
     assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
     if every == 1:
         assert not got.any()
+
+
+# Ordinary heads, few tokens, float32 out: the bounds are 1e-4 to 3e-4 of the values here and tell a weight of 8 bits, a window of one
+# token more or less and a missing newest token from what is promised (test_kv_cpu.py plants each of them in the statement).
+CLOSE = [  # q, heads, group, dim, page, lengths, new rows, window: all of them the kernel for few rows
+    ("bf16", 2, 1, 128, 64, [1, 2, 3, 5, 9, 33], None, 0),
+    ("bf16", 1, 8, 128, 64, [31, 40, 64, 130], None, 0),
+    ("bf16", 2, 3, 64, 32, [40, 129, 7], None, 0),
+    ("bf16", 1, 4, 64, 32, [150, 90], [5, 2], 50),
+    ("bf16", 1, 2, 128, 64, [300, 120], None, 100),
+    ("f32", 2, 3, 64, 32, [50, 40], [20, 40], 0),
+    ("f32", 1, 2, 128, 64, [333, 1, 65], None, 100),
+    ("f32", 1, 1, 64, 128, [40], [40], 7),
+]
+PARTS = {"bf16": 2.0 ** -16, "f32": 2.0 ** -24}               # of a weight, left out at most
+
+
+def close_case(q_type, heads, group, dim, page, lengths, new, window):
+    """A cache of ordinary heads, queries, and the statement's output with its close bounds."""
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(47 + sum(lengths) + dim)
+    c = make(rng, heads, group, dim, page, lengths, new, filled=False)
+    for i, l in enumerate(lengths):
+        okv.append(c.pages, c.table, [(r, i, r) for r in range(l)], *(rng.standard_normal((l, heads, dim)).astype(np.float32) for _ in range(2)))
+    q = rng.standard_normal((c.rows, heads * group, dim)).astype(np.float32)
+    q = _bf16(q) if q_type == "bf16" else q
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(dim ** -0.5), window, close=True)
+    return c, q, want, okv.attention_bound(want, *bounds, PARTS[q_type], 2.0 ** -24)
+
+
+@pytest.mark.parametrize("q_type,heads,group,dim,page,lengths,new,window", CLOSE)
+def test_attention_of_few_rows_keeps_the_bits_it_promises(oracle, b, q_type, heads, group, dim, page, lengths, new, window):
+    import torch
+    c, q, want, bound = close_case(q_type, heads, group, dim, page, lengths, new, window)
+    cache, batch = on_device(b, c)
+    out = torch.empty((c.rows, heads * group * dim), device="cuda")
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), torch.bfloat16 if q_type == "bf16" else torch.float32), cache, 0, batch, dim ** -0.5, out, ws, window=window)
+    worst = np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / bound
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+CLOSE_PROMPTS = [  # the same for the kernel for prompts: weights of one bf16 part, above and below the line
+    ("bf16", 2, 4, 128, 64, [60], [60], 7),
+    ("bf16", 1, 16, 64, 32, [90], [33], 0),
+    ("bf16", 3, 2, 128, 32, [40, 130], [40, 100], 20),
+    ("bf16", 2, 8, 64, 128, [100, 20, 9], [50, 1, 9], 12),
+]
+
+
+def close_prompts_case(*case):
+    """As close_case; twice the scores' bound (an operation per 16 channels there)."""
+    from oracle import kv_cache as okv
+    c, q, want, _ = close_case(*case)
+    bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(c.dim ** -0.5), case[7], close=True)[1:]
+    return c, q, want, okv.attention_bound(want, bounds[0], 2.0 * bounds[1], bounds[2], 2.0 ** -8, 2.0 ** -24)
+
+
+@pytest.mark.parametrize("q_type,heads,group,dim,page,lengths,new,window", CLOSE_PROMPTS)
+def test_attention_of_prompts_sees_the_tokens_it_should(oracle, b, q_type, heads, group, dim, page, lengths, new, window):
+    import torch
+    c, q, want, bound = close_prompts_case(q_type, heads, group, dim, page, lengths, new, window)
+    cache, batch = on_device(b, c)
+    out = torch.empty((c.rows, heads * group * dim), device="cuda")
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), torch.bfloat16), cache, 0, batch, dim ** -0.5, out, ws, window=window)
+    worst = np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / bound
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+WINDOWED = [("f32", 1, 2, 128, [333, 1, 65], None, 100), ("f32", 4, 3, 64, [700, 90], [60, 90], 50),
+            ("f32", 2, 1, 64, [40, 20], [40, 20], 7)]
+
+
+def float32_softmax(c, q, k, v, scale, window, r, o, p):
+    """Attention of one row and head in float32 steps over the cache's values (k, v [tokens, heads, dim] float32)."""
+    import torch
+    lo = max(0, p + 1 - window) if window else 0
+    s = (k[lo:p + 1, o // c.group] @ torch.from_numpy(q[r, o])) * np.float32(scale)
+    return (torch.softmax(s, 0) @ v[lo:p + 1, o // c.group]).numpy()
+
+
+def exactness(got, want, plain):
+    """How many times float32 arithmetic's error (norms), with half a bit of the result beside it."""
+    n = np.linalg.norm
+    return n(got - want) / (2.0 * n(plain - want) + 2.0 ** -25 * n(want))
+
+
+def windowed_case(q_type, heads, group, dim, lengths, new, window):
+    import torch
+    c, q, want, _ = close_case(q_type, heads, group, dim, 64, lengths, new, window)
+    plain = np.zeros(want.shape)
+    for i, l in enumerate(lengths):
+        k, v = (torch.from_numpy(np.array([[c.pages.get(c.table[i, t // 64], h, t % 64, value)[0] for h in range(heads)] for t in range(l)], np.float32)) for value in (0, 1))
+        for r, line, p in (t for t in c.tokens if t[1] == i):
+            for o in range(heads * group):
+                plain[r, o] = float32_softmax(c, q, k, v, dim ** -0.5, window, r, o, p)
+    return c, q, want, plain
+
+
+@pytest.mark.parametrize("q_type,heads,group,dim,lengths,new,window", WINDOWED)
+def test_float32_attention_in_a_window_is_as_exact_as_float32_arithmetic(oracle, b, q_type, heads, group, dim, lengths, new, window):
+    import torch
+    c, q, want, plain = windowed_case(q_type, heads, group, dim, lengths, new, window)
+    cache, batch = on_device(b, c)
+    out = torch.empty((c.rows, heads * group * dim), device="cuda")
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1)), cache, 0, batch, dim ** -0.5, out, ws, window=window)
+    off = exactness(out.double().cpu().numpy().reshape(want.shape), want, plain)
+    assert off <= 1.0, off
