@@ -71,7 +71,8 @@ typedef enum {
  *   inv_freq [dim / 2] double, angle per position (ignored, may be NULL, with QLLM_ROPE_NONE: q_out is then a copy).
  * Fixed arithmetic: a = p * inv_freq[d] in double, c = cos a and s = sin a rounded to float; x1' = x1 c - x2 s and
  * x2' = x2 c + x1 s with products and sum in double, rounded once to float; queries are then rounded to x_dtype, keys go to
- * Eq. (2) as they are.  Rows that are not finite get unspecified codes.
+ * Eq. (2) as they are.  A key or value that is not finite, or whose max - min is not (from 2^128 on), gets
+ * unspecified codes, itself alone.
  * Any 2-byte (bf16) or 4-byte (fp32) aligned rows work; 16-byte aligned rows with 16-byte strides take 16-byte accesses.
  * Errors: NULL / SHAPE / DTYPE (also an unknown rope) / ALIGN / HIP.  rows == 0 or n_seqs == 0: no-op.
  */

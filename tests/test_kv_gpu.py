@@ -1044,3 +1044,123 @@ def test_float32_attention_in_a_window_is_as_exact_as_float32_arithmetic(oracle,
     b.qllm_kv_attention(_t(q.reshape(c.rows, -1)), cache, 0, batch, dim ** -0.5, out, ws, window=window)
     off = exactness(out.double().cpu().numpy().reshape(want.shape), want, plain)
     assert off <= 1.0, off
+
+
+@pytest.mark.parametrize("heads,dim,page,rope", [(2, 64, 32, 0), (3, 128, 64, 2), (1, 128, 32, 1)])
+def test_append_and_read_of_vectors_far_from_zero(oracle, b, heads, dim, page, rope):
+    """Offsets of 10^5 to 10^8 times the range, on both sides of the quotient (2^21) from which codes are made in 64 bits and of the
+    zero point (2^23) from which they are read in 64 bits; tiny and huge ranges."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(48)
+    n = 120
+    c = make(rng, heads, 1, dim, page, [n], [n], filled=False)
+    k, v = (rng.standard_normal((n, heads, dim)) for _ in range(2))
+    for x in (k, v):
+        beta = np.exp2(rng.uniform(15, 27, (n, heads, 1))) * rng.choice([-1.0, 1.0], (n, heads, 1))
+        beta[::7] = rng.choice([2.0 ** 21, 2.0 ** 23, -2.0 ** 21, -2.0 ** 23], beta[::7].shape) + rng.integers(-9, 9, beta[::7].shape)
+        low, high = x.min(-1, keepdims=True), x.max(-1, keepdims=True)
+        x -= np.where(rng.random((n, heads, 1)) < 0.9, beta * (high - low) / 15, 0.0)
+        x *= np.exp2(rng.integers(-80, 81, (n, heads, 1)))
+    k, v = k.astype(np.float32), v.astype(np.float32)
+    inv_freq = 10000.0 ** (-np.arange(0, dim, 2) / dim)
+    turned = okv.rotate(k, [p for _, _, p in c.tokens], inv_freq, rope)
+    okv.append(c.pages, c.table, c.tokens, turned, v)
+    betas = np.abs(okv.quantize(v)[2].astype(np.int64))
+    assert (betas > 2 ** 23).any() and ((betas > 2 ** 21) & (betas < 2 ** 23)).any() and (betas < 2 ** 21).any()
+    cache = b.DeviceKVCache(1, c.n_pages, heads, dim, page, pages=torch.full((1, c.n_pages, heads * page * (dim + 16)), 0xFF, dtype=torch.uint8, device="cuda"))
+    batch = b.DeviceKVBatch(n, _t(c.table), _t(c.length), _t(c.row_start))
+    b.qllm_kv_append(cache, 0, batch, _t(k.reshape(n, -1)), _t(v.reshape(n, -1)), rope=rope, inv_freq=_t(inv_freq) if rope else None)
+    assert np.array_equal(cache.pages[0].cpu().numpy(), c.pages.raw)
+    for td in (torch.float32, torch.bfloat16):
+        outs = [torch.zeros((n, heads * dim), dtype=td, device="cuda") for _ in range(2)]
+        b.qllm_kv_read(cache, 0, batch, *outs)
+        for value, out in enumerate(outs):
+            want = np.array([[c.pages.get(okv.page_at(c.table, c.n_pages, page, line, p), h, p % page, value)[0] for h in range(heads)] for _, line, p in c.tokens])
+            want = want.astype(np.float32)
+            assert np.array_equal(out.float().cpu().numpy().reshape(want.shape), _bf16(want) if td is torch.bfloat16 else want)
+
+
+def test_a_row_that_cannot_be_quantized_leaves_the_others_alone(oracle, b):
+    """NaN, infinities, and finite numbers whose range is none (its codes are unspecified too): every other byte of the pages, and
+    what attention gives to rows that do not see the token."""
+    import torch
+    rng = np.random.default_rng(49)
+    n, heads, dim, page = 70, 2, 128, 32
+    c = make(rng, heads, 2, dim, page, [n], [n], filled=False)
+    k, v = (rng.standard_normal((n, heads, dim)).astype(np.float32) for _ in range(2))
+    q = _t(rng.standard_normal((n, 2 * heads * dim)).astype(np.float32), torch.bfloat16)
+    got = []
+    for bad in (None, np.nan, np.inf, -np.inf, "range"):
+        k2, v2 = k.copy(), v.copy()
+        if bad == "range":
+            k2[40, 1, [3, 77]] = v2[40, 1, [3, 77]] = [3e38, -3e38]
+        elif bad is not None:
+            k2[40, 1, 5] = v2[40, 1, 6] = bad
+        cache, batch = on_device(b, c)
+        b.qllm_kv_append(cache, 0, batch, _t(k2.reshape(n, -1)), _t(v2.reshape(n, -1)))
+        outs = []
+        for rows in (n, 3):                                    # the kernel for prompts, that for few rows
+            few = b.DeviceKVBatch(rows, _t(c.table), _t(np.array([n if rows == n else 40], np.int32)), _t(np.array([0, rows], np.int32)))
+            ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, few, 2 * heads), dtype=torch.uint8, device="cuda")
+            out = b.qllm_kv_attention(q[:rows], cache, 0, few, 0.1, torch.empty_like(q[:rows]), ws).view(rows, 2 * heads, dim)
+            outs += [out[:40].clone(), out[:, :2].clone()]     # rows before the token; the other key/value head
+        ours = cache.pages[0].cpu().numpy().copy()
+        p, place = c.table[0, 40 // page], 40 % page
+        for value in (0, 1):
+            _, code, par = c.pages._at(p, 1, place, value)
+            for at, size in ((code, dim // 2), (par, 4), (par + 4 * page, 4)):
+                ours[p, at:at + size] = 0
+        got.append((ours, outs))
+    for ours, outs in got[1:]:
+        assert np.array_equal(ours, got[0][0]) and all(torch.equal(x, y) and torch.isfinite(x).all() for x, y in zip(outs, got[0][1]))
+
+
+@pytest.mark.parametrize("n,dtype", [(150, "bf16"), (700, "f32"), (5000, "bf16")])
+def test_append_and_read_of_more_sequences_than_a_wave_has_lanes(oracle, b, n, dtype):
+    """The search for a row's sequence takes two and three trips; some sequences have no rows, some no tokens, lines in any order."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(50)
+    heads, dim, page = 1, 64, 32
+    lengths = rng.integers(0, 50, n)
+    new = np.minimum(rng.choice([0, 0, 1, 1, 2, 5], n), lengths)
+    new[n - 1] = 0
+    c = make(rng, heads, 1, dim, page, lengths.tolist(), new.tolist(), slots=rng.permutation(n).tolist(), n_lines=n, rows=int(new.sum()) + 70, filled=False)
+    kv = rng.standard_normal((c.rows, 2, heads, dim)).astype(np.float32)
+    kv = _bf16(kv) if dtype == "bf16" else kv
+    td = torch.bfloat16 if dtype == "bf16" else torch.float32
+    cache, batch = on_device(b, c)
+    b.qllm_kv_append(cache, 0, batch, _t(kv[:, 0].reshape(c.rows, -1), td), _t(kv[:, 1].reshape(c.rows, -1), td))
+    out = torch.full((c.rows, heads * dim), 9.0, device="cuda")
+    b.qllm_kv_read(cache, 0, batch, v_out=out)
+    okv.append(c.pages, c.table, c.tokens, kv[:, 0], kv[:, 1])
+    assert np.array_equal(cache.pages[0].cpu().numpy(), c.pages.raw)
+    want = np.full((c.rows, heads, dim), 9.0, np.float32)
+    for r, line, p in c.tokens:
+        want[r, 0] = c.pages.get(okv.page_at(c.table, c.n_pages, page, line, p), 0, p % page, 1)[0]
+    assert np.array_equal(out.cpu().numpy().reshape(want.shape), want)
+
+
+@pytest.mark.parametrize("q_type,group,most,window", [("bf16", 3, 2, 0), ("f32", 2, 3, 9), ("bf16", 20, 3, 0)])
+def test_attention_of_more_sequences_than_are_listed_with_rows_of_their_own(oracle, b, q_type, group, most, window):
+    """More than 512 sequences of 0 to `most` rows: with few rows each, in float32, and with sequences of the kernel for prompts among them."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(51)
+    n, dim = 600, 64
+    lengths = rng.integers(0, 25, n)
+    new = np.minimum(rng.integers(0, most + 1, n) if group < 20 else rng.choice([1, 2, 3, 3], n), lengths)
+    c = make(rng, 1, group, dim, 32, lengths.tolist(), new.tolist(), slots=rng.permutation(n).tolist(), n_lines=n, rows=int(new.sum()) + 5)
+    assert (c.rows * group > 32 * n) == (group == 20)
+    q = rng.standard_normal((c.rows, group, dim)).astype(np.float32)
+    q = _bf16(q) if q_type == "bf16" else q
+    cache, batch = on_device(b, c)
+    out = torch.full((c.rows, group * dim), 5.0, device="cuda")
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, group), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), torch.bfloat16 if q_type == "bf16" else torch.float32), cache, 0, batch, 0.125, out, ws, window=window)
+    want, *bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.125), window, out=np.full(q.shape, 5.0))
+    got = out.double().cpu().numpy().reshape(want.shape)
+    assert (got[c.rows - 5:] == 5.0).all()
+    worst = np.abs(got - want) / tolerance(want, *bounds, q_type, "f32")
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
