@@ -80,8 +80,8 @@ int32_t qllm_kv_append(const void *q, int64_t ldq, int64_t q_heads, void *q_out,
                        const void *v, int64_t ldv, int32_t x_dtype, int32_t rope, const double *inv_freq,
                        const qllm_kv_cache *cache, const qllm_kv_batch *batch, void *hip_stream);
 
-/* What the cache holds for the step's rows: alpha * (code - beta), rounded once to dtype (fp32 / bf16) in k_out [rows, ldk] and
- * v_out [rows, ldv] (either may be NULL).  Rows whose token is not there are left as they were.  Errors as above. */
+/* What the cache holds for the step's rows: alpha * (code - beta), rounded to float (from |beta| = 2^23 on to double first) and from there to dtype
+ * (fp32 / bf16), in k_out [rows, ldk] and v_out [rows, ldv] (either may be NULL).  Rows whose token is not there are left as they were.  Errors as above. */
 int32_t qllm_kv_read(const qllm_kv_cache *cache, const qllm_kv_batch *batch, void *k_out, int64_t ldk, void *v_out, int64_t ldv,
                      int32_t dtype, void *hip_stream);
 

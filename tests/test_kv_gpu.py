@@ -1164,3 +1164,31 @@ def test_attention_of_more_sequences_than_are_listed_with_rows_of_their_own(orac
     assert (got[c.rows - 5:] == 5.0).all()
     worst = np.abs(got - want) / tolerance(want, *bounds, q_type, "f32")
     assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+def test_what_is_read_is_rounded_to_float_and_then_to_its_type(oracle, b):
+    """bf16 reads go through float32: where the exact product lies next to a border between two bf16 numbers the second rounding may
+    go the other way than a single one would."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(52)
+    dim, page = 64, 256
+    alpha = rng.uniform(0.01, 1.0, 400000).astype(np.float32)
+    codes = np.arange(16)
+    exact = alpha[:, None].astype(np.float64) * (codes - 7.0)                       # 24 + 4 bits: exact in 64
+    step = np.exp2(np.floor(np.log2(np.maximum(np.abs(exact), 1e-9))) - 7)          # bf16 numbers are this far apart
+    once = np.rint(exact / step) * step
+    twice = _bf16(exact.astype(np.float32))
+    odd = np.flatnonzero((once != twice).any(1))
+    assert odd.size > 3
+    raw = np.zeros((1, page * (dim + 16)), np.uint8)
+    pages = okv.Pages(raw, 1, dim, page)
+    chosen = np.concatenate([odd, np.arange(page)])[:page]
+    for t, i in enumerate(chosen):
+        pages.put(0, 0, t, 1, np.tile(codes, dim // 16).astype(np.uint8), alpha[i], 7)
+    cache = b.DeviceKVCache(1, 1, 1, dim, page, pages=_t(raw)[None])
+    batch = b.DeviceKVBatch(page, _t(np.zeros((1, 1), np.int32)), _t(np.array([page], np.int32)), _t(np.array([0, page], np.int32)))
+    out = torch.empty((page, dim), dtype=torch.bfloat16, device="cuda")
+    b.qllm_kv_read(cache, 0, batch, v_out=out)
+    got = out.double().cpu().numpy()[:, :16]
+    assert np.array_equal(got, twice[chosen]) and (got != once[chosen]).any()
