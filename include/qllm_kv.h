@@ -102,7 +102,7 @@ int32_t qllm_kv_read(const qllm_kv_cache *cache, const qllm_kv_batch *batch, voi
  * left out at most, in sequences of many rows 2^-8 (one part, rounded, which is also what is summed below the line).
  * A query that is not finite spoils the output of its own row and head alone.
  * In sequences of many rows with bf16 queries a key whose |scale| alpha is below 2^-90 counts as one of 2^-90 (which is nothing
- * for queries below 2^60), and a token whose value's alpha is less than 2^-100 of another's that the query sees may count for
+ * for queries below 2^30), and a token whose value's alpha is less than 2^-100 of another's that the query sees may count for
  * less than its share below the line.
  * Errors: NULL / SHAPE / DTYPE / ALIGN / WORKSPACE / HIP.  rows == 0 or n_seqs == 0: no-op.
  */

@@ -1192,3 +1192,27 @@ def test_what_is_read_is_rounded_to_float_and_then_to_its_type(oracle, b):
     b.qllm_kv_read(cache, 0, batch, v_out=out)
     got = out.double().cpu().numpy()[:, :16]
     assert np.array_equal(got, twice[chosen]) and (got != once[chosen]).any()
+
+
+@pytest.mark.parametrize("far", [2.0 ** 27, 2.0 ** 30])
+def test_prompts_over_keys_of_the_smallest_ranges(oracle, b, far):
+    """Keys whose alpha is 2^-100, far from zero: their factor counts as 2^-90, which is nothing for queries below 2^30."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(53)
+    heads, group, dim, page, n = 16, 4, 128, 32, 90
+    c = make(rng, heads, group, dim, page, [n], [n])
+    for t in range(n):
+        for h in range(heads):
+            c.pages.put(int(c.table[0, t // page]), h, t % page, 0, rng.integers(0, 16, dim).astype(np.uint8), 2.0 ** -100, int(far * rng.choice([-1, 1]) * rng.uniform(0.5, 1.0)))
+    q = _bf16((np.exp2(rng.uniform(0, 29, (n, heads * group, 1))) * rng.uniform(-1.9, 1.9, (n, heads * group, dim))).astype(np.float32))
+    cache, batch = on_device(b, c)
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    out = torch.empty((n, heads * group * dim), device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(n, -1), torch.bfloat16), cache, 0, batch, 1.0, out, ws)
+    want, absv, err_s, err_o = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(1.0))
+    # the factor in place of 2^-100: a score of up to 2^-90 (15 + |beta|) sum |q|, both sides of it
+    more = 2.0 * 2.0 ** -90 * (15 + far) * np.abs(q.astype(np.float64)).sum(-1, keepdims=True)
+    assert more.max() < 2.0 ** -21
+    worst = np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, absv, err_s + more, err_o, "bf16", "f32")
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
