@@ -95,7 +95,8 @@ int32_t qllm_kv_read(const qllm_kv_cache *cache, const qllm_kv_batch *batch, voi
  *            type, one stride); must not overlap it otherwise.  q_heads <= 2^15, and with G = q_heads / heads: tiles = rows * G / 16 +
  *            n_seqs < 2^23 and tiles * (table_ld * page_tokens / 32 + 8) < 2^31.
  *   workspace  16-byte aligned, qllm_kv_attention_workspace_bytes(cache, batch, q_heads) bytes (read on the host: of the
- *            two structs only the sizes); contents undefined afterwards, two calls in flight at once need one each.
+ *            two structs only the sizes, and whether row_start is NULL; a smaller step may need more); contents undefined
+ *            afterwards, two calls in flight at once need one each.
  * Equal calls give equal bits.
  * Codes enter the matrix cores as exact bf16 integers; scores, maxima and sums are fp32.  The weights (times a value's alpha)
  * meet the values in bf16 parts: with fp32 queries, which come in three parts too, 24 bits; with bf16 queries 2^-16 of each is

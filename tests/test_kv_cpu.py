@@ -480,3 +480,15 @@ def test_exactness_of_float32_rejects_weights_of_16_bits(oracle, case):
     off = lambda **k: tg.exactness(mistaken(c, q, scale, case[6], **k), want, plain)
     assert off(weight_bits=24) <= 1.0 and off(weight_bits=16) > 1.0 and off(weight_bits=8) > 1.0
     assert off(wider=1) > 1.0 and off(wider=-1) > 1.0 and off(newest=1) > 1.0
+
+
+def test_the_workspace_goes_by_the_step_it_is_asked_for():
+    """Sizes and whether row_start is there, no addresses; a call whose workspace is for the other kind, or for a larger step that needs
+    less, is refused."""
+    f = b.raw().qllm_kv_attention_workspace_bytes
+    sizes = dict(rows=60, n_seqs=1, n_slots=1, ld=80, table=None, length=None)
+    bytes_of = lambda **k: f(C.byref(cache(heads=1, pages=None)), C.byref(batch(**{**sizes, **k})), 64)
+    with_rows, without, larger = bytes_of(row_start=A), bytes_of(row_start=None), bytes_of(row_start=A, rows=500)
+    assert with_rows == bytes_of(row_start=64 * A) and without > 0 and with_rows > without and with_rows > larger > 0
+    call = lambda ws_bytes: attend(cache(heads=1), batch(rows=60, n_seqs=1, n_slots=1, ld=80, row_start=A), hq=64, ldq=64 * 128, ldo=64 * 128, ws_bytes=ws_bytes)
+    assert call(with_rows - 1) == WORKSPACE and call(without) == WORKSPACE and call(larger) == WORKSPACE
