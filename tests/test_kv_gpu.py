@@ -1216,3 +1216,26 @@ def test_prompts_over_keys_of_the_smallest_ranges(oracle, b, far):
     assert more.max() < 2.0 ** -21
     worst = np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / tolerance(want, absv, err_s + more, err_o, "bf16", "f32")
     assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+@pytest.mark.parametrize("exponent", [-84, 76])
+@pytest.mark.parametrize("heads,group,dim,lengths,new", KINDS)
+def test_values_at_the_ends_of_their_range(oracle, b, heads, group, dim, lengths, new, exponent):
+    """All values as small and as large as attention's sums are stated to hold: alphas of 2^-87 and of 2^78."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(54)
+    c = make(rng, heads, group, dim, 32, lengths, new)
+    for i, l in enumerate(lengths):
+        k, v = (rng.standard_normal((l, heads, dim)) for _ in range(2))
+        okv.append(c.pages, c.table, [(r, i, r) for r in range(l)], k.astype(np.float32), np.ldexp(v, exponent).astype(np.float32))
+    q = _bf16(rng.standard_normal((c.rows, heads * group, dim)).astype(np.float32))
+    cache, batch = on_device(b, c)
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    out = torch.empty((c.rows, heads * group * dim), device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), torch.bfloat16), cache, 0, batch, 0.1, out, ws)
+    want, absv, err_s, err_o = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(0.1))
+    back = 2.0 ** -exponent                                    # the bounds as they are for values around 1
+    got = out.double().cpu().numpy().reshape(want.shape) * back
+    worst = np.abs(got - want * back) / tolerance(want * back, absv * back, err_s, err_o * back, "bf16", "f32")
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
