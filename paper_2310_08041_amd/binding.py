@@ -718,8 +718,15 @@ def qllm_kv_page_bytes(heads, dim, page_tokens):
     return int(v)
 
 
+def _kept(name):
+    """An attribute that its C struct points into: its contents may change, another array in its place is refused."""
+    return property(lambda self: getattr(self, "_" + name))
+
+
 class DeviceKVCache:
     """The pages of all layers, [layers, n_pages, page bytes] uint8 (made here unless given), and a C struct for each layer."""
+
+    pages = _kept("pages")
 
     def __init__(self, layers, n_pages, heads, dim, page_tokens, pages=None, device="cuda"):
         self.page_bytes = qllm_kv_page_bytes(heads, dim, page_tokens)
@@ -730,7 +737,7 @@ class DeviceKVCache:
         _check_tensor(pages, "pages", _U8_ONLY, shape=(self.layers, self.n_pages, self.page_bytes))
         if not pages.is_contiguous():
             _fail("pages must be contiguous")
-        self.pages, self.device = pages, pages.get_device()
+        self._pages, self.device = pages, pages.get_device()
         step = self.n_pages * self.page_bytes
         self.c = [_KVCache(self.heads, self.dim, self.page_tokens, self.n_pages, _dp(pages) + i * step) for i in range(self.layers)]
         self.ref = [C.byref(c) for c in self.c]
@@ -739,6 +746,8 @@ class DeviceKVCache:
 class DeviceKVBatch:
     """The sequences of a step: table [lines, pages] and length [lines] of the cache's lines, row_start [sequences + 1] (None: one row
     each, in order), slot [sequences] the sequences' lines (None: the lines in order).  int32 device tensors, kept alive here."""
+
+    table, length, row_start, slot = _kept("table"), _kept("length"), _kept("row_start"), _kept("slot")
 
     def __init__(self, rows, table, length, row_start=None, slot=None):
         _need(hasattr(table, "dim") and table.dim() == 2 and table.is_contiguous(), "table must be a contiguous 2-d tensor [lines, pages]")
@@ -752,7 +761,7 @@ class DeviceKVBatch:
         _check_tensor(slot, "slot", _I32_ONLY, numel=self.n_seqs, optional=True)
         _need(row_start is not None or self.rows >= self.n_seqs, f"{self.n_seqs} sequences of one row each need as many rows, there are {self.rows}")
         _need(slot is not None or n_slots >= self.n_seqs, f"{self.n_seqs} sequences, but {n_slots} lines in the table")
-        self.table, self.length, self.row_start, self.slot = table, length, row_start, slot
+        self._table, self._length, self._row_start, self._slot = table, length, row_start, slot
         self.device = table.get_device()
         for name, t in (("length", length), ("row_start", row_start), ("slot", slot)):
             if t is not None and t.get_device() != self.device:
@@ -861,13 +870,15 @@ class KVBook:
     """Which page of a cache belongs to whom: table [lines, pages] (-1: none), length [lines], refs [n_pages], int32 numpy arrays that
     the qllm_kv_*_host calls work on in place."""
 
+    table, length, refs = _kept("table"), _kept("length"), _kept("refs")
+
     def __init__(self, page_tokens, table, length, refs):
         for name, a, dims in (("table", table, 2), ("length", length, 1), ("refs", refs, 1)):
             if not (isinstance(a, np.ndarray) and a.dtype == np.int32 and a.ndim == dims and a.flags.c_contiguous and a.flags.writeable):
                 _fail(f"{name} must be a writeable contiguous int32 array of {dims} dimensions")
         if length.size != table.shape[0]:
             _fail(f"length must hold one entry per line of the table ({table.shape[0]})")
-        self.page_tokens, self.table, self.length, self.refs = int(page_tokens), table, length, refs
+        self.page_tokens, self._table, self._length, self._refs = int(page_tokens), table, length, refs
         self.c = _KVBook(self.page_tokens, table.shape[0], table.shape[1], refs.size, _host_at(table), _host_at(length), _host_at(refs))
 
     @classmethod

@@ -161,6 +161,19 @@ def test_wrappers_refuse_tensors_of_another_device(monkeypatch):
         b._check_on_current(a=here, q=there)
 
 
+def test_arrays_that_the_library_holds_addresses_of_are_not_replaced():
+    """An assignment would leave the C struct with the old array's address, and its memory to the next owner."""
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    book, kv, t = b.KVBook.empty(2, 3, 4, 32), b.DeviceKVCache(1, 5, 2, 64, 32, device="cpu"), b.DeviceKVBatch(3, i32(3, 4), i32(3), slot=i32(3))
+    for owner, names in ((book, ("table", "length", "refs")), (kv, ("pages",)), (t, ("table", "length", "row_start", "slot"))):
+        for name in names:
+            with pytest.raises(AttributeError):
+                setattr(owner, name, getattr(owner, name))
+    book.length[:] = 1                                                       # their contents are the caller's
+    t.length.add_(1)
+    kv.pages.zero_()
+
+
 # ---------------------------------------------------------------- the book
 
 def same(book, plain):
