@@ -4,6 +4,7 @@ Argument marshalling only.  torch supplies device memory and the current HIP str
 the layer runs inside the library's kernels.  Importing this module fails loudly if the library has
 not been built (run `python __graft_entry__.py` or `paper_2310_08041_amd/_build.py`).
 """
+import array
 import ctypes as C
 import os
 
@@ -852,8 +853,8 @@ def qllm_kv_attention(q, cache, layer, batch, scale, out, workspace, window=0, s
 
 def qllm_kv_copy_pages(cache, src, dst, stream=None):
     """Page dst[i] becomes a copy of page src[i] in every layer; src, dst: host arrays (what fork and compaction return)."""
-    src, dst = _np(src, np.int32), _np(dst, np.int32)
-    if src.ndim != 1 or src.shape != dst.shape:
+    src, dst = _host_list(src, "src"), _host_list(dst, "dst")
+    if src.size != dst.size:
         _fail("src and dst must be 1-d arrays of one length")
     if not (cache.device >= 0 and torch.cuda.current_device() == cache.device):
         _check_on_current(pages=cache.pages)
@@ -887,7 +888,18 @@ class KVBook:
 
 
 def _host_list(a, name, size=None):
-    a = np.atleast_1d(_np(a, np.int32))
+    """A list of numbers for the library: int32, whole, none wrapped around.  (array() checks a Python list, faster than numpy converts it.)"""
+    if isinstance(a, (list, tuple)):
+        try:
+            a = np.frombuffer(array.array("i", a), np.int32) if a else np.empty(0, np.int32)
+        except (TypeError, OverflowError):
+            _fail(f"{name} must hold whole numbers of 32 bits")
+    elif not (isinstance(a, np.ndarray) and a.dtype == np.int32):
+        given = np.asarray(a)
+        a = given.astype(np.int32)
+        if given.size and (given.dtype.kind not in "iu" or not (a == given).all()):
+            _fail(f"{name} must hold whole numbers of 32 bits")
+    a = np.ascontiguousarray(np.atleast_1d(a))
     if a.ndim != 1 or (size is not None and a.size != size):
         _fail(f"{name} must be a list" + ("" if size is None else f" of {size}"))
     return a

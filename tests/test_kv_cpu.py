@@ -174,6 +174,29 @@ def test_arrays_that_the_library_holds_addresses_of_are_not_replaced():
     kv.pages.zero_()
 
 
+def test_lists_that_do_not_fit_are_refused_and_not_wrapped_around():
+    """64-bit numbers beyond int32 named line 0, fractions the line below: refused, in any form that a list may come in."""
+    book = b.KVBook.empty(2, 3, 4, 32)
+    b.qllm_kv_reserve_host(book, [0, 1], [5, 6])
+    kv = b.DeviceKVCache(1, 5, 2, 64, 32, device="cpu")
+    far = 2 ** 32
+    for bad in ([far], (far,), [-far], np.array([far]), np.array([-far]), np.array([far], np.uint64), np.array([2 ** 31]), torch.tensor([far]), [0.5], [1.0],
+                np.array([0.5]), torch.tensor([0.0]), [None], ["0"], np.array([True])):
+        for call in (lambda: b.qllm_kv_free_host(book, bad), lambda: b.qllm_kv_reserve_host(book, bad, [1]), lambda: b.qllm_kv_reserve_host(book, [1], bad),
+                     lambda: b.qllm_kv_copy_pages(kv, bad, [1]), lambda: b.qllm_kv_fork_host(book, bad, [1])):
+            with pytest.raises(ValueError, match="whole numbers"):
+                call()
+    assert book.length.tolist() == [5, 6]
+    for good in ([1], (1,), np.array([1]), np.array([1], np.uint8), np.array([0, 1, 2], np.int32)[1::2], torch.tensor([1]), 1, np.int64(1), [np.int64(1)]):
+        b.qllm_kv_reserve_host(book, good, 1)
+    assert book.length.tolist() == [5, 15]
+    b.qllm_kv_free_host(book, [])
+    b.qllm_kv_free_host(book, np.array([]))
+    for bad in ([[0, 1]], np.zeros((1, 2), np.int32)):
+        with pytest.raises(ValueError):
+            b.qllm_kv_free_host(book, bad)
+
+
 # ---------------------------------------------------------------- the book
 
 def same(book, plain):
