@@ -118,11 +118,18 @@ def bench_swiglu(args, w, dev):
     return 0 if result.get("parity_checked", {"ok": True})["ok"] else 1
 
 
+def kv_tokens(sequences, context, shared, page):
+    """Tokens that lie in the cache, each once: whole pages of the shared prompt are there for all lines together, a partly filled one
+    and everything behind it for each line."""
+    whole = shared // page * page
+    return sequences * (context - whole) + whole
+
+
 def bench_kv(args, dev):
     """The cache beside the layers: one decoding step of --sequences lines of --context tokens, --heads query heads on --kv-heads
     key/value heads of 128 channels, bfloat16; the first --shared tokens are one prompt, whose pages all lines share.  A step =
     qllm_kv_append (rotary positions, the new tokens' keys and values as 4-bit codes) and qllm_kv_attention over all of the codes;
-    144 bytes per token and head against HBM."""
+    144 bytes per token and head against HBM, tokens in shared pages once (kv_tokens), however often caches serve them again."""
     import numpy as np
     import torch
 
@@ -132,7 +139,8 @@ def bench_kv(args, dev):
     shared = max(0, min(args.shared, ctx - 1))
     per_line = -(-ctx // page)
     book = b.KVBook.empty(n, per_line, n * per_line, page)
-    cached = (n * (ctx - shared) + shared) * b.qllm_kv_page_bytes(hk, dim, page) // page
+    tokens = kv_tokens(n, ctx, shared, page)
+    cached = tokens * b.qllm_kv_page_bytes(hk, dim, page) // page
     layers = max(2, min(32, -(-(768 << 20) // cached)))                            # past the last-level cache
     g = torch.Generator(device=dev).manual_seed(2310)
     cache = b.DeviceKVCache(layers, n * per_line, hk, dim, page)
@@ -186,14 +194,14 @@ def bench_kv(args, dev):
     ev[1].record()
     torch.cuda.synchronize()
     t_attend = ev[0].elapsed_time(ev[1]) * 1e-3 / args.steps
-    nbytes = float(n * ctx * hk * (dim + 16))
+    nbytes = float(tokens * hk * (dim + 16))
     result = {
         "metric": "decoding step over the 4-bit key/value cache (append + attention), GB/s of codes read", "value": nbytes / (wall / args.steps) / 1e9,
         "unit": "GB/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": wall * 1e3 / args.steps,
         "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
         "dtype": "bf16 (4-bit codes, fp32 scores and sums)", "data": "synthetic",
         "config": {"sequences": n, "context": ctx, "heads": hq, "kv_heads": hk, "dim": dim, "page_tokens": page, "layers": layers, "shared": shared,
-                   "pages_in_use": int((book.refs > 0).sum()),
+                   "pages_in_use": int((book.refs > 0).sum()), "bytes_of_all_sequences": float(n * ctx * hk * (dim + 16)),
                    "warmup_done": {"steps": warm_steps, "gpu_ms": warm_ms}},
         "roofline": {"kernel": "attend_kernel + join_kernel", "bound": "hbm", "achieved": nbytes / t_attend / 1e9, "peak": HBM_PEAK_GBS, "unit": "GB/s",
                      "frac": nbytes / t_attend / 1e9 / HBM_PEAK_GBS, "avg_launch_us": t_attend * 1e6, "algorithmic_bytes": nbytes, "traffic": None},

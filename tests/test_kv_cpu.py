@@ -305,6 +305,20 @@ def test_book_refuses_what_contradicts_itself():
     assert lib.qllm_kv_compact_host(C.byref(made().c), None, None) == NULL
 
 
+@pytest.mark.parametrize("n,ctx,shared,page", [(4, 200, 0, 64), (4, 200, 63, 64), (4, 200, 64, 64), (4, 200, 150, 64), (1, 200, 150, 64), (3, 64, 63, 32), (16, 500, 499, 32)])
+def test_bench_counts_tokens_in_shared_pages_once(n, ctx, shared, page):
+    """Against the book that the bench's cache stage makes: a token of every entry of every page."""
+    import bench
+    per_line = -(-ctx // page)
+    book = b.KVBook.empty(n, per_line, n * per_line, page)
+    if shared:
+        b.qllm_kv_reserve_host(book, [0], [shared])
+        b.qllm_kv_fork_host(book, [0] * (n - 1), list(range(1, n)))
+    b.qllm_kv_reserve_host(book, list(range(n)), [ctx - int(x) for x in book.length])
+    places = {(int(book.table[i, t // page]), t % page) for i in range(n) for t in range(ctx)}
+    assert bench.kv_tokens(n, ctx, shared, page) == len(places)
+
+
 # ---------------------------------------------------------------- pins of the numpy statement
 
 def test_statement_of_the_rotation():
