@@ -132,8 +132,9 @@ def attention(q, pages, table, tokens, length, scale, window=0, out=None, close=
                 out[r, o] = w @ v
                 absv[r, o] = w @ np.abs(v)
                 # sums of dim products (16 + code) q, (16 + beta) sum q, and a few roundings of the score itself
-                if close:  # an operation per 32 channels; the queries' sum: dim / 8 additions and three across lanes
-                    sums = abs(scale) * a[:, 0] * (31.0 * (dim // 32 + 1) + (16.0 + b[:, 0]) * (dim // 8 + 5)) * np.abs(x).sum()
+                if close:  # an operation per 32 channels, off by 2 * 2^-24 of its magnitudes (1.7 measured); the queries' sum: dim / 8
+                    # additions and three across lanes
+                    sums = abs(scale) * a[:, 0] * (2 * 31.0 * (dim // 32 + 1) + (16.0 + b[:, 0]) * (dim // 8 + 5)) * np.abs(x).sum()
                     adds = 4 * (seen.sum() // 128 + 1) + 16  # two operations a step of 32 tokens for each part of the weights, waves and parts joined
                 else:
                     sums = abs(scale) * a[:, 0] * (47.0 + b[:, 0]) * np.abs(x).sum() * (dim + 8)
