@@ -100,7 +100,7 @@ int32_t qllm_kv_read(const qllm_kv_cache *cache, const qllm_kv_batch *batch, voi
  * Equal calls give equal bits.
  * Codes enter the matrix cores as exact bf16 integers; scores, maxima and sums are fp32.  The weights (times a value's alpha)
  * meet the values in bf16 parts: with fp32 queries, which come in three parts too, 24 bits; with bf16 queries 2^-16 of each is
- * left out at most, in sequences of many rows 2^-8 (one part, rounded, which is also what is summed below the line).
+ * left out at most, in sequences of many rows with bf16 out 2^-8 (one part, rounded, which is also what is summed below the line).
  * A query that is not finite spoils the output of its own row and head alone.
  * The fp32 numbers have to hold: (32 + |beta|) sum |q|, and |scale| alpha times that, of every key that a row sees; values whose alphas are
  * all below 2^-88, or some above 2^80, may overflow a sum or lose bits.

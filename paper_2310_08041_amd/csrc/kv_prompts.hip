@@ -12,6 +12,11 @@
 //     1 / alpha_v in the next ones: the zero points' share of the values' sums, and the sum of the weights.
 // The zero points' sums are added to the others every few tiles, so that the two stay small and lose nothing to each other.
 //
+// The weights meet the values in bf16 parts, the same ones above and below the line.  With float32 out two of them, as in the kernel for
+// few rows; with bf16 out one, rounded: error against 64 bits 0.0021 where bf16 out by itself costs 0.0017 (which two parts leave it at).
+// One part and two, us: 2048 tokens x 32 heads 60 and 72 (float32 out 84 and 94), 2000 tokens behind 14000 x 8 heads of 8 1103 and 1450
+// (float32 out 1158 and 1504).
+//
 // Two workgroups share a CU, so that one lays out while the other multiplies.  A launch of no more workgroups than the card holds
 // leaves CUs with one, or with a long and a short one: there a workgroup has two groups of four waves, every other tile of tokens
 // each, each with its own LDS, one of them half a turn behind, and joins their results at the end.  D 128, us, one group first:
@@ -149,7 +154,7 @@ __device__ __forceinline__ int64_t part_at(const AttendArgs &a, int32_t head, in
 template <int D, bool F32O, int GROUPS>
 __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const AttendArgs a)
 {
-    constexpr int KSTEPS = D / 16, DT = D / 32;
+    constexpr int KSTEPS = D / 16, DT = D / 32, WPARTS = F32O ? 2 : 1; // bf16 parts of a weight
     __shared__ __attribute__((aligned(16))) Operands<D> operands[GROUPS][2];
 
     const Step &s = a.s;
@@ -398,25 +403,28 @@ __global__ __launch_bounds__(GROUPS * THREADS, 2) void prompts_kernel(const Atte
         for (int i = 0; i <= DT; ++i) vv[i] = operand_of(0, i);
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-            u32x4 pw;
+            float w[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                pw[e] = pack_bf16(__builtin_amdgcn_exp2f(sc[y >> 1][8 * (y & 1) + 2 * e]), __builtin_amdgcn_exp2f(sc[y >> 1][8 * (y & 1) + 2 * e + 1]));
-            const bf16x8 p = __builtin_bit_cast(bf16x8, pw);
+            for (int e = 0; e < 8; ++e) w[e] = __builtin_amdgcn_exp2f(sc[y >> 1][8 * (y & 1) + e]);
+            bf16x8 p[WPARTS];
+            split8<WPARTS>(w, p);
 #pragma unroll
             for (int i = 0; i <= DT; ++i) {
-                if (i == 0) off = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv[0], p, off, 0, 0, 0);
-                else acc[i - 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv[i], p, acc[i - 1], 0, 0, 0);
+#pragma unroll
+                for (int j = WPARTS - 1; j >= 0; --j) {
+                    if (i == 0) off = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv[0], p[j], off, 0, 0, 0);
+                    else acc[i - 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv[i], p[j], acc[i - 1], 0, 0, 0);
+                }
                 if (y < 3) vv[i] = operand_of(y + 1, i);
             }
         }
         __builtin_amdgcn_sched_group_barrier(0x100, DT + 1, 0);
 #pragma unroll
         for (int i = 0; i < 3 * (DT + 1); ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, WPARTS, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, DT + 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, WPARTS * (DT + 1), 0);
         if (add) {
             const float zero = off[0] + off[1] + off[2];
 #pragma unroll

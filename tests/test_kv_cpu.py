@@ -523,6 +523,13 @@ def test_close_bounds_of_prompts_reject_planted_mistakes(oracle, case):
         assert share(wider=1) > 1.0 and share(wider=-1) > 1.0
 
 
+@pytest.mark.parametrize("case", tg.CLOSE_PROMPTS, ids=str)
+def test_close_bounds_of_two_parts_reject_one(oracle, case):
+    c, q, want, bound = tg.two_part_prompts_case(*case)
+    share = lambda **k: (np.abs(mistaken(c, q, np.float32(c.dim ** -0.5), case[7], **k) - want) / bound).max()
+    assert share(weight_bits=17) <= 1.0 and share(weight_bits=9) > 1.0 and share(weight_bits=8) > 1.0
+
+
 @pytest.mark.parametrize("case", tg.WINDOWED, ids=str)
 def test_exactness_of_float32_rejects_weights_of_16_bits(oracle, case):
     c, q, want, plain = tg.windowed_case(*case)

@@ -1239,3 +1239,24 @@ def test_values_at_the_ends_of_their_range(oracle, b, heads, group, dim, lengths
     got = out.double().cpu().numpy().reshape(want.shape) * back
     worst = np.abs(got - want * back) / tolerance(want * back, absv * back, err_s, err_o * back, "bf16", "f32")
     assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+@pytest.mark.parametrize("q_type,heads,group,dim,page,lengths,new,window", CLOSE_PROMPTS)
+def test_attention_of_prompts_with_float32_out_keeps_two_parts_of_a_weight(oracle, b, q_type, heads, group, dim, page, lengths, new, window):
+    """What the kernel for few rows keeps: a caller who asks for float32 gets it whatever the number of rows."""
+    import torch
+    c, q, want, bound = two_part_prompts_case(q_type, heads, group, dim, page, lengths, new, window)
+    cache, batch = on_device(b, c)
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, heads * group), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    out = torch.empty((c.rows, heads * group * dim), device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(c.rows, -1), torch.bfloat16), cache, 0, batch, dim ** -0.5, out, ws, window=window)
+    worst = np.abs(out.double().cpu().numpy().reshape(want.shape) - want) / bound
+    assert worst.max() <= 1.0, (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+def two_part_prompts_case(*case):
+    """As close_prompts_case, 2^-16 of a weight left out."""
+    from oracle import kv_cache as okv
+    c, q, want, _ = close_case(*case)
+    bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(c.dim ** -0.5), case[7], close=True)[1:]
+    return c, q, want, okv.attention_bound(want, bounds[0], 2.0 * bounds[1], bounds[2], 2.0 ** -16, 2.0 ** -24)
