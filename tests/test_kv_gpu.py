@@ -1260,3 +1260,39 @@ def two_part_prompts_case(*case):
     c, q, want, _ = close_case(*case)
     bounds = okv.attention(q, c.pages, c.table, c.tokens, c.length, np.float32(c.dim ** -0.5), case[7], close=True)[1:]
     return c, q, want, okv.attention_bound(want, bounds[0], 2.0 * bounds[1], bounds[2], 2.0 ** -16, 2.0 ** -24)
+
+
+@pytest.mark.parametrize("q_type,heads,group,new", [("bf16", 1, 3, [2, 0, 5, 1]), ("f32", 2, 2, [30, 1, 0, 40]), ("bf16", 16, 8, [90, 0, 33, 1]), ("bf16", 1, 20, [3, 2, 1] * 40)])
+def test_rows_before_the_first_sequence_and_a_line_named_more_than_once(oracle, b, q_type, heads, group, new):
+    """row_start may begin behind row 0, attention and read may name a line twice: rows of no sequence stay as they were."""
+    import torch
+    from oracle import kv_cache as okv
+    rng = np.random.default_rng(55)
+    dim, page, lead, tail = 64, 32, 7, 4
+    n, hq = len(new), heads * group
+    slots = [i % 3 for i in range(n)]
+    c = make(rng, heads, group, dim, page, [100, 47, 130], None)
+    start = (lead + np.concatenate([[0], np.cumsum(new)])).astype(np.int32)
+    rows = int(start[-1]) + tail
+    tokens = okv.rows_of(rows, start, np.array(slots), c.length)
+    q = rng.standard_normal((rows, hq, dim)).astype(np.float32)
+    q = _bf16(q) if q_type == "bf16" else q
+    cache, _ = on_device(b, c)
+    batch = b.DeviceKVBatch(rows, _t(c.table), _t(c.length), _t(start), _t(np.array(slots, np.int32)))
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, hq), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    out = torch.full((rows, hq * dim), 5.0, device="cuda")
+    b.qllm_kv_attention(_t(q.reshape(rows, -1), torch.bfloat16 if q_type == "bf16" else torch.float32), cache, 0, batch, 0.125, out, ws)
+    k_out, v_out = (torch.full((rows, heads * dim), 9.0, device="cuda") for _ in range(2))
+    b.qllm_kv_read(cache, 0, batch, k_out, v_out)
+    want, *bounds = okv.attention(q, c.pages, c.table, tokens, c.length, np.float32(0.125), out=np.full(q.shape, 5.0))
+    got = out.double().cpu().numpy().reshape(want.shape)
+    off = np.abs(got - want) / tolerance(want, *bounds, q_type, "f32")
+    assert off.max() <= 1.0, (off.max(), np.unravel_index(off.argmax(), off.shape))
+    k_got, v_got = (x.cpu().numpy().reshape(rows, heads, dim) for x in (k_out, v_out))
+    for r in [*range(lead), *range(rows - tail, rows)]:
+        assert (got[r] == 5.0).all() and (k_got[r] == 9.0).all() and (v_got[r] == 9.0).all()
+    for r, line, p in tokens:
+        at = okv.page_at(c.table, c.n_pages, page, line, p)
+        for h in range(heads):
+            assert np.array_equal(k_got[r, h], c.pages.get(at, h, p % page, 0)[0].astype(np.float32))
+            assert np.array_equal(v_got[r, h], c.pages.get(at, h, p % page, 1)[0].astype(np.float32))
