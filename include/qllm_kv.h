@@ -29,7 +29,7 @@ extern "C" {
  *   alpha of the values  [page_tokens] float        beta of the values  [page_tokens] int32
  * qllm_kv_append writes alphas from 2^-126 on.  Attention takes what others wrote too: an alpha of 0 (a page of zero bytes, tokens that
  * a length counts before they are appended) is a key or value of 0, a value's alpha below 2^-126 may count as 0, and one that is
- * negative or not finite spoils the rows that see the token.  What lies in places of no token may be anything.
+ * negative or not finite may spoil the rows that see the token.  What lies in places of no token may be anything.
  */
 typedef struct {
     int64_t heads, dim, page_tokens, n_pages;
@@ -80,8 +80,9 @@ int32_t qllm_kv_append(const void *q, int64_t ldq, int64_t q_heads, void *q_out,
                        const void *v, int64_t ldv, int32_t x_dtype, int32_t rope, const double *inv_freq,
                        const qllm_kv_cache *cache, const qllm_kv_batch *batch, void *hip_stream);
 
-/* What the cache holds for the step's rows: alpha * (code - beta), rounded to float (from |beta| = 2^23 on to double first) and from there to dtype
- * (fp32 / bf16), in k_out [rows, ldk] and v_out [rows, ldv] (either may be NULL).  Rows whose token is not there are left as they were.  Errors as above. */
+/* What the cache holds for the step's rows: alpha * (code - beta), rounded to float (from |beta| = 2^23 on to double first) and
+ * from there to dtype (fp32 / bf16), in k_out [rows, ldk] and v_out [rows, ldv] (either may be NULL).  Rows whose token is not there
+ * are left as they were.  Errors as above. */
 int32_t qllm_kv_read(const qllm_kv_cache *cache, const qllm_kv_batch *batch, void *k_out, int64_t ldk, void *v_out, int64_t ldv,
                      int32_t dtype, void *hip_stream);
 
@@ -102,8 +103,8 @@ int32_t qllm_kv_read(const qllm_kv_cache *cache, const qllm_kv_batch *batch, voi
  * meet the values in bf16 parts: with fp32 queries, which come in three parts too, 24 bits; with bf16 queries 2^-16 of each is
  * left out at most, in sequences of many rows with bf16 out 2^-8 (one part, rounded, which is also what is summed below the line).
  * A query that is not finite spoils the output of its own row and head alone.
- * The fp32 numbers have to hold: (32 + |beta|) sum |q|, and |scale| alpha times that, of every key that a row sees; values whose alphas are
- * all below 2^-88, or some above 2^80, may overflow a sum or lose bits.
+ * The fp32 numbers have to hold: (32 + |beta|) sum |q|, and |scale| alpha times that, of every key that a row sees; values whose
+ * alphas are all below 2^-88, or some above 2^80, may overflow a sum or lose bits.
  * In sequences of many rows with bf16 queries a key whose |scale| alpha is below 2^-90 counts as one of 2^-90 (which is nothing
  * for queries below 2^30), and a token whose value's alpha is less than 2^-100 of another's that the query sees may count for
  * less than its share below the line.
