@@ -1296,3 +1296,33 @@ def test_rows_before_the_first_sequence_and_a_line_named_more_than_once(oracle, 
         for h in range(heads):
             assert np.array_equal(k_got[r, h], c.pages.get(at, h, p % page, 0)[0].astype(np.float32))
             assert np.array_equal(v_got[r, h], c.pages.get(at, h, p % page, 1)[0].astype(np.float32))
+
+
+@pytest.mark.parametrize("heads,group,dim,lengths,new", [(2, 16, 128, [3000], [130]), (4, 16, 128, [2600, 400, 1500], [70, 1, 40])])
+def test_prompts_shared_by_workgroups_write_over_their_queries(oracle, b, heads, group, dim, lengths, new):
+    """A tile's parts read its queries in several workgroups, the output comes from a second kernel: the same bits in place and
+    through a graph."""
+    import torch
+    rng = np.random.default_rng(56)
+    c = make(rng, heads, group, dim, 64, lengths, new)
+    hq = heads * group
+    cache, batch = on_device(b, c)
+    q = _t(rng.standard_normal((c.rows, hq * dim)).astype(np.float32), torch.bfloat16)
+    ws = torch.empty(b.qllm_kv_attention_workspace_bytes(cache, batch, hq), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    want = b.qllm_kv_attention(q, cache, 0, batch, 0.1, torch.empty_like(q), ws)
+    over = q.clone()
+    b.qllm_kv_attention(over, cache, 0, batch, 0.1, over, ws)
+    assert torch.equal(over, want)
+    torch.cuda.synchronize()
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        b.qllm_kv_attention(over, cache, 0, batch, 0.1, over, ws)
+    for _ in range(3):
+        over.copy_(q)
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(over, want)
+        assert torch.equal(b.qllm_kv_attention(q, cache, 0, batch, 0.1, torch.empty_like(q), ws), want)
