@@ -61,6 +61,19 @@ class _KVBatch(C.Structure):
                 ("table_ld", C.c_int64), ("table", C.c_void_p), ("length", C.c_void_p)]
 
 
+class _Gather(C.Structure):
+    _fields_ = [("C_in", C.c_int64), ("C_out", C.c_int64), ("n_computed", C.c_int64), ("index", C.c_void_p)]
+
+
+ADAPTER_PARTS, ADAPTER_RANKS = 4, 256
+
+
+class _Adapters(C.Structure):
+    _fields_ = [("n_adapters", C.c_int64), ("C", C.c_int64), ("O", C.c_int64), ("rank", C.c_int64), ("n_parts", C.c_int32),
+                ("part_O", C.c_int64 * ADAPTER_PARTS), ("w_dtype", C.c_int32), ("A", C.c_void_p), ("B", C.c_void_p), ("scale", C.c_void_p),
+                ("ranks", C.c_void_p)]
+
+
 class _KVBook(C.Structure):
     _fields_ = [("page_tokens", C.c_int64), ("n_slots", C.c_int64), ("table_ld", C.c_int64), ("n_pages", C.c_int64), ("table", C.c_void_p),
                 ("length", C.c_void_p), ("refs", C.c_void_p)]
@@ -119,6 +132,13 @@ _sigs = {
     "qllm_kv_fork_host": (_i64, [C.POINTER(_KVBook), _vp, _vp, _i64, _vp, _vp]),
     "qllm_kv_free_host": (_i32, [C.POINTER(_KVBook), _vp, _i64]),
     "qllm_kv_compact_host": (_i64, [C.POINTER(_KVBook), _vp, _vp]),
+    "qllm_gather_map_host": (_i32, [_vp, _vp, _vp, _i64, _i64, _vp, C.POINTER(_i64), C.POINTER(_i64)]),
+    "qllm_add_norm_quant": (_i32, [_vp, _i32, _i64, _vp, _i32, _i64, _i64, _i64, _vp, _i64, _i32, _vp, _vp, _f, C.POINTER(_Gather), _i32,
+                                   C.POINTER(_QAct), _vp, _i64, _vp, _i64, _i32, _vp]),
+    "qllm_adapter_plan_bytes": (_i64, [_i64, _i64]),
+    "qllm_adapter_plan": (_i32, [_i64, _i64, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "qllm_adapter_workspace_bytes": (_i64, [C.POINTER(_Adapters), _i64]),
+    "qllm_adapter_apply": (_i32, [_vp, _i32, _i64, _i64, C.POINTER(_Adapters), _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _i64, _vp]),
     "qllm_probe_mfma": (_i32, [_i32, _i32, _vp, _vp]),
     "qllm_probe_mfma_fp6": (_i32, [_i32, _i32, _vp, _vp]),
     "qllm_probe_stream": (_i32, [_vp, _vp, _i64, _i32, _vp]),
@@ -985,3 +1005,155 @@ def qllm_probe_layer_half(half, x, norm, gamma, beta, eps, dmap, a_bits, weight,
 def raw():
     """The ctypes library handle, for tests that pass deliberately bad arguments."""
     return _lib
+
+
+# ---------------------------------------------------------------- between the layers (include/qllm_block.h)
+
+def qllm_gather_map_host(row_ptr, src, scale, C_in):
+    """A CSR map as qllm_add_norm_quant reads it: (index int32 array, number of computed channels)."""
+    row_ptr, src, scale = _np(row_ptr, np.int32), _np(src, np.int32), _np(scale, np.float32)
+    _need(row_ptr.ndim == 1 and row_ptr.size >= 2 and src.size == scale.size and row_ptr[-1] == src.size and (np.diff(row_ptr) >= 0).all(),
+          "row_ptr, src and scale are no CSR map")
+    n, computed = _i64(0), _i64(0)
+    args = (_hp(row_ptr), _hp(src), _hp(scale), int(C_in), row_ptr.size - 1)
+    _chk(_lib.qllm_gather_map_host(*args, None, C.byref(n), C.byref(computed)), "qllm_gather_map_host(size)")
+    index = np.empty(n.value, np.int32)
+    _chk(_lib.qllm_gather_map_host(*args, _hp(index), C.byref(n), C.byref(computed)), "qllm_gather_map_host")
+    return index, computed.value
+
+
+class DeviceGather:
+    """Device copy of a reassembly map's index for qllm_add_norm_quant; the map as qllm_build_map_host returns it."""
+
+    index = _kept("index")
+
+    def __init__(self, row_ptr, src, scale, C_in, device="cuda"):
+        index, computed = qllm_gather_map_host(row_ptr, src, scale, C_in)
+        self._index, self.C_in, self.C_out = torch.from_numpy(index).to(device), int(C_in), int(np.size(row_ptr) - 1)
+        self.c = _Gather(self.C_in, self.C_out, computed, _dp(self._index))
+        self.ref = C.byref(self.c)
+
+
+def _check_here(**tensors):
+    """Everything on the device that the call runs on; the list is walked twice only if something is wrong."""
+    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    for t in tensors.values():
+        if t is not None and (t.get_device() != here or here < 0):
+            _check_on_current(**tensors)
+
+
+def qllm_add_norm_quant(x, residual, sum_out, norm, gamma, beta, eps, out=None, bits=8, gather=None, y_out=None, values_out=None, stream=None):
+    """sum_out = residual + x (rounded to the residual's dtype), its norm, the reassembly of `gather` (DeviceGather or None) and Eq. (2) at
+    `bits` into out (DeviceQAct or None).  x [N, C] (None: nothing is added), residual and sum_out [N, C] (sum_out may be residual, x or
+    None), y_out [N, C] the normalised rows, values_out [N, C_out] what the codes stand for (one dtype, either may be None)."""
+    if not (hasattr(residual, "dim") and residual.dim() == 2):
+        _fail("residual must be a 2-d tensor [tokens, channels]")
+    N, Cc = residual.shape
+    ldr = _check_rows(residual, "residual", _FLOATS, N, Cc)
+    ldx = _check_rows(x, "x", _FLOATS, N, Cc) if x is not None else 0
+    lds = _check_rows(sum_out, "sum_out", (residual.dtype,), N, Cc) if sum_out is not None else 0
+    ldy = _check_rows(y_out, "y_out", _FLOATS, N, Cc) if y_out is not None else 0
+    K = Cc if gather is None else gather.C_out
+    if gather is not None and gather.C_in != Cc:
+        _fail(f"the map takes {gather.C_in} channels, residual has {Cc}")
+    if out is not None and (out.N != N or out.K != K or out.bits != int(bits)):
+        _fail(f"out holds {out.N} rows of {out.K} codes of {out.bits} bits, the call makes {N} of {K} of {int(bits)}")
+    ldv = 0
+    if values_out is not None:
+        if out is None:
+            _fail("values_out needs out")
+        ldv = _check_rows(values_out, "values_out", _FLOATS if y_out is None else (y_out.dtype,), N, K)
+    if int(norm) not in (NORM_NONE, NORM_LAYER, NORM_RMS):
+        _fail(f"unknown norm {norm}")
+    if int(norm) != NORM_NONE:
+        _check_tensor(gamma, "gamma", _F32_ONLY, numel=Cc)
+        _check_tensor(beta, "beta", _F32_ONLY, numel=Cc, optional=True)
+    else:
+        gamma = beta = None
+    _check_here(x=x, residual=residual, sum_out=sum_out, gamma=gamma, beta=beta, y_out=y_out, values_out=values_out,
+                index=None if gather is None else gather.index, codes=None if out is None else out.codes)
+    o = y_out if y_out is not None else values_out
+    _chk(_lib.qllm_add_norm_quant(_dp(x), _x_dtype(x) if x is not None else F32, ldx, _dp(residual), _x_dtype(residual), ldr, N, Cc, _dp(sum_out), lds,
+                                  int(norm), _dp(gamma), _dp(beta), float(eps), None if gather is None else gather.ref, int(bits),
+                                  None if out is None else C.byref(out.c), _dp(y_out), ldy, _dp(values_out), ldv,
+                                  F32 if o is None else _x_dtype(o), _stream(stream)), "qllm_add_norm_quant")
+
+
+class DeviceAdapters:
+    """A pool of low-rank adapters for one projection: A [places, parts * rank, C] and B [places, O, rank] (fp32 / bf16, rank a multiple
+    of 8), scale [places] float32 (None: 1), ranks [places] int32, each adapter's own (None: all), parts the outputs of each part of a
+    fused projection (None: one part).  Kept alive here; their contents may change, an adapter is loaded by writing its place."""
+
+    A, B, scale, ranks = _kept("A"), _kept("B"), _kept("scale"), _kept("ranks")
+
+    def __init__(self, A, B, scale=None, ranks=None, parts=None):
+        _need(hasattr(A, "dim") and A.dim() == 3 and hasattr(B, "dim") and B.dim() == 3, "A must be [places, parts * rank, C], B [places, O, rank]")
+        self.n_adapters, self.O, self.rank = (int(v) for v in B.shape)
+        self.parts = [self.O] if parts is None else [int(o) for o in parts]
+        _need(1 <= len(self.parts) <= ADAPTER_PARTS and min(self.parts) > 0 and sum(self.parts) == self.O, f"parts {self.parts} of {self.O} outputs")
+        _need(0 < self.rank <= ADAPTER_RANKS and self.rank % 8 == 0, f"a rank of {self.rank}")
+        self.C = int(A.shape[2])
+        _check_tensor(A, "A", _FLOATS, shape=(self.n_adapters, len(self.parts) * self.rank, self.C))
+        _check_tensor(B, "B", (A.dtype,))
+        _need(A.is_contiguous() and B.is_contiguous(), "A and B must be contiguous")
+        _check_tensor(scale, "scale", _F32_ONLY, numel=self.n_adapters, optional=True)
+        _check_tensor(ranks, "ranks", _I32_ONLY, numel=self.n_adapters, optional=True)
+        self._A, self._B, self._scale, self._ranks, self.device = A, B, scale, ranks, A.get_device()
+        for name, t in (("B", B), ("scale", scale), ("ranks", ranks)):
+            if t is not None and t.get_device() != self.device:
+                _fail(f"{name} is on another device than A")
+        self.c = _Adapters(self.n_adapters, self.C, self.O, self.rank, len(self.parts), (C.c_int64 * ADAPTER_PARTS)(*self.parts), _x_dtype(A),
+                           _dp(A), _dp(B), _dp(scale), _dp(ranks))
+        self.ref = C.byref(self.c)
+
+
+def qllm_adapter_plan_bytes(rows, n_adapters):
+    v = _lib.qllm_adapter_plan_bytes(int(rows), int(n_adapters))
+    _chk(v if v < 0 else 0, "qllm_adapter_plan_bytes")
+    return int(v)
+
+
+class DeviceAdapterPlan:
+    """Room for the plan of a step of `rows` rows over pools of n_adapters places."""
+
+    words = _kept("words")
+
+    def __init__(self, rows, n_adapters, device="cuda"):
+        self.rows, self.n_adapters = int(rows), int(n_adapters)
+        self._words = torch.zeros(qllm_adapter_plan_bytes(rows, n_adapters) // 4, dtype=torch.int32, device=device)
+        self.device = self._words.get_device()
+
+
+def qllm_adapter_plan(plan, adapter, row_start=None, stream=None):
+    """Fills the plan (DeviceAdapterPlan) of a step: adapter [sequences] int32, place in the pool (outside of it: none), row_start
+    [sequences + 1] int32 the sequences' rows (None: one row each).  Once a step, for all layers and projections."""
+    _check_tensor(adapter, "adapter", _I32_ONLY, numel=adapter.numel())
+    _check_tensor(row_start, "row_start", _I32_ONLY, numel=adapter.numel() + 1, optional=True)
+    _need(row_start is not None or adapter.numel() <= plan.rows, f"{adapter.numel()} sequences of one row each need as many rows, there are {plan.rows}")
+    _check_here(adapter=adapter, row_start=row_start, plan=plan.words)
+    _chk(_lib.qllm_adapter_plan(plan.rows, adapter.numel(), _dp(row_start), _dp(adapter), plan.n_adapters, _dp(plan.words), 4 * plan.words.numel(),
+                                _stream(stream)), "qllm_adapter_plan")
+
+
+def qllm_adapter_workspace_bytes(adapters, rows):
+    v = _lib.qllm_adapter_workspace_bytes(adapters.ref, int(rows))
+    _chk(v if v < 0 else 0, "qllm_adapter_workspace_bytes")
+    return int(v)
+
+
+def qllm_adapter_apply(x, adapters, plan, y, out, workspace, stream=None):
+    """out = y + each row's adapter on x: x [rows, C], y and out [rows, O] of one dtype (out may be y); plan a filled DeviceAdapterPlan;
+    workspace uint8, qllm_adapter_workspace_bytes(adapters, rows) of it."""
+    rows = plan.rows
+    ldx = _check_rows(x, "x", _FLOATS, rows, adapters.C)
+    ldy = _check_rows(y, "y", _FLOATS, rows, adapters.O)
+    ldo = _check_rows(out, "out", (y.dtype,), rows, adapters.O)
+    if plan.n_adapters != adapters.n_adapters:
+        _fail(f"a plan for pools of {plan.n_adapters} places, the adapters have {adapters.n_adapters}")
+    if not (isinstance(workspace, torch.Tensor) and workspace.dtype is torch.uint8 and workspace.is_contiguous()):
+        _check_tensor(workspace, "workspace", _U8_ONLY)
+        _fail("workspace must be contiguous")
+    _check_here(x=x, y=y, out=out, workspace=workspace, plan=plan.words, adapters=adapters.A)
+    _chk(_lib.qllm_adapter_apply(_dp(x), _x_dtype(x), ldx, rows, adapters.ref, _dp(plan.words), 4 * plan.words.numel(), _dp(y), ldy, _dp(out), ldo,
+                                 _x_dtype(y), _dp(workspace), workspace.numel(), _stream(stream)), "qllm_adapter_apply")
+    return out

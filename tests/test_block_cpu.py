@@ -1,0 +1,203 @@
+"""What stands between the layers without a GPU: refusals of every entry point before anything is launched, the index of a map."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from helpers import random_csr_map
+from paper_2310_08041_amd import binding as b
+
+NULL, SHAPE, BITS, DTYPE, MAP, ALIGN, WORKSPACE = -1, -2, -3, -4, -5, -6, -7
+A = 0x10000                                    # never dereferenced: every call below fails before a launch, or has nothing to do
+
+
+def add_norm(x=2 * A, xd=b.BF16, ldx=64, r=A, rd=b.BF16, ldr=64, N=0, Cc=64, s=3 * A, lds=64, norm=2, gamma=A, beta=None, gather=None, bits=8, out="q", codes=A,
+             scale=A, zero=A, rowsum=A, y=None, ldy=64, v=None, ldv=64, od=b.BF16):
+    q = b._QAct(codes, scale, zero, rowsum) if out else None
+    return b.raw().qllm_add_norm_quant(x, xd, ldx, r, rd, ldr, N, Cc, s, lds, norm, gamma, beta, 1e-5, None if gather is None else C.byref(gather), bits,
+                                       None if q is None else C.byref(q), y, ldy, v, ldv, od, None)
+
+
+def test_add_norm_refusals():
+    assert add_norm() == 0 and add_norm(s=A) == 0 and add_norm(s=2 * A) == 0 and add_norm(x=None, xd=9) == 0 and add_norm(out=None, codes=None, bits=3) == 0 and add_norm(s=None) == 0
+    for kw in (dict(r=None), dict(gamma=None), dict(codes=None), dict(scale=None), dict(zero=None), dict(rowsum=None), dict(out=None, v=A),
+               dict(gather=b._Gather(64, 64, 0, None))):
+        assert add_norm(**kw) == NULL, kw
+    assert add_norm(norm=0, gamma=None) == 0 and add_norm(norm=1, beta=A) == 0
+    for kw in (dict(N=-1), dict(N=1 << 31), dict(Cc=0), dict(Cc=32769, ldx=40000, ldr=40000, lds=40000), dict(ldx=63), dict(ldr=63), dict(lds=63),
+               dict(y=A, ldy=63), dict(v=A, ldv=63), dict(s=A, r=A, lds=65), dict(s=2 * A, ldx=65), dict(s=2 * A, xd=b.F32),
+               dict(gather=b._Gather(63, 64, 0, A)), dict(gather=b._Gather(64, 0, 0, A)), dict(gather=b._Gather(64, 32769, 0, A)),
+               dict(gather=b._Gather(64, 64, 65, A)), dict(gather=b._Gather(64, 64, -1, A)), dict(gather=b._Gather(64, 70, 0, A), v=A),
+               dict(Cc=32768, ldx=32768, ldr=32768, lds=32768, gather=b._Gather(32768, 32768, 7681, A))):
+        assert add_norm(**kw) == SHAPE, kw
+    for bits in (0, 3, 5, 7, 16):
+        assert add_norm(bits=bits) == BITS
+    for kw in (dict(xd=2), dict(rd=-1), dict(y=A, od=7), dict(v=A, od=7), dict(norm=3), dict(norm=-1)):
+        assert add_norm(**kw) == DTYPE, kw
+    assert add_norm(od=7) == 0                  # nothing of that type is asked for
+    for kw in (dict(x=A + 1), dict(r=A + 1), dict(r=A + 2, rd=b.F32), dict(s=A + 1), dict(gamma=A + 2), dict(beta=A + 1), dict(y=A + 1),
+               dict(y=A + 2, od=b.F32), dict(v=A + 1), dict(codes=A + 8), dict(scale=A + 2), dict(zero=A + 1), dict(rowsum=A + 2),
+               dict(gather=b._Gather(64, 64, 0, A + 8))):
+        assert add_norm(**kw) == ALIGN, kw
+
+
+def test_add_norm_binding_refuses():
+    x, r = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(4, 64)
+    g = torch.ones(64)
+
+    def call(x=x, r=r, s=None, norm=2, gamma=g, beta=None, **kw):
+        with pytest.raises((ValueError, b.QllmError)) as e:
+            b.qllm_add_norm_quant(x, r, s, norm, gamma, beta, 1e-5, **kw)
+        return str(e.value)
+
+    assert "device" in call()                   # everything but the device is in order
+    assert "residual" in call(r=None) and "residual" in call(r=torch.zeros(4)) and "residual" in call(r=r.double())
+    assert "x has" in call(x=x[:, :63]) and "x has" in call(x=x.half()) and "stride" in call(x=torch.zeros(64, 4, dtype=torch.bfloat16).t())
+    assert "sum_out" in call(s=torch.zeros(4, 64, dtype=torch.bfloat16)) and "sum_out" in call(s=r[:3])
+    assert "gamma" in call(gamma=None) and "gamma" in call(gamma=g[:5]) and "beta" in call(beta=g.double())
+    assert "norm" in call(norm=5)
+    assert "y_out" in call(y_out=torch.zeros(4, 65)) and "values_out needs" in call(values_out=r)
+    q = b.DeviceQAct(4, 64, 8, device="cpu")
+    assert "values_out" in call(out=q, values_out=torch.zeros(4, 65)) and "values_out" in call(out=q, y_out=r.clone(), values_out=x.clone())
+    assert "out holds" in call(out=q, bits=4) and "out holds" in call(out=b.DeviceQAct(5, 64, 8, device="cpu"))
+    csr = random_csr_map(np.random.default_rng(0), 60, 64, 7)
+    assert "map takes" in call(out=q, gather=b.DeviceGather(*csr, 60, device="cpu"))
+
+
+def apply_index(y, index, computed, C_in, C_out):
+    """What the device does with the index, in plain Python."""
+    S = (C_in + 7) // 8
+    padded = -(-C_out // 256) * 256
+    places = index[:padded // 2].view(np.uint16)
+    first = index[padded // 2:padded // 2 + computed + 1]
+    entries = index[padded // 2 + (computed + 2) // 2 * 2:].reshape(-1, 2)
+    row = np.zeros(8 * S + computed, np.float32)
+    for c in range(C_in):
+        row[(c % 8) * S + c // 8] = y[c]
+    for j in range(computed):
+        e = entries[first[j]:first[j + 1]]
+        v = e[:, 1].copy().view(np.float32)
+        t = np.float32(v[0] * row[e[0, 0]])
+        for k in range(1, len(e)):
+            t = np.float32(t + np.float32(v[k] * row[e[k, 0]]))
+        row[8 * S + j] = t
+    assert (places[C_out:] == 0).all()
+    return row[places[:C_out]]
+
+
+def test_gather_map_is_the_map(oracle):
+    rng = np.random.default_rng(1)
+    for C_in, C_out, special in ((1, 1, 2), (1, 40, 2), (7, 9, 1), (64, 64, 100), (65, 300, 3), (513, 511, 7), (1000, 1, 1)):
+        csr = random_csr_map(rng, C_in, C_out, special)
+        index, computed = b.qllm_gather_map_host(*csr, C_in)
+        y = rng.standard_normal((1, C_in)).astype(np.float32)
+        assert np.array_equal(apply_index(y[0], index, computed, C_in, C_out), oracle.apply_map(y, *csr)[0])
+        assert index.size % 2 == 0 and index.dtype == np.int32
+
+
+def test_gather_map_refusals():
+    one = np.array([1.0], np.float32)
+    i32 = lambda *v: np.array(v, np.int32)  # noqa: E731
+    for row_ptr, src, scale, C_in, status in ((i32(0, 1), i32(1), one, 1, MAP), (i32(0, 1), i32(-1), one, 4, MAP), (i32(0, 0, 1), i32(0), one, 4, MAP),
+                                              (i32(0, 1), i32(0), one, 0, SHAPE), (i32(0, 1), i32(0), one, 32769, SHAPE)):
+        with pytest.raises(b.QllmError) as e:
+            b.qllm_gather_map_host(row_ptr, src, scale, C_in)
+        assert e.value.status == status
+    for row_ptr, src, scale in ((i32(0), i32(), one[:0]), (i32(0, 2), i32(0), one), (i32(0, 1), i32(0), one[:0]), (i32(0, 3, 1), i32(0), one)):
+        with pytest.raises(ValueError):
+            b.qllm_gather_map_host(row_ptr, src, scale, 4)
+    with pytest.raises(b.QllmError) as e:       # a row and its computed channels have to fit on chip together
+        b.qllm_gather_map_host(np.arange(7682, dtype=np.int32), np.zeros(7681, np.int32), np.full(7681, 0.5, np.float32), 32768)
+    assert e.value.status == SHAPE
+    assert b.qllm_gather_map_host(np.arange(7681, dtype=np.int32), np.zeros(7680, np.int32), np.full(7680, 0.5, np.float32), 32768)[1] == 7680
+    n, m = C.c_int64(), C.c_int64()
+    p = np.zeros(4, np.int32).ctypes.data
+    for args in ((None, p, p, 4, 1, None, C.byref(n), C.byref(m)), (p, None, p, 4, 1, None, C.byref(n), C.byref(m)), (p, p, None, 4, 1, None, C.byref(n), C.byref(m)),
+                 (p, p, p, 4, 1, None, None, C.byref(m)), (p, p, p, 4, 1, None, C.byref(n), None)):
+        assert b.raw().qllm_gather_map_host(*args) == NULL
+
+
+# ---------------------------------------------------------------- adapters
+
+def pool(n=4, Cc=64, O=96, rank=16, n_parts=1, part_O=(96, 0, 0, 0), wd=b.BF16, Ap=A, Bp=A, scale=None, ranks=None):
+    return b._Adapters(n, Cc, O, rank, n_parts, (C.c_int64 * 4)(*part_O), wd, Ap, Bp, scale, ranks)
+
+
+def apply(w=None, x=A, xd=b.BF16, ldx=64, rows=8, plan=A, plan_bytes=1 << 30, y=A, ldy=96, out=A, ldo=96, yd=b.BF16, ws=A, ws_bytes=1 << 30, no_w=False):
+    w = w or pool()
+    return b.raw().qllm_adapter_apply(x, xd, ldx, rows, None if no_w else C.byref(w), plan, plan_bytes, y, ldy, out, ldo, yd, ws, ws_bytes, None)
+
+
+BAD_POOLS = [dict(n=0), dict(n=8193), dict(Cc=0), dict(Cc=1 << 24), dict(O=0), dict(O=1 << 24), dict(rank=0), dict(rank=4), dict(rank=12), dict(rank=264),
+             dict(rank=-8), dict(n_parts=0), dict(n_parts=5), dict(part_O=(95, 0, 0, 0)), dict(part_O=(97, 0, 0, 0)), dict(n_parts=2),
+             dict(n_parts=2, part_O=(100, -4, 0, 0)), dict(n_parts=3, part_O=(50, 46, 0, 0))]
+
+
+def test_adapter_refusals():
+    ws = lambda w, rows: b.raw().qllm_adapter_workspace_bytes(None if w is None else C.byref(w), rows)  # noqa: E731
+    for kw in BAD_POOLS:
+        assert apply(pool(**kw)) == SHAPE, kw
+        assert ws(pool(**kw), 8) == SHAPE, kw
+    assert ws(None, 8) == NULL and ws(pool(), -1) == SHAPE and ws(pool(), 1 << 24) == SHAPE and ws(pool(), 0) == 0
+    need = ws(pool(), 8)
+    assert need >= 8 * 16 * 4
+    assert apply(no_w=True) == NULL
+    for name in ("x", "plan", "y", "out"):
+        assert apply(**{name: None}) == NULL, name
+    assert apply(pool(Ap=None)) == NULL and apply(pool(Bp=None)) == NULL
+    for kw in (dict(rows=-1), dict(rows=1 << 24), dict(ldx=63), dict(ldy=95), dict(ldo=95), dict(ldo=100)):
+        assert apply(**kw) == SHAPE, kw
+    assert apply(pool(O=8000000, part_O=(8000000, 0, 0, 0)), rows=1 << 23, ldy=8000000, ldo=8000000, ws_bytes=1 << 50, plan_bytes=1 << 40) == SHAPE
+    for kw in (dict(xd=2), dict(yd=-1), dict(w=pool(wd=5))):
+        assert apply(**kw) == DTYPE, kw
+    for kw in (dict(x=A + 1), dict(y=A + 1), dict(out=A + 1), dict(plan=A + 8), dict(ws=A + 4), dict(w=pool(Ap=A + 8)), dict(w=pool(Bp=A + 4)),
+               dict(w=pool(scale=A + 2)), dict(w=pool(ranks=A + 1)), dict(x=A + 2, xd=b.F32)):
+        assert apply(**kw) == ALIGN, kw
+    assert apply(ws_bytes=need - 1) == WORKSPACE and apply(ws=None) == WORKSPACE
+    assert apply(plan_bytes=b.qllm_adapter_plan_bytes(8, 4) - 1) == WORKSPACE
+    assert apply(rows=0, x=None, y=None, out=None, plan=None, ws=None) == 0
+
+
+def test_adapter_plan_refusals():
+    plan = lambda rows=8, seqs=3, rs=A, ad=A, n=4, p=A, size=1 << 30: b.raw().qllm_adapter_plan(rows, seqs, rs, ad, n, p, size, None)  # noqa: E731
+    assert plan(rows=-1) == SHAPE and plan(rows=1 << 24) == SHAPE and plan(seqs=-1) == SHAPE and plan(seqs=(1 << 20) + 1) == SHAPE
+    assert plan(n=0) == SHAPE and plan(n=8193) == SHAPE and plan(rs=None, seqs=9) == SHAPE
+    assert plan(ad=None) == NULL and plan(p=None) == NULL
+    assert plan(rs=A + 2) == ALIGN and plan(ad=A + 1) == ALIGN and plan(p=A + 8) == ALIGN
+    assert plan(size=b.qllm_adapter_plan_bytes(8, 4) - 1) == WORKSPACE
+    assert b.raw().qllm_adapter_plan_bytes(8, 0) == SHAPE and b.raw().qllm_adapter_plan_bytes(-1, 4) == SHAPE
+
+
+def test_adapter_binding_refuses():
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt)  # noqa: E731
+
+    def bad(*a, **kw):
+        with pytest.raises(ValueError) as e:
+            b.DeviceAdapters(*a, **kw)
+        return str(e.value)
+
+    a, bb = z(3, 16, 40), z(3, 24, 16)
+    assert "A must be" in bad(a[0], bb) and "A has shape" in bad(a, z(2, 24, 16)) and "dtype" in bad(a, bb.float()) and "dtype" in bad(a.half(), bb.half())
+    assert "rank" in bad(z(3, 12, 40), z(3, 24, 12)) and "rank" in bad(z(3, 264, 4), z(3, 4, 264)) and "parts" in bad(a, bb, parts=[10, 10])
+    assert "parts" in bad(a, bb, parts=[24, 0]) and "parts" in bad(a, bb, parts=[]) and "A has shape" in bad(a, bb, parts=[12, 12])
+    assert "contiguous" in bad(z(3, 32, 40)[:, :16], bb) and "scale" in bad(a, bb, scale=z(2, dt=torch.float32)) and "ranks" in bad(a, bb, ranks=z(3))
+    ad, plan = b.DeviceAdapters(a, bb), b.DeviceAdapterPlan(5, 3, device="cpu")
+    ws = torch.zeros(b.qllm_adapter_workspace_bytes(ad, 5), dtype=torch.uint8)
+    with pytest.raises(AttributeError):
+        ad.A = a
+
+    def call(x=z(5, 40), ad=ad, plan=plan, y=z(5, 24), out=z(5, 24), ws=ws):
+        with pytest.raises(ValueError) as e:
+            b.qllm_adapter_apply(x, ad, plan, y, out, ws)
+        return str(e.value)
+
+    assert "device" in call()
+    assert "x has" in call(x=z(4, 40)) and "x has" in call(x=z(5, 41)) and "y has" in call(y=z(5, 25)) and "out has" in call(out=z(5, 24, dt=torch.float32))
+    assert "places" in call(plan=b.DeviceAdapterPlan(5, 4, device="cpu")) and "workspace" in call(ws=None) and "workspace" in call(ws=ws.float())
+    with pytest.raises(ValueError):
+        b.qllm_adapter_plan(plan, z(6, dt=torch.int32))
+    with pytest.raises(ValueError):
+        b.qllm_adapter_plan(plan, z(2, dt=torch.int32), z(2, dt=torch.int32))
+    with pytest.raises(ValueError):
+        b.qllm_adapter_plan(plan, z(2, dt=torch.int64))
