@@ -33,11 +33,11 @@ inline int64_t most_tiles(int64_t rows, int64_t n_adapters)
     const int64_t groups = n_adapters + 1; // those without one are a group too
     return rows / TILE + (rows < groups ? rows : groups);
 }
-// words: head, rows in order, tiles of {adapter, first place in the order, rows, -}
-inline int64_t order_words(int64_t rows) { return (rows + 3) / 4 * 4; }
-inline int64_t plan_words(int64_t rows, int64_t n_adapters) { return PLAN_HEAD_WORDS + order_words(rows) + 4 * most_tiles(rows, n_adapters); }
+// words: head, tiles of {adapter, rows of the tiles before it, its rows, -}, then TILE rows for each tile, so that a workgroup asks for
+// all it needs of the plan at once
+inline int64_t plan_words(int64_t rows, int64_t n_adapters) { return PLAN_HEAD_WORDS + (4 + TILE) * most_tiles(rows, n_adapters); }
 
-// ---- the plan: rows counted per adapter, the adapters' places in the order summed up, the sequences put there.  In which order the
+// ---- the plan: rows counted per adapter, the adapters' tiles numbered, the sequences put there.  In which order the
 // sequences of one adapter come (an atomic decides) is no part of any result.
 __global__ __launch_bounds__(PLAN_THREADS) void adapter_plan_kernel(int32_t rows, int32_t n_seqs, const int32_t *row_start,
                                                                    const int32_t *adapter, int32_t n_adapters, int32_t most, int32_t *plan)
@@ -46,8 +46,9 @@ __global__ __launch_bounds__(PLAN_THREADS) void adapter_plan_kernel(int32_t rows
     __shared__ uint32_t part_rows[PLAN_THREADS / 64], part_tiles[PLAN_THREADS / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int groups = n_adapters + 1;
-    int32_t *order = plan + PLAN_HEAD_WORDS;
-    int4 *tiles = reinterpret_cast<int4 *>(order + (rows + 3) / 4 * 4);
+    int4 *tiles = reinterpret_cast<int4 *>(plan + PLAN_HEAD_WORDS);
+    int32_t *order = plan + PLAN_HEAD_WORDS + 4 * (int64_t)most;
+    const int64_t places = (int64_t)most * TILE;
     for (int g = tid; g < groups; g += PLAN_THREADS) next[g] = 0;
     __syncthreads();
     auto group_of = [&](int i) {
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void adapter_plan_kernel(int32_t rows
     }
     for (int g = g0; g < g1; ++g) {
         const uint32_t n = min(next[g], (uint32_t)rows);
-        next[g] = before_rows;
+        next[g] = min(before_tiles, (uint32_t)most) * TILE;
         for (uint32_t at = 0; at < n; at += TILE, ++before_tiles)
             if (before_tiles < (uint32_t)most) tiles[before_tiles] = make_int4(g, (int32_t)min(before_rows + at, (uint32_t)rows), (int32_t)min(n - at, (uint32_t)TILE), 0);
         before_rows += n;
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void adapter_plan_kernel(int32_t rows
     if (!row_start) {
         for (int i = tid; i < min(n_seqs, rows); i += PLAN_THREADS) {
             const uint32_t at = atomicAdd(&next[group_of(i)], 1u);
-            if (at < (uint32_t)rows) order[at] = i;
+            if (at < places) order[at] = i;
         }
         return;
     }
@@ -107,7 +108,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void adapter_plan_kernel(int32_t rows
         if (lane == 0) at = atomicAdd(&next[group_of(i)], (uint32_t)n);
         at = __builtin_amdgcn_readfirstlane(at);
         for (int j = lane; j < n; j += 64)
-            if (at + j < (uint32_t)rows) order[at + j] = row + j;
+            if ((int64_t)at + j < places) order[(int64_t)at + j] = row + j;
     }
 }
 
@@ -117,45 +118,42 @@ struct ApplyArgs {
     int64_t ldx, ldy, ldo, C, O;
     const float *scale;
     const int32_t *ranks, *plan;
-    float *h; // [slices][rows in the plan's order][parts * rank]
-    int32_t rows, n_adapters, rank, wide, slices, blocks_per_slice; // wide: parts * rank; blocks of 64 channels
-    int32_t n_parts, part_end[QLLM_ADAPTER_PARTS], block_end[QLLM_ADAPTER_PARTS]; // columns, blocks of columns, summed up
+    float *h; // [slices][rows in the order of the tiles][parts * rank]
+    int32_t rows, n_adapters, most, rank, wide, slices, blocks_per_slice; // most: tiles; wide: parts * rank; blocks of 64 channels
+    int32_t n_parts, part_end[QLLM_ADAPTER_PARTS], columns, block_end[QLLM_ADAPTER_PARTS]; // columns, of a block, blocks, summed up
 };
 
 struct Tile {
     int32_t adapter, first, count, rank; // count 0: none
+    const int32_t *rows;
 };
+// tile t < most_tiles(...): its words are there to be read whatever they hold
 __device__ __forceinline__ Tile tile_of(const ApplyArgs &a, uint32_t t)
 {
-    const int4 head = *reinterpret_cast<const int4 *>(a.plan);
-    Tile tile{0, 0, 0, 0};
+    const int4 head = *reinterpret_cast<const int4 *>(a.plan), w = reinterpret_cast<const int4 *>(a.plan + PLAN_HEAD_WORDS)[t];
+    Tile tile{0, 0, 0, 0, a.plan + PLAN_HEAD_WORDS + 4 * (int64_t)a.most + (int64_t)t * TILE};
     if (head.y != a.rows || head.z != a.n_adapters || t >= (uint32_t)head.x) return tile;
-    const int4 w = reinterpret_cast<const int4 *>(a.plan + PLAN_HEAD_WORDS + (a.rows + 3) / 4 * 4)[t];
     if (w.x < 0 || w.x > a.n_adapters || w.y < 0 || w.y >= a.rows || w.z <= 0) return tile;
     tile.adapter = w.x, tile.first = w.y, tile.count = min(min(w.z, TILE), a.rows - w.y);
     if (w.x < a.n_adapters) tile.rank = a.ranks ? min(max(a.ranks[w.x], 0), a.rank) : a.rank;
     return tile;
 }
-// the row at a place of the order, -1 where there is none
-__device__ __forceinline__ int32_t row_at(const ApplyArgs &a, int32_t place)
-{
-    const int32_t row = a.plan[PLAN_HEAD_WORDS + place];
-    return row >= 0 && row < a.rows ? row : -1;
-}
+__device__ __forceinline__ int32_t checked_row(const ApplyArgs &a, int32_t row) { return row >= 0 && row < a.rows ? row : -1; }
 
-// Sixteen neighbouring channels of one row of x or A, a lane's share of a block of 64 (four lanes a row).
+// A lane's share of a block of 64 channels of one row of x or A (four lanes a row): channels 8 q .. + 7 and 32 + 8 q .. + 7, so that
+// the four lanes read 64 bytes (bf16) in a row.
 template <typename T>
 struct Sixteen {
     Eight<T> e[2];
     __device__ __forceinline__ void load(const T *p, int n)
     {
         e[0].load(p, n);
-        e[1].load(p + 8, n - 8);
+        e[1].load(p + 32, n - 32);
     }
 };
 
-// ---- h = x A^T.  Lane l of a wave holds channels 16 (l / 16) .. + 15 of a block of 64 of row l mod 16 of either operand (the order of
-// the channels is the same in both, so any will do): whole 128-byte lines of bf16.  The block's waves take the slice's blocks in turn.
+// ---- h = x A^T.  Lane l of a wave holds its share (q = l / 16) of row l mod 16 of either operand; the order of the channels is the
+// same in both, so any will do.  The four waves take the slice's blocks in turn, the next one's loads in flight.
 template <typename XT, typename WT, int MT, int NT>
 __device__ __forceinline__ void down_tile(const ApplyArgs &a, const Tile &tile, int first_rank, float *part)
 {
@@ -165,28 +163,46 @@ __device__ __forceinline__ void down_tile(const ApplyArgs &a, const Tile &tile, 
     const WT *w[NT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-        const int32_t row = row_at(a, tile.first + min(m * 16 + r16, tile.count - 1));
-        x[m] = static_cast<const XT *>(a.x) + (int64_t)max(row, 0) * a.ldx + 16 * quarter;
+        const int32_t row = checked_row(a, tile.rows[min(m * 16 + r16, tile.count - 1)]);
+        x[m] = static_cast<const XT *>(a.x) + (int64_t)max(row, 0) * a.ldx + 8 * quarter;
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int at = min(first_rank + n * 16 + r16, a.wide - 1), p = at / a.rank, r = min(at - p * a.rank, tile.rank - 1);
-        w[n] = static_cast<const WT *>(a.A) + ((int64_t)tile.adapter * a.wide + p * a.rank + r) * a.C + 16 * quarter;
+        w[n] = static_cast<const WT *>(a.A) + ((int64_t)tile.adapter * a.wide + p * a.rank + r) * a.C + 8 * quarter;
     }
     f32x4 acc[MT][NT];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int64_t begin = (int64_t)blockIdx.y * a.blocks_per_slice * 64, end = min(begin + (int64_t)a.blocks_per_slice * 64, a.C);
-    for (int64_t c = begin + 64 * wave; c < end; c += 64 * 4) {
-        Sixteen<XT> xe[MT];
-        Sixteen<WT> we[NT];
-        const int left = (int)min(a.C - c - 16 * quarter, (int64_t)16);
+    const int C = (int)a.C, begin = blockIdx.y * a.blocks_per_slice * 64, end = min(begin + a.blocks_per_slice * 64, C);
+    Sixteen<XT> xe[MT];
+    Sixteen<WT> we[NT];
+    auto request = [&](int c) {
+        if (c + 64 <= C) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) xe[m].load(x[m] + c, left);
+            for (int m = 0; m < MT; ++m) xe[m].load(x[m] + c, 64);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) we[n].load(w[n] + c, left);
+            for (int n = 0; n < NT; ++n) we[n].load(w[n] + c, 64);
+        } else { // the row's last block
+            const int left = C - c - 8 * quarter;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) xe[m].load(x[m] + c, left);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) we[n].load(w[n] + c, left);
+        }
+    };
+    int c = begin + 64 * wave;
+    if (c < end) request(c);
+    for (; c < end; c += 64 * 4) {
+        Sixteen<XT> xn[MT];
+        Sixteen<WT> wn[NT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) xn[m] = xe[m];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) wn[n] = we[n];
+        if (c + 64 * 4 < end) request(c + 64 * 4);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             if constexpr (HALF) {
@@ -194,13 +210,13 @@ __device__ __forceinline__ void down_tile(const ApplyArgs &a, const Tile &tile, 
                 for (int m = 0; m < MT; ++m)
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
-                        acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, we[n].e[h].q), __builtin_bit_cast(bf16x8, xe[m].e[h].q), acc[m][n], 0, 0, 0);
+                        acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wn[n].e[h].q), __builtin_bit_cast(bf16x8, xn[m].e[h].q), acc[m][n], 0, 0, 0);
             } else {
                 float xv[MT][8], wv[NT][8];
 #pragma unroll
-                for (int m = 0; m < MT; ++m) xe[m].e[h].widen(xv[m]);
+                for (int m = 0; m < MT; ++m) xn[m].e[h].widen(xv[m]);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) we[n].e[h].widen(wv[n]);
+                for (int n = 0; n < NT; ++n) wn[n].e[h].widen(wv[n]);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -228,7 +244,7 @@ __device__ __forceinline__ void down_tile(const ApplyArgs &a, const Tile &tile, 
 }
 
 template <typename XT, typename WT, int NT>
-__global__ __launch_bounds__(256) void down_kernel(const ApplyArgs a)
+__global__ __launch_bounds__(256, 2) void down_kernel(const ApplyArgs a)
 {
     __shared__ __align__(16) float part[4 * TILE * NT * 16];
     const Tile tile = tile_of(a, blockIdx.x);
@@ -238,155 +254,286 @@ __global__ __launch_bounds__(256) void down_kernel(const ApplyArgs a)
     else down_tile<XT, WT, 4, NT>(a, tile, first_rank, part);
 }
 
-// ---- the slices' sums
-__global__ __launch_bounds__(256) void join_kernel(float *h, int64_t words4, int32_t slices)
+// ---- the slices' sums: JOINERS neighbouring lanes add up every JOINERS-th slice each, then theirs are added
+constexpr int JOINERS = 8;
+__device__ __forceinline__ f32x4 joined(const float *h, int64_t stride, int slices, int joiner)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= words4) return;
-    f32x4 *at = reinterpret_cast<f32x4 *>(h) + i;
-    f32x4 s = at[0];
-    for (int k = 1; k < slices; ++k) s += at[k * words4];
-    at[0] = s;
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k0 = joiner; k0 < slices; k0 += 4 * JOINERS) { // four loads in flight; what is past the last slice is read from it, and dropped
+        f32x4 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const f32x4 *>(h + min(k0 + u * JOINERS, slices - 1) * stride);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (k0 + u * JOINERS < slices) s += v[u];
+    }
+#pragma unroll
+    for (int d = 1; d < JOINERS; d <<= 1) {
+        f32x4 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = __shfl_xor(s[j], d, 64);
+        s += o;
+    }
+    return s;
 }
 
-// ---- out = y + (scale h) B^T.  The columns are the rows of the matrix operation and the tile's rows its columns: lane l gets 16
-// neighbouring columns (4 of each of 4 operations) of row l mod 16, whose reads and writes of y are whole lines.
-// h goes through LDS, with bf16 weights as PARTS bf16 numbers that add up to it, one after the other along the sum.
-template <typename WT, typename YT, int MT>
-__device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, int p, int column, int end, void *staged, int32_t *rows_of)
+__global__ __launch_bounds__(256) void join_kernel(float *h, int64_t words4, int32_t slices)
+{
+    const int64_t i = (int64_t)blockIdx.x * (256 / JOINERS) + threadIdx.x / JOINERS, at = i < words4 ? i : words4 - 1;
+    const f32x4 s = joined(h + 4 * at, 4 * words4, slices, threadIdx.x % JOINERS);
+    if (i < words4 && threadIdx.x % JOINERS == 0) reinterpret_cast<f32x4 *>(h)[at] = s;
+}
+
+// ---- out = y + (scale h) B^T.  Rows are the rows of the matrix operation and four operations take the columns 4 n + t, t = 0 .. 3, so
+// that lane l gets 4 neighbouring columns of 4 rows and 16 lanes a whole piece of a row of y: its reads and writes are whole lines.
+// h goes through LDS, with bf16 weights as PARTS bf16 numbers that add up to it, behind one another in a row.
+template <typename T>
+struct Four; // 4 neighbouring elements of a row of y
+template <>
+struct Four<float> {
+    u32x4 q;
+    __device__ __forceinline__ void load(const float *p, int n)
+    {
+        if (n >= 4) {
+            q = *reinterpret_cast<const u32x4_at4 *>(p);
+        } else {
+            q = u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (j < n) q[j] = __float_as_uint(p[j]);
+        }
+    }
+    __device__ __forceinline__ void add(const float *v)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[j] = __float_as_uint(__uint_as_float(q[j]) + v[j]);
+    }
+    __device__ __forceinline__ void store(float *p, int n) const
+    {
+        if (n >= 4) {
+            *reinterpret_cast<u32x4_at4 *>(p) = q;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (j < n) p[j] = __uint_as_float(q[j]);
+        }
+    }
+};
+template <>
+struct Four<uint16_t> {
+    u32x2 q;
+    __device__ __forceinline__ void load(const uint16_t *p, int n)
+    {
+        if (n >= 4) {
+            q = *reinterpret_cast<const u32x2_at2 *>(p);
+        } else {
+            q = u32x2{0, 0};
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (j < n) q[j / 2] |= (uint32_t)p[j] << (16 * (j & 1));
+        }
+    }
+    __device__ __forceinline__ void add(const float *v)
+    {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) q[k] = to_bf16(__uint_as_float(q[k] << 16) + v[2 * k], __uint_as_float(q[k] & 0xffff0000u) + v[2 * k + 1]);
+    }
+    __device__ __forceinline__ void store(uint16_t *p, int n) const
+    {
+        if (n >= 4) {
+            *reinterpret_cast<u32x2_at2 *>(p) = q;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (j < n) p[j] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
+        }
+    }
+};
+
+// Ranks that one step of the second product takes, and elements of a row of h in LDS.
+template <typename WT>
+constexpr int STEP = sizeof(WT) == 2 ? 32 : 16;
+template <typename WT, typename YT>
+constexpr int PARTS = sizeof(WT) == 4 ? 1 : sizeof(YT) == 2 ? 2 : 3;
+template <typename WT, typename YT>
+__host__ __device__ __forceinline__ int staged_stride(int rank)
+{
+    return PARTS<WT, YT> * ((rank + STEP<WT> - 1) / STEP<WT> * STEP<WT>) + (sizeof(WT) == 2 ? 8 : 4);
+}
+
+// A wave has MT groups of 16 rows and 64 columns at a time, the next columns' y and B in flight; the waves of a workgroup share out the
+// tile's rows and then its columns.  WHOLE: no column of the last 64 is past the end.
+template <typename WT, typename YT, int MT, bool WHOLE>
+__device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, int p, int column, int end, uint8_t *staged)
 {
     constexpr bool HALF = sizeof(WT) == 2;
-    constexpr int PARTS = HALF ? (sizeof(YT) == 2 ? 2 : 3) : 1;
+    constexpr int P = PARTS<WT, YT>, S = STEP<WT>;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r16 = lane & 15, quarter = lane >> 4;
-    const int octets = a.rank / 8, steps = HALF ? (PARTS * octets + 3) / 4 : (a.rank + 15) / 16;
-    const int stride = HALF ? steps * 32 + 8 : steps * 16 + 4; // elements of a row in LDS
-    uint16_t *hb = static_cast<uint16_t *>(staged);
-    float *hf = static_cast<float *>(staged);
-    if (tid < MT * 16) rows_of[tid] = tid < tile.count ? row_at(a, tile.first + tid) : -1;
-    const float scale = tile.rank == 0 ? 0.0f : a.scale ? a.scale[tile.adapter] : 1.0f;
-    const int cells = HALF ? a.rank / 4 : steps * 4; // of 4 ranks, a row
-    for (int i = tid; i < MT * 16 * cells; i += 256) {
-        const int m = i / cells, r = 4 * (i - m * cells);
-        f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (m < tile.count && r < tile.rank) {
-            const float *h = a.h + (int64_t)(tile.first + m) * a.wide + p * a.rank + r;
-            for (int k = 0; k < a.slices; ++k) s += *reinterpret_cast<const f32x4 *>(h + (int64_t)k * a.rows * a.wide);
+    const int sharers = tile.count <= 16 * MT ? 1 : 2; // groups of MT * 16 rows
+    const int first = 16 * MT * (wave & (sharers - 1)), turns = 4 / sharers;
+    const YT *y[MT][4];
+    bool there[MT][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int at = first + 16 * m + 4 * quarter;
+        const int4 four = *reinterpret_cast<const int4 *>(tile.rows + at);
+        const int32_t rows[4] = {four.x, four.y, four.z, four.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int32_t row = at + i < tile.count ? checked_row(a, rows[i]) : -1;
+            there[m][i] = row >= 0;
+            y[m][i] = static_cast<const YT *>(a.y) + (int64_t)max(row, 0) * a.ldy + column + 4 * r16;
+        }
+    }
+    // B of 4 columns a lane in a step: ranks 8 q .. + 7 (bf16) or 4 q .. + 3 (fp32) of each
+    const WT *B = static_cast<const WT *>(a.B) + ((int64_t)min(tile.adapter, a.n_adapters - 1) * a.O + column) * a.rank;
+    const int steps = (tile.rank + S - 1) / S;
+    auto load_b = [&](u32x4 *b, int at, int step) { // at: of the workgroup's columns
+        const int r = step * S + quarter * (S / 4), o = at + 4 * r16;
+        const uint32_t from = r < tile.rank ? r : 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) b[t] = *reinterpret_cast<const u32x4 *>(B + (uint32_t)((WHOLE ? o + t : min(o + t, end - column - 1)) * a.rank + from));
+    };
+    auto mask_b = [&](u32x4 *b, int step) { // past the adapter's own ranks: zeros
+        if (tile.rank >= (step + 1) * S) return;
+        const int r = step * S + quarter * (S / 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int one = HALF ? r + 2 * j : r + j;
+            const uint32_t keep = one >= tile.rank ? 0u : HALF && one + 1 >= tile.rank ? 0xffffu : 0xffffffffu;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) b[t][j] &= keep;
+        }
+    };
+    Four<YT> ye[MT][4];
+    u32x4 b[2][4];
+    auto request = [&](int at) {
+        const int left = WHOLE ? 64 : end - column - at - 4 * r16;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ye[m][i].load(y[m][i] + at, left);
+        if (steps > 0) load_b(b[0], at, 0);
+        if (steps > 1) load_b(b[1], at, 1);
+    };
+    const int width = end - column;
+    int at = 64 * (wave / sharers);
+    if (at < width) request(at);
+
+    // scale h into LDS, the tile's rows (what lies in others reaches only results that are not stored)
+    const int padded = (a.rank + S - 1) / S * S, stride = staged_stride<WT, YT>(a.rank);
+    if (tile.rank > 0) {
+        const float scale = a.scale ? a.scale[tile.adapter] : 1.0f;
+        const int cells = padded / 4, all = tile.count * cells; // of 4 ranks, a row
+        const float *h = a.h + (int64_t)tile.first * a.wide + p * a.rank;
+        auto stage = [&](int i, f32x4 s) {
+            const int row = i / cells, r = 4 * (i - row * cells);
 #pragma unroll
             for (int j = 0; j < 4; ++j) s[j] = r + j < tile.rank ? s[j] * scale : 0.0f;
-        }
-        if constexpr (HALF) {
+            if constexpr (HALF) {
+                uint16_t *to = reinterpret_cast<uint16_t *>(staged) + row * stride + r;
 #pragma unroll
-            for (int part = 0; part < PARTS; ++part) {
-                const uint32_t lo = to_bf16(s[0], s[1]), hi = to_bf16(s[2], s[3]);
-                *reinterpret_cast<uint2 *>(hb + m * stride + part * a.rank + r) = make_uint2(lo, hi);
-                s[0] -= __uint_as_float(lo << 16), s[1] -= __uint_as_float(lo & 0xffff0000u);
-                s[2] -= __uint_as_float(hi << 16), s[3] -= __uint_as_float(hi & 0xffff0000u);
+                for (int part = 0; part < P; ++part) {
+                    const uint32_t lo = to_bf16(s[0], s[1]), hi = to_bf16(s[2], s[3]);
+                    *reinterpret_cast<uint2 *>(to + part * padded) = make_uint2(lo, hi);
+                    s[0] -= __uint_as_float(lo << 16), s[1] -= __uint_as_float(lo & 0xffff0000u);
+                    s[2] -= __uint_as_float(hi << 16), s[3] -= __uint_as_float(hi & 0xffff0000u);
+                }
+            } else {
+                *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(staged) + row * stride + r) = s;
+            }
+        };
+        auto cell = [&](int i) { // any i: that of a rank or row past the end is read at another place
+            const int row = min(i / cells, tile.count - 1), r = min(4 * (i % cells), a.rank - 4);
+            return h + row * a.wide + r;
+        };
+        if (a.slices > 1) {
+            for (int i0 = 0; i0 < all; i0 += 256 / JOINERS) {
+                const int i = i0 + tid / JOINERS;
+                const f32x4 s = joined(cell(i), (int64_t)a.rows * a.wide, a.slices, tid % JOINERS);
+                if (i < all && tid % JOINERS == 0) stage(i, s);
             }
         } else {
-            *reinterpret_cast<f32x4 *>(hf + m * stride + r) = s;
+            for (int i0 = tid; i0 < all; i0 += 256 * 4) {
+                f32x4 s[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s[k] = *reinterpret_cast<const f32x4 *>(cell(i0 + 256 * k));
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (i0 + 256 * k < all) stage(i0 + 256 * k, s[k]);
+            }
         }
+        __syncthreads();
     }
-    if constexpr (HALF) { // what the last operation reads past the parts
-        const int pad = steps * 4 - PARTS * octets;
-        for (int i = tid; i < MT * 16 * pad; i += 256)
-            *reinterpret_cast<uint4 *>(hb + (i / pad) * stride + PARTS * a.rank + 8 * (i % pad)) = make_uint4(0, 0, 0, 0);
-    }
-    __syncthreads();
-
-    const WT *B = static_cast<const WT *>(a.B) + (int64_t)tile.adapter * a.O * a.rank;
-    for (int o0 = column + 64 * wave; o0 < end; o0 += 256) {
+    const WT *mine = reinterpret_cast<const WT *>(staged) + (first + r16) * stride + quarter * (S / 4);
+    for (; at < width; at += 64 * turns) {
+        Four<YT> yn[MT][4];
+        u32x4 bn[2][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            bn[0][i] = b[0][i], bn[1][i] = b[1][i];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) yn[m][i] = ye[m][i];
+        }
+        if (at + 64 * turns < width) request(at + 64 * turns);
         f32x4 acc[MT][4];
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int t = 0; t < 4; ++t) acc[m][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        const int oc = o0 + 16 * quarter, left = end - oc;
-        Eight<YT> ye[MT][2];
-        if (tile.count > 0) {
+        for (int step = 0; step < steps; ++step) {
+            u32x4 now[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) now[t] = bn[0][t], bn[0][t] = bn[1][t];
+            if (step + 2 < steps) load_b(bn[1], at, step + 2);
+            mask_b(now, step);
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const int32_t row = rows_of[m * 16 + r16];
-                const YT *y = static_cast<const YT *>(a.y) + (int64_t)max(row, 0) * a.ldy + oc;
-                ye[m][0].load(y, row < 0 ? 0 : left);
-                ye[m][1].load(y + 8, row < 0 ? 0 : left - 8);
-            }
-        }
-        if (tile.rank > 0) {
-            for (int k = 0; k < steps; ++k) {
                 if constexpr (HALF) {
-                    const int octet = 4 * k + quarter, r = 8 * (octet % octets);
-                    const bool there = octet < PARTS * octets && r < tile.rank;
-                    bf16x8 hv[MT];
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) hv[m] = *reinterpret_cast<const bf16x8 *>(hb + (m * 16 + r16) * stride + 32 * k + 8 * quarter);
+                    for (int part = 0; part < P; ++part) {
+                        const bf16x8 h = *reinterpret_cast<const bf16x8 *>(mine + m * 16 * stride + part * padded + S * step);
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const int o = min(o0 + 16 * (r16 >> 2) + 4 * t + (r16 & 3), end - 1);
-                        u32x4 b = {0, 0, 0, 0};
-                        if (there) b = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint16_t *>(B) + (int64_t)o * a.rank + r);
-                        if (r + 8 > tile.rank)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                if (r + 2 * j >= tile.rank) b[j] = 0;
-                                else if (r + 2 * j + 1 >= tile.rank) b[j] &= 0xffffu;
-                            }
-#pragma unroll
-                        for (int m = 0; m < MT; ++m) acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), hv[m], acc[m][t], 0, 0, 0);
+                        for (int t = 0; t < 4; ++t) acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h, __builtin_bit_cast(bf16x8, now[t]), acc[m][t], 0, 0, 0);
                     }
                 } else {
-                    const int r = 16 * k + 4 * quarter;
-                    f32x4 hv[MT];
+                    const f32x4 h = *reinterpret_cast<const f32x4 *>(mine + m * 16 * stride + S * step);
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) hv[m] = *reinterpret_cast<const f32x4 *>(hf + (m * 16 + r16) * stride + r);
+                    for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const int o = min(o0 + 16 * (r16 >> 2) + 4 * t + (r16 & 3), end - 1);
-                        f32x4 b = {0.0f, 0.0f, 0.0f, 0.0f};
-                        if (r < tile.rank) b = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(B) + (int64_t)o * a.rank + r);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float bj = r + j < tile.rank ? b[j] : 0.0f;
-#pragma unroll
-                            for (int m = 0; m < MT; ++m) acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(bj, hv[m][j], acc[m][t], 0, 0, 0);
-                        }
-                    }
+                        for (int t = 0; t < 4; ++t) acc[m][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(h[j], __uint_as_float(now[t][j]), acc[m][t], 0, 0, 0);
                 }
             }
         }
+        const int left = WHOLE ? 64 : width - at - 4 * r16;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const int32_t row = rows_of[m * 16 + r16];
-            if (row < 0) continue;
-            YT *out = static_cast<YT *>(a.out) + (int64_t)row * a.ldo + oc;
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                float v[8];
-                ye[m][half].widen(v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += acc[m][2 * half + j / 4][j % 4];
-                if (tile.rank > 0) ye[m][half].round(v);
-                ye[m][half].store(out + 8 * half, left - 8 * half);
+            for (int i = 0; i < 4; ++i) {
+                if (!there[m][i]) continue;
+                const float v[4] = {acc[m][0][i], acc[m][1][i], acc[m][2][i], acc[m][3][i]};
+                if (tile.rank > 0) yn[m][i].add(v); // else a copy, bit for bit
+                YT *out = static_cast<YT *>(a.out) + (y[m][i] - static_cast<const YT *>(a.y)) + at;
+                if (a.ldo != a.ldy) out += (int64_t)checked_row(a, tile.rows[first + 16 * m + 4 * quarter + i]) * (a.ldo - a.ldy);
+                yn[m][i].store(out, left);
             }
-        }
     }
 }
 
-constexpr int COLUMNS = 256; // a workgroup's at a time
-
 template <typename WT, typename YT>
-__global__ __launch_bounds__(256) void up_kernel(const ApplyArgs a)
+__global__ __launch_bounds__(256, 2) void up_kernel(const ApplyArgs a)
 {
     extern __shared__ __align__(16) uint8_t staged[];
-    __shared__ int32_t rows_of[TILE];
     const int blocks = a.block_end[a.n_parts - 1], block = (int)(blockIdx.x % (uint32_t)blocks);
     const Tile tile = tile_of(a, blockIdx.x / (uint32_t)blocks);
     if (tile.count == 0 || (tile.rank == 0 && a.out == a.y)) return;
     int p = 0, b = block, from = 0;
     for (int k = 0; k + 1 < QLLM_ADAPTER_PARTS; ++k)
         if (p == k && k + 1 < a.n_parts && block >= a.block_end[k]) p = k + 1, b = block - a.block_end[k], from = a.part_end[k];
-    const int column = from + b * COLUMNS, end = min(column + COLUMNS, a.part_end[p]);
-    if (tile.count <= 16) up_tile<WT, YT, 1>(a, tile, p, column, end, staged, rows_of);
-    else up_tile<WT, YT, 4>(a, tile, p, column, end, staged, rows_of);
+    const int column = from + b * a.columns, end = min(column + a.columns, a.part_end[p]);
+    const bool whole = ((end - column) & 63) == 0;
+    if (tile.count <= 16) whole ? up_tile<WT, YT, 1, true>(a, tile, p, column, end, staged) : up_tile<WT, YT, 1, false>(a, tile, p, column, end, staged);
+    else whole ? up_tile<WT, YT, 2, true>(a, tile, p, column, end, staged) : up_tile<WT, YT, 2, false>(a, tile, p, column, end, staged);
 }
 
 int32_t launched(const char *what)
@@ -413,15 +560,23 @@ int32_t check_sizes(const qllm_adapters *w, int64_t rows)
     return sum == w->O ? QLLM_OK : QLLM_ERR_SHAPE;
 }
 
-// The slices of C: as many as fill the card with tiles (the most there can be), none shorter than a turn of the four waves.
+// The fewest tiles that the rows can make: what a launch counts on to fill the card.
+inline int64_t fewest_tiles(int64_t rows) { return rows > TILE ? (rows + TILE - 1) / TILE : 1; }
+
+// The slices of C: two workgroups a CU, none shorter than a turn of the four waves.
 void slices_of(const qllm_adapters *w, int64_t rows, int32_t *slices, int32_t *blocks_per_slice)
 {
-    const int64_t blocks = (w->C + 63) / 64, turns = (blocks + 3) / 4, groups = (w->n_parts * w->rank + 63) / 64;
-    const int64_t tiles = most_tiles(rows, w->n_adapters) * groups;
-    const int64_t want = tiles > 0 ? (1024 + tiles - 1) / tiles : 1, most = want < turns ? want : turns;
-    const int64_t each = (turns + most - 1) / most;
+    const int64_t blocks = (w->C + 63) / 64, turns = (blocks + 3) / 4, tiles = fewest_tiles(rows) * ((w->n_parts * w->rank + 63) / 64);
+    const int64_t want = (512 + tiles - 1) / tiles, most = want < turns ? want : turns, each = (turns + most - 1) / most;
     *blocks_per_slice = (int32_t)(4 * each);
     *slices = (int32_t)((turns + each - 1) / each);
+}
+
+// Columns of a workgroup of the second product, a multiple of 256: few enough for three workgroups a CU, at most 1024.
+int32_t columns_of(const qllm_adapters *w, int64_t rows)
+{
+    const int64_t each = w->O * fewest_tiles(rows) / 768 / 256 * 256;
+    return (int32_t)(each < 256 ? 256 : each > 1024 ? 1024 : each);
 }
 
 } // namespace
@@ -472,8 +627,7 @@ void run_down(const ApplyArgs &a, unsigned tiles, hipStream_t stream)
 template <typename WT, typename YT>
 int32_t run_up(const ApplyArgs &a, unsigned tiles, hipStream_t stream)
 {
-    constexpr int PARTS = sizeof(WT) == 2 ? (sizeof(YT) == 2 ? 2 : 3) : 1;
-    const size_t lds = sizeof(WT) == 2 ? (size_t)TILE * ((PARTS * a.rank / 8 + 3) / 4 * 32 + 8) * 2 : (size_t)TILE * ((a.rank + 15) / 16 * 16 + 4) * 4;
+    const size_t lds = (size_t)TILE * staged_stride<WT, YT>(a.rank) * sizeof(WT);
     auto *kernel = up_kernel<WT, YT>;
     if (lds > 48 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -512,11 +666,12 @@ extern "C" int32_t qllm_adapter_apply(const void *x, int32_t x_dtype, int64_t ld
     a.ldx = ldx, a.ldy = ldy, a.ldo = ldo, a.C = w->C, a.O = w->O;
     a.scale = w->scale, a.ranks = w->ranks, a.plan = static_cast<const int32_t *>(plan), a.h = static_cast<float *>(workspace);
     a.rows = (int32_t)rows, a.n_adapters = (int32_t)w->n_adapters, a.rank = (int32_t)w->rank, a.wide = (int32_t)(w->n_parts * w->rank);
+    a.most = (int32_t)most_tiles(rows, w->n_adapters), a.columns = columns_of(w, rows);
     slices_of(w, rows, &a.slices, &a.blocks_per_slice);
     a.n_parts = w->n_parts;
     for (int p = 0; p < w->n_parts; ++p) {
         a.part_end[p] = (int32_t)w->part_O[p] + (p ? a.part_end[p - 1] : 0);
-        a.block_end[p] = (int32_t)((w->part_O[p] + COLUMNS - 1) / COLUMNS) + (p ? a.block_end[p - 1] : 0);
+        a.block_end[p] = (int32_t)((w->part_O[p] + a.columns - 1) / a.columns) + (p ? a.block_end[p - 1] : 0);
     }
     const int64_t tiles = most_tiles(rows, w->n_adapters);
     if (tiles * a.block_end[a.n_parts - 1] > INT32_MAX) return QLLM_ERR_SHAPE;
@@ -528,7 +683,7 @@ extern "C" int32_t qllm_adapter_apply(const void *x, int32_t x_dtype, int64_t ld
     if (const int32_t e = launched("adapters, first product: launch")) return e;
     if (a.slices > 1 && rows > TILE) {
         const int64_t words4 = rows * a.wide / 4;
-        hipLaunchKernelGGL(join_kernel, dim3((unsigned)((words4 + 255) / 256)), dim3(256), 0, stream, a.h, words4, a.slices);
+        hipLaunchKernelGGL(join_kernel, dim3((unsigned)((words4 * JOINERS + 255) / 256)), dim3(256), 0, stream, a.h, words4, a.slices);
         if (const int32_t e = launched("adapters, sums: launch")) return e;
         a.slices = 1;
     }

@@ -12,6 +12,8 @@ namespace qllm_detail {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
 typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_at2 __attribute__((aligned(2)));
 typedef __bf16 bf16_pair __attribute__((ext_vector_type(2)));
 typedef float f32_pair __attribute__((ext_vector_type(2)));
 
