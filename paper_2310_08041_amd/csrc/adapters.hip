@@ -120,6 +120,7 @@ struct ApplyArgs {
     const int32_t *ranks, *plan;
     float *h; // [slices][rows in the order of the tiles][parts * rank]
     int32_t rows, n_adapters, most, rank, wide, slices, blocks_per_slice; // most: tiles; wide: parts * rank; blocks of 64 channels
+    bool stream; // y and out past the caches, which B and h need
     int32_t n_parts, part_end[QLLM_ADAPTER_PARTS], columns, block_end[QLLM_ADAPTER_PARTS]; // columns, of a block, blocks, summed up
 };
 
@@ -140,24 +141,24 @@ __device__ __forceinline__ Tile tile_of(const ApplyArgs &a, uint32_t t)
 }
 __device__ __forceinline__ int32_t checked_row(const ApplyArgs &a, int32_t row) { return row >= 0 && row < a.rows ? row : -1; }
 
-// A lane's share of a block of 64 channels of one row of x or A (four lanes a row): channels 8 q .. + 7 and 32 + 8 q .. + 7, so that
-// the four lanes read 64 bytes (bf16) in a row.
-template <typename T>
-struct Sixteen {
-    Eight<T> e[2];
+// A lane's share of a block of 32 H channels of one row of x or A, 128 bytes of x (four lanes a row): channels 8 q .. + 7 of each 32.
+template <typename T, int H>
+struct Share {
+    Eight<T> e[H];
     __device__ __forceinline__ void load(const T *p, int n)
     {
-        e[0].load(p, n);
-        e[1].load(p + 32, n - 32);
+#pragma unroll
+        for (int h = 0; h < H; ++h) e[h].load(p + 32 * h, n - 32 * h);
     }
 };
 
 // ---- h = x A^T.  Lane l of a wave holds its share (q = l / 16) of row l mod 16 of either operand; the order of the channels is the
 // same in both, so any will do.  The four waves take the slice's blocks in turn, the next one's loads in flight.
 template <typename XT, typename WT, int MT, int NT>
-__device__ __forceinline__ void down_tile(const ApplyArgs &a, const Tile &tile, int first_rank, float *part)
+__device__ __forceinline__ void down_tile(const ApplyArgs &a, const Tile &tile, int slice, int first_rank, float *part)
 {
     constexpr bool HALF = sizeof(XT) == 2 && sizeof(WT) == 2;
+    constexpr int H = HALF ? 2 : 1, BLOCK = 32 * H; // the same for any MT: a row's sums do not depend on its tile's other rows
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, quarter = lane >> 4;
     const XT *x[MT];
     const WT *w[NT];
@@ -176,15 +177,15 @@ __device__ __forceinline__ void down_tile(const ApplyArgs &a, const Tile &tile, 
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[m][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int C = (int)a.C, begin = blockIdx.y * a.blocks_per_slice * 64, end = min(begin + a.blocks_per_slice * 64, C);
-    Sixteen<XT> xe[MT];
-    Sixteen<WT> we[NT];
+    const int C = (int)a.C, begin = slice * a.blocks_per_slice * 64, end = min(begin + a.blocks_per_slice * 64, C);
+    Share<XT, H> xe[MT];
+    Share<WT, H> we[NT];
     auto request = [&](int c) {
-        if (c + 64 <= C) {
+        if (c + BLOCK <= C) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) xe[m].load(x[m] + c, 64);
+            for (int m = 0; m < MT; ++m) xe[m].load(x[m] + c, BLOCK);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) we[n].load(w[n] + c, 64);
+            for (int n = 0; n < NT; ++n) we[n].load(w[n] + c, BLOCK);
         } else { // the row's last block
             const int left = C - c - 8 * quarter;
 #pragma unroll
@@ -193,18 +194,18 @@ __device__ __forceinline__ void down_tile(const ApplyArgs &a, const Tile &tile, 
             for (int n = 0; n < NT; ++n) we[n].load(w[n] + c, left);
         }
     };
-    int c = begin + 64 * wave;
+    int c = begin + BLOCK * wave;
     if (c < end) request(c);
-    for (; c < end; c += 64 * 4) {
-        Sixteen<XT> xn[MT];
-        Sixteen<WT> wn[NT];
+    for (; c < end; c += BLOCK * 4) {
+        Share<XT, H> xn[MT];
+        Share<WT, H> wn[NT];
 #pragma unroll
         for (int m = 0; m < MT; ++m) xn[m] = xe[m];
 #pragma unroll
         for (int n = 0; n < NT; ++n) wn[n] = we[n];
-        if (c + 64 * 4 < end) request(c + 64 * 4);
+        if (c + BLOCK * 4 < end) request(c + BLOCK * 4);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < H; ++h) {
             if constexpr (HALF) {
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
@@ -232,7 +233,7 @@ __device__ __forceinline__ void down_tile(const ApplyArgs &a, const Tile &tile, 
 #pragma unroll
         for (int n = 0; n < NT; ++n) *reinterpret_cast<f32x4 *>(part + ((wave * MT + m) * 16 + r16) * (NT * 16) + n * 16 + 4 * quarter) = acc[m][n];
     __syncthreads();
-    float *h = a.h + ((int64_t)blockIdx.y * a.rows + tile.first) * a.wide + first_rank;
+    float *h = a.h + ((int64_t)slice * a.rows + tile.first) * a.wide + first_rank;
     for (int i = threadIdx.x; i < MT * 16 * NT * 4; i += 256) {
         const int row = i / (NT * 4), r4 = i - row * (NT * 4);
         if (row >= tile.count || first_rank + 4 * r4 >= a.wide) continue;
@@ -243,15 +244,17 @@ __device__ __forceinline__ void down_tile(const ApplyArgs &a, const Tile &tile, 
     }
 }
 
+// Neighbouring workgroups, on XCDs in turn, are a tile's slices: with 8 slices, or 16, a slice's part of A is in one L2 alone.
 template <typename XT, typename WT, int NT>
 __global__ __launch_bounds__(256, 2) void down_kernel(const ApplyArgs a)
 {
     __shared__ __align__(16) float part[4 * TILE * NT * 16];
-    const Tile tile = tile_of(a, blockIdx.x);
+    const int slice = (int)(blockIdx.x % (uint32_t)a.slices);
+    const Tile tile = tile_of(a, blockIdx.x / (uint32_t)a.slices);
     if (tile.count == 0 || tile.rank == 0) return;
-    const int first_rank = blockIdx.z * NT * 16;
-    if (tile.count <= 16) down_tile<XT, WT, 1, NT>(a, tile, first_rank, part);
-    else down_tile<XT, WT, 4, NT>(a, tile, first_rank, part);
+    const int first_rank = blockIdx.y * NT * 16;
+    if (tile.count <= 16) down_tile<XT, WT, 1, NT>(a, tile, slice, first_rank, part);
+    else down_tile<XT, WT, 4, NT>(a, tile, slice, first_rank, part);
 }
 
 // ---- the slices' sums: JOINERS neighbouring lanes add up every JOINERS-th slice each, then theirs are added
@@ -287,15 +290,16 @@ __global__ __launch_bounds__(256) void join_kernel(float *h, int64_t words4, int
 // ---- out = y + (scale h) B^T.  Rows are the rows of the matrix operation and four operations take the columns 4 n + t, t = 0 .. 3, so
 // that lane l gets 4 neighbouring columns of 4 rows and 16 lanes a whole piece of a row of y: its reads and writes are whole lines.
 // h goes through LDS, with bf16 weights as PARTS bf16 numbers that add up to it, behind one another in a row.
-template <typename T>
-struct Four; // 4 neighbouring elements of a row of y
-template <>
-struct Four<float> {
+template <typename T, bool STREAM>
+struct Four; // 4 neighbouring elements of a row of y; STREAM: past the caches
+template <bool STREAM>
+struct Four<float, STREAM> {
     u32x4 q;
     __device__ __forceinline__ void load(const float *p, int n)
     {
         if (n >= 4) {
-            q = *reinterpret_cast<const u32x4_at4 *>(p);
+            if constexpr (STREAM) q = __builtin_nontemporal_load(reinterpret_cast<const u32x4_at4 *>(p));
+            else q = *reinterpret_cast<const u32x4_at4 *>(p);
         } else {
             q = u32x4{0, 0, 0, 0};
 #pragma unroll
@@ -311,7 +315,8 @@ struct Four<float> {
     __device__ __forceinline__ void store(float *p, int n) const
     {
         if (n >= 4) {
-            *reinterpret_cast<u32x4_at4 *>(p) = q;
+            if constexpr (STREAM) __builtin_nontemporal_store(q, reinterpret_cast<u32x4_at4 *>(p));
+            else *reinterpret_cast<u32x4_at4 *>(p) = q;
         } else {
 #pragma unroll
             for (int j = 0; j < 3; ++j)
@@ -319,13 +324,14 @@ struct Four<float> {
         }
     }
 };
-template <>
-struct Four<uint16_t> {
+template <bool STREAM>
+struct Four<uint16_t, STREAM> {
     u32x2 q;
     __device__ __forceinline__ void load(const uint16_t *p, int n)
     {
         if (n >= 4) {
-            q = *reinterpret_cast<const u32x2_at2 *>(p);
+            if constexpr (STREAM) q = __builtin_nontemporal_load(reinterpret_cast<const u32x2_at2 *>(p));
+            else q = *reinterpret_cast<const u32x2_at2 *>(p);
         } else {
             q = u32x2{0, 0};
 #pragma unroll
@@ -341,7 +347,8 @@ struct Four<uint16_t> {
     __device__ __forceinline__ void store(uint16_t *p, int n) const
     {
         if (n >= 4) {
-            *reinterpret_cast<u32x2_at2 *>(p) = q;
+            if constexpr (STREAM) __builtin_nontemporal_store(q, reinterpret_cast<u32x2_at2 *>(p));
+            else *reinterpret_cast<u32x2_at2 *>(p) = q;
         } else {
 #pragma unroll
             for (int j = 0; j < 3; ++j)
@@ -363,7 +370,7 @@ __host__ __device__ __forceinline__ int staged_stride(int rank)
 
 // A wave has MT groups of 16 rows and 64 columns at a time, the next columns' y and B in flight; the waves of a workgroup share out the
 // tile's rows and then its columns.  WHOLE: no column of the last 64 is past the end.
-template <typename WT, typename YT, int MT, bool WHOLE>
+template <typename WT, typename YT, int MT, bool WHOLE, bool STREAM>
 __device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, int p, int column, int end, uint8_t *staged)
 {
     constexpr bool HALF = sizeof(WT) == 2;
@@ -405,7 +412,7 @@ __device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, in
             for (int t = 0; t < 4; ++t) b[t][j] &= keep;
         }
     };
-    Four<YT> ye[MT][4];
+    Four<YT, STREAM> ye[MT][4];
     u32x4 b[2][4];
     auto request = [&](int at) {
         const int left = WHOLE ? 64 : end - column - at - 4 * r16;
@@ -467,7 +474,7 @@ __device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, in
     }
     const WT *mine = reinterpret_cast<const WT *>(staged) + (first + r16) * stride + quarter * (S / 4);
     for (; at < width; at += 64 * turns) {
-        Four<YT> yn[MT][4];
+        Four<YT, STREAM> yn[MT][4];
         u32x4 bn[2][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -531,9 +538,16 @@ __global__ __launch_bounds__(256, 2) void up_kernel(const ApplyArgs a)
     for (int k = 0; k + 1 < QLLM_ADAPTER_PARTS; ++k)
         if (p == k && k + 1 < a.n_parts && block >= a.block_end[k]) p = k + 1, b = block - a.block_end[k], from = a.part_end[k];
     const int column = from + b * a.columns, end = min(column + a.columns, a.part_end[p]);
-    const bool whole = ((end - column) & 63) == 0;
-    if (tile.count <= 16) whole ? up_tile<WT, YT, 1, true>(a, tile, p, column, end, staged) : up_tile<WT, YT, 1, false>(a, tile, p, column, end, staged);
-    else whole ? up_tile<WT, YT, 2, true>(a, tile, p, column, end, staged) : up_tile<WT, YT, 2, false>(a, tile, p, column, end, staged);
+    const int form = ((end - column) & 63) != 0 ? 0 : a.stream ? 2 : 1;
+    if (tile.count <= 16) {
+        if (form == 2) up_tile<WT, YT, 1, true, true>(a, tile, p, column, end, staged);
+        else if (form == 1) up_tile<WT, YT, 1, true, false>(a, tile, p, column, end, staged);
+        else up_tile<WT, YT, 1, false, false>(a, tile, p, column, end, staged);
+    } else {
+        if (form == 2) up_tile<WT, YT, 2, true, true>(a, tile, p, column, end, staged);
+        else if (form == 1) up_tile<WT, YT, 2, true, false>(a, tile, p, column, end, staged);
+        else up_tile<WT, YT, 2, false, false>(a, tile, p, column, end, staged);
+    }
 }
 
 int32_t launched(const char *what)
@@ -563,20 +577,29 @@ int32_t check_sizes(const qllm_adapters *w, int64_t rows)
 // The fewest tiles that the rows can make: what a launch counts on to fill the card.
 inline int64_t fewest_tiles(int64_t rows) { return rows > TILE ? (rows + TILE - 1) / TILE : 1; }
 
-// The slices of C: two workgroups a CU, none shorter than a turn of the four waves.
+// The slices of C: two workgroups a CU, none shorter than a turn of the four waves (256 channels).
 void slices_of(const qllm_adapters *w, int64_t rows, int32_t *slices, int32_t *blocks_per_slice)
 {
-    const int64_t blocks = (w->C + 63) / 64, turns = (blocks + 3) / 4, tiles = fewest_tiles(rows) * ((w->n_parts * w->rank + 63) / 64);
+    const int64_t turns = (w->C + 255) / 256, tiles = fewest_tiles(rows) * ((w->n_parts * w->rank + 63) / 64);
     const int64_t want = (512 + tiles - 1) / tiles, most = want < turns ? want : turns, each = (turns + most - 1) / most;
     *blocks_per_slice = (int32_t)(4 * each);
     *slices = (int32_t)((turns + each - 1) / each);
 }
 
-// Columns of a workgroup of the second product, a multiple of 256: few enough for three workgroups a CU, at most 1024.
+// Columns of a workgroup of the second product: the multiple of 256 with the least work in a row, in rounds of two workgroups a CU, each
+// as long as its columns and about 300 more (the trips to the plan, to h, to the first y).  Up to 512 rows are taken for single tokens of
+// many requests, with as many tiles as there are halfway between the fewest and the most.
 int32_t columns_of(const qllm_adapters *w, int64_t rows)
 {
-    const int64_t each = w->O * fewest_tiles(rows) / 768 / 256 * 256;
-    return (int32_t)(each < 256 ? 256 : each > 1024 ? 1024 : each);
+    const int64_t fewest = fewest_tiles(rows), tiles = rows <= 512 ? (fewest + most_tiles(rows, w->n_adapters)) / 2 : fewest;
+    int64_t best = 256, least = INT64_MAX;
+    for (int64_t columns = 256; columns <= 2048; columns += 256) {
+        int64_t blocks = 0;
+        for (int p = 0; p < w->n_parts; ++p) blocks += (w->part_O[p] + columns - 1) / columns;
+        const int64_t cost = (tiles * blocks + 511) / 512 * (columns + 300);
+        if (cost < least) least = cost, best = columns;
+    }
+    return (int32_t)best;
 }
 
 } // namespace
@@ -617,7 +640,7 @@ template <typename XT, typename WT>
 void run_down(const ApplyArgs &a, unsigned tiles, hipStream_t stream)
 {
     const int frags = (a.wide + 15) / 16;
-    const dim3 grid(tiles, (unsigned)a.slices, (unsigned)((frags + 3) / 4));
+    const dim3 grid(tiles * (unsigned)a.slices, (unsigned)((frags + 3) / 4));
     if (frags == 1) hipLaunchKernelGGL((down_kernel<XT, WT, 1>), grid, dim3(256), 0, stream, a);
     else if (frags == 2) hipLaunchKernelGGL((down_kernel<XT, WT, 2>), grid, dim3(256), 0, stream, a);
     else if (frags == 3) hipLaunchKernelGGL((down_kernel<XT, WT, 3>), grid, dim3(256), 0, stream, a);
@@ -673,6 +696,10 @@ extern "C" int32_t qllm_adapter_apply(const void *x, int32_t x_dtype, int64_t ld
         a.part_end[p] = (int32_t)w->part_O[p] + (p ? a.part_end[p - 1] : 0);
         a.block_end[p] = (int32_t)((w->part_O[p] + a.columns - 1) / a.columns) + (p ? a.block_end[p - 1] : 0);
     }
+    // Where rows and parts are whole lines (prompts through 5120 -> 27648 130 : 124 us); lines that two waves share are better met in the
+    // caches (1700 rows of 4999 fp32 31 : 21).
+    a.stream = !misses(y, 128) && !misses(out, 128) && (ldy * ys % 128 | ldo * ys % 128) == 0;
+    for (int p = 0; p + 1 < w->n_parts; ++p) a.stream = a.stream && a.part_end[p] * ys % 128 == 0;
     const int64_t tiles = most_tiles(rows, w->n_adapters);
     if (tiles * a.block_end[a.n_parts - 1] > INT32_MAX) return QLLM_ERR_SHAPE;
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
