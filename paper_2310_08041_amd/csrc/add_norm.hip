@@ -14,6 +14,7 @@
 #include <stdint.h>
 
 #include "fused_common.h"
+#include "pack_codes.h"
 #include "qllm_block.h"
 #include "rows.h"
 #include "wave_reduce.h"
@@ -21,6 +22,9 @@
 using namespace qllm_detail;
 
 namespace {
+
+constexpr int MOST_LANES = 1024;
+constexpr int MANY_ROWS = 512;
 
 struct AddNormArgs {
     const void *x, *residual;
@@ -30,8 +34,8 @@ struct AddNormArgs {
     int32_t N, C, norm, o_bf16;
     double eps, inv_C;
     const uint32_t *places; // of 8 output channels: 4 words
-    const int32_t *first;
-    const int2 *entries;
+    const uint4 *computed;  // see qllm_gather_map_host
+    const int2 *more;
     int32_t n_computed, S, K, groups; // groups of 8 codes in a row, padding included
     uint8_t *codes;
     int64_t row_bytes;
@@ -40,20 +44,14 @@ struct AddNormArgs {
     int32_t bits;
 };
 
-// the 8 codes of a group, one byte each, to the row's packed bytes
-__device__ __forceinline__ void store_codes(uint8_t *row, int g, int bits, const uint32_t *c)
+// 8 clamped codes into the row's group g; returns their sum
+template <int BITS>
+__device__ __forceinline__ int32_t put_codes(uint8_t *row, int g, uint32_t *c, uint32_t bias, uint32_t live)
 {
-    if (bits == 8) {
-        reinterpret_cast<uint2 *>(row)[g] = make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
-    } else if (bits == 4) {
-        reinterpret_cast<uint32_t *>(row)[g] = c[0] | c[1] << 4 | c[2] << 8 | c[3] << 12 | c[4] << 16 | c[5] << 20 | c[6] << 24 | c[7] << 28;
-    } else {
-        const uint32_t lo = c[0] | c[1] << 6 | c[2] << 12 | c[3] << 18, hi = c[4] | c[5] << 6 | c[6] << 12 | c[7] << 18;
-        uint16_t *to = reinterpret_cast<uint16_t *>(row + (int64_t)g * 6);
-        to[0] = (uint16_t)lo;
-        to[1] = (uint16_t)(lo >> 16 | hi << 8);
-        to[2] = (uint16_t)(hi >> 8);
-    }
+    uint32_t w0, w1;
+    pack_clamped<BITS>(c, bias, live, w0, w1);
+    store_group<BITS>(row, g, w0, w1);
+    return code_sum<BITS>(w0, w1);
 }
 
 __device__ __forceinline__ void store_out(void *to, int64_t at, bool bf16, const float *v, int n)
@@ -69,29 +67,33 @@ __device__ __forceinline__ void store_out(void *to, int64_t at, bool bf16, const
     }
 }
 
-template <int WAVES>
-__device__ __forceinline__ double over_waves(double v, double *slots)
+// Over the workgroup's waves (16 at most): lane l of every wave takes the slot of wave l mod 16, and a butterfly adds them.
+__device__ __forceinline__ double over_waves(double v, double *slots, int waves)
 {
     v = wave_sum(v);
-    if constexpr (WAVES == 1) return v;
-    if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
+    if (waves == 1) return v;
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) slots[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = slots[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) v += slots[w];
-    return v;
+    return dpp_addd_row16((lane & 15) < waves ? slots[lane & 15] : 0.0);
 }
 
-template <typename XT, typename RT, int THREADS, int ITERS, bool MAPPED>
-__global__ __launch_bounds__(THREADS) void add_norm_kernel(const AddNormArgs a)
+// WHOLE: every chunk of 8 channels, in and out, is in the row as a whole or not at all.
+template <typename XT, typename RT, int ITERS, bool MAPPED, bool WHOLE>
+__global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs a)
 {
-    constexpr int WAVES = THREADS / 64;
     extern __shared__ __align__(16) float places[]; // MAPPED: y by places, then the computed channels
-    __shared__ double red_d[2][WAVES];
-    __shared__ float red_f[2][WAVES];
-    __shared__ int32_t red_i[WAVES];
+    __shared__ double red_d[2][16];
+    __shared__ float red_f[2][16];
+    __shared__ int32_t red_i[16];
+    const int THREADS = blockDim.x, WAVES = THREADS >> 6;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int64_t row = blockIdx.x;
+    // elements of chunk `it` of the lane that are there, in a row of n
+    auto there = [&](int it, int n) {
+        const int left = n - (tid + it * THREADS) * GROUP;
+        return WHOLE ? (left > 0 ? GROUP : 0) : left;
+    };
 
     // ---- s = round(residual + x)
     float v[ITERS][GROUP];
@@ -103,8 +105,8 @@ __global__ __launch_bounds__(THREADS) void add_norm_kernel(const AddNormArgs a)
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
             const int c0 = (tid + it * THREADS) * GROUP;
-            re[it].load(r + c0, a.C - c0);
-            if (a.x) xe[it].load(x + c0, a.C - c0);
+            re[it].load(r + c0, there(it, a.C));
+            if (a.x) xe[it].load(x + c0, there(it, a.C));
         }
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
@@ -116,59 +118,77 @@ __global__ __launch_bounds__(THREADS) void add_norm_kernel(const AddNormArgs a)
 #pragma unroll
                 for (int j = 0; j < GROUP; ++j) v[it][j] += u[j];
                 re[it].round(v[it]);
-                if (a.sum) re[it].store(static_cast<RT *>(a.sum) + row * a.lds + c0, a.C - c0);
+                if (a.sum) re[it].template store<(ITERS > 1)>(static_cast<RT *>(a.sum) + row * a.lds + c0, there(it, a.C)); // not read soon: past the caches
                 re[it].widen(v[it]);
             }
         }
     }
 
+    // what depends on the map and on gamma alone is asked for while the statistics are on their way
+    Eight<float> gamma[ITERS];
+    uint4 place[MAPPED ? ITERS : 1];
+    uint4 computed = make_uint4(0, 0, 0, 0); // the first that falls to the lane
+    if (a.norm != QLLM_NORM_NONE) {
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it) {
+            const int c0 = (tid + it * THREADS) * GROUP;
+            gamma[it].load(a.gamma + c0, there(it, a.C));
+        }
+    }
+    if constexpr (MAPPED) {
+        if (tid < a.n_computed) computed = a.computed[tid];
+    }
+
     // ---- y = norm(s); elements past the row are 0 and stay out of the sums
     float mu = 0.0f, rstd = 1.0f;
     if (a.norm == QLLM_NORM_RMS) {
-        double q = 0.0;
+        double q[2] = {0.0, 0.0}; // two chains
 #pragma unroll
         for (int it = 0; it < ITERS; ++it)
 #pragma unroll
-            for (int j = 0; j < GROUP; ++j) q = __builtin_fma((double)v[it][j], (double)v[it][j], q);
-        rstd = rsqrt_to_f32(over_waves<WAVES>(q, red_d[0]) * a.inv_C + a.eps);
+            for (int j = 0; j < GROUP; ++j) q[j & 1] = __builtin_fma((double)v[it][j], (double)v[it][j], q[j & 1]);
+        rstd = rsqrt_to_f32(over_waves(q[0] + q[1], red_d[0], WAVES) * a.inv_C + a.eps);
     } else if (a.norm == QLLM_NORM_LAYER) {
         double s = 0.0, q = 0.0;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it)
 #pragma unroll
             for (int j = 0; j < GROUP; ++j) s += (double)v[it][j];
-        const double mean = over_waves<WAVES>(s, red_d[0]) * a.inv_C;
+        const double mean = over_waves(s, red_d[0], WAVES) * a.inv_C;
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it)
+#pragma unroll
+            for (int j = 0; j < GROUP; ++j) asm volatile("" : "+v"(v[it][j])); // converted again rather than kept in 64 bits over the sum
 #pragma unroll
         for (int it = 0; it < ITERS; ++it)
 #pragma unroll
             for (int j = 0; j < GROUP; ++j) {
                 const double d = (double)v[it][j] - mean;
-                if ((tid + it * THREADS) * GROUP + j < a.C) q = __builtin_fma(d, d, q);
+                if (j < there(it, a.C)) q = __builtin_fma(d, d, q);
             }
-        rstd = rsqrt_to_f32(over_waves<WAVES>(q, red_d[1]) * a.inv_C + a.eps);
+        rstd = rsqrt_to_f32(over_waves(q, red_d[1], WAVES) * a.inv_C + a.eps);
         mu = (float)mean;
     }
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
         const int c0 = (tid + it * THREADS) * GROUP;
         if (a.norm != QLLM_NORM_NONE) {
-            Eight<float> e;
             float g[GROUP];
-            e.load(a.gamma + c0, a.C - c0);
-            e.widen(g);
+            gamma[it].widen(g);
 #pragma unroll
             for (int j = 0; j < GROUP; ++j) {
                 if (a.norm == QLLM_NORM_LAYER) v[it][j] -= mu;
                 v[it][j] = v[it][j] * rstd * g[j];
             }
             if (a.norm == QLLM_NORM_LAYER && a.beta) {
-                e.load(a.beta + c0, a.C - c0);
+                Eight<float> e;
+                e.load(a.beta + c0, there(it, a.C));
                 e.widen(g);
 #pragma unroll
                 for (int j = 0; j < GROUP; ++j) v[it][j] += g[j];
             }
         }
-        if (a.y) store_out(a.y, row * a.ldy + c0, a.o_bf16, v[it], a.C - c0);
+        if (a.y) store_out(a.y, row * a.ldy + c0, a.o_bf16, v[it], there(it, a.C));
         if constexpr (MAPPED) {
             if (c0 < a.C)
 #pragma unroll
@@ -179,47 +199,52 @@ __global__ __launch_bounds__(THREADS) void add_norm_kernel(const AddNormArgs a)
 
     // ---- x^: computed channels first, then one read for every channel
     if constexpr (MAPPED) {
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it) place[it] = reinterpret_cast<const uint4 *>(a.places)[min(tid + it * THREADS, a.groups - 1)];
         __syncthreads();
         for (int j = tid; j < a.n_computed; j += THREADS) {
-            const int32_t e0 = a.first[j], e1 = a.first[j + 1];
-            int2 e = a.entries[e0];
-            float sum = __int_as_float(e.y) * places[e.x];
-            for (int k = e0 + 1; k < e1; ++k) {
-                e = a.entries[k];
-                sum = sum + __int_as_float(e.y) * places[e.x];
+            if (j != tid) computed = a.computed[j];
+            float sum = __uint_as_float(computed.y) * places[computed.x & 0xffffu];
+            sum = sum + __uint_as_float(computed.z) * places[computed.x >> 16];
+            if (computed.w != 0u) { // entries beyond the second
+                const int2 *more = a.more + computed.w;
+                const int count = more[0].x;
+                for (int k = 1; k <= count; ++k) sum = sum + __int_as_float(more[k].y) * places[more[k].x];
             }
             places[GROUP * a.S + j] = sum;
         }
         __syncthreads();
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
-            const int g = tid + it * THREADS;
-            if (g < a.groups) {
-                const uint4 p = reinterpret_cast<const uint4 *>(a.places)[g];
-                const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+            const uint32_t w[4] = {place[it].x, place[it].y, place[it].z, place[it].w};
 #pragma unroll
-                for (int j = 0; j < GROUP; ++j) v[it][j] = places[j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu];
-            }
+            for (int j = 0; j < GROUP; ++j) v[it][j] = places[j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu];
         }
     }
 
     // ---- Eq. (2)
     float mn = __builtin_inff(), mx = -__builtin_inff();
 #pragma unroll
-    for (int it = 0; it < ITERS; ++it)
+    for (int it = 0; it < ITERS; ++it) {
+        const int n = there(it, a.K);
+        if (n >= GROUP) {
 #pragma unroll
-        for (int j = 0; j < GROUP; ++j)
-            if ((tid + it * THREADS) * GROUP + j < a.K) {
-                mn = fminf(mn, v[it][j]);
-                mx = fmaxf(mx, v[it][j]);
+            for (int j = 0; j < GROUP; j += 2) { // three operands an instruction
+                mn = fminf(fminf(mn, v[it][j]), v[it][j + 1]);
+                mx = fmaxf(fmaxf(mx, v[it][j]), v[it][j + 1]);
             }
+        } else if (!WHOLE && n > 0) {
+#pragma unroll
+            for (int j = 0; j < GROUP - 1; ++j)
+                if (j < n) mn = fminf(mn, v[it][j]), mx = fmaxf(mx, v[it][j]);
+        }
+    }
     wave_minmax(mn, mx);
-    if constexpr (WAVES > 1) {
+    if (WAVES > 1) {
         if (lane == 0) red_f[0][wave] = mn, red_f[1][wave] = mx;
         __syncthreads();
-        mn = red_f[0][0], mx = red_f[1][0];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) mn = fminf(mn, red_f[0][w]), mx = fmaxf(mx, red_f[1][w]);
+        const int w = min(lane & 15, WAVES - 1);
+        mn = dpp_min_row16(red_f[0][w]), mx = dpp_max_row16(red_f[1][w]);
     }
     const int32_t qmax = (1 << a.bits) - 1;
     const float range = mx - mn, alpha = range > 0.0f ? range / (float)qmax : 1.0f, inv = 1.0f / alpha;
@@ -227,50 +252,43 @@ __global__ __launch_bounds__(THREADS) void add_norm_kernel(const AddNormArgs a)
     int32_t beta;
     if (fast) beta = -rne_product_fast(mn, inv);
     else beta = (int32_t)fmin(fmax(-rne_product_slow(mn, inv), -2147483647.0), 2147483647.0);
-    // floats in [2^23, 2^24) are integers and order like their bit patterns: a code is clamped as such a float
-    const float lowest = __int_as_float(MAGIC_BITS - beta), highest = __int_as_float(MAGIC_BITS - beta + qmax);
     uint8_t *to = a.codes + row * a.row_bytes;
     int32_t sum = 0;
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
-        const int g = tid + it * THREADS;
+        const int g = tid + it * THREADS, n = there(it, a.K);
         if (g >= a.groups) continue;
+        const uint32_t live = n >= GROUP ? 0xffu : n > 0 ? (1u << n) - 1u : 0u;
         uint32_t c[GROUP];
-        float stands[GROUP];
+        const uint32_t bias = clamp_codes(v[it], qmax, fast, inv, beta, c);
+        if (a.values) {
+            float stands[GROUP];
 #pragma unroll
-        for (int j = 0; j < GROUP; ++j) {
-            if (fast) {
-                c[j] = __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fmaf(v[it][j], inv, MAGIC), lowest, highest)) - (uint32_t)(MAGIC_BITS - beta);
-                stands[j] = alpha * (float)((int32_t)c[j] - beta);
-            } else {
-                const double q = fmin(fmax(rne_product_slow(v[it][j], inv) + (double)beta, 0.0), (double)qmax);
-                c[j] = (uint32_t)q;
-                stands[j] = (float)((double)alpha * (q - (double)beta));
-            }
-            if (g * GROUP + j >= a.K) c[j] = 0;
-            sum += (int32_t)c[j];
+            for (int j = 0; j < GROUP; ++j) // the float that a fast code is clamped as is 1.5 * 2^23 + code - beta
+                stands[j] = fast ? alpha * (__uint_as_float(c[j]) - MAGIC) : (float)((double)alpha * ((double)c[j] - (double)beta));
+            store_out(a.values, row * a.ldv + (int64_t)g * GROUP, a.o_bf16, stands, n);
         }
-        store_codes(to, g, a.bits, c);
-        if (a.values) store_out(a.values, row * a.ldv + (int64_t)g * GROUP, a.o_bf16, stands, a.K - g * GROUP);
+        if (a.bits == 8) sum += put_codes<8>(to, g, c, bias, live);
+        else if (a.bits == 4) sum += put_codes<4>(to, g, c, bias, live);
+        else sum += put_codes<6>(to, g, c, bias, live);
     }
     sum = wave_sum_i32(sum);
-    if constexpr (WAVES > 1) {
+    if (WAVES > 1) {
         if (lane == 0) red_i[wave] = sum;
         __syncthreads();
+        sum = dpp_add_row16((lane & 15) < WAVES ? red_i[lane & 15] : 0);
     }
     if (tid == 0) {
-        if constexpr (WAVES > 1)
-            for (int w = 1; w < WAVES; ++w) sum += red_i[w];
         a.alpha[row] = alpha;
         a.zero[row] = beta;
         a.rowsum[row] = sum;
     }
 }
 
-template <typename XT, typename RT, int THREADS, int ITERS, bool MAPPED>
-int32_t launch(const AddNormArgs &a, hipStream_t stream)
+template <typename XT, typename RT, int ITERS, bool MAPPED>
+int32_t launch(const AddNormArgs &a, int units, hipStream_t stream)
 {
-    auto *kernel = add_norm_kernel<XT, RT, THREADS, ITERS, MAPPED>;
+    auto *kernel = a.C % GROUP == 0 && a.K % GROUP == 0 ? add_norm_kernel<XT, RT, ITERS, MAPPED, true> : add_norm_kernel<XT, RT, ITERS, MAPPED, false>;
     const size_t lds = MAPPED ? (size_t)(GROUP * a.S + a.n_computed) * sizeof(float) : 0;
     if (lds > 48 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -280,8 +298,9 @@ int32_t launch(const AddNormArgs &a, hipStream_t stream)
             return QLLM_ERR_HIP;
         }
     }
+    const int lanes = (units + ITERS * 64 - 1) / (ITERS * 64) * 64;
     (void)hipGetLastError(); // drop any stale error of the calling thread: only this launch is judged
-    hipLaunchKernelGGL(kernel, dim3((unsigned)a.N), dim3(THREADS), lds, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)a.N), dim3(lanes), lds, stream, a);
     const hipError_t e = hipGetLastError();
     if (e == hipSuccess) return QLLM_OK;
     qllm_note_hip_error("add_norm: launch", hipGetErrorName(e));
@@ -292,12 +311,10 @@ template <typename XT, typename RT, bool MAPPED>
 int32_t by_width(const AddNormArgs &a, hipStream_t stream)
 {
     const int units = a.S > a.groups ? a.S : a.groups; // chunks of 8 channels, in or out
-    if (units <= 64) return launch<XT, RT, 64, 1, MAPPED>(a, stream);
-    if (units <= 256) return launch<XT, RT, 256, 1, MAPPED>(a, stream);
-    if (units <= 512) return launch<XT, RT, 512, 1, MAPPED>(a, stream);
-    if (units <= 1024) return launch<XT, RT, 1024, 1, MAPPED>(a, stream);
-    if (units <= 2048) return launch<XT, RT, 1024, 2, MAPPED>(a, stream);
-    return launch<XT, RT, 1024, 4, MAPPED>(a, stream);
+    const bool many = a.N >= MANY_ROWS;
+    if (units <= MOST_LANES && (!many || units <= 64)) return launch<XT, RT, 1, MAPPED>(a, units, stream);
+    if (units <= 2 * MOST_LANES) return launch<XT, RT, 2, MAPPED>(a, units, stream);
+    return launch<XT, RT, 4, MAPPED>(a, units, stream);
 }
 
 template <typename XT, typename RT>
@@ -358,8 +375,8 @@ extern "C" int32_t qllm_add_norm_quant(const void *x, int32_t x_dtype, int64_t l
         a.bits = bits;
         if (gather) {
             a.places = reinterpret_cast<const uint32_t *>(gather->index);
-            a.first = gather->index + padded / 2;
-            a.entries = reinterpret_cast<const int2 *>(a.first + (gather->n_computed + 2) / 2 * 2);
+            a.computed = reinterpret_cast<const uint4 *>(gather->index + padded / 2);
+            a.more = reinterpret_cast<const int2 *>(gather->index + padded / 2 + 4 * gather->n_computed);
             a.n_computed = (int32_t)gather->n_computed;
         }
     }

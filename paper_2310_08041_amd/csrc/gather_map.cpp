@@ -11,39 +11,51 @@ extern "C" int32_t qllm_gather_map_host(const int32_t *row_ptr, const int32_t *s
     if (C_in <= 0 || C_in > QLLM_MAX_CHANNELS || C_out <= 0 || C_out > QLLM_MAX_CHANNELS) return QLLM_ERR_SHAPE;
     if (row_ptr[0] != 0) return QLLM_ERR_MAP;
     const int64_t S = (C_in + 7) / 8, padded = (C_out + QLLM_K_PAD - 1) / QLLM_K_PAD * QLLM_K_PAD;
-    int64_t computed = 0, entries = 0;
+    int64_t computed = 0, more = 1; // the first pair of `more` is no row's
     for (int64_t ch = 0; ch < C_out; ++ch) {
         if (row_ptr[ch + 1] <= row_ptr[ch]) return QLLM_ERR_MAP;
         for (int64_t e = row_ptr[ch]; e < row_ptr[ch + 1]; ++e)
             if (src[e] < 0 || src[e] >= C_in) return QLLM_ERR_MAP;
         if (row_ptr[ch + 1] - row_ptr[ch] == 1 && scale[row_ptr[ch]] == 1.0f) continue;
         ++computed;
-        entries += row_ptr[ch + 1] - row_ptr[ch];
+        if (row_ptr[ch + 1] - row_ptr[ch] > 2) more += row_ptr[ch + 1] - row_ptr[ch] - 1;
     }
     if (8 * S + computed > QLLM_GATHER_PLACES) return QLLM_ERR_SHAPE;
-    const int64_t at_first = padded / 2, at_entries = at_first + (computed + 2) / 2 * 2, len = at_entries + 2 * entries;
+    const int64_t at_computed = padded / 2, at_more = at_computed + 4 * computed, len = at_more + 2 * more;
     *index_len = len;
     *n_computed = computed;
     if (!index) return QLLM_OK;
     memset(index, 0, (size_t)len * sizeof(int32_t));
     auto place_of = [S](int64_t c) { return (c & 7) * S + (c >> 3); };
-    int64_t j = 0, at = 0;
+    auto bits_of = [](float f) {
+        int32_t v;
+        memcpy(&v, &f, sizeof v);
+        return v;
+    };
+    int64_t j = 0, at = 1;
     for (int64_t ch = 0; ch < C_out; ++ch) {
         int64_t place;
-        const int64_t e0 = row_ptr[ch], e1 = row_ptr[ch + 1];
-        if (e1 - e0 == 1 && scale[e0] == 1.0f) {
+        const int64_t e0 = row_ptr[ch], n = row_ptr[ch + 1] - e0;
+        if (n == 1 && scale[e0] == 1.0f) {
             place = place_of(src[e0]);
         } else {
             place = 8 * S + j;
-            index[at_first + j++] = (int32_t)at;
-            for (int64_t e = e0; e < e1; ++e, ++at) {
-                index[at_entries + 2 * at] = (int32_t)place_of(src[e]);
-                memcpy(&index[at_entries + 2 * at + 1], &scale[e], sizeof(float));
+            int32_t *c = index + at_computed + 4 * j++;
+            const int64_t second = n > 1 ? e0 + 1 : e0;
+            c[0] = (int32_t)((uint32_t)place_of(src[e0]) | (uint32_t)place_of(src[second]) << 16);
+            c[1] = bits_of(scale[e0]);
+            c[2] = n > 1 ? bits_of(scale[second]) : 0;
+            if (n > 2) {
+                c[3] = (int32_t)at;
+                index[at_more + 2 * at++] = (int32_t)(n - 2);
+                for (int64_t e = e0 + 2; e < e0 + n; ++e, ++at) {
+                    index[at_more + 2 * at] = (int32_t)place_of(src[e]);
+                    index[at_more + 2 * at + 1] = bits_of(scale[e]);
+                }
             }
         }
         const uint32_t word = (uint32_t)index[ch / 2];
         index[ch / 2] = (int32_t)(ch & 1 ? word | (uint32_t)place << 16 : word | (uint32_t)place);
     }
-    index[at_first + j] = (int32_t)at;
     return QLLM_OK;
 }

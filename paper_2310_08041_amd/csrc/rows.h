@@ -53,10 +53,12 @@ struct Eight<uint16_t> {
 #pragma unroll
         for (int k = 0; k < 4; ++k) q[k] = to_bf16(v[2 * k], v[2 * k + 1]);
     }
+    template <bool STREAM = false>
     __device__ __forceinline__ void store(uint16_t *p, int n) const
     {
         if (n >= 8) {
-            *reinterpret_cast<u32x4_at2 *>(p) = q;
+            if constexpr (STREAM) __builtin_nontemporal_store(q, reinterpret_cast<u32x4_at2 *>(p));
+            else *reinterpret_cast<u32x4_at2 *>(p) = q;
         } else {
 #pragma unroll
             for (int j = 0; j < 7; ++j)
@@ -91,11 +93,17 @@ struct Eight<float> {
 #pragma unroll
         for (int j = 0; j < 4; ++j) a[j] = __float_as_uint(v[j]), b[j] = __float_as_uint(v[j + 4]);
     }
+    template <bool STREAM = false>
     __device__ __forceinline__ void store(float *p, int n) const
     {
         if (n >= 8) {
-            reinterpret_cast<u32x4_at4 *>(p)[0] = a;
-            reinterpret_cast<u32x4_at4 *>(p)[1] = b;
+            if constexpr (STREAM) {
+                __builtin_nontemporal_store(a, reinterpret_cast<u32x4_at4 *>(p));
+                __builtin_nontemporal_store(b, reinterpret_cast<u32x4_at4 *>(p) + 1);
+            } else {
+                reinterpret_cast<u32x4_at4 *>(p)[0] = a;
+                reinterpret_cast<u32x4_at4 *>(p)[1] = b;
+            }
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {

@@ -70,17 +70,16 @@ def apply_index(y, index, computed, C_in, C_out):
     S = (C_in + 7) // 8
     padded = -(-C_out // 256) * 256
     places = index[:padded // 2].view(np.uint16)
-    first = index[padded // 2:padded // 2 + computed + 1]
-    entries = index[padded // 2 + (computed + 2) // 2 * 2:].reshape(-1, 2)
-    row = np.zeros(8 * S + computed, np.float32)
+    computed = index[padded // 2:padded // 2 + 4 * computed].reshape(-1, 4)
+    more = index[padded // 2 + computed.size:].reshape(-1, 2)
+    row = np.zeros(8 * S + len(computed), np.float32)
     for c in range(C_in):
         row[(c % 8) * S + c // 8] = y[c]
-    for j in range(computed):
-        e = entries[first[j]:first[j + 1]]
-        v = e[:, 1].copy().view(np.float32)
-        t = np.float32(v[0] * row[e[0, 0]])
-        for k in range(1, len(e)):
-            t = np.float32(t + np.float32(v[k] * row[e[k, 0]]))
+    for j, c in enumerate(computed):
+        scale = c[1:3].copy().view(np.float32)
+        t = np.float32(np.float32(scale[0] * row[c[0] & 0xffff]) + np.float32(scale[1] * row[(int(c[0]) >> 16) & 0xffff]))
+        for place, bits in more[c[3] + 1:c[3] + 1 + more[c[3], 0]] if c[3] else ():
+            t = np.float32(t + np.float32(np.int32(bits).view(np.float32) * row[place]))
         row[8 * S + j] = t
     assert (places[C_out:] == 0).all()
     return row[places[:C_out]]
@@ -148,7 +147,8 @@ def test_adapter_refusals():
     assert apply(pool(Ap=None)) == NULL and apply(pool(Bp=None)) == NULL
     for kw in (dict(rows=-1), dict(rows=1 << 24), dict(ldx=63), dict(ldy=95), dict(ldo=95), dict(ldo=100)):
         assert apply(**kw) == SHAPE, kw
-    assert apply(pool(O=8000000, part_O=(8000000, 0, 0, 0)), rows=1 << 23, ldy=8000000, ldo=8000000, ws_bytes=1 << 50, plan_bytes=1 << 40) == SHAPE
+    most = (1 << 24) - 1                        # rows and columns each at their limit: more workgroups than a launch can have
+    assert apply(pool(O=most, part_O=(most, 0, 0, 0)), rows=most, ldy=most, ldo=most, ws_bytes=1 << 50, plan_bytes=1 << 50) == SHAPE
     for kw in (dict(xd=2), dict(yd=-1), dict(w=pool(wd=5))):
         assert apply(**kw) == DTYPE, kw
     for kw in (dict(x=A + 1), dict(y=A + 1), dict(out=A + 1), dict(plan=A + 8), dict(ws=A + 4), dict(w=pool(Ap=A + 8)), dict(w=pool(Bp=A + 4)),
