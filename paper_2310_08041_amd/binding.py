@@ -1034,12 +1034,17 @@ class DeviceGather:
         self.ref = C.byref(self.c)
 
 
-def _check_here(**tensors):
-    """Everything on the device that the call runs on; the list is walked twice only if something is wrong."""
-    here = torch.cuda.current_device() if torch.cuda.is_available() else -1
-    for t in tensors.values():
-        if t is not None and (t.get_device() != here or here < 0):
-            _check_on_current(**tensors)
+def _check_here(names, *tensors):
+    """Everything on the device that the call runs on (the first of the tensors is one); names, in one string, are looked at only if
+    something is wrong."""
+    here = tensors[0].get_device()
+    if here >= 0 and here == (torch.cuda.current_device() if _raw_device is None else _raw_device()):
+        for t in tensors:
+            if t is not None and t.get_device() != here:
+                break
+        else:
+            return
+    _check_on_current(**dict(zip(names.split(), tensors)))
 
 
 def qllm_add_norm_quant(x, residual, sum_out, norm, gamma, beta, eps, out=None, bits=8, gather=None, y_out=None, values_out=None, stream=None):
@@ -1056,27 +1061,31 @@ def qllm_add_norm_quant(x, residual, sum_out, norm, gamma, beta, eps, out=None, 
     K = Cc if gather is None else gather.C_out
     if gather is not None and gather.C_in != Cc:
         _fail(f"the map takes {gather.C_in} channels, residual has {Cc}")
-    if out is not None and (out.N != N or out.K != K or out.bits != int(bits)):
-        _fail(f"out holds {out.N} rows of {out.K} codes of {out.bits} bits, the call makes {N} of {K} of {int(bits)}")
+    norm, bits, eps = int(norm), int(bits), float(eps)
+    if out is not None and (out.N != N or out.K != K or out.bits != bits):
+        _fail(f"out holds {out.N} rows of {out.K} codes of {out.bits} bits, the call makes {N} of {K} of {bits}")
     ldv = 0
     if values_out is not None:
         if out is None:
             _fail("values_out needs out")
         ldv = _check_rows(values_out, "values_out", _FLOATS if y_out is None else (y_out.dtype,), N, K)
-    if int(norm) not in (NORM_NONE, NORM_LAYER, NORM_RMS):
-        _fail(f"unknown norm {norm}")
-    if int(norm) != NORM_NONE:
-        _check_tensor(gamma, "gamma", _F32_ONLY, numel=Cc)
-        _check_tensor(beta, "beta", _F32_ONLY, numel=Cc, optional=True)
-    else:
+    if norm == NORM_NONE:
         gamma = beta = None
-    _check_here(x=x, residual=residual, sum_out=sum_out, gamma=gamma, beta=beta, y_out=y_out, values_out=values_out,
-                index=None if gather is None else gather.index, codes=None if out is None else out.codes)
+    elif norm not in (NORM_LAYER, NORM_RMS):
+        _fail(f"unknown norm {norm}")
+    else:
+        if not (isinstance(gamma, torch.Tensor) and gamma.dtype is torch.float32 and gamma.numel() == Cc and gamma.is_contiguous()):
+            _check_tensor(gamma, "gamma", _F32_ONLY, numel=Cc)
+        _check_tensor(beta, "beta", _F32_ONLY, numel=Cc, optional=True)
+    _check_here("residual x sum_out gamma beta y_out values_out index codes", residual, x, sum_out, gamma, beta, y_out, values_out,
+                None if gather is None else gather._index, None if out is None else out.codes)
     o = y_out if y_out is not None else values_out
-    _chk(_lib.qllm_add_norm_quant(_dp(x), _x_dtype(x) if x is not None else F32, ldx, _dp(residual), _x_dtype(residual), ldr, N, Cc, _dp(sum_out), lds,
-                                  int(norm), _dp(gamma), _dp(beta), float(eps), None if gather is None else gather.ref, int(bits),
-                                  None if out is None else C.byref(out.c), _dp(y_out), ldy, _dp(values_out), ldv,
-                                  F32 if o is None else _x_dtype(o), _stream(stream)), "qllm_add_norm_quant")
+    _chk(_lib.qllm_add_norm_quant(None if x is None else x.data_ptr(), F32 if x is None else _x_dtype(x), ldx, residual.data_ptr(), _x_dtype(residual),
+                                  ldr, N, Cc, None if sum_out is None else sum_out.data_ptr(), lds, norm, None if gamma is None else gamma.data_ptr(),
+                                  None if beta is None else beta.data_ptr(), eps, None if gather is None else gather.ref, bits,
+                                  None if out is None else C.byref(out.c), None if y_out is None else y_out.data_ptr(), ldy,
+                                  None if values_out is None else values_out.data_ptr(), ldv, F32 if o is None else _x_dtype(o), _stream(stream)),
+         "qllm_add_norm_quant")
 
 
 class DeviceAdapters:
@@ -1121,7 +1130,7 @@ class DeviceAdapterPlan:
     def __init__(self, rows, n_adapters, device="cuda"):
         self.rows, self.n_adapters = int(rows), int(n_adapters)
         self._words = torch.zeros(qllm_adapter_plan_bytes(rows, n_adapters) // 4, dtype=torch.int32, device=device)
-        self.device = self._words.get_device()
+        self.at, self.bytes = _dp(self._words), 4 * self._words.numel()
 
 
 def qllm_adapter_plan(plan, adapter, row_start=None, stream=None):
@@ -1130,8 +1139,8 @@ def qllm_adapter_plan(plan, adapter, row_start=None, stream=None):
     _check_tensor(adapter, "adapter", _I32_ONLY, numel=adapter.numel())
     _check_tensor(row_start, "row_start", _I32_ONLY, numel=adapter.numel() + 1, optional=True)
     _need(row_start is not None or adapter.numel() <= plan.rows, f"{adapter.numel()} sequences of one row each need as many rows, there are {plan.rows}")
-    _check_here(adapter=adapter, row_start=row_start, plan=plan.words)
-    _chk(_lib.qllm_adapter_plan(plan.rows, adapter.numel(), _dp(row_start), _dp(adapter), plan.n_adapters, _dp(plan.words), 4 * plan.words.numel(),
+    _check_here("adapter row_start plan", adapter, row_start, plan._words)
+    _chk(_lib.qllm_adapter_plan(plan.rows, adapter.numel(), _dp(row_start), _dp(adapter), plan.n_adapters, plan.at, plan.bytes,
                                 _stream(stream)), "qllm_adapter_plan")
 
 
@@ -1153,7 +1162,7 @@ def qllm_adapter_apply(x, adapters, plan, y, out, workspace, stream=None):
     if not (isinstance(workspace, torch.Tensor) and workspace.dtype is torch.uint8 and workspace.is_contiguous()):
         _check_tensor(workspace, "workspace", _U8_ONLY)
         _fail("workspace must be contiguous")
-    _check_here(x=x, y=y, out=out, workspace=workspace, plan=plan.words, adapters=adapters.A)
-    _chk(_lib.qllm_adapter_apply(_dp(x), _x_dtype(x), ldx, rows, adapters.ref, _dp(plan.words), 4 * plan.words.numel(), _dp(y), ldy, _dp(out), ldo,
-                                 _x_dtype(y), _dp(workspace), workspace.numel(), _stream(stream)), "qllm_adapter_apply")
+    _check_here("x y out workspace plan adapters", x, y, out, workspace, plan._words, adapters._A)
+    _chk(_lib.qllm_adapter_apply(x.data_ptr(), _x_dtype(x), ldx, rows, adapters.ref, plan.at, plan.bytes, y.data_ptr(), ldy, out.data_ptr(), ldo,
+                                 _x_dtype(y), workspace.data_ptr(), workspace.numel(), _stream(stream)), "qllm_adapter_apply")
     return out

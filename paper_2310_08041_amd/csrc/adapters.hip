@@ -258,7 +258,7 @@ __global__ __launch_bounds__(256, 2) void down_kernel(const ApplyArgs a)
 }
 
 // ---- the slices' sums: JOINERS neighbouring lanes add up every JOINERS-th slice each, then theirs are added
-constexpr int JOINERS = 8;
+constexpr int JOINERS = 8, JOINED = 32;
 __device__ __forceinline__ f32x4 joined(const float *h, int64_t stride, int slices, int joiner)
 {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -577,11 +577,13 @@ int32_t check_sizes(const qllm_adapters *w, int64_t rows)
 // The fewest tiles that the rows can make: what a launch counts on to fill the card.
 inline int64_t fewest_tiles(int64_t rows) { return rows > TILE ? (rows + TILE - 1) / TILE : 1; }
 
-// The slices of C: two workgroups a CU, none shorter than a turn of the four waves (256 channels).
+// The slices of C: two workgroups a CU, none shorter than a turn of the four waves (256 channels), for few rows two turns where that leaves
+// 16 slices (the second product adds up as many as JOINED itself).
 void slices_of(const qllm_adapters *w, int64_t rows, int32_t *slices, int32_t *blocks_per_slice)
 {
     const int64_t turns = (w->C + 255) / 256, tiles = fewest_tiles(rows) * ((w->n_parts * w->rank + 63) / 64);
-    const int64_t want = (512 + tiles - 1) / tiles, most = want < turns ? want : turns, each = (turns + most - 1) / most;
+    const int64_t want = rows > TILE ? (512 + tiles - 1) / tiles : turns > 32 ? turns / 2 : 16;
+    const int64_t most = want < turns ? want : turns, each = (turns + most - 1) / most;
     *blocks_per_slice = (int32_t)(4 * each);
     *slices = (int32_t)((turns + each - 1) / each);
 }
@@ -708,7 +710,7 @@ extern "C" int32_t qllm_adapter_apply(const void *x, int32_t x_dtype, int64_t ld
     if (wb) xb ? run_down<uint16_t, uint16_t>(a, (unsigned)tiles, stream) : run_down<float, uint16_t>(a, (unsigned)tiles, stream);
     else xb ? run_down<uint16_t, float>(a, (unsigned)tiles, stream) : run_down<float, float>(a, (unsigned)tiles, stream);
     if (const int32_t e = launched("adapters, first product: launch")) return e;
-    if (a.slices > 1 && rows > TILE) {
+    if (a.slices > 1 && (rows > TILE || a.slices > JOINED)) {
         const int64_t words4 = rows * a.wide / 4;
         hipLaunchKernelGGL(join_kernel, dim3((unsigned)((words4 * JOINERS + 255) / 256)), dim3(256), 0, stream, a.h, words4, a.slices);
         if (const int32_t e = launched("adapters, sums: launch")) return e;

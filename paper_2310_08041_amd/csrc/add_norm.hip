@@ -44,12 +44,12 @@ struct AddNormArgs {
     int32_t bits;
 };
 
-// 8 clamped codes into the row's group g; returns their sum
+// the codes of the live ones of 8 values into the row's group g (of the others: 0); returns their sum
 template <int BITS>
-__device__ __forceinline__ int32_t put_codes(uint8_t *row, int g, uint32_t *c, uint32_t bias, uint32_t live)
+__device__ __forceinline__ int32_t put_codes(uint8_t *row, int g, const float *v, uint32_t live, float inv, int32_t beta)
 {
     uint32_t w0, w1;
-    pack_clamped<BITS>(c, bias, live, w0, w1);
+    quant_pack<BITS>(v, live, 1, inv, beta, w0, w1);
     store_group<BITS>(row, g, w0, w1);
     return code_sum<BITS>(w0, w1);
 }
@@ -65,6 +65,12 @@ __device__ __forceinline__ void store_out(void *to, int64_t at, bool bf16, const
         e.round(v);
         e.store(static_cast<float *>(to) + at, n);
     }
+}
+
+__device__ __forceinline__ void put_out(void *to, int64_t at, bool bf16, float v)
+{
+    if (bf16) static_cast<uint16_t *>(to)[at] = (uint16_t)to_bf16(v, 0.0f);
+    else static_cast<float *>(to)[at] = v;
 }
 
 // Over the workgroup's waves (16 at most): lane l of every wave takes the slot of wave l mod 16, and a butterfly adds them.
@@ -85,7 +91,7 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
     extern __shared__ __align__(16) float places[]; // MAPPED: y by places, then the computed channels
     __shared__ double red_d[2][16];
     __shared__ float red_f[2][16];
-    __shared__ int32_t red_i[16];
+    __shared__ uint32_t arrived; // waves << 24, and the sum of their codes
     const int THREADS = blockDim.x, WAVES = THREADS >> 6;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int64_t row = blockIdx.x;
@@ -197,10 +203,22 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
     }
     if (!a.codes) return;
 
-    // ---- x^: computed channels first, then one read for every channel
+    // ---- x^: computed channels by lanes of their own, and one read for every channel.  What is read in the place of a computed channel
+    // here is a NaN, which the minimum and the maximum pass over, or its value already: that lane brings it into them.
+    float mn = __builtin_inff(), mx = -__builtin_inff();
+    auto gather = [&]() {
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it) {
+            const uint32_t w[4] = {place[it].x, place[it].y, place[it].z, place[it].w};
+#pragma unroll
+            for (int j = 0; j < GROUP; ++j)
+                v[it][j] = __hip_atomic_load(&places[j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        }
+    };
     if constexpr (MAPPED) {
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) place[it] = reinterpret_cast<const uint4 *>(a.places)[min(tid + it * THREADS, a.groups - 1)];
+        for (int j = tid; j < a.n_computed; j += THREADS) places[GROUP * a.S + j] = __builtin_nanf("");
         __syncthreads();
         for (int j = tid; j < a.n_computed; j += THREADS) {
             if (j != tid) computed = a.computed[j];
@@ -211,19 +229,13 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
                 const int count = more[0].x;
                 for (int k = 1; k <= count; ++k) sum = sum + __int_as_float(more[k].y) * places[more[k].x];
             }
-            places[GROUP * a.S + j] = sum;
+            __hip_atomic_store(&places[GROUP * a.S + j], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            mn = fminf(mn, sum), mx = fmaxf(mx, sum);
         }
-        __syncthreads();
-#pragma unroll
-        for (int it = 0; it < ITERS; ++it) {
-            const uint32_t w[4] = {place[it].x, place[it].y, place[it].z, place[it].w};
-#pragma unroll
-            for (int j = 0; j < GROUP; ++j) v[it][j] = places[j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xffffu];
-        }
+        gather();
     }
 
     // ---- Eq. (2)
-    float mn = __builtin_inff(), mx = -__builtin_inff();
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
         const int n = there(it, a.K);
@@ -242,10 +254,12 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
     wave_minmax(mn, mx);
     if (WAVES > 1) {
         if (lane == 0) red_f[0][wave] = mn, red_f[1][wave] = mx;
+        if (tid == 0) arrived = 0;
         __syncthreads();
         const int w = min(lane & 15, WAVES - 1);
         mn = dpp_min_row16(red_f[0][w]), mx = dpp_max_row16(red_f[1][w]);
     }
+    if constexpr (MAPPED) gather(); // the computed channels' values are there now
     const int32_t qmax = (1 << a.bits) - 1;
     const float range = mx - mn, alpha = range > 0.0f ? range / (float)qmax : 1.0f, inv = 1.0f / alpha;
     const bool fast = fabsf(mn * inv) < FAST_LIMIT && fabsf(mx * inv) < FAST_LIMIT;
@@ -259,30 +273,35 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
         const int g = tid + it * THREADS, n = there(it, a.K);
         if (g >= a.groups) continue;
         const uint32_t live = n >= GROUP ? 0xffu : n > 0 ? (1u << n) - 1u : 0u;
-        uint32_t c[GROUP];
-        const uint32_t bias = clamp_codes(v[it], qmax, fast, inv, beta, c);
-        if (a.values) {
+        float inv_of = inv;
+        int32_t beta_of = beta;
+        if (!fast) { // rare: the codes one by one, to be packed as values that are codes already
+#pragma unroll
+            for (int j = 0; j < GROUP; ++j) {
+                const uint32_t code = slow_code(v[it][j], inv, beta, qmax);
+                if (a.values && j < n) put_out(a.values, row * a.ldv + (int64_t)g * GROUP + j, a.o_bf16, (float)((double)alpha * ((double)code - (double)beta)));
+                v[it][j] = (float)code;
+            }
+            inv_of = 1.0f, beta_of = 0;
+        } else if (a.values) {
+            // a code is clamped as a float in [2^23, 2^24); what is left of it without 1.5 * 2^23 is code - beta
+            const float lowest = __int_as_float(MAGIC_BITS - beta), highest = __int_as_float(MAGIC_BITS - beta + qmax);
             float stands[GROUP];
 #pragma unroll
-            for (int j = 0; j < GROUP; ++j) // the float that a fast code is clamped as is 1.5 * 2^23 + code - beta
-                stands[j] = fast ? alpha * (__uint_as_float(c[j]) - MAGIC) : (float)((double)alpha * ((double)c[j] - (double)beta));
+            for (int j = 0; j < GROUP; ++j) stands[j] = alpha * (__builtin_amdgcn_fmed3f(__builtin_fmaf(v[it][j], inv, MAGIC), lowest, highest) - MAGIC);
             store_out(a.values, row * a.ldv + (int64_t)g * GROUP, a.o_bf16, stands, n);
         }
-        if (a.bits == 8) sum += put_codes<8>(to, g, c, bias, live);
-        else if (a.bits == 4) sum += put_codes<4>(to, g, c, bias, live);
-        else sum += put_codes<6>(to, g, c, bias, live);
+        if (a.bits == 8) sum += put_codes<8>(to, g, v[it], live, inv_of, beta_of);
+        else if (a.bits == 4) sum += put_codes<4>(to, g, v[it], live, inv_of, beta_of);
+        else sum += put_codes<6>(to, g, v[it], live, inv_of, beta_of);
     }
     sum = wave_sum_i32(sum);
-    if (WAVES > 1) {
-        if (lane == 0) red_i[wave] = sum;
-        __syncthreads();
-        sum = dpp_add_row16((lane & 15) < WAVES ? red_i[lane & 15] : 0);
+    if (lane == 0) {
+        // the wave that comes last has the row's sum: no barrier for it (below 2^23: 32768 codes of 8 bits)
+        const uint32_t before = WAVES > 1 ? atomicAdd(&arrived, (1u << 24) + (uint32_t)sum) : 0u;
+        if (before >> 24 == (uint32_t)(WAVES - 1)) a.rowsum[row] = (int32_t)((before + (uint32_t)sum) & 0xffffffu);
     }
-    if (tid == 0) {
-        a.alpha[row] = alpha;
-        a.zero[row] = beta;
-        a.rowsum[row] = sum;
-    }
+    if (tid == 0) a.alpha[row] = alpha, a.zero[row] = beta;
 }
 
 template <typename XT, typename RT, int ITERS, bool MAPPED>

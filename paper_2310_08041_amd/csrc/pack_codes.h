@@ -19,26 +19,23 @@ __device__ __noinline__ uint32_t slow_code(float x, float inv, int32_t beta, int
 // with lo = MAGIC_BITS - beta (one median-of-three) leaves lo + code.  The values are packed with
 // shift-and-add in wrapping 32-bit arithmetic and the common offset lo * (1 + 2^BITS + 2^(2 BITS) + ...)
 // is taken off once.  `live`: bit k clear forces code k to 0 (channels past the end of the row).
-// In two steps: the clamped bit patterns and what they have in common,
-__device__ __forceinline__ uint32_t clamp_codes(const float *val, int32_t qmax, int32_t fast, float inv, int32_t beta, uint32_t *c)
+template <int BITS>
+__device__ __forceinline__ void quant_pack(const float *val, uint32_t live, int32_t fast, float inv, int32_t beta,
+                                           uint32_t &w0, uint32_t &w1)
 {
+    constexpr int QMAX = (1 << BITS) - 1;
+    uint32_t c[GROUP], bias = 0;
     if (fast) {
         // floats in [2^23, 2^24) are integers and order like their bit patterns: clamp them as floats
-        const float lo = __int_as_float(MAGIC_BITS - beta), hi = __int_as_float(MAGIC_BITS - beta + qmax);
+        const float lo = __int_as_float(MAGIC_BITS - beta), hi = __int_as_float(MAGIC_BITS - beta + QMAX);
+        bias = (uint32_t)(MAGIC_BITS - beta);
 #pragma unroll
         for (int k = 0; k < GROUP; ++k)
             c[k] = __float_as_uint(__builtin_amdgcn_fmed3f(__builtin_fmaf(val[k], inv, MAGIC), lo, hi));
-        return (uint32_t)(MAGIC_BITS - beta);
-    }
+    } else {
 #pragma unroll
-    for (int k = 0; k < GROUP; ++k) c[k] = slow_code(val[k], inv, beta, qmax); // rare; kept out of line
-    return 0;
-}
-
-// and the packing of the codes c - bias.
-template <int BITS>
-__device__ __forceinline__ void pack_clamped(uint32_t *c, uint32_t bias, uint32_t live, uint32_t &w0, uint32_t &w1)
-{
+        for (int k = 0; k < GROUP; ++k) c[k] = slow_code(val[k], inv, beta, QMAX); // rare; kept out of line
+    }
     if (live != 0xffu) {
 #pragma unroll
         for (int k = 0; k < GROUP; ++k) c[k] = (live >> k & 1u) ? c[k] : bias;
@@ -70,15 +67,6 @@ __device__ __forceinline__ void pack_clamped(uint32_t *c, uint32_t bias, uint32_
         w0 = h0 | (h1 << 24);
         w1 = h1 >> 8;
     }
-}
-
-template <int BITS>
-__device__ __forceinline__ void quant_pack(const float *val, uint32_t live, int32_t fast, float inv, int32_t beta,
-                                           uint32_t &w0, uint32_t &w1)
-{
-    uint32_t c[GROUP];
-    const uint32_t bias = clamp_codes(val, (1 << BITS) - 1, fast, inv, beta, c);
-    pack_clamped<BITS>(c, bias, live, w0, w1);
 }
 
 // Sum of the 8 codes of a packed group.
