@@ -120,9 +120,12 @@ struct ApplyArgs {
     const int32_t *ranks, *plan;
     float *h; // [slices][rows in the order of the tiles][parts * rank]
     int32_t rows, n_adapters, most, rank, wide, slices, blocks_per_slice; // most: tiles; wide: parts * rank; blocks of 64 channels
+    QuotientBy by_rank, by_cells, by_slices, by_blocks; // the last two: m 0 where a launch is too large for the multiplication
     bool stream; // y and out past the caches, which B and h need
     int32_t n_parts, part_end[QLLM_ADAPTER_PARTS], columns, block_end[QLLM_ADAPTER_PARTS]; // columns, of a block, blocks, summed up
 };
+
+__device__ __forceinline__ uint32_t divide(uint32_t x, const QuotientBy &by) { return by.m || by.d == 1u ? by.divide(x) : x / by.d; }
 
 struct Tile {
     int32_t adapter, first, count, rank; // count 0: none
@@ -169,7 +172,7 @@ __device__ __forceinline__ void down_tile(const ApplyArgs &a, const Tile &tile, 
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int at = min(first_rank + n * 16 + r16, a.wide - 1), p = at / a.rank, r = min(at - p * a.rank, tile.rank - 1);
+        const int at = min(first_rank + n * 16 + r16, a.wide - 1), p = (int)a.by_rank.divide((uint32_t)at), r = min(at - p * a.rank, tile.rank - 1);
         w[n] = static_cast<const WT *>(a.A) + ((int64_t)tile.adapter * a.wide + p * a.rank + r) * a.C + 8 * quarter;
     }
     f32x4 acc[MT][NT];
@@ -249,8 +252,9 @@ template <typename XT, typename WT, int NT>
 __global__ __launch_bounds__(256, 2) void down_kernel(const ApplyArgs a)
 {
     __shared__ __align__(16) float part[4 * TILE * NT * 16];
-    const int slice = (int)(blockIdx.x % (uint32_t)a.slices);
-    const Tile tile = tile_of(a, blockIdx.x / (uint32_t)a.slices);
+    const uint32_t t = divide(blockIdx.x, a.by_slices);
+    const int slice = (int)(blockIdx.x - t * a.by_slices.d);
+    const Tile tile = tile_of(a, t);
     if (tile.count == 0 || tile.rank == 0) return;
     const int first_rank = blockIdx.y * NT * 16;
     if (tile.count <= 16) down_tile<XT, WT, 1, NT>(a, tile, slice, first_rank, part);
@@ -434,7 +438,7 @@ __device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, in
         const int cells = padded / 4, all = tile.count * cells; // of 4 ranks, a row
         const float *h = a.h + (int64_t)tile.first * a.wide + p * a.rank;
         auto stage = [&](int i, f32x4 s) {
-            const int row = i / cells, r = 4 * (i - row * cells);
+            const int row = (int)a.by_cells.divide((uint32_t)i), r = 4 * (i - row * cells);
 #pragma unroll
             for (int j = 0; j < 4; ++j) s[j] = r + j < tile.rank ? s[j] * scale : 0.0f;
             if constexpr (HALF) {
@@ -451,8 +455,8 @@ __device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, in
             }
         };
         auto cell = [&](int i) { // any i: that of a rank or row past the end is read at another place
-            const int row = min(i / cells, tile.count - 1), r = min(4 * (i % cells), a.rank - 4);
-            return h + row * a.wide + r;
+            const int row = (int)a.by_cells.divide((uint32_t)i);
+            return h + min(row, tile.count - 1) * a.wide + min(4 * (i - row * cells), a.rank - 4);
         };
         if (a.slices > 1) {
             for (int i0 = 0; i0 < all; i0 += 256 / JOINERS) {
@@ -531,8 +535,9 @@ template <typename WT, typename YT>
 __global__ __launch_bounds__(256, 2) void up_kernel(const ApplyArgs a)
 {
     extern __shared__ __align__(16) uint8_t staged[];
-    const int blocks = a.block_end[a.n_parts - 1], block = (int)(blockIdx.x % (uint32_t)blocks);
-    const Tile tile = tile_of(a, blockIdx.x / (uint32_t)blocks);
+    const uint32_t t = divide(blockIdx.x, a.by_blocks);
+    const int block = (int)(blockIdx.x - t * a.by_blocks.d);
+    const Tile tile = tile_of(a, t);
     if (tile.count == 0 || (tile.rank == 0 && a.out == a.y)) return;
     int p = 0, b = block, from = 0;
     for (int k = 0; k + 1 < QLLM_ADAPTER_PARTS; ++k)
@@ -704,6 +709,14 @@ extern "C" int32_t qllm_adapter_apply(const void *x, int32_t x_dtype, int64_t ld
     for (int p = 0; p + 1 < w->n_parts; ++p) a.stream = a.stream && a.part_end[p] * ys % 128 == 0;
     const int64_t tiles = most_tiles(rows, w->n_adapters);
     if (tiles * a.block_end[a.n_parts - 1] > INT32_MAX) return QLLM_ERR_SHAPE;
+    auto by = [](int64_t d, int64_t most) { // of numbers up to `most`
+        QuotientBy q = quotient_by((uint32_t)d);
+        if (most * d >= (1ll << 32)) q.m = 0;
+        return q;
+    };
+    const int32_t step = w->w_dtype == QLLM_BF16 ? STEP<uint16_t> : STEP<float>;
+    a.by_rank = quotient_by((uint32_t)w->rank), a.by_cells = quotient_by((uint32_t)((w->rank + step - 1) / step * step / 4));
+    a.by_slices = by(a.slices, tiles * a.slices), a.by_blocks = by(a.block_end[a.n_parts - 1], tiles * a.block_end[a.n_parts - 1]);
     hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
     (void)hipGetLastError();
     const bool xb = x_dtype == QLLM_BF16, wb = w->w_dtype == QLLM_BF16, yb = y_dtype == QLLM_BF16;
