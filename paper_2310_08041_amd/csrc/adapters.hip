@@ -593,17 +593,21 @@ void slices_of(const qllm_adapters *w, int64_t rows, int32_t *slices, int32_t *b
     *slices = (int32_t)((turns + each - 1) / each);
 }
 
-// Columns of a workgroup of the second product: the multiple of 256 with the least work in a row, in rounds of two workgroups a CU, each
-// as long as its columns and about 300 more (the trips to the plan, to h, to the first y).  Up to 512 rows are taken for single tokens of
-// many requests, with as many tiles as there are halfway between the fewest and the most.
+// Columns of a workgroup of the second product: the multiple of 256 with the least work in a row, in rounds of three workgroups a CU (two are
+// resident, and as they end at different times a round half as large again costs no more), each as long as its columns and about 300 more
+// (the trips to the plan, to h, to the first y).  1700 rows x 4999 fp32 256 columns 20.9 us, 512 23.8; 4400 x 27648 bf16 256 columns
+// 137, 1280 or 2048 120, 4096 156.  Up to 512 rows are taken for single tokens of many requests, whose workgroups are alike: rounds of two a
+// CU, with as many tiles as there are halfway between the fewest and the most (256 rows on 12 adapters, 12288 columns, 512 columns 9.9 us,
+// 256 11.3).
 int32_t columns_of(const qllm_adapters *w, int64_t rows)
 {
     const int64_t fewest = fewest_tiles(rows), tiles = rows <= 512 ? (fewest + most_tiles(rows, w->n_adapters)) / 2 : fewest;
+    const int64_t slots = rows <= 512 ? 512 : 768;
     int64_t best = 256, least = INT64_MAX;
     for (int64_t columns = 256; columns <= 2048; columns += 256) {
         int64_t blocks = 0;
         for (int p = 0; p < w->n_parts; ++p) blocks += (w->part_O[p] + columns - 1) / columns;
-        const int64_t cost = (tiles * blocks + 511) / 512 * (columns + 300);
+        const int64_t cost = (tiles * blocks + slots - 1) / slots * (columns + 300);
         if (cost < least) least = cost, best = columns;
     }
     return (int32_t)best;
