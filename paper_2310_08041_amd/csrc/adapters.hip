@@ -262,8 +262,8 @@ __global__ __launch_bounds__(256, 2) void down_kernel(const ApplyArgs a)
 }
 
 // ---- the slices' sums: JOINERS neighbouring lanes add up every JOINERS-th slice each, then theirs are added
-constexpr int JOINERS = 8, JOINED = 32;
-__device__ __forceinline__ f32x4 joined(const float *h, int64_t stride, int slices, int joiner)
+constexpr int JOINERS = 8, JOINED = 32, JOINED_CELLS = 1024;
+__device__ __forceinline__ f32x4 slices_of_lane(const float *h, int64_t stride, int slices, int joiner)
 {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int k0 = joiner; k0 < slices; k0 += 4 * JOINERS) { // four loads in flight; what is past the last slice is read from it, and dropped
@@ -274,6 +274,10 @@ __device__ __forceinline__ f32x4 joined(const float *h, int64_t stride, int slic
         for (int u = 0; u < 4; ++u)
             if (k0 + u * JOINERS < slices) s += v[u];
     }
+    return s;
+}
+__device__ __forceinline__ f32x4 over_joiners(f32x4 s)
+{
 #pragma unroll
     for (int d = 1; d < JOINERS; d <<= 1) {
         f32x4 o;
@@ -287,7 +291,7 @@ __device__ __forceinline__ f32x4 joined(const float *h, int64_t stride, int slic
 __global__ __launch_bounds__(256) void join_kernel(float *h, int64_t words4, int32_t slices)
 {
     const int64_t i = (int64_t)blockIdx.x * (256 / JOINERS) + threadIdx.x / JOINERS, at = i < words4 ? i : words4 - 1;
-    const f32x4 s = joined(h + 4 * at, 4 * words4, slices, threadIdx.x % JOINERS);
+    const f32x4 s = over_joiners(slices_of_lane(h + 4 * at, 4 * words4, slices, threadIdx.x % JOINERS));
     if (i < words4 && threadIdx.x % JOINERS == 0) reinterpret_cast<f32x4 *>(h)[at] = s;
 }
 
@@ -459,10 +463,16 @@ __device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, in
             return h + min(row, tile.count - 1) * a.wide + min(4 * (i - row * cells), a.rank - 4);
         };
         if (a.slices > 1) {
-            for (int i0 = 0; i0 < all; i0 += 256 / JOINERS) {
-                const int i = i0 + tid / JOINERS;
-                const f32x4 s = joined(cell(i), (int64_t)a.rows * a.wide, a.slices, tid % JOINERS);
-                if (i < all && tid % JOINERS == 0) stage(i, s);
+            constexpr int AT_ONCE = 4; // trips to h in flight
+            for (int i0 = tid / JOINERS; i0 < all; i0 += AT_ONCE * (256 / JOINERS)) {
+                f32x4 s[AT_ONCE];
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) s[k] = slices_of_lane(cell(i0 + k * (256 / JOINERS)), (int64_t)a.rows * a.wide, a.slices, tid % JOINERS);
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) {
+                    s[k] = over_joiners(s[k]);
+                    if (i0 + k * (256 / JOINERS) < all && tid % JOINERS == 0) stage(i0 + k * (256 / JOINERS), s[k]);
+                }
             }
         } else {
             for (int i0 = tid; i0 < all; i0 += 256 * 4) {
@@ -727,7 +737,7 @@ extern "C" int32_t qllm_adapter_apply(const void *x, int32_t x_dtype, int64_t ld
     if (wb) xb ? run_down<uint16_t, uint16_t>(a, (unsigned)tiles, stream) : run_down<float, uint16_t>(a, (unsigned)tiles, stream);
     else xb ? run_down<uint16_t, float>(a, (unsigned)tiles, stream) : run_down<float, float>(a, (unsigned)tiles, stream);
     if (const int32_t e = launched("adapters, first product: launch")) return e;
-    if (a.slices > 1 && (rows > TILE || a.slices > JOINED)) {
+    if (a.slices > 1 && (a.slices > JOINED || rows * w->rank > JOINED_CELLS)) {
         const int64_t words4 = rows * a.wide / 4;
         hipLaunchKernelGGL(join_kernel, dim3((unsigned)((words4 * JOINERS + 255) / 256)), dim3(256), 0, stream, a.h, words4, a.slices);
         if (const int32_t e = launched("adapters, sums: launch")) return e;
