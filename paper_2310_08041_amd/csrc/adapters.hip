@@ -262,7 +262,7 @@ __global__ __launch_bounds__(256, 2) void down_kernel(const ApplyArgs a)
 }
 
 // ---- the slices' sums: JOINERS neighbouring lanes add up every JOINERS-th slice each, then theirs are added
-constexpr int JOINERS = 8, JOINED = 32, JOINED_CELLS = 1024;
+constexpr int JOINERS = 8, JOINED = 32, JOINED_ROWS = 16, JOINED_RANKS = 1024;
 __device__ __forceinline__ f32x4 slices_of_lane(const float *h, int64_t stride, int slices, int joiner)
 {
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -421,15 +421,19 @@ __device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, in
         }
     };
     Four<YT, STREAM> ye[MT][4];
-    u32x4 b[2][4];
+    // steps of B asked for with the columns: for prompts one, whose registers count more (5120 -> 27648 109 us, two 120, three 121), for single
+    // tokens two (16 adapters of up to 64 ranks 8.5, one 9.6)
+    constexpr int AHEAD = MT == 1 ? 2 : 1;
+    u32x4 b[AHEAD][4];
     auto request = [&](int at) {
         const int left = WHOLE ? 64 : end - column - at - 4 * r16;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int i = 0; i < 4; ++i) ye[m][i].load(y[m][i] + at, left);
-        if (steps > 0) load_b(b[0], at, 0);
-        if (steps > 1) load_b(b[1], at, 1);
+#pragma unroll
+        for (int step = 0; step < AHEAD; ++step)
+            if (step < steps) load_b(b[step], at, step);
     };
     const int width = end - column;
     int at = 64 * (wave / sharers);
@@ -489,10 +493,11 @@ __device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, in
     const WT *mine = reinterpret_cast<const WT *>(staged) + (first + r16) * stride + quarter * (S / 4);
     for (; at < width; at += 64 * turns) {
         Four<YT, STREAM> yn[MT][4];
-        u32x4 bn[2][4];
+        u32x4 bn[AHEAD][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            bn[0][i] = b[0][i], bn[1][i] = b[1][i];
+#pragma unroll
+            for (int step = 0; step < AHEAD; ++step) bn[step][i] = b[step][i];
 #pragma unroll
             for (int m = 0; m < MT; ++m) yn[m][i] = ye[m][i];
         }
@@ -505,8 +510,12 @@ __device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, in
         for (int step = 0; step < steps; ++step) {
             u32x4 now[4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) now[t] = bn[0][t], bn[0][t] = bn[1][t];
-            if (step + 2 < steps) load_b(bn[1], at, step + 2);
+            for (int t = 0; t < 4; ++t) {
+                now[t] = bn[0][t];
+#pragma unroll
+                for (int k = 1; k < AHEAD; ++k) bn[k - 1][t] = bn[k][t];
+            }
+            if (step + AHEAD < steps) load_b(bn[AHEAD - 1], at, step + AHEAD);
             mask_b(now, step);
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
@@ -737,7 +746,7 @@ extern "C" int32_t qllm_adapter_apply(const void *x, int32_t x_dtype, int64_t ld
     if (wb) xb ? run_down<uint16_t, uint16_t>(a, (unsigned)tiles, stream) : run_down<float, uint16_t>(a, (unsigned)tiles, stream);
     else xb ? run_down<uint16_t, float>(a, (unsigned)tiles, stream) : run_down<float, float>(a, (unsigned)tiles, stream);
     if (const int32_t e = launched("adapters, first product: launch")) return e;
-    if (a.slices > 1 && (a.slices > JOINED || rows * w->rank > JOINED_CELLS)) {
+    if (a.slices > 1 && (a.slices > JOINED || rows > JOINED_ROWS || rows * w->rank > JOINED_RANKS)) {
         const int64_t words4 = rows * a.wide / 4;
         hipLaunchKernelGGL(join_kernel, dim3((unsigned)((words4 * JOINERS + 255) / 256)), dim3(256), 0, stream, a.h, words4, a.slices);
         if (const int32_t e = launched("adapters, sums: launch")) return e;
