@@ -1079,6 +1079,8 @@ def qllm_add_norm_quant(x, residual, sum_out, norm, gamma, beta, eps, out=None, 
         _check_tensor(beta, "beta", _F32_ONLY, numel=Cc, optional=True)
     _check_here("residual x sum_out gamma beta y_out values_out index codes", residual, x, sum_out, gamma, beta, y_out, values_out,
                 None if gather is None else gather._index, None if out is None else out.codes)
+    if N == 0:                                         # no rows: nothing to point at
+        return
     o = y_out if y_out is not None else values_out
     _chk(_lib.qllm_add_norm_quant(None if x is None else x.data_ptr(), F32 if x is None else _x_dtype(x), ldx, residual.data_ptr(), _x_dtype(residual),
                                   ldr, N, Cc, None if sum_out is None else sum_out.data_ptr(), lds, norm, None if gamma is None else gamma.data_ptr(),

@@ -471,11 +471,13 @@ __device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, in
             for (int i0 = tid / JOINERS; i0 < all; i0 += AT_ONCE * (256 / JOINERS)) {
                 f32x4 s[AT_ONCE];
 #pragma unroll
-                for (int k = 0; k < AT_ONCE; ++k) s[k] = slices_of_lane(cell(i0 + k * (256 / JOINERS)), (int64_t)a.rows * a.wide, a.slices, tid % JOINERS);
+                for (int k = 0; k < AT_ONCE; ++k)
+                    if (k == 0 || i0 + k * (256 / JOINERS) < all) s[k] = slices_of_lane(cell(i0 + k * (256 / JOINERS)), (int64_t)a.rows * a.wide, a.slices, tid % JOINERS);
 #pragma unroll
                 for (int k = 0; k < AT_ONCE; ++k) {
+                    if (k > 0 && i0 + k * (256 / JOINERS) >= all) continue; // the same for a cell's eight lanes
                     s[k] = over_joiners(s[k]);
-                    if (i0 + k * (256 / JOINERS) < all && tid % JOINERS == 0) stage(i0 + k * (256 / JOINERS), s[k]);
+                    if (tid % JOINERS == 0) stage(i0 + k * (256 / JOINERS), s[k]);
                 }
             }
         } else {

@@ -231,6 +231,83 @@ def test_norm_many_rows():
         assert torch.equal(one.codes[0], q.codes[i]) and torch.equal(t[0], s[i]) and one.scale[0] == q.scale[i] and one.rowsum[0] == q.rowsum[i]
 
 
+@gpu
+def test_norm_as_many_computed_channels_as_fit():
+    """The widest row with as many computed channels as there is room for on chip, some of many entries."""
+    b = binding()
+    c, computed = 32768, 7680
+    rng = np.random.default_rng(9)
+    count = np.ones(computed, np.int64)
+    count[::7], count[5] = 3, 300
+    row_ptr = np.concatenate([[0], np.cumsum(count)]).astype(np.int32)
+    src, scale = rng.integers(0, c, row_ptr[-1]).astype(np.int32), rng.uniform(-1, 1, row_ptr[-1]).astype(np.float32)
+    r = draw(rng, 3, c, BF16)
+    e = expected(None, r, BF16, "rms", np.ones(c, np.float32), None, 1e-5, (row_ptr, src, scale), 8)
+    q = b.DeviceQAct(3, computed, 8)
+    b.qllm_add_norm_quant(None, torch.from_numpy(r).cuda().bfloat16(), None, 2, torch.ones(c, device="cuda"), None, 1e-5, q, 8,
+                          gather=b.DeviceGather(row_ptr, src, scale, c))
+    assert np.array_equal(q.codes.cpu().numpy()[:, :computed], e["codes"]) and np.array_equal(q.rowsum.cpu().numpy(), e["rowsum"])
+
+
+@gpu
+def test_norm_no_rows():
+    b = binding()
+    r = torch.empty((0, 64), device="cuda")
+    b.qllm_add_norm_quant(r, r, r, 2, torch.ones(64, device="cuda"), None, 1e-5, b.DeviceQAct(0, 64, 8), 8, y_out=r)
+
+
+FAR = (1 << 31) + 8                                # a row stride whose second row lies past 2^32 bytes of bf16
+
+
+def far_rows(c, seed):
+    """Two rows of c bf16 channels, FAR elements apart."""
+    t = torch.empty(FAR + c + 8, dtype=BF16, device="cuda").as_strided((2, c), (FAR, 1))
+    return t.copy_(torch.randn((2, c), generator=torch.Generator().manual_seed(seed)))
+
+
+@gpu
+def test_norm_rows_far_apart():
+    b = binding()
+    c = 1000
+    x, r = far_rows(c, 1), far_rows(c, 2)
+    g = torch.ones(c, device="cuda")
+    q, q2, near = b.DeviceQAct(2, c, 4), b.DeviceQAct(2, c, 4), r.contiguous()
+    y = far_rows(c, 3)
+    b.qllm_add_norm_quant(x.contiguous(), near, near, 2, g, None, 1e-5, q2, 4)
+    b.qllm_add_norm_quant(x, r, r, 2, g, None, 1e-5, q, 4, y_out=y)
+    assert torch.equal(q.codes, q2.codes) and torch.equal(r, near) and torch.equal(q.scale, q2.scale)
+    assert torch.isfinite(y.float()).all()
+
+
+@gpu
+def test_norm_on_two_streams_at_once():
+    """Nothing is shared between calls: the same bits beside another call on another stream."""
+    b = binding()
+    n, c = 900, 2048
+    rng = np.random.default_rng(4)
+    csr = random_csr_map(rng, c, 2040, 9)
+    gather, g = b.DeviceGather(*csr, c), torch.ones(c, device="cuda")
+    sets = []
+    for k in range(2):
+        x, r = (torch.randn(n, c, device="cuda").bfloat16() for _ in range(2))
+        sets.append((x, r, torch.empty_like(r), b.DeviceQAct(n, 2040, 6)))
+    want = []
+    for x, r, s, q in sets:
+        b.qllm_add_norm_quant(x, r, s, 2, g, None, 1e-5, q, 6, gather=gather)
+        torch.cuda.synchronize()
+        want.append((s.clone(), q.codes.clone(), q.rowsum.clone()))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for (x, r, s, q), st in zip(sets, streams):
+            s.zero_(), q.codes.zero_(), q.rowsum.zero_()
+        torch.cuda.synchronize()
+        for (x, r, s, q), st in zip(sets, streams):
+            b.qllm_add_norm_quant(x, r, s, 2, g, None, 1e-5, q, 6, gather=gather, stream=st)
+        torch.cuda.synchronize()
+        for (x, r, s, q), w in zip(sets, want):
+            assert torch.equal(s, w[0]) and torch.equal(q.codes, w[1]) and torch.equal(q.rowsum, w[2])
+
+
 # ---------------------------------------------------------------- adapters
 
 U = 2.0 ** -24
@@ -457,6 +534,80 @@ def test_adapter_many_sequences_and_adapters():
 def test_adapter_long_inputs():
     check_adapters(news=[1, 2, 40], names=[0, 1, 1], n_adapters=2, rank=64, c=28672, parts=[64])
     check_adapters(news=[130], names=[1], n_adapters=2, rank=16, c=13824, parts=[40], xd=F32, wd=F32, yd=F32)
+
+
+@gpu
+def test_adapter_largest_pool():
+    check_adapters(news=[1] * 40, names=[(i * 997) % 8192 for i in range(39)] + [8191], n_adapters=8192, rank=8, c=24, parts=[16], single=True)
+
+
+@gpu
+def test_adapter_many_rows():
+    check_adapters(news=[30000, 1, 0, 9000], names=[1, 0, 0, -1], n_adapters=2, rank=8, c=40, parts=[24], tail=3)
+
+
+@gpu
+def test_adapter_rows_far_apart():
+    b = binding()
+    s = make_adapters(news=[1, 1], names=[1, 0], n_adapters=2, rank=16, c=300, parts=[200])
+    near, (ad, plan, ws) = apply(s)
+    x, y, out = far_rows(300, 1), far_rows(200, 2), far_rows(200, 3)
+    x.copy_(s["x"]), y.copy_(s["y"])
+    b.qllm_adapter_apply(x, ad, plan, y, out, ws)
+    assert torch.equal(out, near)
+    b.qllm_adapter_apply(x, ad, plan, y, y, ws)
+    assert torch.equal(y, near)
+
+
+@gpu
+def test_adapter_on_two_streams_at_once():
+    """One plan and one pool, a workspace each."""
+    b = binding()
+    s = make_adapters(news=[40, 3, 90], names=[0, 1, 2], n_adapters=3, rank=32, c=2000, parts=[500, 300], yd=F32)
+    want, (ad, plan, ws) = apply(s)
+    sets = [(torch.cuda.Stream(), torch.empty_like(ws), torch.empty_like(want)) for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for st, w, out in sets:
+            b.qllm_adapter_apply(s["x"], ad, plan, s["y"], out, w, stream=st)
+        torch.cuda.synchronize()
+        for _, _, out in sets:
+            assert torch.equal(out, want)
+            out.zero_()
+        torch.cuda.synchronize()
+
+
+@gpu
+def test_adapter_another_batch_in_a_captured_step():
+    """A graph of the plan and the call serves whatever the arrays hold at the replay."""
+    b = binding()
+    s = make_adapters(news=[1] * 30, names=[0] * 30, n_adapters=4, rank=16, c=256, parts=[128], yd=F32)
+    ad = b.DeviceAdapters(s["A"], s["B"], s["scale"], None, s["parts"])
+    plan, out = b.DeviceAdapterPlan(30, 4), torch.empty_like(s["y"])
+    ws = torch.empty(b.qllm_adapter_workspace_bytes(ad, 30), dtype=torch.uint8, device="cuda")
+
+    def step():
+        b.qllm_adapter_plan(plan, s["adapter"])
+        b.qllm_adapter_apply(s["x"], ad, plan, s["y"], out, ws)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(4):
+        names = [(i * (k + 3) + k) % 6 - 1 for i in range(30)]
+        s["adapter"].copy_(torch.tensor(names, dtype=torch.int32))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        want, bound = adapters_reference(s, [(slice(i, i + 1), a) for i, a in enumerate(names)])
+        assert (np.abs(got.double().cpu().numpy() - want) <= bound).all()
+        out.zero_()
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(out, got)
 
 
 # ---------------------------------------------------------------- together
