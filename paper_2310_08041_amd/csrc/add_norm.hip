@@ -84,7 +84,7 @@ __device__ __forceinline__ double over_waves(double v, double *slots, int waves)
     return dpp_addd_row16((lane & 15) < waves ? slots[lane & 15] : 0.0);
 }
 
-// WHOLE: every chunk of 8 channels, in and out, is in the row as a whole or not at all.
+// WHOLE: every chunk of 8 input channels is in the row as a whole or not at all.
 template <typename XT, typename RT, int ITERS, bool MAPPED, bool WHOLE>
 __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs a)
 {
@@ -95,9 +95,10 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
     const int THREADS = blockDim.x, WAVES = THREADS >> 6;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int64_t row = blockIdx.x;
-    // elements of chunk `it` of the lane that are there, in a row of n
-    auto there = [&](int it, int n) {
-        const int left = n - (tid + it * THREADS) * GROUP;
+    // elements of chunk `it` of the lane that are there, of a row of n and of the row that came
+    auto left_of = [&](int it, int n) { return n - (tid + it * THREADS) * GROUP; };
+    auto there = [&](int it) {
+        const int left = left_of(it, a.C);
         return WHOLE ? (left > 0 ? GROUP : 0) : left;
     };
 
@@ -111,8 +112,8 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
             const int c0 = (tid + it * THREADS) * GROUP;
-            re[it].load(r + c0, there(it, a.C));
-            if (a.x) xe[it].load(x + c0, there(it, a.C));
+            re[it].load(r + c0, there(it));
+            if (a.x) xe[it].load(x + c0, there(it));
         }
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
 #pragma unroll
                 for (int j = 0; j < GROUP; ++j) v[it][j] += u[j];
                 re[it].round(v[it]);
-                if (a.sum) re[it].template store<(ITERS > 1)>(static_cast<RT *>(a.sum) + row * a.lds + c0, there(it, a.C)); // not read soon: past the caches
+                if (a.sum) re[it].template store<(ITERS > 1)>(static_cast<RT *>(a.sum) + row * a.lds + c0, there(it)); // not read soon: past the caches
                 re[it].widen(v[it]);
             }
         }
@@ -138,7 +139,7 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
             const int c0 = (tid + it * THREADS) * GROUP;
-            gamma[it].load(a.gamma + c0, there(it, a.C));
+            gamma[it].load(a.gamma + c0, there(it));
         }
     }
     if constexpr (MAPPED) {
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
 #pragma unroll
             for (int j = 0; j < GROUP; ++j) {
                 const double d = (double)v[it][j] - mean;
-                if (j < there(it, a.C)) q = __builtin_fma(d, d, q);
+                if (j < there(it)) q = __builtin_fma(d, d, q);
             }
         rstd = rsqrt_to_f32(over_waves(q, red_d[1], WAVES) * a.inv_C + a.eps);
         mu = (float)mean;
@@ -188,13 +189,13 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
             }
             if (a.norm == QLLM_NORM_LAYER && a.beta) {
                 Eight<float> e;
-                e.load(a.beta + c0, there(it, a.C));
+                e.load(a.beta + c0, there(it));
                 e.widen(g);
 #pragma unroll
                 for (int j = 0; j < GROUP; ++j) v[it][j] += g[j];
             }
         }
-        if (a.y) store_out(a.y, row * a.ldy + c0, a.o_bf16, v[it], there(it, a.C));
+        if (a.y) store_out(a.y, row * a.ldy + c0, a.o_bf16, v[it], there(it));
         if constexpr (MAPPED) {
             if (c0 < a.C)
 #pragma unroll
@@ -238,14 +239,14 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
     // ---- Eq. (2)
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
-        const int n = there(it, a.K);
+        const int n = left_of(it, a.K);
         if (n >= GROUP) {
 #pragma unroll
             for (int j = 0; j < GROUP; j += 2) { // three operands an instruction
                 mn = fminf(fminf(mn, v[it][j]), v[it][j + 1]);
                 mx = fmaxf(fmaxf(mx, v[it][j]), v[it][j + 1]);
             }
-        } else if (!WHOLE && n > 0) {
+        } else if (n > 0) {
 #pragma unroll
             for (int j = 0; j < GROUP - 1; ++j)
                 if (j < n) mn = fminf(mn, v[it][j]), mx = fmaxf(mx, v[it][j]);
@@ -270,7 +271,7 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
     int32_t sum = 0;
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
-        const int g = tid + it * THREADS, n = there(it, a.K);
+        const int g = tid + it * THREADS, n = left_of(it, a.K);
         if (g >= a.groups) continue;
         const uint32_t live = n >= GROUP ? 0xffu : n > 0 ? (1u << n) - 1u : 0u;
         float inv_of = inv;
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
 template <typename XT, typename RT, int ITERS, bool MAPPED>
 int32_t launch(const AddNormArgs &a, int units, hipStream_t stream)
 {
-    auto *kernel = a.C % GROUP == 0 && a.K % GROUP == 0 ? add_norm_kernel<XT, RT, ITERS, MAPPED, true> : add_norm_kernel<XT, RT, ITERS, MAPPED, false>;
+    auto *kernel = a.C % GROUP == 0 ? add_norm_kernel<XT, RT, ITERS, MAPPED, true> : add_norm_kernel<XT, RT, ITERS, MAPPED, false>;
     const size_t lds = MAPPED ? (size_t)(GROUP * a.S + a.n_computed) * sizeof(float) : 0;
     if (lds > 48 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
