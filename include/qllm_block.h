@@ -33,9 +33,10 @@ typedef struct {
 /* HOST pointers.  Call once with index == NULL to get *index_len (int32 words) and *n_computed, then with index pointing at that
  * many words.  Input channel c has place (c mod 8) S + c / 8 with S = ceil(C_in / 8), the j-th computed channel 8 S + j.  Layout:
  *   places    for the output channels up to the next multiple of QLLM_K_PAD, two 16-bit numbers a word, the lower first (past C_out: 0)
- *   computed  [n_computed][4]: {place | place << 16, scale, scale, -} of the first two entries (one entry: a second of scale 0), and
- *             where in `more` the others are (0: there are none)
- *   more      pairs of words: {n, 0}, then n entries {place, scale}; pair 0 is no row's
+ *   computed  [n_computed][8]: {place | place << 16, place | place << 16, scale, scale, scale, scale, m, 0} of the first four entries
+ *             (one that is not there: the first one's place, scale 0); m: 0 for up to two entries, 1 for up to four, else where in
+ *             `more` the others are
+ *   more      pairs of words: {n, 0}, then n entries {place, scale}; pairs 0 and 1 are no row's
  * Errors: NULL, SHAPE (also more places than QLLM_GATHER_PLACES), MAP. */
 int32_t qllm_gather_map_host(const int32_t *row_ptr, const int32_t *src, const float *scale, int64_t C_in, int64_t C_out,
                              int32_t *index, int64_t *index_len, int64_t *n_computed);

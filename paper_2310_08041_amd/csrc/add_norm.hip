@@ -26,6 +26,13 @@ namespace {
 constexpr int MOST_LANES = 1024;
 constexpr int MANY_ROWS = 512;
 
+// see qllm_gather_map_host
+struct alignas(16) Computed {
+    uint32_t place01, place23;
+    float scale[4];
+    int32_t more, none;
+};
+
 struct AddNormArgs {
     const void *x, *residual;
     void *sum, *y, *values;
@@ -34,7 +41,7 @@ struct AddNormArgs {
     int32_t N, C, norm, o_bf16;
     double eps, inv_C;
     const uint32_t *places; // of 8 output channels: 4 words
-    const uint4 *computed;  // see qllm_gather_map_host
+    const Computed *computed;
     const int2 *more;
     int32_t n_computed, S, K, groups; // groups of 8 codes in a row, padding included
     uint8_t *codes;
@@ -134,7 +141,7 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
     // what depends on the map and on gamma alone is asked for while the statistics are on their way
     Eight<float> gamma[ITERS];
     uint4 place[MAPPED ? ITERS : 1];
-    uint4 computed = make_uint4(0, 0, 0, 0); // the first that falls to the lane
+    Computed computed = {}; // the first that falls to the lane
     if (a.norm != QLLM_NORM_NONE) {
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
@@ -143,6 +150,8 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
         }
     }
     if constexpr (MAPPED) {
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it) place[it] = reinterpret_cast<const uint4 *>(a.places)[min(tid + it * THREADS, a.groups - 1)];
         if (tid < a.n_computed) computed = a.computed[tid];
     }
 
@@ -217,18 +226,20 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
         }
     };
     if constexpr (MAPPED) {
-#pragma unroll
-        for (int it = 0; it < ITERS; ++it) place[it] = reinterpret_cast<const uint4 *>(a.places)[min(tid + it * THREADS, a.groups - 1)];
         for (int j = tid; j < a.n_computed; j += THREADS) places[GROUP * a.S + j] = __builtin_nanf("");
         __syncthreads();
         for (int j = tid; j < a.n_computed; j += THREADS) {
             if (j != tid) computed = a.computed[j];
-            float sum = __uint_as_float(computed.y) * places[computed.x & 0xffffu];
-            sum = sum + __uint_as_float(computed.z) * places[computed.x >> 16];
-            if (computed.w != 0u) { // entries beyond the second
-                const int2 *more = a.more + computed.w;
-                const int count = more[0].x;
-                for (int k = 1; k <= count; ++k) sum = sum + __int_as_float(more[k].y) * places[more[k].x];
+            float sum = computed.scale[0] * places[computed.place01 & 0xffffu];
+            sum = sum + computed.scale[1] * places[computed.place01 >> 16];
+            if (computed.more) { // entries beyond the second
+                sum = sum + computed.scale[2] * places[computed.place23 & 0xffffu];
+                sum = sum + computed.scale[3] * places[computed.place23 >> 16];
+                if (computed.more > 1) { // beyond the fourth
+                    const int2 *more = a.more + computed.more;
+                    const int count = more[0].x;
+                    for (int k = 1; k <= count; ++k) sum = sum + __int_as_float(more[k].y) * places[more[k].x];
+                }
             }
             __hip_atomic_store(&places[GROUP * a.S + j], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
             mn = fminf(mn, sum), mx = fmaxf(mx, sum);
@@ -395,8 +406,8 @@ extern "C" int32_t qllm_add_norm_quant(const void *x, int32_t x_dtype, int64_t l
         a.bits = bits;
         if (gather) {
             a.places = reinterpret_cast<const uint32_t *>(gather->index);
-            a.computed = reinterpret_cast<const uint4 *>(gather->index + padded / 2);
-            a.more = reinterpret_cast<const int2 *>(gather->index + padded / 2 + 4 * gather->n_computed);
+            a.computed = reinterpret_cast<const Computed *>(gather->index + padded / 2);
+            a.more = reinterpret_cast<const int2 *>(gather->index + padded / 2 + 8 * gather->n_computed);
             a.n_computed = (int32_t)gather->n_computed;
         }
     }

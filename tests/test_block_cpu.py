@@ -70,16 +70,18 @@ def apply_index(y, index, computed, C_in, C_out):
     S = (C_in + 7) // 8
     padded = -(-C_out // 256) * 256
     places = index[:padded // 2].view(np.uint16)
-    computed = index[padded // 2:padded // 2 + 4 * computed].reshape(-1, 4)
+    computed = index[padded // 2:padded // 2 + 8 * computed].reshape(-1, 8)
     more = index[padded // 2 + computed.size:].reshape(-1, 2)
     row = np.zeros(8 * S + len(computed), np.float32)
     for c in range(C_in):
         row[(c % 8) * S + c // 8] = y[c]
     for j, c in enumerate(computed):
-        scale = c[1:3].copy().view(np.float32)
-        t = np.float32(np.float32(scale[0] * row[c[0] & 0xffff]) + np.float32(scale[1] * row[(int(c[0]) >> 16) & 0xffff]))
-        for place, bits in more[c[3] + 1:c[3] + 1 + more[c[3], 0]] if c[3] else ():
-            t = np.float32(t + np.float32(np.int32(bits).view(np.float32) * row[place]))
+        entries = list(zip(c[:2].copy().view(np.uint16), c[2:6].copy().view(np.float32)))[:4 if c[6] else 2]
+        if c[6] > 1:
+            entries += [(place, np.int32(bits).view(np.float32)) for place, bits in more[c[6] + 1:c[6] + 1 + more[c[6], 0]]]
+        t = np.float32(0.0)
+        for place, scale in entries:
+            t = np.float32(t + np.float32(scale * row[place]))
         row[8 * S + j] = t
     assert (places[C_out:] == 0).all()
     return row[places[:C_out]]
@@ -87,8 +89,8 @@ def apply_index(y, index, computed, C_in, C_out):
 
 def test_gather_map_is_the_map(oracle):
     rng = np.random.default_rng(1)
-    for C_in, C_out, special in ((1, 1, 2), (1, 40, 2), (7, 9, 1), (64, 64, 100), (65, 300, 3), (513, 511, 7), (1000, 1, 1)):
-        csr = random_csr_map(rng, C_in, C_out, special)
+    for C_in, C_out, special in ((1, 1, 2), (1, 40, 2), (7, 9, 1), (64, 64, 100), (65, 300, 3), (513, 511, 7), (1000, 1, 1), (900, 800, 2)):
+        csr = random_csr_map(rng, C_in, C_out, special, longest=9)
         index, computed = b.qllm_gather_map_host(*csr, C_in)
         y = rng.standard_normal((1, C_in)).astype(np.float32)
         assert np.array_equal(apply_index(y[0], index, computed, C_in, C_out), oracle.apply_map(y, *csr)[0])
