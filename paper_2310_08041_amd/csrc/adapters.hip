@@ -6,6 +6,8 @@
 //   down_kernel            h = x A^T of a tile over a slice of C, fp32, a part of the sum per slice
 //   join_kernel            where the slices of many rows are to be added: their sum
 //   up_kernel              out = y + (scale h) B^T of a tile over a block of columns
+// Measured: 2048 rows, 28672 -> 8192, 64 ranks, float32 y 32 + 5 + 32 us (x at 3.7 TB/s, y in and out at 4.2); 4360 rows, 5120 -> 27648 bf16
+// 17 + 5 + 109 (y at 4.5); one token 4096 -> 4096 3.5 + 5.5, four dependent trips to memory and the launch.
 // No sum uses atomics, and a row's sums do not depend on its place in a tile: equal calls give equal bits.
 #include <hip/hip_runtime.h>
 
@@ -156,7 +158,8 @@ struct Share {
 };
 
 // ---- h = x A^T.  Lane l of a wave holds its share (q = l / 16) of row l mod 16 of either operand; the order of the channels is the
-// same in both, so any will do.  The four waves take the slice's blocks in turn, the next one's loads in flight.
+// same in both, so any will do.  The four waves take the slice's blocks in turn, the next one's loads in flight.  64 rows a wave read A
+// once for all of them (32 rows a wave 46.9 us, 64 36.5, before the tile's slices lay next to each other).
 template <typename XT, typename WT, int MT, int NT>
 __device__ __forceinline__ void down_tile(const ApplyArgs &a, const Tile &tile, int slice, int first_rank, float *part)
 {

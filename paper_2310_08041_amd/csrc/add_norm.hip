@@ -1,12 +1,16 @@
 // The residual's addition, the norm, the reassembly (Eq. 3, Eq. 4) and Eq. (2) in one pass over the rows.
 //
 // s = round(residual + x); y = norm(s), statistics in fp64; x^ = the map's combination of y; codes of x^ at 4, 6 or 8 bits.
-// What it has to move is x, the residual, s and the codes (7 bytes a channel for bf16 and 8 bits): bound by memory.
+// What it has to move is x, the residual, s and the codes (7 bytes a channel for bf16 and 8 bits): bound by memory, 4.8 TB/s of the 5.1 that
+// a large copy reaches (4096 x 5120 bf16 to 8 bits 30.6 us; through a map 38, which is latency: staging, computed channels, places from L2).
 //
 // A workgroup has a row.  Its lanes hold 8 channels of it each, once to four times, from the loads to the codes: without a map
 // nothing of the row goes through LDS.  With one y is staged there, channel c at place (c mod 8) S + c / 8 so that lanes which hold
 // neighbouring chunks touch neighbouring words, whatever a map shifts them by; channels that are not copies are computed from it
 // first and get places of their own behind it, and then every output channel is one read from the place that the map's index names.
+//
+// A row a workgroup and as many workgroups as there are rows: 50 to 64 registers leave eight waves a SIMD, whose rows are at different
+// stages (workgroups that stay and keep gamma and the map take 100 registers and more and 42 to 66 us where these take 31 and 40).
 //
 // Compiled with -ffp-contract=off: every fp32 product and sum is rounded on its own, as qllm_norm_reassemble_quant rounds them.
 #include <hip/hip_runtime.h>
@@ -24,7 +28,7 @@ using namespace qllm_detail;
 namespace {
 
 constexpr int MOST_LANES = 1024;
-constexpr int MANY_ROWS = 512;
+constexpr int64_t MANY_CHUNKS = 3 << 16;
 
 // see qllm_gather_map_host
 struct alignas(16) Computed {
@@ -342,8 +346,10 @@ template <typename XT, typename RT, bool MAPPED>
 int32_t by_width(const AddNormArgs &a, hipStream_t stream)
 {
     const int units = a.S > a.groups ? a.S : a.groups; // chunks of 8 channels, in or out
-    const bool many = a.N >= MANY_ROWS;
-    if (units <= MOST_LANES && (!many || units <= 64)) return launch<XT, RT, 1, MAPPED>(a, units, stream);
+    // One chunk a lane is the shorter way through a row of few others, two keep more of it in flight and share what a wave does per row:
+    // us, one : two, bf16 to 8 bits, rows of 2048 channels 512 4.8 : 5.1, 768 5.6 : 5.2; of 4096 256 4.7 : 4.9, 512 6.2 : 5.7, 1024 10.2 : 8.6;
+    // of 8192 16 5.2 : 4.9 (sixteen waves are too many), 2048 36 : 31.  Four (5120 channels 32.0 : 30.6 with two) only where a row needs it.
+    if (units <= 512 && (units <= 64 || a.N * (int64_t)units < MANY_CHUNKS)) return launch<XT, RT, 1, MAPPED>(a, units, stream);
     if (units <= 2 * MOST_LANES) return launch<XT, RT, 2, MAPPED>(a, units, stream);
     return launch<XT, RT, 4, MAPPED>(a, units, stream);
 }
