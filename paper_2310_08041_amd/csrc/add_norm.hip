@@ -29,6 +29,7 @@ namespace {
 
 constexpr int MOST_LANES = 1024;
 constexpr int64_t MANY_CHUNKS = 3 << 16;
+constexpr int64_t MOST_LAUNCHED = 1ll << 31; // lanes of a launch, which counts them in 32 bits; more rows take another
 
 // see qllm_gather_map_host
 struct alignas(16) Computed {
@@ -41,6 +42,7 @@ struct AddNormArgs {
     const void *x, *residual;
     void *sum, *y, *values;
     int64_t ldx, ldr, lds, ldy, ldv;
+    int64_t first; // row of the launch
     const float *gamma, *beta;
     int32_t N, C, norm, o_bf16;
     double eps, inv_C;
@@ -105,7 +107,7 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
     __shared__ uint32_t arrived; // waves << 24, and the sum of their codes
     const int THREADS = blockDim.x, WAVES = THREADS >> 6;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const int64_t row = blockIdx.x;
+    const int64_t row = a.first + blockIdx.x;
     // elements of chunk `it` of the lane that are there, of a row of n and of the row that came
     auto left_of = [&](int it, int n) { return n - (tid + it * THREADS) * GROUP; };
     auto there = [&](int it) {
@@ -321,7 +323,7 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
 }
 
 template <typename XT, typename RT, int ITERS, bool MAPPED>
-int32_t launch(const AddNormArgs &a, int units, hipStream_t stream)
+int32_t launch(AddNormArgs a, int units, hipStream_t stream)
 {
     auto *kernel = a.C % GROUP == 0 ? add_norm_kernel<XT, RT, ITERS, MAPPED, true> : add_norm_kernel<XT, RT, ITERS, MAPPED, false>;
     const size_t lds = MAPPED ? (size_t)(GROUP * a.S + a.n_computed) * sizeof(float) : 0;
@@ -335,11 +337,14 @@ int32_t launch(const AddNormArgs &a, int units, hipStream_t stream)
     }
     const int lanes = (units + ITERS * 64 - 1) / (ITERS * 64) * 64;
     (void)hipGetLastError(); // drop any stale error of the calling thread: only this launch is judged
-    hipLaunchKernelGGL(kernel, dim3((unsigned)a.N), dim3(lanes), lds, stream, a);
-    const hipError_t e = hipGetLastError();
-    if (e == hipSuccess) return QLLM_OK;
-    qllm_note_hip_error("add_norm: launch", hipGetErrorName(e));
-    return QLLM_ERR_HIP;
+    for (const int64_t most = MOST_LAUNCHED / lanes; a.first < a.N; a.first += most) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(a.N - a.first < most ? a.N - a.first : most)), dim3(lanes), lds, stream, a);
+        const hipError_t e = hipGetLastError();
+        if (e == hipSuccess) continue;
+        qllm_note_hip_error("add_norm: launch", hipGetErrorName(e));
+        return QLLM_ERR_HIP;
+    }
+    return QLLM_OK;
 }
 
 template <typename XT, typename RT, bool MAPPED>

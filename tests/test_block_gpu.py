@@ -280,6 +280,24 @@ def test_norm_rows_far_apart():
 
 
 @gpu
+def test_norm_more_rows_than_a_launch():
+    """A launch counts its lanes in 32 bits; the same bits as from calls of a quarter of the rows."""
+    b = binding()
+    n, c = (1 << 25) + 5, 8
+    r, g = torch.randn(n, c, device="cuda", dtype=BF16), torch.ones(c, device="cuda")
+    q = b.DeviceQAct(n, c, 4)
+    for t in (q.codes, q.scale, q.zero, q.rowsum):
+        t.zero_()
+    b.qllm_add_norm_quant(None, r, None, 2, g, None, 1e-5, q, 4)
+    for i in range(0, n, 1 << 23):
+        k = min(1 << 23, n - i)
+        part = b.DeviceQAct(k, c, 4)
+        b.qllm_add_norm_quant(None, r[i:i + k], None, 2, g, None, 1e-5, part, 4)
+        for all_rows, rows in ((q.codes, part.codes), (q.scale, part.scale), (q.zero, part.zero), (q.rowsum, part.rowsum)):
+            assert torch.equal(all_rows[i:i + k], rows), i
+
+
+@gpu
 def test_norm_on_two_streams_at_once():
     """Nothing is shared between calls: the same bits beside another call on another stream."""
     b = binding()
