@@ -1138,6 +1138,7 @@ class DeviceAdapterPlan:
 def qllm_adapter_plan(plan, adapter, row_start=None, stream=None):
     """Fills the plan (DeviceAdapterPlan) of a step: adapter [sequences] int32, place in the pool (outside of it: none), row_start
     [sequences + 1] int32 the sequences' rows (None: one row each).  Once a step, for all layers and projections."""
+    _need(isinstance(adapter, torch.Tensor), "adapter must be a torch tensor")
     _check_tensor(adapter, "adapter", _I32_ONLY, numel=adapter.numel())
     _check_tensor(row_start, "row_start", _I32_ONLY, numel=adapter.numel() + 1, optional=True)
     _need(row_start is not None or adapter.numel() <= plan.rows, f"{adapter.numel()} sequences of one row each need as many rows, there are {plan.rows}")

@@ -29,6 +29,7 @@ constexpr int PLAN_HEAD_WORDS = 4;   // {tiles, rows, adapters of the pool, -}
 constexpr int PLAN_THREADS = 1024;
 constexpr int MOST_ADAPTERS = 8192;
 constexpr int64_t MOST_ROWS = 1 << 24, MOST_SEQS = 1 << 20;
+constexpr int64_t MOST_BLOCKS = 1 << 24; // of 256 lanes: a launch counts its lanes in 32 bits
 
 inline int64_t most_tiles(int64_t rows, int64_t n_adapters)
 {
@@ -736,7 +737,7 @@ extern "C" int32_t qllm_adapter_apply(const void *x, int32_t x_dtype, int64_t ld
     a.stream = !misses(y, 128) && !misses(out, 128) && (ldy * ys % 128 | ldo * ys % 128) == 0;
     for (int p = 0; p + 1 < w->n_parts; ++p) a.stream = a.stream && a.part_end[p] * ys % 128 == 0;
     const int64_t tiles = most_tiles(rows, w->n_adapters);
-    if (tiles * a.block_end[a.n_parts - 1] > INT32_MAX) return QLLM_ERR_SHAPE;
+    if (tiles * a.block_end[a.n_parts - 1] >= MOST_BLOCKS) return QLLM_ERR_SHAPE;
     auto by = [](int64_t d, int64_t most) { // of numbers up to `most`
         QuotientBy q = quotient_by((uint32_t)d);
         if (most * d >= (1ll << 32)) q.m = 0;

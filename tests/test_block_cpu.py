@@ -161,6 +161,11 @@ def test_adapter_refusals():
     assert apply(rows=0, x=None, y=None, out=None, plan=None, ws=None) == 0
 
 
+def test_adapter_launch_limit():
+    most, o = (1 << 24) - 1, 1 << 17            # 262148 tiles of 64 blocks of 2048 columns: over 2^24, whose 256 lanes each 32 bits count
+    assert apply(pool(O=o, part_O=(o, 0, 0, 0)), rows=most, ldy=o, ldo=o, ws_bytes=1 << 50, plan_bytes=1 << 50) == SHAPE
+
+
 def test_adapter_plan_refusals():
     plan = lambda rows=8, seqs=3, rs=A, ad=A, n=4, p=A, size=1 << 30: b.raw().qllm_adapter_plan(rows, seqs, rs, ad, n, p, size, None)  # noqa: E731
     assert plan(rows=-1) == SHAPE and plan(rows=1 << 24) == SHAPE and plan(seqs=-1) == SHAPE and plan(seqs=(1 << 20) + 1) == SHAPE
@@ -203,3 +208,5 @@ def test_adapter_binding_refuses():
         b.qllm_adapter_plan(plan, z(2, dt=torch.int32), z(2, dt=torch.int32))
     with pytest.raises(ValueError):
         b.qllm_adapter_plan(plan, z(2, dt=torch.int64))
+    with pytest.raises(ValueError):
+        b.qllm_adapter_plan(plan, [0, 1])
