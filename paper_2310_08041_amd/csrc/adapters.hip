@@ -266,6 +266,7 @@ __global__ __launch_bounds__(256, 2) void down_kernel(const ApplyArgs a)
 }
 
 // ---- the slices' sums: JOINERS neighbouring lanes add up every JOINERS-th slice each, then theirs are added
+// (by the second product itself for few rows and ranks: 64 rows on as many adapters would gain 1 us with it, 256 rows on 8 lose 2, on 2 8)
 constexpr int JOINERS = 8, JOINED = 32, JOINED_ROWS = 16, JOINED_RANKS = 1024;
 __device__ __forceinline__ f32x4 slices_of_lane(const float *h, int64_t stride, int slices, int joiner)
 {
@@ -608,11 +609,14 @@ int32_t check_sizes(const qllm_adapters *w, int64_t rows)
 inline int64_t fewest_tiles(int64_t rows) { return rows > TILE ? (rows + TILE - 1) / TILE : 1; }
 
 // The slices of C: two workgroups a CU, none shorter than a turn of the four waves (256 channels), for few rows two turns where that leaves
-// 16 slices (the second product adds up as many as JOINED itself).
+// 16 slices.  The second product adds up as many as JOINED itself, and up to 4 turns are shorter than another launch if its sums are few
+// (28672 -> 8192, 16 ranks, 1 row 10.6 us, 56 slices and their sum 13.5, 16 rows on 16 adapters 12.2 : 16.3; of 64 ranks 16 rows on 2
+// adapters 16.6 : 14.9; 200000 channels fp32, 25 turns, 39 : 21).
 void slices_of(const qllm_adapters *w, int64_t rows, int32_t *slices, int32_t *blocks_per_slice)
 {
     const int64_t turns = (w->C + 255) / 256, tiles = fewest_tiles(rows) * ((w->n_parts * w->rank + 63) / 64);
-    const int64_t want = rows > TILE ? (512 + tiles - 1) / tiles : turns > 32 ? turns / 2 : 16;
+    const bool joins = rows <= JOINED_ROWS && rows * w->rank <= JOINED_RANKS / 2 && turns <= 4 * JOINED;
+    const int64_t want = rows > TILE ? (512 + tiles - 1) / tiles : turns <= 32 ? 16 : joins && turns > 2 * JOINED ? JOINED : turns / 2;
     const int64_t most = want < turns ? want : turns, each = (turns + most - 1) / most;
     *blocks_per_slice = (int32_t)(4 * each);
     *slices = (int32_t)((turns + each - 1) / each);

@@ -549,6 +549,14 @@ def test_adapter_many_sequences_and_adapters():
 
 
 @gpu
+@pytest.mark.parametrize("c", [16385, 16640, 20001, 28672, 32768, 32769])
+def test_adapter_few_rows_of_long_inputs(c):
+    """As many slices as the second product adds up by itself, some of several turns, the last one shorter or none."""
+    check_adapters(news=[1, 3], names=[2, 0], n_adapters=3, rank=16, c=c, parts=[72, 40])
+    check_adapters(news=[1], names=[0], n_adapters=1, rank=24, c=c, parts=[33], xd=F32, wd=F32, yd=F32)
+
+
+@gpu
 def test_adapter_long_inputs():
     check_adapters(news=[1, 2, 40], names=[0, 1, 1], n_adapters=2, rank=64, c=28672, parts=[64])
     check_adapters(news=[130], names=[1], n_adapters=2, rank=16, c=13824, parts=[40], xd=F32, wd=F32, yd=F32)
