@@ -105,8 +105,8 @@ int32_t qllm_adapter_plan(int64_t rows, int64_t n_seqs, const int32_t *row_start
  *   x    [rows, ldx] x_dtype, C columns: what the projection's input was before it was quantized (qllm_add_norm_quant's y_out).
  *   y    [rows, ldy] y_dtype, O columns; out [rows, ldo] y_dtype, may be y itself (one stride), must not overlap it, x, A or B otherwise.
  *   plan      of qllm_adapter_plan for these rows and this n_adapters; of other numbers: nothing is done.
- *   workspace 16-byte aligned, qllm_adapter_workspace_bytes(adapters, rows) bytes (of the struct only sizes are read); contents
- *             undefined afterwards, two calls in flight at once need one each.
+ *   workspace 16-byte aligned, qllm_adapter_workspace_bytes(adapters, rows) bytes (of the struct only sizes are read; never less
+ *             for more rows); contents undefined afterwards, two calls in flight at once need one each.
  * Equal calls give equal bits.
  * The first product takes bf16 x and A through the bf16 matrix cores, other types as fp32; sums are fp32.  Its result meets B with 24
  * bits (fp32 B or y) or 16 bits (bf16 B and y: in two bf16 parts, which leaves out 2^-17 of it); the sum with y is fp32, rounded once.

@@ -669,9 +669,10 @@ extern "C" int64_t qllm_adapter_workspace_bytes(const qllm_adapters *w, int64_t 
 {
     const int32_t rc = check_sizes(w, rows);
     if (rc != QLLM_OK) return rc;
-    int32_t slices, each;
-    slices_of(w, rows, &slices, &each);
-    return slices * rows * w->n_parts * w->rank * (int64_t)sizeof(float);
+    // At least slices * rows, and never less for more rows: up to TILE rows slices <= turns; beyond, slices <= 512 / ceil(rows / TILE) + 1.
+    const int64_t turns = (w->C + 255) / 256, few = turns * (rows < TILE ? rows : TILE), many = 512 * TILE + rows;
+    const int64_t all = turns * rows < many ? turns * rows : many;
+    return (few > all ? few : all) * w->n_parts * w->rank * (int64_t)sizeof(float);
 }
 
 namespace {

@@ -161,6 +161,13 @@ def test_adapter_refusals():
     assert apply(rows=0, x=None, y=None, out=None, plan=None, ws=None) == 0
 
 
+def test_adapter_workspace_of_more_rows_serves_fewer():
+    rows = sorted({1, 16, 17, 63, 64, 65, 128, 129, 2048, 10000, 16384, 16385, 21900, 32704, 32768, 32769, 40000, 100000, (1 << 24) - 1})
+    for c in (1, 256, 257, 5000, 28672, 200000, (1 << 24) - 1):
+        sizes = [b.raw().qllm_adapter_workspace_bytes(C.byref(pool(Cc=c)), r) for r in rows]
+        assert sizes == sorted(sizes) and sizes[0] >= 16 * 4, c
+
+
 def test_adapter_launch_limit():
     most, o = (1 << 24) - 1, 1 << 17            # 262148 tiles of 64 blocks of 2048 columns: over 2^24, whose 256 lanes each 32 bits count
     assert apply(pool(O=o, part_O=(o, 0, 0, 0)), rows=most, ldy=o, ldo=o, ws_bytes=1 << 50, plan_bytes=1 << 50) == SHAPE
