@@ -373,12 +373,14 @@ struct Four<uint16_t, STREAM> {
 // Ranks that one step of the second product takes, and elements of a row of h in LDS.
 template <typename WT>
 constexpr int STEP = sizeof(WT) == 2 ? 32 : 16;
-template <typename WT, typename YT>
-constexpr int PARTS = sizeof(WT) == 4 ? 1 : sizeof(YT) == 2 ? 2 : 3;
-template <typename WT, typename YT>
+// Three bf16 numbers hold all 24 bits of h, whatever y's type: two leave out 2^-17 of each rank, which shows in a bf16 result where the
+// ranks cancel (and in 1 of 10^3 outputs otherwise, as a rounding the other way).
+template <typename WT>
+constexpr int PARTS = sizeof(WT) == 4 ? 1 : 3;
+template <typename WT>
 __host__ __device__ __forceinline__ int staged_stride(int rank)
 {
-    return PARTS<WT, YT> * ((rank + STEP<WT> - 1) / STEP<WT> * STEP<WT>) + (sizeof(WT) == 2 ? 8 : 4);
+    return PARTS<WT> * ((rank + STEP<WT> - 1) / STEP<WT> * STEP<WT>) + (sizeof(WT) == 2 ? 8 : 4);
 }
 
 // A wave has MT groups of 16 rows and 64 columns at a time, the next columns' y and B in flight; the waves of a workgroup share out the
@@ -387,7 +389,7 @@ template <typename WT, typename YT, int MT, bool WHOLE, bool STREAM>
 __device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, int p, int column, int end, uint8_t *staged)
 {
     constexpr bool HALF = sizeof(WT) == 2;
-    constexpr int P = PARTS<WT, YT>, S = STEP<WT>;
+    constexpr int P = PARTS<WT>, S = STEP<WT>;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r16 = lane & 15, quarter = lane >> 4;
     const int sharers = tile.count <= 16 * MT ? 1 : 2; // groups of MT * 16 rows
     const int first = 16 * MT * (wave & (sharers - 1)), turns = 4 / sharers;
@@ -445,7 +447,7 @@ __device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, in
     if (at < width) request(at);
 
     // scale h into LDS, the tile's rows (what lies in others reaches only results that are not stored)
-    const int padded = (a.rank + S - 1) / S * S, stride = staged_stride<WT, YT>(a.rank);
+    const int padded = (a.rank + S - 1) / S * S, stride = staged_stride<WT>(a.rank);
     if (tile.rank > 0) {
         const float scale = a.scale ? a.scale[tile.adapter] : 1.0f;
         const int cells = padded / 4, all = tile.count * cells; // of 4 ranks, a row
@@ -691,7 +693,7 @@ void run_down(const ApplyArgs &a, unsigned tiles, hipStream_t stream)
 template <typename WT, typename YT>
 int32_t run_up(const ApplyArgs &a, unsigned tiles, hipStream_t stream)
 {
-    const size_t lds = (size_t)TILE * staged_stride<WT, YT>(a.rank) * sizeof(WT);
+    const size_t lds = (size_t)TILE * staged_stride<WT>(a.rank) * sizeof(WT);
     auto *kernel = up_kernel<WT, YT>;
     if (lds > 48 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);

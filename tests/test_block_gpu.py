@@ -704,3 +704,39 @@ def test_step_between_two_layers_on_a_stream_and_as_a_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(u, v) for u, v in zip(want, (total, normed, act.codes, act.scale, y))), i
     assert all(torch.equal(u, v) for u, v in zip(eager, want))       # flipped an even number of times
+
+
+# ---------------------------------------------------------------- adapters, sums of whole numbers: every result is one number
+
+def differences(rank, c, o, yd, seed, rows=45):
+    """A step whose adapter takes the difference of ranks 2 j and 2 j + 1: h is a whole number of 18 to 23 bits that differs between the
+    two in its last few, so out = y + a small whole number.  Three channels are not zero."""
+    rng = np.random.default_rng([seed, rank, c])
+    s = make_adapters(news=[1, rows - 1], names=[1, 0], n_adapters=2, rank=rank, c=c, parts=[o], yd=yd, scale=False)
+    at = [0, c // 2, c - 1]
+    x, A = np.zeros((rows, c), np.int64), np.zeros((2, rank, c), np.int64)
+    x[:, at] = rng.integers(1, 4, (rows, 3)) * np.array([1 << 13, 1 << 6, 1])
+    A[:, ::2, at] = rng.integers(32, 128, (2, rank // 2, 3))
+    A[:, 1::2] = A[:, ::2]
+    A[:, 1::2, c - 1] = 64 + rng.integers(0, 4, (2, rank // 2))
+    A[:, ::2, c - 1] = 64 + rng.integers(0, 4, (2, rank // 2))
+    B = np.zeros((2, o, rank), np.int64)
+    B[:, :, ::2] = rng.choice([-1, 1], (2, o, rank // 2))
+    B[:, :, 1::2] = -B[:, :, ::2]
+    y = rng.integers(-4, 5, (rows, o))
+    for name, v in (("x", x), ("A", A), ("B", B), ("y", y)):
+        s[name].copy_(torch.from_numpy(v.astype(np.float32)))
+    h = np.stack([x[n] @ A[1 if n == 0 else 0].T for n in range(rows)])
+    return s, y + np.stack([B[1 if n == 0 else 0] @ h[n] for n in range(rows)])
+
+
+@gpu
+@pytest.mark.parametrize("rank", [8, 24, 64, 136, 256])
+@pytest.mark.parametrize("yd", [BF16, F32])
+def test_adapter_ranks_that_nearly_cancel(rank, yd):
+    """What h loses on its way to B shows where two ranks cancel.  Every product and sum here is a whole number below 2^24 times the step
+    of its part, so out is the whole number rounded once."""
+    for c, o in ((96, 70), (300, 300)):
+        s, want = differences(rank, c, o, yd, seed=1)
+        out, _ = apply(s)
+        assert torch.equal(out.cpu(), torch.from_numpy(want.astype(np.float32)).to(yd))
