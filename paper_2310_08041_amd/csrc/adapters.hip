@@ -459,11 +459,11 @@ __device__ __forceinline__ void up_tile(const ApplyArgs &a, const Tile &tile, in
             if constexpr (HALF) {
                 uint16_t *to = reinterpret_cast<uint16_t *>(staged) + row * stride + r;
 #pragma unroll
-                for (int part = 0; part < P; ++part) {
-                    const uint32_t lo = to_bf16(s[0], s[1]), hi = to_bf16(s[2], s[3]);
-                    *reinterpret_cast<uint2 *>(to + part * padded) = make_uint2(lo, hi);
-                    s[0] -= __uint_as_float(lo << 16), s[1] -= __uint_as_float(lo & 0xffff0000u);
-                    s[2] -= __uint_as_float(hi << 16), s[3] -= __uint_as_float(hi & 0xffff0000u);
+                for (int part = 0; part < P; ++part) { // the upper 8 bits of what is left, which are never past the largest bf16
+                    uint32_t upper[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) upper[j] = __float_as_uint(s[j]) & 0xffff0000u, s[j] -= __uint_as_float(upper[j]);
+                    *reinterpret_cast<uint2 *>(to + part * padded) = make_uint2(upper[0] >> 16 | upper[1], upper[2] >> 16 | upper[3]);
                 }
             } else {
                 *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(staged) + row * stride + r) = s;

@@ -740,3 +740,17 @@ def test_adapter_ranks_that_nearly_cancel(rank, yd):
         s, want = differences(rank, c, o, yd, seed=1)
         out, _ = apply(s)
         assert torch.equal(out.cpu(), torch.from_numpy(want.astype(np.float32)).to(yd))
+
+
+@gpu
+@pytest.mark.parametrize("wd", [BF16, F32])
+@pytest.mark.parametrize("yd", [BF16, F32])
+def test_adapter_sums_near_the_largest_float(wd, yd):
+    """h between the largest bf16 and the largest fp32 number, either sign, against a small B: x's only channel times 2^-100, once rounded."""
+    s = make_adapters(news=[1, 40], names=[0, 0], n_adapters=1, rank=8, c=70, parts=[33], xd=F32, wd=wd, yd=yd, scale=False, ranks=[1], junk=False)
+    for name in ("x", "A", "B", "y"):
+        s[name].zero_()
+    top = torch.tensor(np.linspace(3.3896e38, 3.4028e38, 41).astype(np.float32)) * torch.tensor([1.0, -1.0]).repeat(21)[:41]
+    s["x"][:, 69], s["A"][0, 0, 69], s["B"][0, :, 0] = top.cuda(), 1.0, 2.0 ** -100
+    out, _ = apply(s)
+    assert torch.equal(out.cpu(), (top.double() * 2.0 ** -100).to(yd)[:, None].expand(41, 33))
