@@ -14,6 +14,7 @@
 #include <stdint.h>
 
 #include "fused_common.h"
+#include "lds_limit.h"
 #include "qllm_block.h"
 #include "rows.h"
 
@@ -27,7 +28,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr int TILE = 64;             // rows of a tile
 constexpr int PLAN_HEAD_WORDS = 4;   // {tiles, rows, adapters of the pool, -}
 constexpr int PLAN_THREADS = 1024;
-constexpr int MOST_ADAPTERS = 8192;
+constexpr int MOST_ADAPTERS = 8192, MOST_RANKS = 256;
 constexpr int64_t MOST_ROWS = 1 << 24, MOST_SEQS = 1 << 20;
 constexpr int64_t MOST_BLOCKS = 1 << 24; // of 256 lanes: a launch counts its lanes in 32 bits
 
@@ -598,7 +599,7 @@ int32_t check_sizes(const qllm_adapters *w, int64_t rows)
     if (!w) return QLLM_ERR_NULL;
     if (rows < 0 || rows >= MOST_ROWS || w->n_adapters <= 0 || w->n_adapters > MOST_ADAPTERS) return QLLM_ERR_SHAPE;
     if (w->C <= 0 || w->C >= (1 << 24) || w->O <= 0 || w->O >= (1 << 24)) return QLLM_ERR_SHAPE;
-    if (w->rank <= 0 || w->rank > 256 || w->rank % 8 != 0 || w->n_parts < 1 || w->n_parts > QLLM_ADAPTER_PARTS) return QLLM_ERR_SHAPE;
+    if (w->rank <= 0 || w->rank > MOST_RANKS || w->rank % 8 != 0 || w->n_parts < 1 || w->n_parts > QLLM_ADAPTER_PARTS) return QLLM_ERR_SHAPE;
     int64_t sum = 0;
     for (int p = 0; p < w->n_parts; ++p) {
         if (w->part_O[p] <= 0 || w->part_O[p] > w->O) return QLLM_ERR_SHAPE;
@@ -696,12 +697,8 @@ int32_t run_up(const ApplyArgs &a, unsigned tiles, hipStream_t stream)
     const size_t lds = (size_t)TILE * staged_stride<WT>(a.rank) * sizeof(WT);
     auto *kernel = up_kernel<WT, YT>;
     if (lds > 48 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e != hipSuccess) {
-            (void)hipGetLastError();
-            qllm_note_hip_error("adapters: raising the LDS limit", hipGetErrorName(e));
-            return QLLM_ERR_HIP;
-        }
+        const int32_t e = raise_lds_limit(reinterpret_cast<const void *>(kernel), TILE * staged_stride<WT>(MOST_RANKS) * (int)sizeof(WT), "adapters: raising the LDS limit");
+        if (e != QLLM_OK) return e;
     }
     hipLaunchKernelGGL(kernel, dim3((unsigned)a.block_end[a.n_parts - 1] * tiles), dim3(256), lds, stream, a);
     return QLLM_OK;

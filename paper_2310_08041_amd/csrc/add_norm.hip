@@ -18,6 +18,7 @@
 #include <stdint.h>
 
 #include "fused_common.h"
+#include "lds_limit.h"
 #include "pack_codes.h"
 #include "qllm_block.h"
 #include "rows.h"
@@ -328,12 +329,8 @@ int32_t launch(AddNormArgs a, int units, hipStream_t stream)
     auto *kernel = a.C % GROUP == 0 ? add_norm_kernel<XT, RT, ITERS, MAPPED, true> : add_norm_kernel<XT, RT, ITERS, MAPPED, false>;
     const size_t lds = MAPPED ? (size_t)(GROUP * a.S + a.n_computed) * sizeof(float) : 0;
     if (lds > 48 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e != hipSuccess) {
-            (void)hipGetLastError();
-            qllm_note_hip_error("add_norm: raising the LDS limit", hipGetErrorName(e));
-            return QLLM_ERR_HIP;
-        }
+        const int32_t e = raise_lds_limit(reinterpret_cast<const void *>(kernel), QLLM_GATHER_PLACES * (int)sizeof(float), "add_norm: raising the LDS limit");
+        if (e != QLLM_OK) return e;
     }
     const int lanes = (units + ITERS * 64 - 1) / (ITERS * 64) * 64;
     (void)hipGetLastError(); // drop any stale error of the calling thread: only this launch is judged

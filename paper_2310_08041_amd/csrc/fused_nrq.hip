@@ -27,6 +27,7 @@
 
 #include "qllm.h"
 #include "fused_common.h"
+#include "lds_limit.h"
 
 using namespace qllm_detail;
 
@@ -402,13 +403,9 @@ template <typename K>
 int32_t launch_with_lds(K kernel, dim3 grid, dim3 block, size_t lds_bytes, hipStream_t stream, const FusedArgs &args)
 {
     if (lds_bytes > 48 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds_bytes);
-        if (e != hipSuccess) {
-            (void)hipGetLastError();
-            qllm_note_hip_error("fused kernel: raising the LDS limit", hipGetErrorName(e));
-            return QLLM_ERR_HIP;
-        }
+        constexpr int most = QLLM_MAX_CHANNELS * (int)sizeof(float); // a row
+        const int32_t e = raise_lds_limit(reinterpret_cast<const void *>(kernel), most, "fused kernel: raising the LDS limit");
+        if (e != QLLM_OK) return e;
     }
     (void)hipGetLastError(); // drop any stale error of the calling thread: only this launch is judged
     hipLaunchKernelGGL(kernel, grid, block, lds_bytes, stream, args);

@@ -1,5 +1,7 @@
 """What stands between the layers without a GPU: refusals of every entry point before anything is launched, the index of a map."""
 import ctypes as C
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -217,3 +219,81 @@ def test_adapter_binding_refuses():
         b.qllm_adapter_plan(plan, z(2, dt=torch.int64))
     with pytest.raises(ValueError):
         b.qllm_adapter_plan(plan, [0, 1])
+
+
+# ---------------------------------------------------------------- launches, on a runtime that only takes note of them
+
+RUNTIME = r"""
+#include <stddef.h>
+#include <map>
+struct dim3 { unsigned x, y, z; };
+static std::map<const void *, size_t> limit;       // of dynamic LDS, per kernel
+static int error, raises;
+static void (*between)();
+extern "C" {
+void fake_between(void (*f)()) { between = f; }    // called once, between the next raised limit and its launch
+int fake_raises() { return raises; }
+int hipGetDevice(int *d) { *d = 0; return 0; }
+int hipDeviceGetAttribute(int *v, int, int) { *v = 256; return 0; }
+int hipGetLastError() { int e = error; error = 0; return e; }
+const char *hipGetErrorName(int) { return "fake"; }
+struct Shape { dim3 grid, block; size_t lds; void *stream; };
+static Shape next;
+int __hipPushCallConfiguration(dim3 g, dim3 b, size_t lds, void *s) { next = Shape{g, b, lds, s}; return 0; }
+int __hipPopCallConfiguration(dim3 *g, dim3 *b, size_t *lds, void **s) { *g = next.grid, *b = next.block, *lds = next.lds, *s = next.stream; return 0; }
+int hipFuncSetAttribute(const void *f, int, int v) { ++raises; limit[f] = v; return 0; }
+int hipLaunchKernel(const void *f, dim3, dim3, void **, size_t lds, void *)
+{
+    if (lds > 48 * 1024 && between) { void (*call)() = between; between = nullptr; call(); }
+    size_t most = limit.count(f) ? limit[f] : 64 * 1024;
+    if (lds > most) error = 1;
+    return error;
+}
+}
+"""
+SMALLER_BETWEEN = r"""
+import ctypes as C, sys
+fake = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)     # in front of the library's own runtime
+lib = C.CDLL(sys.argv[2])
+A, vp, i64, i32 = 0x10000, C.c_void_p, C.c_int64, C.c_int32
+
+class Adapters(C.Structure):
+    _fields_ = [("n", i64), ("C", i64), ("O", i64), ("rank", i64), ("parts", i32), ("part_O", i64 * 4), ("w", i32), ("A", vp), ("B", vp), ("scale", vp), ("ranks", vp)]
+
+class Gather(C.Structure):
+    _fields_ = [("C_in", i64), ("C_out", i64), ("computed", i64), ("index", vp)]
+
+class QAct(C.Structure):
+    _fields_ = [("codes", vp), ("scale", vp), ("zero", vp), ("rowsum", vp)]
+
+def adapters(rank):
+    w = Adapters(4, 64, 96, rank, 1, (i64 * 4)(96, 0, 0, 0), 1, A, A, None, None)
+    return lib.qllm_adapter_apply(vp(A), 1, i64(64), i64(8), C.byref(w), vp(A), i64(1 << 30), vp(A), i64(96), vp(A), i64(96), 1, vp(A), i64(1 << 30), None)
+
+def norm(c):
+    g, q = Gather(c, c, 0, A), QAct(A, A, A, A)
+    return lib.qllm_add_norm_quant(vp(A), 1, i64(c), vp(A), 1, i64(c), i64(1), i64(c), vp(A), i64(c), 2, vp(A), None, C.c_float(1e-5), C.byref(g), 8, C.byref(q),
+                                   None, i64(0), None, i64(0), 1, None)
+
+def absmax(c):
+    return lib.qllm_norm_channel_absmax(vp(A), 1, i64(1), i64(c), i64(c), 2, vp(A), None, C.c_float(1e-5), vp(A), vp(A), i64(0), None)
+
+for call, large, small in ((adapters, 256, 224), (norm, 32768, 24576), (absmax, 32768, 24576)):
+    said = []
+    other = C.CFUNCTYPE(None)(lambda: said.append(call(small)))
+    fake.fake_between(other)
+    said.append(call(large))
+    before = fake.fake_raises()
+    said += [call(small), call(large)]
+    assert said == [0, 0, 0, 0], (call.__name__, said)
+    assert fake.fake_raises() == before, call.__name__
+"""
+
+
+def test_a_smaller_launch_between_a_limit_and_its_launch(tmp_path):
+    """The limit of dynamic LDS belongs to the kernel: what another thread launches with less must not lower it.  That thread's call comes
+    from inside the launch here, so that nothing depends on time."""
+    (tmp_path / "fake.cpp").write_text(RUNTIME)
+    subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", str(tmp_path / "fake.cpp"), "-o", str(tmp_path / "fake.so")], check=True)
+    done = subprocess.run([sys.executable, "-c", SMALLER_BETWEEN, str(tmp_path / "fake.so"), b.LIB_PATH], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=120)
+    assert done.returncode == 0, done.stdout
