@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+import test_block_gpu as tg
 from helpers import random_csr_map
 from paper_2310_08041_amd import binding as b
 
@@ -297,3 +298,15 @@ def test_a_smaller_launch_between_a_limit_and_its_launch(tmp_path):
     subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", str(tmp_path / "fake.cpp"), "-o", str(tmp_path / "fake.so")], check=True)
     done = subprocess.run([sys.executable, "-c", SMALLER_BETWEEN, str(tmp_path / "fake.so"), b.LIB_PATH], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=120)
     assert done.returncode == 0, done.stdout
+
+
+@pytest.mark.parametrize("c", [65, 257, 8193, 16385, 28672, 32769])
+def test_whole_numbers_show_a_channel_that_is_left_out(c):
+    """What the device tests compare with changes in every row of an adapter when any one channel at an end, a wave's or a slice's border
+    is left out of the sums."""
+    x, A, B, y = tg.whole_numbers(6, 2, 8, c, 24, 0)
+    of = [(slice(0, 2), 1), (slice(2, 5), 0), (slice(5, 6), -1)]
+    want = tg.whole_result(x, A, B, y, of)
+    assert (want == np.round(want)).all() and np.abs(want).max() < 1 << 24 and np.array_equal(want[5], y[5])
+    for at in sorted({0, 31, 63, 64, 127, 255, 256, 511, 512, 1023, 1024, c // 2, c - 64, c - 33, c - 9, c - 2, c - 1} & set(range(c))):
+        assert (tg.whole_result(x, A, B, y, of, without=at) != want)[:5].any(1).all(), at

@@ -754,3 +754,58 @@ def test_adapter_sums_near_the_largest_float(wd, yd):
     s["x"][:, 69], s["A"][0, 0, 69], s["B"][0, :, 0] = top.cuda(), 1.0, 2.0 ** -100
     out, _ = apply(s)
     assert torch.equal(out.cpu(), (top.double() * 2.0 ** -100).to(yd)[:, None].expand(41, 33))
+
+
+def whole_numbers(rows, n_adapters, rank, c, o, seed):
+    """x, A, B and y of small whole numbers, none of x, A and B 0, so that every sum is a whole number below 2^24, exact in whatever order
+    it is made, and one channel that is left out of it shows.  A [adapters, rank, c]."""
+    assert 3 * 3 * 2 * 2 * c * rank < 1 << 24
+    rng = np.random.default_rng([seed, rows, rank, c, o])
+    sign = lambda *s: rng.choice([-1, 1], s)  # noqa: E731
+    return (sign(rows, c) * rng.integers(1, 4, (rows, c)), sign(n_adapters, rank, c) * rng.integers(1, 4, (n_adapters, rank, c)),
+            sign(n_adapters, o, rank) * rng.integers(1, 3, (n_adapters, o, rank)), rng.integers(-9, 10, (rows, o)))
+
+
+def whole_result(x, A, B, y, of, without=None):
+    """out, exact: of: (rows, adapter) pairs, adapter a's scale 1 + a % 2; without: a channel that is left out."""
+    out = y.astype(np.float64)
+    for rs, a in of:
+        if 0 <= a < A.shape[0]:
+            xa, Aa = x[rs].astype(np.float64), A[a].astype(np.float64)
+            if without is not None:
+                xa[:, without] = 0.0
+            out[rs] += (1 + a % 2) * (xa @ Aa.T) @ B[a].astype(np.float64).T
+    return out
+
+
+def check_whole_numbers(news, names, n_adapters, rank, c, o, xd=BF16, wd=BF16, yd=F32, seed=0, **kw):
+    s = make_adapters(news=news, names=names, n_adapters=n_adapters, rank=rank, c=c, parts=[o], xd=xd, wd=wd, yd=yd, **kw)
+    x, A, B, y = whole_numbers(sum(news), n_adapters, rank, c, o, seed)
+    for name, v in (("x", x), ("A", A), ("B", B), ("y", y)):
+        s[name].copy_(torch.from_numpy(v.astype(np.float32)))
+    s["scale"].copy_(torch.tensor([1.0 + a % 2 for a in range(n_adapters)]))
+    out, _ = apply(s)
+    assert torch.equal(out.cpu(), torch.from_numpy(whole_result(x, A, B, y, s["of"])).to(yd))
+
+
+LONG = [1, 9, 63, 65, 255, 257, 1025, 4097, 8193, 16385, 16640, 20001, 28672, 32768, 32769]
+
+
+@gpu
+@pytest.mark.parametrize("c", LONG)
+def test_adapter_whole_numbers(c):
+    """Equality, however long the inputs: the last slice of one channel, one wave's last block, a slice of the sum are each seen."""
+    for yd in (F32, BF16):
+        check_whole_numbers([1, 3], [2, 1], 3, 8, c, 40, yd=yd)
+        check_whole_numbers([1], [0], 1, 8, c, 33, xd=F32, wd=F32, yd=yd, pad=1, lead=1)
+        check_whole_numbers([2, 17], [0, 1], 2, 8, c, 24, xd=F32, wd=BF16, yd=yd)
+        check_whole_numbers([70, 40, 1], [1, 0, 1], 2, 8, c, 24, yd=yd)
+        check_whole_numbers([70, 2], [1, 0], 2, 8, c, 24, xd=F32, wd=F32, yd=yd)
+
+
+@gpu
+@pytest.mark.parametrize("rank", [16, 40, 64])
+def test_adapter_whole_numbers_of_more_ranks(rank):
+    for c in (4097, 7169):
+        check_whole_numbers([1, 9], [1, 0], 2, rank, c, 40)
+        check_whole_numbers([80], [0], 2, rank, c, 40, xd=F32, wd=F32)
