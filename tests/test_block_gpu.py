@@ -809,3 +809,41 @@ def test_adapter_whole_numbers_of_more_ranks(rank):
     for c in (4097, 7169):
         check_whole_numbers([1, 9], [1, 0], 2, rank, c, 40)
         check_whole_numbers([80], [0], 2, rank, c, 40, xd=F32, wd=F32)
+
+
+@gpu
+def test_norm_rows_far_apart_of_every_output():
+    """The normalised rows and what the codes stand for, with rows past 2^32 bytes apart, are those of rows next to each other."""
+    b = binding()
+    c, k = 1000, 1003
+    rng = np.random.default_rng(8)
+    csr = random_csr_map(rng, c, k, 9)
+    x, r, g = far_rows(c, 1), far_rows(c, 2), torch.rand(c, device="cuda") + 0.5
+    for gather, n in ((None, c), (b.DeviceGather(*csr, c), k)):
+        near = dict(s=torch.empty((2, c), dtype=BF16, device="cuda"), y=torch.empty((2, c), dtype=BF16, device="cuda"), v=torch.empty((2, n), dtype=BF16, device="cuda"))
+        far = dict(s=far_rows(c, 3), y=far_rows(c, 4), v=far_rows(n, 5))
+        q = b.DeviceQAct(2, n, 8), b.DeviceQAct(2, n, 8)
+        for t in far.values():
+            t.fill_(float("nan"))
+        b.qllm_add_norm_quant(x.contiguous(), r.contiguous(), near["s"], 2, g, None, 1e-5, q[0], 8, gather=gather, y_out=near["y"], values_out=near["v"])
+        b.qllm_add_norm_quant(x, r, far["s"], 2, g, None, 1e-5, q[1], 8, gather=gather, y_out=far["y"], values_out=far["v"])
+        for name in far:
+            assert torch.equal(far[name], near[name]), name
+        assert torch.equal(q[0].codes, q[1].codes) and torch.equal(q[0].rowsum, q[1].rowsum)
+        del far
+
+
+@gpu
+@pytest.mark.parametrize("yd", [BF16, F32])
+def test_adapter_sequences_in_another_order(yd):
+    """The same sequences in another order of rows: each row's bits are the same."""
+    news, names = [5, 30, 1, 64, 2, 17, 90], [2, 1, 2, 2, -1, 0, 1]
+    s = make_adapters(news=news, names=names, n_adapters=3, rank=16, c=700, parts=[100, 60], yd=yd, ranks=[16, 9, 3])
+    out, _ = apply(s)
+    rows = [list(range(sum(news[:i]), sum(news[:i + 1]))) for i in range(len(news))]
+    for order in ([6, 5, 4, 3, 2, 1, 0], [3, 0, 6, 1, 5, 2, 4], [2, 3, 0, 4, 1, 6, 5]):
+        at = torch.tensor([n for i in order for n in rows[i]], device="cuda")
+        starts = np.cumsum([0] + [news[i] for i in order])
+        moved, _ = apply(dict(s, x=s["x"][at], y=s["y"][at], row_start=torch.tensor(starts, dtype=torch.int32).cuda(),
+                              adapter=torch.tensor([names[i] for i in order], dtype=torch.int32).cuda()))
+        assert torch.equal(moved, out[at]), order
