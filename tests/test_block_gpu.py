@@ -847,3 +847,70 @@ def test_adapter_sequences_in_another_order(yd):
         moved, _ = apply(dict(s, x=s["x"][at], y=s["y"][at], row_start=torch.tensor(starts, dtype=torch.int32).cuda(),
                               adapter=torch.tensor([names[i] for i in order], dtype=torch.int32).cuda()))
         assert torch.equal(moved, out[at]), order
+
+
+def guarded(size):
+    """Exactly `size` bytes between two guards of 4096, all of one pattern; the bytes and a check of the guards."""
+    store = torch.full((size + 8192,), 0xA5, dtype=torch.uint8, device="cuda")
+
+    def kept():
+        return bool((store[:4096] == 0xA5).all()) and bool((store[4096 + size:] == 0xA5).all())
+
+    return store[4096:4096 + size], kept
+
+
+def apply_guarded(s, out, single=False):
+    """apply() with a plan and a workspace of exactly the bytes asked for, through the C entries; both hold whatever was there before."""
+    b = binding()
+    ad = b.DeviceAdapters(s["A"], s["B"], s["scale"], s["ranks"], s["parts"])
+    rows, here = s["rows"], torch.cuda.current_stream().cuda_stream
+    plan, plan_kept = guarded(b.qllm_adapter_plan_bytes(rows, s["n_adapters"]))
+    ws, ws_kept = guarded(b.qllm_adapter_workspace_bytes(ad, rows))
+    code = {F32: b.F32, BF16: b.BF16}
+    for _ in range(2):
+        assert 0 == b.raw().qllm_adapter_plan(rows, s["adapter"].numel(), None if single else s["row_start"].data_ptr(), s["adapter"].data_ptr(), s["n_adapters"],
+                                              plan.data_ptr(), plan.numel(), here)
+        assert 0 == b.raw().qllm_adapter_apply(s["x"].data_ptr(), code[s["x"].dtype], s["x"].stride(0), rows, ad.ref, plan.data_ptr(), plan.numel(),
+                                               s["y"].data_ptr(), s["y"].stride(0), out.data_ptr(), out.stride(0), code[s["y"].dtype], ws.data_ptr(), ws.numel(), here)
+        torch.cuda.synchronize()
+        assert plan_kept() and ws_kept()
+    return out
+
+
+@gpu
+def test_adapter_guards_of_plan_and_workspace():
+    """Many slices, many adapters, many ranks, many rows, one row: nothing is written beside the bytes that the sizes name."""
+    for kw, single in ((dict(news=[1] * 16, names=[i % 3 for i in range(16)], n_adapters=3, rank=24, c=32768, parts=[40]), True),
+                       (dict(news=[3, 1], names=[0, 1], n_adapters=2, rank=8, c=200001, parts=[24], xd=F32, wd=F32, yd=F32), False),
+                       (dict(news=[1] * 40, names=[(i * 997) % 8192 for i in range(40)], n_adapters=8192, rank=8, c=24, parts=[16]), True),
+                       (dict(news=[65, 64, 63, 1], names=[0, 1, 2, 0], n_adapters=3, rank=256, c=4096, parts=[24, 24]), False),
+                       (dict(news=[1000, 3000, 200], names=[1, 0, 5], n_adapters=2, rank=16, c=5000, parts=[24], tail=3), False),
+                       (dict(news=[1], names=[0], n_adapters=1, rank=8, c=1, parts=[1]), True)):
+        s = make_adapters(**kw)
+        want, _ = apply(s, single=single)
+        assert torch.equal(apply_guarded(s, torch.full_like(s["y"], 3.0), single=single), want)
+
+
+@gpu
+@pytest.mark.parametrize("starts", [[0, 30, 0, 30], [-5, 100, 7, 1 << 30], [1 << 30, -(1 << 31), 5, 3], [30, 30, 30, 30], [0, 70, 0, 70], [-1, -1, 70, 0]])
+def test_adapter_guards_with_contradictory_arrays(starts):
+    for names in ([1 << 30, -7, 2], [0, 0, 0], [2, 1, 2]):
+        s = make_adapters(news=[10, 10, 10], names=[0, 1, 2], n_adapters=3, rank=8, c=70, parts=[24], pad=4, lead=8)
+        s = dict(s, row_start=torch.tensor(starts, dtype=torch.int32).cuda(), adapter=torch.tensor(names, dtype=torch.int32).cuda())
+        out_store = torch.full((40 * 40,), 3.0, dtype=BF16, device="cuda")
+        out = out_store[100:100 + 30 * 28].view(30, 28)[:, :24]
+        apply_guarded(s, out)
+        out.fill_(3.0)
+        assert (out_store == 3.0).all()
+
+
+@gpu
+def test_adapter_guards_with_many_sequences_on_the_same_rows():
+    """3000 sequences of all rows each, on one adapter and on many: every count and place goes past what the plan has room for."""
+    n = 3000
+    s = make_adapters(news=[100], names=[0], n_adapters=50, rank=8, c=40, parts=[16], yd=F32)
+    starts = torch.tensor([0, 100] * (n // 2) + [0], dtype=torch.int32).cuda()
+    for names in ([7] * n, [i % 50 for i in range(n)]):
+        t = dict(s, row_start=starts, adapter=torch.tensor(names, dtype=torch.int32).cuda())
+        out = apply_guarded(t, torch.full_like(s["y"], 3.0))
+        assert torch.isfinite(out).all()
