@@ -914,3 +914,67 @@ def test_adapter_guards_with_many_sequences_on_the_same_rows():
         t = dict(s, row_start=starts, adapter=torch.tensor(names, dtype=torch.int32).cuda())
         out = apply_guarded(t, torch.full_like(s["y"], 3.0))
         assert torch.isfinite(out).all()
+
+
+def whole_step(rows, n_adapters, rank, c, parts, yd, a_of, seed=0, live=None):
+    """A step made on the device, a row a sequence, of small whole numbers as above; live: the channels of x that are not 0 (None: all).
+    a_of: each row's adapter."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    one = lambda most, *s: (torch.randint(1, most + 1, s, generator=g, device="cuda", dtype=torch.int8) * (2 * torch.randint(0, 2, s, generator=g, device="cuda", dtype=torch.int8) - 1)).to(BF16)  # noqa: E731
+    o = sum(parts)
+    x = one(3, rows, c)
+    if live is not None:
+        keep = torch.zeros(c, dtype=torch.bool, device="cuda")
+        keep[live] = True
+        x *= keep
+    A, B = one(3, n_adapters, len(parts) * rank, c), torch.empty((n_adapters, o, rank), dtype=BF16, device="cuda")
+    for a in range(n_adapters):
+        B[a] = one(2, o, rank)
+    return dict(x=x, A=A, B=B, y=one(9, rows, o).to(yd), scale=None, ranks=None, parts=parts, rank=rank, n_adapters=n_adapters, rows=rows, c=c,
+                adapter=torch.tensor(a_of, dtype=torch.int32).cuda())
+
+
+def check_whole_step(s, live=None):
+    """In place, against products in 64 bits, a row at a time where rows are long."""
+    y = s["y"].clone()
+    apply(s, out=s["y"], single=True)
+    at = slice(None) if live is None else live
+    o = sum(s["parts"])
+    for a in sorted(set(s["adapter"].tolist())):
+        rows = torch.nonzero(s["adapter"] == a)[:, 0]
+        for some in rows.split(max(1, (1 << 25) // o)):
+            want = y[some].double()
+            if 0 <= a < s["n_adapters"]:
+                col = 0
+                for p, width in enumerate(s["parts"]):
+                    h = s["x"][some][:, at].double() @ s["A"][a, p * s["rank"]:(p + 1) * s["rank"]][:, at].double().T.contiguous()
+                    want[:, col:col + width] += h @ s["B"][a, col:col + width].double().T.contiguous()
+                    col += width
+            assert torch.equal(s["y"][some], want.to(y.dtype)), a
+
+
+@gpu
+@pytest.mark.parametrize("yd", [BF16, F32])
+@pytest.mark.parametrize("rows,parts", [(256, [4096, 4096, 4096]), (256, [4095, 2, 8190]), (4200, [13824, 13824]), (4200, [27000]), (1100, [12288, 1]), (60, [40000])])
+def test_adapter_blocks_of_many_columns(rows, parts, yd):
+    """Workgroups of the second product that take more than 256 columns, in tiles of few and of many rows, of whole and of other widths."""
+    few = [(i * 7) % 17 - 1 for i in range(rows)] if rows <= 256 else [i // 1500 for i in range(rows)]
+    s = whole_step(rows, 16 if rows <= 256 else 2, 16, 72, parts, yd, few)
+    check_whole_step(s)
+
+
+@gpu
+def test_adapter_more_slices_than_the_short_division_takes():
+    """4 tiles of 32768 slices of the longest input: 2^32 and more in the product that the multiplication in place of a division stands for."""
+    c = (1 << 24) - 1
+    live = torch.tensor([0, 1, 63, 255, 256, 511, 512, 513, 8191, 1 << 20, (1 << 23) + 5, c - 513, c - 256, c - 255, c - 2, c - 1], device="cuda")
+    s = whole_step(5, 4, 8, c, [40], F32, [3, 1, -1, 0, 2], live=live)
+    check_whole_step(s, live)
+
+
+@gpu
+def test_adapter_more_columns_than_the_short_division_takes():
+    """65 tiles of 8192 blocks of 2048 columns: as above, for the second product."""
+    s = whole_step(64, 63, 8, 16, [(1 << 24) - 1], BF16, list(range(63)) + [-1])
+    check_whole_step(s)
+    torch.cuda.empty_cache()
