@@ -278,7 +278,12 @@ __global__ __launch_bounds__(MOST_LANES) void add_norm_kernel(const AddNormArgs 
         const int w = min(lane & 15, WAVES - 1);
         mn = dpp_min_row16(red_f[0][w]), mx = dpp_max_row16(red_f[1][w]);
     }
-    if constexpr (MAPPED) gather(); // the computed channels' values are there now
+    if constexpr (MAPPED) {
+        // The computed channels' values are there now.  A wave alone has had no barrier: its LDS operations are done in their order, which
+        // the fence keeps the compiler to without an instruction.
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        gather();
+    }
     const int32_t qmax = (1 << a.bits) - 1;
     const float range = mx - mn, alpha = range > 0.0f ? range / (float)qmax : 1.0f, inv = 1.0f / alpha;
     const bool fast = fabsf(mn * inv) < FAST_LIMIT && fabsf(mx * inv) < FAST_LIMIT;
