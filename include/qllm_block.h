@@ -109,7 +109,7 @@ int32_t qllm_adapter_plan(int64_t rows, int64_t n_seqs, const int32_t *row_start
  *             for more rows); contents undefined afterwards, two calls in flight at once need one each.
  * Equal calls give equal bits.
  * The first product takes bf16 x and A through the bf16 matrix cores, other types as fp32; sums are fp32.  Its result times scale_a meets B
- * with all its 24 bits (bf16 B: in three bf16 parts); the sum with y is fp32, rounded once.
+ * with all its 24 bits (bf16 B: in three bf16 parts, from 2^-110 on; nothing below 2^-133); the sum with y is fp32, rounded once.
  * A row of x that is not finite spoils its own row of out; an adapter that is not finite the rows that name it.
  * Limits: rows < 2^24, (rows / 64 + n_adapters + 1) * (O / 256 + n_parts) <= 2^24.
  * Errors: NULL / SHAPE / DTYPE / ALIGN / WORKSPACE / HIP.  rows == 0: no-op.

@@ -1049,8 +1049,8 @@ def _check_here(names, *tensors):
 
 def qllm_add_norm_quant(x, residual, sum_out, norm, gamma, beta, eps, out=None, bits=8, gather=None, y_out=None, values_out=None, stream=None):
     """sum_out = residual + x (rounded to the residual's dtype), its norm, the reassembly of `gather` (DeviceGather or None) and Eq. (2) at
-    `bits` into out (DeviceQAct or None).  x [N, C] (None: nothing is added), residual and sum_out [N, C] (sum_out may be residual, x or
-    None), y_out [N, C] the normalised rows, values_out [N, C_out] what the codes stand for (one dtype, either may be None)."""
+    `bits` into out (DeviceQAct or None).  x [N, C] (None: nothing is added, and sum_out is not written, whatever it is), residual and
+    sum_out [N, C] (sum_out may be residual, x or None), y_out [N, C] the normalised rows, values_out [N, C_out] what the codes stand for (one dtype, either may be None)."""
     if not (hasattr(residual, "dim") and residual.dim() == 2):
         _fail("residual must be a 2-d tensor [tokens, channels]")
     N, Cc = residual.shape

@@ -978,3 +978,29 @@ def test_adapter_more_columns_than_the_short_division_takes():
     s = whole_step(64, 63, 8, 16, [(1 << 24) - 1], BF16, list(range(63)) + [-1])
     check_whole_step(s)
     torch.cuda.empty_cache()
+
+
+@gpu
+def test_adapter_sums_near_the_smallest_float():
+    """h of 24 bits whose last one is the smallest bf16 number, 2^-133: all of them reach B; of h below, what is 2^-133 and more."""
+    s = make_adapters(news=[1, 40], names=[0, 0], n_adapters=1, rank=8, c=70, parts=[33], xd=F32, yd=F32, scale=False, ranks=[1], junk=False)
+    for name in ("x", "A", "B", "y"):
+        s[name].zero_()
+    s["A"][0, 0, 69], s["B"][0, :, 0] = 1.0, 2.0 ** 100
+    for lowest, most in ((1 << 23, 1 << 24), (1, 1 << 16)):
+        h = torch.from_numpy(np.random.default_rng(0).integers(lowest, most, 41).astype(np.float64) * 2.0 ** -133)
+        s["x"][:, 69] = h.float().cuda()
+        out, _ = apply(s)
+        assert torch.equal(out.cpu(), (h * 2.0 ** 100).float()[:, None].expand(41, 33))
+
+
+@gpu
+def test_norm_without_x_leaves_sum_out():
+    """Nothing is added, and sum_out is not written."""
+    b = binding()
+    r, s = torch.randn(5, 300, device="cuda"), torch.full((5, 300), 7.0, device="cuda")
+    q, w = b.DeviceQAct(5, 300, 8), b.DeviceQAct(5, 300, 8)
+    g = torch.ones(300, device="cuda")
+    b.qllm_add_norm_quant(None, r, s, 2, g, None, 1e-5, q, 8)
+    b.qllm_add_norm_quant(None, r, None, 2, g, None, 1e-5, w, 8)
+    assert (s == 7.0).all() and torch.equal(q.codes, w.codes) and torch.equal(q.scale, w.scale)
