@@ -7,7 +7,7 @@
 //   join_kernel            where the slices of many rows are to be added: their sum
 //   up_kernel              out = y + (scale h) B^T of a tile over a block of columns
 // Measured: 2048 rows, 28672 -> 8192, 64 ranks, float32 y 32 + 5 + 32 us (x at 3.7 TB/s, y in and out at 4.2); 4360 rows, 5120 -> 27648 bf16
-// 17 + 5 + 109 (y at 4.5); one token 4096 -> 4096 3.5 + 5.5, four dependent trips to memory and the launch.
+// 18 + 5 + 110 (y at 4.4); one token 4096 -> 4096 3.5 + 5.5, four dependent trips to memory and the launch.
 // No sum uses atomics, and a row's sums do not depend on its place in a tile: equal calls give equal bits.
 #include <hip/hip_runtime.h>
 

@@ -2,7 +2,7 @@
 //
 // s = round(residual + x); y = norm(s), statistics in fp64; x^ = the map's combination of y; codes of x^ at 4, 6 or 8 bits.
 // What it has to move is x, the residual, s and the codes (7 bytes a channel for bf16 and 8 bits): bound by memory, 4.8 TB/s of the 5.1 that
-// a large copy reaches (4096 x 5120 bf16 to 8 bits 30.6 us; through a map 38, which is latency: staging, computed channels, places from L2).
+// a large copy reaches (4096 x 5120 bf16 to 8 bits 30.7 us; through a map 35, which is latency: staging, computed channels, places from L2).
 //
 // A workgroup has a row.  Its lanes hold 8 channels of it each, once to four times, from the loads to the codes: without a map
 // nothing of the row goes through LDS.  With one y is staged there, channel c at place (c mod 8) S + c / 8 so that lanes which hold
